@@ -1,0 +1,408 @@
+// Attention of a batch over a prefix that all its requests share and over each request's own paged
+// cache (include/wt_serve.h): the warp kernel and the merge.
+//
+// Keys are split over CTAs (and over the warps of a CTA); each part gives, per (token, head), the
+// sum O of p v, the sum l of p and the reference m the p were taken against, p = 2^(s - m) with
+// s = scale log2(e) q.k.  Parts are joined exactly as softmax splits: O = sum_i 2^(m_i - m) O_i,
+// l = sum_i 2^(m_i - m) l_i, m = max m_i, out = O / l; a part without a key has m = -infinity, and
+// a token without any gets zeros.
+//
+// attend_warp_kernel takes a CTA per (rows, kv head, keys of one request): rows are the (token,
+// head) pairs that share a kv head, 16 or 32 of them, and each of 4 warps streams its own tiles of
+// 16 keys through a ring of its own in shared memory (16-byte cp.async, absent keys zero-filled, so
+// what a page holds past its last key never reaches a product), with m16n8k16 MMAs on them.  No warp
+// waits for another before the end.  Bound: HBM (or L2) for up to 32 rows.
+#include <algorithm>
+
+#include "wt_device.cuh"
+#include "wt_serve.h"
+
+namespace wt {
+
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kKeys = 16;    // keys of a tile
+constexpr int kStages = 3;   // tiles of a warp's ring
+constexpr int kStatusInvalid = -1;
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if constexpr (DT == WT_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// New tokens and own keys of request b, clamped to the descriptor.
+struct Request {
+  int t0, n, len;
+};
+__device__ __forceinline__ Request request_of(const wt_attend_desc &d, int b, int *status, bool tell) {
+  int t0 = __ldg(d.begin + b), t1 = __ldg(d.begin + b + 1), len = d.max_len > 0 ? __ldg(d.len + b) : 0;
+  if (t0 < 0 || t1 < t0 || t1 > d.n_tokens || t1 - t0 > d.max_new || len < 0 || len > d.max_len) {
+    if (tell && status) atomicCAS(status, 0, kStatusInvalid);
+    t0 = min(max(t0, 0), d.n_tokens);
+    t1 = min(max(t1, t0), min(d.n_tokens, t0 + d.max_new));
+    len = min(max(len, 0), d.max_len);
+  }
+  return {t0, t1 - t0, len};
+}
+
+// ND: 16-element groups of head_dim (rounded up).  MT: tiles of 16 rows.
+template <int DT, int ND, int MT>
+__global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_constant__ AttendPlan P) {
+  constexpr int kPitch = ND * 32 + 16;              // bytes of a staged row: 8 rows hit 8 different bank groups
+  constexpr int kTileBytes = 2 * kKeys * kPitch;    // K rows, then V rows
+  constexpr int kRows = 16 * MT;
+  __shared__ uint32_t there[kWarps][kStages];  // bit r: key r of the staged tile exists
+  extern __shared__ __align__(16) uint8_t smem[];
+  const wt_attend_desc &d = P.d;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
+  const int hk = blockIdx.x % d.kv_heads, rt = blockIdx.x / d.kv_heads % P.row_tiles;
+  const int keys_of = blockIdx.x / (d.kv_heads * P.row_tiles);  // (request, split), then the prefix's splits
+  const int G = P.G, D = d.head_dim;
+  // the last "request" is the shared prefix with every token of the batch, where it is taken here
+  const bool pre = keys_of >= d.n_req * P.own_splits;
+  const int b = pre ? 0 : keys_of / P.own_splits;
+  const int split = pre ? keys_of - d.n_req * P.own_splits : keys_of % P.own_splits;
+  Request rq;
+  int64_t k0, k1;
+  if (pre) {
+    rq = {0, d.n_tokens, 0};
+    k0 = (int64_t)split * P.pre_len;
+    k1 = min(d.prefix_len, k0 + P.pre_len);
+  } else {
+    rq = request_of(d, b, P.status, hk == 0 && rt == 0 && split == 0 && tid == 0);
+    k0 = (int64_t)split * P.own_len;
+    k1 = min((int64_t)rq.len, k0 + P.own_len);
+  }
+  const int rows = rq.n * G, row0 = rt * kRows;
+  if (row0 >= rows) return;
+  const int part = (pre ? P.own_splits : 0) + split;
+  if (k0 >= k1) return;  // the merge knows from the length that there is nothing
+
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * kStages * kTileBytes;
+  // columns past head_dim stay zero: no copy touches them
+  for (int i = tid; i < kWarps * kStages * kTileBytes / 16; i += kThreads)
+    reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+
+  // queries as A operands
+  uint32_t qf[MT][ND][4];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = row0 + i * 16 + g + e * 8;
+      const bool ok = r < rows;
+      const uint16_t *src = static_cast<const uint16_t *>(d.q) +
+                            (ok ? (int64_t)(rq.t0 + r / G) * d.q_stride + (int64_t)(hk * G + r % G) * D : 0);
+#pragma unroll
+      for (int k = 0; k < ND; ++k)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const int col = k * 16 + f * 8 + q * 2;
+          qf[i][k][e + 2 * f] = ok && col < D ? __ldg(reinterpret_cast<const uint32_t *>(src + col)) : 0u;
+        }
+    }
+
+  float o[MT][2 * ND][4], m[MT][2], l[MT][2];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+#pragma unroll
+    for (int j = 0; j < 2 * ND; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][j][e] = 0.0f;
+    m[i][0] = m[i][1] = -INFINITY;
+    l[i][0] = l[i][1] = 0.0f;
+  }
+  const float sl = d.scale * 1.4426950408889634f;
+
+  const int tiles = (int)((k1 - k0 + kKeys - 1) / kKeys);
+  const int chunks = D / 8;  // 16-byte pieces of a row
+  // Tile i of this warp (tiles warp, warp + 4, ...) into its ring: lane r (r < 16) knows the row of
+  // key r, and the lanes copy whole rows together.
+  auto fetch = [&](int i) {
+    const int tile = warp + i * kWarps;
+    if (tile < tiles) {
+      const int64_t key = k0 + (int64_t)tile * kKeys + (lane & 15);
+      uint64_t src = 0;  // 0: an absent key
+      if (key < k1) {
+        const uint8_t *base = static_cast<const uint8_t *>(lane < 16 ? (pre ? d.prefix_k : d.k_pages)
+                                                                     : (pre ? d.prefix_v : d.v_pages));
+        if (pre) {
+          src = reinterpret_cast<uint64_t>(base + 2 * (key * d.prefix_stride + hk * d.prefix_head));
+        } else {
+          const int pg = (int)key / d.page, in = (int)key - pg * d.page;
+          const int page = __ldg(d.table + (int64_t)b * d.table_stride + pg);
+          if (page >= 0 && page < d.n_pages)
+            src = reinterpret_cast<uint64_t>(base + 2 * (((int64_t)page * d.page + in) * d.kv_heads + hk) * D);
+          else if (P.status)
+            atomicCAS(P.status, 0, kStatusInvalid);
+        }
+      }
+      const uint32_t dst = ring + (i % kStages) * kTileBytes;
+      const uint32_t found = __ballot_sync(0xffffffffu, src != 0);
+      if (lane == 0) there[warp][i % kStages] = found;
+      for (int c0 = 0; c0 < 32 * chunks; c0 += 32) {
+        const int c = c0 + lane, row = c / chunks, in = c - row * chunks;  // rows 0..15: K, 16..31: V
+        const uint64_t a = __shfl_sync(0xffffffffu, src, row);
+        cp16(dst + row * kPitch + in * 16, reinterpret_cast<const void *>(a ? a + in * 16 : reinterpret_cast<uint64_t>(d.q)), a != 0);
+      }
+    }
+    cp_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) fetch(i);
+
+  // keys a row may see: all but the tail for own keys
+  int64_t sees[MT][2];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = row0 + i * 16 + g + e * 8;
+      sees[i][e] = pre ? k1 : min(k1, (int64_t)rq.len - rq.n + 1 + r / G);
+    }
+
+  for (int i = 0; warp + i * kWarps < tiles; ++i) {
+    fetch(i + kStages - 1);
+    cp_wait<kStages - 1>();
+    __syncwarp();
+    const uint32_t kt = ring + (i % kStages) * kTileBytes, vt = kt + kKeys * kPitch;
+    const int64_t key0 = k0 + (int64_t)(warp + i * kWarps) * kKeys;
+    const uint32_t found = there[warp][i % kStages];
+    float s[MT][2][4];
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[a][j][e] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < ND; ++k) {
+      uint32_t kf[4];  // keys 0-7 and 8-15, each in two halves of 8 elements
+      ldsm4(kf, kt + ((lane & 7) + (lane >> 4) * 8) * kPitch + k * 32 + ((lane >> 3) & 1) * 16);
+#pragma unroll
+      for (int a = 0; a < MT; ++a) {
+        mma16816<DT>(s[a][0], qf[a][k][0], qf[a][k][1], qf[a][k][2], qf[a][k][3], kf[0], kf[1]);
+        mma16816<DT>(s[a][1], qf[a][k][0], qf[a][k][1], qf[a][k][2], qf[a][k][3], kf[2], kf[3]);
+      }
+    }
+    uint32_t pf[MT][4];
+#pragma unroll
+    for (int a = 0; a < MT; ++a) {
+      float mx[2] = {m[a][0], m[a][1]};
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = j * 8 + q * 2 + (e & 1);
+          s[a][j][e] = (found >> r & 1) && key0 + r < sees[a][e >> 1] ? s[a][j][e] * sl : -INFINITY;
+          mx[e >> 1] = fmaxf(mx[e >> 1], s[a][j][e]);
+        }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
+        mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
+        const float ref = mx[e] > -INFINITY ? mx[e] : 0.0f;
+        const float f = exp2_approx(m[a][e] - ref);
+        m[a][e] = mx[e];
+        l[a][e] *= f;
+#pragma unroll
+        for (int j = 0; j < 2 * ND; ++j) {
+          o[a][j][2 * e] *= f;
+          o[a][j][2 * e + 1] *= f;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            float &p = s[a][j][2 * e + z];
+            p = exp2_approx(p - ref);
+            l[a][e] += p;
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        pf[a][2 * j] = pack2<DT>(s[a][j][0], s[a][j][1]);
+        pf[a][2 * j + 1] = pack2<DT>(s[a][j][2], s[a][j][3]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < ND; ++k) {
+      uint32_t vf[4];  // 16 keys x 16 elements
+      ldsm4t(vf, vt + (lane & 15) * kPitch + k * 32 + (lane >> 4) * 16);
+#pragma unroll
+      for (int a = 0; a < MT; ++a) {
+        mma16816<DT>(o[a][2 * k], pf[a][0], pf[a][1], pf[a][2], pf[a][3], vf[0], vf[1]);
+        mma16816<DT>(o[a][2 * k + 1], pf[a][0], pf[a][1], pf[a][2], pf[a][3], vf[2], vf[3]);
+      }
+    }
+    __syncwarp();  // every lane has read the tile before a later fetch overwrites it
+  }
+  cp_wait<0>();
+  __syncthreads();
+
+  // join the four warps: one row of tiles at a time
+  constexpr int kCols = ND * 16;
+  float *so = reinterpret_cast<float *>(smem);           // [kWarps][16][kCols]
+  float2 *sml = reinterpret_cast<float2 *>(so + kWarps * 16 * kCols);  // [kWarps][16]
+  static_assert((kWarps * 16 * kCols + 2 * kWarps * 16) * 4 <= kWarps * kStages * kTileBytes, "fits the rings");
+#pragma unroll
+  for (int a = 0; a < MT; ++a) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float s = l[a][e];
+      s += __shfl_xor_sync(0xffffffffu, s, 1);
+      s += __shfl_xor_sync(0xffffffffu, s, 2);
+      if (q == 0) sml[warp * 16 + g + e * 8] = make_float2(m[a][e], s);
+#pragma unroll
+      for (int j = 0; j < 2 * ND; ++j)
+        *reinterpret_cast<float2 *>(so + (warp * 16 + g + e * 8) * kCols + j * 8 + q * 2) =
+            make_float2(o[a][j][2 * e], o[a][j][2 * e + 1]);
+    }
+    __syncthreads();
+    for (int r = warp; r < 16; r += kWarps) {
+      const int row = row0 + a * 16 + r;
+      if (row >= rows) break;
+      float mm = -INFINITY, f[kWarps], ll = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) mm = fmaxf(mm, sml[w * 16 + r].x);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 v = sml[w * 16 + r];
+        f[w] = v.x > -INFINITY ? exp2_approx(v.x - mm) : 0.0f;
+        ll += f[w] * v.y;
+      }
+      const int64_t at = (int64_t)part * d.n_tokens * d.heads + (int64_t)(rq.t0 + row / G) * d.heads + hk * G + row % G;
+      for (int c = lane; c < D; c += 32) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) v += f[w] * so[(w * 16 + r) * kCols + c];
+        P.o[at * D + c] = v;
+      }
+      if (lane == 0) P.ml[at] = make_float2(mm, ll);
+    }
+    __syncthreads();
+  }
+}
+
+// out[t, h] = sum over the parts, one warp per (token, head).
+template <int DT>
+__global__ void __launch_bounds__(256) attend_merge_kernel(const __grid_constant__ AttendPlan P) {
+  const wt_attend_desc &d = P.d;
+  const int lane = threadIdx.x & 31;
+  const int b = blockIdx.y;
+  const Request rq = request_of(d, b, nullptr, false);
+  const int i = blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (i >= rq.n * d.heads) return;
+  const int64_t row = (int64_t)rq.t0 * d.heads + i, rows = (int64_t)d.n_tokens * d.heads;
+  const int own = P.own_splits ? (rq.len + P.own_len - 1) / P.own_len : 0, all = own + P.pre_splits;
+  const int D = d.head_dim;
+  auto part = [&](int k) { return (int64_t)(k < own ? k : P.own_splits + k - own) * rows + row; };
+  float m = -INFINITY;
+  for (int k = lane; k < all; k += 32) m = fmaxf(m, P.ml[part(k)].x);
+#pragma unroll
+  for (int s = 16; s; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+  float o[4] = {0, 0, 0, 0}, l = 0.0f;
+  for (int k = 0; k < all; ++k) {
+    const float2 v = P.ml[part(k)];
+    if (v.x == -INFINITY) continue;
+    const float f = exp2_approx(v.x - m);
+    l += f * v.y;
+    const float *src = P.o + part(k) * D;
+    if (lane * 4 < D) {
+      const float4 x = *reinterpret_cast<const float4 *>(src + lane * 4);
+      o[0] += f * x.x, o[1] += f * x.y, o[2] += f * x.z, o[3] += f * x.w;
+    }
+  }
+  if (lane * 4 < D) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    uint16_t *dst = static_cast<uint16_t *>(d.out) + (row / d.heads) * d.out_stride + (row % d.heads) * D + lane * 4;
+    *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<DT>(o[0] * inv, o[1] * inv), pack2<DT>(o[2] * inv, o[3] * inv));
+  }
+}
+
+template <int ND>
+constexpr size_t warp_smem() {
+  return (size_t)kWarps * kStages * 2 * kKeys * (ND * 32 + 16);
+}
+
+template <int DT, int ND>
+cudaError_t run_warp(const AttendPlan &P, cudaStream_t s) {
+  const unsigned grid = (unsigned)(P.d.kv_heads * P.row_tiles * (P.d.n_req * P.own_splits + P.pre_splits));
+  if (grid == 0) return cudaSuccess;
+  if (P.rows_tile == 16) attend_warp_kernel<DT, ND, 1><<<grid, kThreads, warp_smem<ND>(), s>>>(P);
+  else attend_warp_kernel<DT, ND, 2><<<grid, kThreads, warp_smem<ND>(), s>>>(P);
+  return cudaGetLastError();
+}
+
+template <int DT>
+cudaError_t run_dim(const AttendPlan &P, cudaStream_t s) {
+  if (P.d.head_dim <= 64) return run_warp<DT, 4>(P, s);
+  if (P.d.head_dim <= 96) return run_warp<DT, 6>(P, s);
+  return run_warp<DT, 8>(P, s);
+}
+
+template <int DT, int ND>
+cudaError_t prepare_warp() {
+  cudaError_t e = cudaFuncSetAttribute(attend_warp_kernel<DT, ND, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)warp_smem<ND>());
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(attend_warp_kernel<DT, ND, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)warp_smem<ND>());
+  return e;
+}
+
+}  // namespace
+
+cudaError_t attend_prepare() {
+  cudaError_t e = prepare_warp<WT_BF16, 4>();
+  if (e == cudaSuccess) e = prepare_warp<WT_BF16, 6>();
+  if (e == cudaSuccess) e = prepare_warp<WT_BF16, 8>();
+  if (e == cudaSuccess) e = prepare_warp<WT_F16, 4>();
+  if (e == cudaSuccess) e = prepare_warp<WT_F16, 6>();
+  if (e == cudaSuccess) e = prepare_warp<WT_F16, 8>();
+  return e;
+}
+
+cudaError_t launch_attend_warp(const AttendPlan &P, cudaStream_t s) {
+  return P.d.dtype == WT_BF16 ? run_dim<WT_BF16>(P, s) : run_dim<WT_F16>(P, s);
+}
+
+cudaError_t launch_attend_merge(const AttendPlan &P, cudaStream_t s) {
+  const dim3 grid((unsigned)((P.d.max_new * P.d.heads + 7) / 8), (unsigned)P.d.n_req);
+  if (P.d.dtype == WT_BF16) attend_merge_kernel<WT_BF16><<<grid, 256, 0, s>>>(P);
+  else attend_merge_kernel<WT_F16><<<grid, 256, 0, s>>>(P);
+  return cudaGetLastError();
+}
+
+}  // namespace wt

@@ -46,6 +46,7 @@
 #include "wt_fnv.h"
 #include "wt_kernels.h"
 #include "wt_q8rows.h"
+#include "wt_serve.h"
 
 #ifndef MADV_POPULATE_READ
 #define MADV_POPULATE_READ 22
@@ -431,6 +432,17 @@ struct Ring {
 
 Ring g_ring[64];
 
+// Scratch memory of the serving calls on one stream.  `done` follows its latest use outside a
+// capture; one taken for a capture belongs to that graph until the handle closes.
+struct Workspace {
+  unsigned long long capture_id = 0;  // nonzero: of that stream capture
+  unsigned long long stream_id = 0;   // the stream's number; its address in a capture
+  void *p = nullptr;
+  size_t n = 0;
+  cudaEvent_t done = nullptr;
+  bool used = false;
+};
+
 }  // namespace
 
 struct wt_handle {
@@ -462,6 +474,7 @@ struct wt_handle {
   int *status = nullptr;
   std::vector<cudaEvent_t> events;
   std::list<Plan *> plans;
+  std::vector<Workspace *> workspaces;  // of the serving calls (wt_serve.h), one per stream
   std::atomic<uint64_t> kernel_launches{0};
   wt_open_phases open_times{};
   std::mutex mu;
@@ -626,6 +639,7 @@ int prepare_device(int dev) {
     CU(wt::gemm_cols_umma_prepare());
     CU(wt::gemm_q8_rows_prepare());
     CU(wt::gemm_short_prepare());
+    CU(wt::serve_prepare());
     g_prepared[dev] = true;
   }
   return WT_OK;
@@ -2260,6 +2274,15 @@ int run_plan(wt_handle *h, Plan *P, const wt_gemv_desc *d, cudaStream_t s, bool 
   return WT_OK;
 }
 
+void destroy_workspace(int dev, Workspace *w) {
+  if (w->done) {
+    if (w->used) cudaEventSynchronize(w->done);
+    ev_destroy(w->done);
+  }
+  cached_free(false, dev, w->p, w->n);
+  delete w;
+}
+
 int close_impl(wt_handle *h) {
   int rc = WT_OK;
   if (!h->host_only && h->device >= 0) {
@@ -2277,6 +2300,8 @@ int close_impl(wt_handle *h) {
     h->trace.clear();
     for (Plan *P : h->plans) destroy_plan(P);
     h->plans.clear();
+    for (Workspace *w : h->workspaces) destroy_workspace(h->device, w);
+    h->workspaces.clear();
     for (cudaEvent_t e : h->events) ev_destroy(e);
     h->events.clear();
     status_give(h->device, h->status);
@@ -2315,6 +2340,140 @@ bool wt::fault_injected(const char *site) {
   if (len != strlen(site) || strncmp(e, site, len) != 0) return false;
   const int n = colon ? atoi(colon + 1) : 1;
   return ++count == n;
+}
+
+// ------------------------------------------------------------------ what wt_serve.cpp needs of a handle
+int wt::serve_error(int code, const char *fmt, ...) {
+  char buf[1024];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return set_err(code, "%s", buf);
+}
+
+int wt::serve_cuda_error(cudaError_t e, const char *what) { return cuda_err(e, what); }
+
+int wt::serve_context(wt_handle *h, const char *call, ServeContext *out) {
+  if (!h) return set_err(WT_EINVAL, "%s: NULL handle", call);
+  if (h->host_only) return set_err(WT_ENOTSUP, "%s: handle was opened host-only", call);
+  *out = {h->device, h->status};
+  return WT_OK;
+}
+
+bool wt::serve_inside_mapping(const wt_handle *h, const void *p, uint64_t n) {
+  return !h->by_base.empty() && inside_mapping(h, p, n);
+}
+
+bool wt::serve_range_ok(const void *p, uint64_t n) {
+  RangeCache c;
+  return device_range_ok(p, n, c);
+}
+
+void wt::serve_lock(wt_handle *h) { h->mu.lock(); }
+void wt::serve_unlock(wt_handle *h) { h->mu.unlock(); }
+
+void wt::serve_launched(wt_handle *h, int kernels) { h->kernel_launches += (uint64_t)kernels; }
+
+int wt::serve_tensor_map(void *out, const void *base, int rank, const uint64_t *dims, const uint64_t *strides,
+                         const uint32_t *box) {
+  EncodeTiledFn fn = encode_tiled();
+  if (!fn) return set_err(WT_ECUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  cuuint64_t d[5], st[5];
+  cuuint32_t bx[5], es[5];
+  for (int i = 0; i < rank; ++i) {
+    d[i] = dims[i];
+    bx[i] = box[i];
+    es[i] = 1;
+    if (i) st[i - 1] = strides[i - 1];
+  }
+  CUtensorMap m;
+  const CUresult r = fn(&m, CU_TENSOR_MAP_DATA_TYPE_UINT16, (cuuint32_t)rank, const_cast<void *>(base), d, st, bx, es,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return set_err(WT_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+  memcpy(out, &m, sizeof m);
+  return WT_OK;
+}
+
+int wt::serve_workspace(wt_handle *h, cudaStream_t s, size_t n, ServeWorkspace *out) {
+  *out = {};
+  cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+  unsigned long long capture = 0, id = 0;
+  if (cudaStreamGetCaptureInfo(s, &cs, &capture) != cudaSuccess) {
+    cudaGetLastError();
+    cs = cudaStreamCaptureStatusNone;
+  }
+  if (cs != cudaStreamCaptureStatusActive) capture = 0;
+  // a stream's number is its own for good, unlike its address, but cannot be asked for in a capture
+  if (capture) id = reinterpret_cast<uintptr_t>(s);
+  else CU(cudaStreamGetId(s, &id));
+  // a capture forbids allocations that might synchronise, unless the thread allows them
+  struct Relax {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    bool on;
+    explicit Relax(bool b) : on(b) {
+      if (on) cudaThreadExchangeStreamCaptureMode(&mode);
+    }
+    ~Relax() {
+      if (on) cudaThreadExchangeStreamCaptureMode(&mode);
+    }
+  };
+  Workspace *w = nullptr;
+  size_t eager = 0;
+  for (Workspace *q : h->workspaces) {
+    if (q->capture_id == capture && q->stream_id == id && q->n >= n) w = q;
+    eager += q->capture_id == 0;
+  }
+  if (w) {
+    *out = {w->p, w};
+    return WT_OK;
+  }
+  Relax relax(capture != 0);
+  if (!capture) {
+    // a smaller one of this stream, or the oldest of too many streams, goes once its work is done
+    constexpr size_t kStreams = 8;
+    for (size_t i = 0; i < h->workspaces.size();) {
+      Workspace *q = h->workspaces[i];
+      if (q->capture_id == 0 && (q->stream_id == id || eager >= kStreams)) {
+        h->workspaces.erase(h->workspaces.begin() + (long)i);
+        destroy_workspace(h->device, q);
+        --eager;
+      } else {
+        ++i;
+      }
+    }
+  }
+  try {
+    size_t cap = 1 << 16;
+    while (cap < n) cap *= 2;
+    std::unique_ptr<Workspace> own(new Workspace);
+    h->workspaces.reserve(h->workspaces.size() + 1);
+    own->stream_id = id;
+    own->capture_id = capture;
+    if (!capture) CU(ev_create(&own->done, cudaEventDisableTiming));
+    const cudaError_t e = wt::fault_injected("alloc") ? cudaErrorMemoryAllocation : cached_alloc(false, h->device, &own->p, cap);
+    if (e != cudaSuccess) {
+      cudaGetLastError();
+      ev_destroy(own->done);
+      return set_err(WT_ENOMEM, "a workspace of %zu bytes: %s", cap, cudaGetErrorString(e));
+    }
+    own->n = cap;
+    w = own.release();
+    h->workspaces.push_back(w);
+  } catch (const std::bad_alloc &) {
+    return set_err(WT_ENOMEM, "out of host memory");
+  }
+  *out = {w->p, w};
+  return WT_OK;
+}
+
+int wt::serve_workspace_done(wt_handle *h, cudaStream_t s, const ServeWorkspace &sw) {
+  Workspace *w = static_cast<Workspace *>(sw.entry);
+  if (!w || w->capture_id) return WT_OK;
+  CU(cudaEventRecord(w->done, s));
+  w->used = true;
+  return WT_OK;
 }
 
 // ====================================================================== C ABI

@@ -1,0 +1,299 @@
+// C ABI of a serving step (include/wt_serve.h): argument checks, splits and launches.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "wt_kernels.h"
+#include "wt_serve.h"
+
+namespace {
+
+using wt::serve_error;
+
+#define CU(call)                                                    \
+  do {                                                              \
+    cudaError_t e_ = (call);                                        \
+    if (e_ != cudaSuccess) return wt::serve_cuda_error(e_, #call);  \
+  } while (0)
+
+struct Lock {
+  wt_handle *h;
+  explicit Lock(wt_handle *hh) : h(hh) { wt::serve_lock(h); }
+  ~Lock() { wt::serve_unlock(h); }
+};
+
+bool aligned(const void *p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// Bytes from the first to one past the last element of `rows` rows of `row` elements, `pitch`
+// elements apart.  Sizes are below 2^31 and pitches below 2^40, so nothing overflows.
+uint64_t extent(uint64_t rows, uint64_t pitch, uint64_t row, uint64_t elem) {
+  return rows == 0 || row == 0 ? 0 : ((rows - 1) * pitch + row) * elem;
+}
+constexpr int64_t kMaxPitch = 1ll << 40;
+
+int check_buffer(const char *call, const char *name, const void *p, uint64_t n, uintptr_t align) {
+  if (n == 0) return WT_OK;
+  if (!p) return serve_error(WT_EINVAL, "%s: %s is NULL", call, name);
+  if (!aligned(p, align)) return serve_error(WT_EINVAL, "%s: %s is not on a %d-byte boundary", call, name, (int)align);
+  if (!wt::serve_range_ok(p, n)) return serve_error(WT_EINVAL, "%s: %s runs past the end of its device allocation", call, name);
+  return WT_OK;
+}
+
+int check_output(wt_handle *h, const char *call, const char *name, const void *p, uint64_t n, uintptr_t align) {
+  int rc = check_buffer(call, name, p, n, align);
+  if (rc == WT_OK && n && wt::serve_inside_mapping(h, p, n))
+    rc = serve_error(WT_EINVAL, "%s: %s lies inside a read-only mapping", call, name);
+  return rc;
+}
+
+bool overlap(const void *a, uint64_t na, const void *b, uint64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return na && nb && x < y + nb && y < x + na;
+}
+
+#define CHECK(expr)          \
+  do {                       \
+    int rc_ = (expr);        \
+    if (rc_) return rc_;     \
+  } while (0)
+
+int check_adapt(wt_handle *h, const wt_adapt_desc &d, size_t i) {
+  const char *call = "wt_adapt";
+  if (d.dtype != WT_BF16 && d.dtype != WT_F16)
+    return serve_error(d.dtype >= WT_F32 && d.dtype <= WT_U8 ? WT_ENOTSUP : WT_EINVAL,
+                       "%s: desc %zu: dtype %d: x, A and B are bf16 or f16", call, i, d.dtype);
+  if (d.T < 0 || d.K < 0 || d.M < 0 || d.S < 0 || d.R < 0 || d.S > WT_ADAPT_MAX_SLOTS || d.R > WT_ADAPT_MAX_RANK)
+    return serve_error(WT_EINVAL, "%s: desc %zu: T %d, K %d, M %d, S %d (up to %d) or R %d (up to %d) out of range", call, i,
+                       d.T, d.K, d.M, d.S, WT_ADAPT_MAX_SLOTS, d.R, WT_ADAPT_MAX_RANK);
+  const uint64_t T = d.T, K = d.K, M = d.M, S = d.S, R = d.R;
+  if (d.ldx < d.K || d.ldy < d.M || (d.base && d.ldbase < d.M) || d.a_slot < (int64_t)(R * K) || d.b_slot < (int64_t)(M * R) ||
+      d.ldx > kMaxPitch || d.ldy > kMaxPitch || d.ldbase > kMaxPitch || d.a_slot > kMaxPitch || d.b_slot > kMaxPitch)
+    return serve_error(WT_EINVAL, "%s: desc %zu: a pitch is shorter than its row, or not below 2^40", call, i);
+  if (T == 0 || M == 0) return WT_OK;
+  const uint64_t yn = extent(T, d.ldy, M, 4), bn = d.base ? extent(T, d.ldbase, M, 4) : 0;
+  CHECK(check_output(h, call, "y", d.y, yn, 4));
+  CHECK(check_buffer(call, "base", d.base, bn, 4));
+  if (d.base == d.y) {
+    if (d.ldbase != d.ldy) return serve_error(WT_EINVAL, "%s: desc %zu: base is y, with another pitch", call, i);
+  } else if (overlap(d.y, yn, d.base, bn)) {
+    return serve_error(WT_EINVAL, "%s: desc %zu: base overlaps y", call, i);
+  }
+  CHECK(check_buffer(call, "slot", d.slot, 4 * T, 4));
+  if (S == 0 || R == 0) return WT_OK;
+  CHECK(check_buffer(call, "x", d.x, extent(T, d.ldx, K, 2), 2));
+  CHECK(check_buffer(call, "A", d.A, extent(S, d.a_slot, R * K, 2), 2));
+  CHECK(check_buffer(call, "B", d.B, extent(S, d.b_slot, M * R, 2), 2));
+  if (d.rank) CHECK(check_buffer(call, "rank", d.rank, 4 * S, 4));
+  if (d.scale) CHECK(check_buffer(call, "scale", d.scale, 4 * S, 4));
+  return WT_OK;
+}
+
+int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
+  wt::ServeContext ctx;
+  CHECK(wt::serve_context(h, "wt_adapt", &ctx));
+  if (n && !d) return serve_error(WT_EINVAL, "wt_adapt: NULL descriptors");
+  for (size_t i = 0; i < n; ++i) CHECK(check_adapt(h, d[i], i));
+  for (size_t i = 0; i < n;) {
+    // up to 8 descriptors of one type a launch
+    wt::AdaptLaunch L;
+    L.n = 0;
+    int max_R = 0, max_T = 0;
+    const int dtype = d[i].dtype;
+    size_t j = i;
+    for (; j < n && L.n < wt::kAdaptProjs && d[j].dtype == dtype; ++j) {
+      if (d[j].T == 0 || d[j].M == 0) continue;
+      L.p[L.n++].d = d[j];
+      max_R = std::max(max_R, d[j].R);
+      max_T = std::max(max_T, d[j].T);
+    }
+    i = j;
+    if (L.n == 0) continue;
+    uint64_t all = 0;
+    const int tile = wt::adapt_tile(max_T);
+    for (int k = 0; k < L.n; ++k) {
+      wt::AdaptProj &P = L.p[k];
+      const wt_adapt_desc &e = P.d;
+      const bool copy = e.base != e.y;
+      P.items = (uint32_t)(std::min(e.S + (copy ? 1 : 0), e.T) + e.T / tile);
+      all += P.items;
+      P.vec = 0;
+      if (e.K % 8 == 0 && e.ldx % 8 == 0 && e.a_slot % 8 == 0 && aligned(e.x, 16) && aligned(e.A, 16)) P.vec |= 1;
+      // a lane reads 4 elements of a row of B where no rank is above 16, else 8
+      const int el = max_R <= 16 ? 4 : 8;
+      if (e.R % el == 0 && e.b_slot % el == 0 && aligned(e.B, 2 * el)) P.vec |= 2;
+      if (e.ldy % 4 == 0 && aligned(e.y, 16) && (!e.base || (e.ldbase % 4 == 0 && aligned(e.base, 16)))) P.vec |= 4;
+    }
+    if (all > (1u << 27)) return serve_error(WT_EINVAL, "wt_adapt: %llu work items in one launch", (unsigned long long)all);
+    CU(wt::launch_adapt(L, max_R, max_T, ctx.status, s));
+    wt::serve_launched(h, 1);
+  }
+  return WT_OK;
+}
+
+int check_attend(wt_handle *h, const wt_attend_desc &d) {
+  const char *call = "wt_attend";
+  if (d.dtype != WT_BF16 && d.dtype != WT_F16)
+    return serve_error(d.dtype >= WT_F32 && d.dtype <= WT_U8 ? WT_ENOTSUP : WT_EINVAL,
+                       "%s: dtype %d: queries and caches are bf16 or f16", call, d.dtype);
+  if (d.n_req < 0 || d.n_req > 65535 || d.n_tokens < 0 || d.max_new < 0 || d.prefix_len < 0 || d.prefix_len > 0x7fffffff ||
+      d.max_len < 0 || d.n_pages < 0)
+    return serve_error(WT_EINVAL, "%s: n_req %d, n_tokens %d, max_new %d, prefix_len %lld, max_len %d or n_pages %d out of range",
+                       call, d.n_req, d.n_tokens, d.max_new, (long long)d.prefix_len, d.max_len, d.n_pages);
+  if (d.heads < 1 || d.kv_heads < 1 || d.heads > 65536 || d.heads % d.kv_heads || d.heads / d.kv_heads > 128)
+    return serve_error(WT_EINVAL, "%s: heads %d is not up to 128 times kv_heads %d", call, d.heads, d.kv_heads);
+  if (d.head_dim < 8 || d.head_dim % 8)
+    return serve_error(WT_EINVAL, "%s: head_dim %d is not a multiple of 8", call, d.head_dim);
+  if (d.head_dim > 128) return serve_error(WT_ENOTSUP, "%s: head_dim %d is above 128", call, d.head_dim);
+  if (!std::isfinite(d.scale)) return serve_error(WT_EINVAL, "%s: scale is not finite", call);
+  const int64_t row = (int64_t)d.heads * d.head_dim, D = d.head_dim;
+  if (d.q_stride < row || d.out_stride < row || d.q_stride % 8 || d.out_stride % 8 || d.q_stride > kMaxPitch ||
+      d.out_stride > kMaxPitch)
+    return serve_error(WT_EINVAL, "%s: token pitches %lld and %lld are not multiples of 8 of at least heads * head_dim", call,
+                       (long long)d.q_stride, (long long)d.out_stride);
+  if ((int64_t)d.n_tokens * d.heads > 0x7fffffff) return serve_error(WT_EINVAL, "%s: n_tokens * heads above 2^31-1", call);
+  if (d.n_req == 0 || d.n_tokens == 0 || d.max_new == 0) return WT_OK;
+  CHECK(check_buffer(call, "q", d.q, extent(d.n_tokens, d.q_stride, row, 2), 16));
+  CHECK(check_output(h, call, "out", d.out, extent(d.n_tokens, d.out_stride, row, 2), 16));
+  CHECK(check_buffer(call, "begin", d.begin, 4 * ((uint64_t)d.n_req + 1), 4));
+  if (d.prefix_len) {
+    if (d.prefix_head < D || d.prefix_head % 8 || d.prefix_stride < D || d.prefix_stride % 8 || d.prefix_head > kMaxPitch ||
+        d.prefix_stride > kMaxPitch)
+      return serve_error(WT_EINVAL, "%s: prefix pitches %lld and %lld are not multiples of 8 of at least head_dim", call,
+                         (long long)d.prefix_stride, (long long)d.prefix_head);
+    // dense either way round: [key, head, dim] or [head, key, dim]
+    const uint64_t n = 2 * ((uint64_t)(d.prefix_len - 1) * d.prefix_stride + (uint64_t)(d.kv_heads - 1) * d.prefix_head + D);
+    CHECK(check_buffer(call, "prefix_k", d.prefix_k, n, 16));
+    CHECK(check_buffer(call, "prefix_v", d.prefix_v, n, 16));
+  }
+  if (d.max_len) {
+    if (d.page < 1 || d.table_stride < 0 || d.table_stride > 0x7fffffff || (int64_t)d.max_len > d.table_stride * d.page)
+      return serve_error(WT_EINVAL, "%s: max_len %d does not fit %lld pages of %d keys", call, d.max_len,
+                         (long long)d.table_stride, d.page);
+    const uint64_t n = (uint64_t)d.n_pages * d.page * d.kv_heads * D * 2;
+    CHECK(check_buffer(call, "k_pages", d.k_pages, n, 16));
+    CHECK(check_buffer(call, "v_pages", d.v_pages, n, 16));
+    CHECK(check_buffer(call, "table", d.table, extent(d.n_req, d.table_stride, d.table_stride, 4), 4));
+    CHECK(check_buffer(call, "len", d.len, 4 * (uint64_t)d.n_req, 4));
+  }
+  return WT_OK;
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
+  wt::ServeContext ctx;
+  CHECK(wt::serve_context(h, "wt_attend", &ctx));
+  if (!dp) return serve_error(WT_EINVAL, "wt_attend: NULL descriptor");
+  CHECK(check_attend(h, *dp));
+  wt::AttendPlan P = {};
+  P.d = *dp;
+  wt_attend_desc &d = P.d;
+  if (d.n_req == 0 || d.n_tokens == 0 || d.max_new == 0) return WT_OK;
+  d.max_new = std::min(d.max_new, d.n_tokens);
+  P.G = d.heads / d.kv_heads;
+  P.status = ctx.status;
+  const int64_t own_rows = (int64_t)d.max_new * P.G, pre_rows = (int64_t)d.n_tokens * P.G;
+  P.rows_tile = std::max(d.max_len ? own_rows : 0, d.prefix_len ? pre_rows : 0) <= 16 ? 16 : 32;
+  P.row_tiles = (int)ceil_div(std::max(d.max_len ? own_rows : 0, d.prefix_len ? pre_rows : 0), P.rows_tile);
+  // Splits: 4 CTAs per SM over all of them, of at least 64 keys (one tile for each warp).
+  const int64_t want = 4 * wt::num_sms();
+  auto split = [&](int64_t keys, int64_t ctas, int &splits, int &len) {
+    const int64_t n = std::max<int64_t>(1, std::min(ceil_div(keys, 64), ceil_div(want, ctas)));
+    len = (int)(ceil_div(ceil_div(keys, n), 64) * 64);
+    splits = (int)ceil_div(keys, len);
+  };
+  if (d.max_len) split(d.max_len, (int64_t)d.n_req * d.kv_heads * ceil_div(own_rows, P.rows_tile), P.own_splits, P.own_len);
+  if (d.prefix_len) split(d.prefix_len, d.kv_heads * ceil_div(pre_rows, P.rows_tile), P.pre_splits, P.pre_len);
+  const int64_t parts = P.own_splits + P.pre_splits, rows = (int64_t)d.n_tokens * d.heads;
+  if ((int64_t)d.kv_heads * P.row_tiles * ((int64_t)d.n_req * P.own_splits + P.pre_splits) > 0x7fffffff)
+    return serve_error(WT_EINVAL, "wt_attend: too many tokens, heads and keys for one launch");
+  const size_t ob = (size_t)(parts * rows * d.head_dim * 4 + 255) / 256 * 256;
+  Lock lock(h);
+  wt::ServeWorkspace w;
+  CHECK(wt::serve_workspace(h, s, ob + (size_t)(parts * rows) * sizeof(float2), &w));
+  P.o = static_cast<float *>(w.p);
+  P.ml = reinterpret_cast<float2 *>(static_cast<uint8_t *>(w.p) + ob);
+  cudaError_t e = parts ? wt::launch_attend_warp(P, s) : cudaSuccess;
+  if (e == cudaSuccess) e = wt::launch_attend_merge(P, s);
+  const int rc = wt::serve_workspace_done(h, s, w);
+  CU(e);
+  wt::serve_launched(h, parts ? 2 : 1);
+  return rc;
+}
+
+int probs_impl(wt_handle *h, const wt_probs_desc *d, cudaStream_t s) {
+  const char *call = "wt_probs";
+  wt::ServeContext ctx;
+  CHECK(wt::serve_context(h, call, &ctx));
+  if (!d) return serve_error(WT_EINVAL, "%s: NULL descriptor", call);
+  if (d->rows < 0 || d->rows > (1 << 27) || d->vocab < 0 || d->vocab > (1 << 30) || d->ldl < d->vocab || d->ldp < d->vocab ||
+      d->ldl > kMaxPitch || d->ldp > kMaxPitch)
+    return serve_error(WT_EINVAL, "%s: rows %d, vocab %d or a pitch out of range", call, d->rows, d->vocab);
+  if (d->rows == 0 || d->vocab == 0) return WT_OK;
+  const uint64_t ln = extent(d->rows, d->ldl, d->vocab, 4), pn = extent(d->rows, d->ldp, d->vocab, 4);
+  CHECK(check_buffer(call, "logits", d->logits, ln, 4));
+  CHECK(check_output(h, call, "p", d->p, pn, 4));
+  if (d->p == d->logits ? d->ldp != d->ldl : overlap(d->p, pn, d->logits, ln))
+    return serve_error(WT_EINVAL, "%s: p overlaps the logits", call);
+  if (d->temp) CHECK(check_buffer(call, "temp", d->temp, 4 * (uint64_t)d->rows, 4));
+  CU(wt::launch_probs(*d, s));
+  wt::serve_launched(h, 1);
+  return WT_OK;
+}
+
+int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {
+  const char *call = "wt_verify";
+  wt::ServeContext ctx;
+  CHECK(wt::serve_context(h, call, &ctx));
+  if (!d) return serve_error(WT_EINVAL, "%s: NULL descriptor", call);
+  if (d->n_req < 0 || d->n_req > (1 << 24) || d->n_drafted < 0 || d->max_draft < 0 || d->max_draft > (1 << 20) || d->vocab < 1 ||
+      d->vocab > WT_VERIFY_MAX_VOCAB || d->ldp < d->vocab || d->ldp > kMaxPitch ||
+      (d->q && (d->ldq < d->vocab || d->ldq > kMaxPitch)))
+    return serve_error(WT_EINVAL, "%s: n_req %d, n_drafted %d, max_draft %d, vocab %d (up to %d) or a pitch out of range", call,
+                       d->n_req, d->n_drafted, d->max_draft, d->vocab, WT_VERIFY_MAX_VOCAB);
+  if (d->n_req == 0) return WT_OK;
+  const uint64_t B = d->n_req, n = d->n_drafted;
+  CHECK(check_buffer(call, "p", d->p, extent(n + B, d->ldp, d->vocab, 4), 4));
+  if (d->q) CHECK(check_buffer(call, "q", d->q, extent(n, d->ldq, d->vocab, 4), 4));
+  CHECK(check_buffer(call, "drafted", d->drafted, 4 * n, 4));
+  CHECK(check_buffer(call, "begin", d->begin, 4 * (B + 1), 4));
+  CHECK(check_buffer(call, "u", d->u, 4 * n, 4));
+  CHECK(check_buffer(call, "u_draw", d->u_draw, 4 * B, 4));
+  CHECK(check_output(h, call, "accepted", d->accepted, 4 * B, 4));
+  CHECK(check_output(h, call, "tokens", d->tokens, 4 * B * ((uint64_t)d->max_draft + 1), 4));
+  CU(wt::launch_verify(*d, ctx.status, s));
+  wt::serve_launched(h, 1);
+  return WT_OK;
+}
+
+}  // namespace
+
+cudaError_t wt::serve_prepare() {
+  cudaError_t e = adapt_prepare();
+  if (e == cudaSuccess) e = attend_prepare();
+  return e;
+}
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+int wt_adapt(wt_handle *h, const wt_adapt_desc *d, size_t n, void *stream) {
+  return adapt_impl(h, d, n, static_cast<cudaStream_t>(stream));
+}
+
+int wt_attend(wt_handle *h, const wt_attend_desc *d, void *stream) {
+  return attend_impl(h, d, static_cast<cudaStream_t>(stream));
+}
+
+int wt_probs(wt_handle *h, const wt_probs_desc *d, void *stream) {
+  return probs_impl(h, d, static_cast<cudaStream_t>(stream));
+}
+
+int wt_verify(wt_handle *h, const wt_verify_desc *d, void *stream) {
+  return verify_impl(h, d, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
+#pragma GCC visibility pop

@@ -1,0 +1,81 @@
+// Internal interface between wt_serve.cpp (argument checks, routing), the handle's owner
+// (wt_host.cpp) and the kernels of a serving step.  Not part of the public C ABI.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "../../include/wt_serve.h"
+
+namespace wt {
+
+// ---------------------------------------------------------------- the handle (wt_host.cpp)
+struct ServeContext {
+  int device;
+  int *status;  // device status word
+};
+// Refuses NULL and host-only handles.
+int serve_context(wt_handle *h, const char *call, ServeContext *out);
+bool serve_inside_mapping(const wt_handle *h, const void *p, uint64_t n);
+// false only when [p, p + n) starts inside a device allocation and runs past its end
+bool serve_range_ok(const void *p, uint64_t n);
+void serve_launched(wt_handle *h, int kernels);
+// The handle's mutex, held from serve_workspace to serve_workspace_done.
+void serve_lock(wt_handle *h);
+void serve_unlock(wt_handle *h);
+// A workspace of at least n bytes for calls on stream s (256-byte aligned).  The caller makes the
+// matching serve_workspace_done after its last launch (also after a failed one).
+struct ServeWorkspace {
+  void *p = nullptr;
+  void *entry = nullptr;
+};
+int serve_workspace(wt_handle *h, cudaStream_t s, size_t n, ServeWorkspace *out);
+int serve_workspace_done(wt_handle *h, cudaStream_t s, const ServeWorkspace &w);
+// cuTensorMapEncodeTiled of a 16-bit tensor with the 128-byte swizzle; strides in bytes for dims 1..
+int serve_tensor_map(void *out, const void *base, int rank, const uint64_t *dims, const uint64_t *strides,
+                     const uint32_t *box);
+int serve_error(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+int serve_cuda_error(cudaError_t e, const char *what);
+
+cudaError_t serve_prepare();  // one-time function attributes of every kernel below
+
+// ---------------------------------------------------------------- wt_adapt.cu
+constexpr int kAdaptProjs = 8;  // projections of one launch
+struct AdaptProj {
+  wt_adapt_desc d;
+  uint32_t items;  // upper bound of (slot, token tile) work items
+  uint32_t vec;    // bit 0: A and x load in 16-byte vectors; bit 1: B does; bit 2: base and y do
+};
+struct AdaptLaunch {
+  AdaptProj p[kAdaptProjs];
+  int n;
+};
+cudaError_t adapt_prepare();
+int adapt_tile(int max_T);  // tokens of one work item
+cudaError_t launch_adapt(const AdaptLaunch &L, int max_R, int max_T, int *status, cudaStream_t s);
+
+// ---------------------------------------------------------------- wt_draw.cu
+cudaError_t launch_probs(const wt_probs_desc &d, cudaStream_t s);
+cudaError_t launch_verify(const wt_verify_desc &d, int *status, cudaStream_t s);
+
+// ---------------------------------------------------------------- wt_attend.cu
+// Partial results of one (token, head): O [head_dim] fp32 not yet divided by l, and (m, l) with m in
+// units of log2 (scores times scale log2 e).
+struct AttendPlan {
+  wt_attend_desc d;
+  int G;          // heads / kv_heads
+  int rows_tile;  // rows (token, head-in-group) of one CTA of the warp kernel: 16 or 32
+  int row_tiles;  // tiles that the longest request (or the prefix's rows) takes
+  int own_splits, own_len;  // own keys per split
+  int pre_splits, pre_len;  // prefix keys per split of the warp kernel (0: not taken there)
+  float *o;                 // [own_splits + pre_splits][n_tokens * heads][head_dim]
+  float2 *ml;               // [own_splits + pre_splits][n_tokens * heads]
+  int *status;
+};
+cudaError_t attend_prepare();
+cudaError_t launch_attend_warp(const AttendPlan &P, cudaStream_t s);
+cudaError_t launch_attend_merge(const AttendPlan &P, cudaStream_t s);
+
+}  // namespace wt

@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libwt.so (include/wt.h), same names as the C ABI.
+"""Thin ctypes binding of libwt.so (include/wt.h, wt_dlpack.h, wt_serve.h), same names as the C ABI.
 
 Argument marshalling only: every step of the path runs in the library's C++
 and CUDA code.  Pointers are plain integers (``tensor.data_ptr()``), streams
@@ -38,8 +38,11 @@ SYMBOLS = ("wt_last_error", "wt_abi_version", "wt_open", "wt_num_tensors", "wt_n
            "wt_checksum_plain", "wt_checksum_noalloc", "wt_device_status", "wt_residency",
            "wt_kernel_launches", "wt_trace", "wt_pass_stamps", "wt_open_times", "wt_live", "wt_close",
            # include/wt_dlpack.h
-           "wt_dlpack_file", "wt_dlpack_tensor", "wt_dlpack_release", "wt_dlpack_live")
+           "wt_dlpack_file", "wt_dlpack_tensor", "wt_dlpack_release", "wt_dlpack_live",
+           # include/wt_serve.h
+           "wt_adapt", "wt_attend", "wt_probs", "wt_verify")
 WT_DLPACK_DEVICE, WT_DLPACK_HOST = 0, 1
+WT_ADAPT_MAX_RANK, WT_ADAPT_MAX_SLOTS, WT_VERIFY_MAX_VOCAB = 128, 4096, 1 << 18
 kDLCPU, kDLCUDA = 1, 2
 
 
@@ -59,6 +62,40 @@ class GemvDesc(C.Structure):
     _fields_ = [("W", C.c_void_p), ("dtype", C.c_int32), ("cols", C.c_int32),
                 ("M", C.c_uint64), ("K", C.c_uint64), ("x", C.c_void_p), ("y", C.c_void_p),
                 ("wait_event", C.c_void_p), ("scale", C.c_void_p)]
+
+
+class AdaptDesc(C.Structure):
+    """wt_adapt_desc (serving.adapters makes one from tensors)."""
+    _fields_ = [("x", C.c_void_p), ("base", C.c_void_p), ("y", C.c_void_p), ("slot", C.c_void_p), ("A", C.c_void_p),
+                ("B", C.c_void_p), ("rank", C.c_void_p), ("scale", C.c_void_p), ("ldx", C.c_int64),
+                ("ldbase", C.c_int64), ("ldy", C.c_int64), ("a_slot", C.c_int64), ("b_slot", C.c_int64),
+                ("dtype", C.c_int32), ("T", C.c_int32), ("K", C.c_int32), ("M", C.c_int32), ("S", C.c_int32),
+                ("R", C.c_int32)]
+
+
+class AttendDesc(C.Structure):
+    """wt_attend_desc (serving.attention makes one from tensors)."""
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("begin", C.c_void_p), ("prefix_k", C.c_void_p),
+                ("prefix_v", C.c_void_p), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("table", C.c_void_p),
+                ("len", C.c_void_p), ("q_stride", C.c_int64), ("out_stride", C.c_int64), ("prefix_stride", C.c_int64),
+                ("prefix_head", C.c_int64), ("table_stride", C.c_int64), ("prefix_len", C.c_int64),
+                ("dtype", C.c_int32), ("n_req", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32),
+                ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page", C.c_int32),
+                ("n_pages", C.c_int32), ("max_len", C.c_int32), ("scale", C.c_float), ("pad", C.c_int32)]
+
+
+class ProbsDesc(C.Structure):
+    """wt_probs_desc (serving.probabilities makes one from tensors)."""
+    _fields_ = [("logits", C.c_void_p), ("p", C.c_void_p), ("temp", C.c_void_p), ("ldl", C.c_int64), ("ldp", C.c_int64),
+                ("rows", C.c_int32), ("vocab", C.c_int32)]
+
+
+class VerifyDesc(C.Structure):
+    """wt_verify_desc (serving.verification makes one from tensors)."""
+    _fields_ = [("p", C.c_void_p), ("q", C.c_void_p), ("drafted", C.c_void_p), ("begin", C.c_void_p), ("u", C.c_void_p),
+                ("u_draw", C.c_void_p), ("accepted", C.c_void_p), ("tokens", C.c_void_p), ("ldp", C.c_int64),
+                ("ldq", C.c_int64), ("n_req", C.c_int32), ("n_drafted", C.c_int32), ("max_draft", C.c_int32),
+                ("vocab", C.c_int32)]
 
 
 class LiveCounts(C.Structure):
@@ -129,6 +166,10 @@ def lib(path: str = LIB_PATH):
     L.wt_open_times.argtypes = [vp, C.POINTER(OpenPhases)]
     L.wt_live.argtypes = [C.POINTER(LiveCounts)]
     L.wt_close.argtypes = [vp]
+    L.wt_adapt.argtypes = [vp, C.POINTER(AdaptDesc), sz, vp]
+    L.wt_attend.argtypes = [vp, C.POINTER(AttendDesc), vp]
+    L.wt_probs.argtypes = [vp, C.POINTER(ProbsDesc), vp]
+    L.wt_verify.argtypes = [vp, C.POINTER(VerifyDesc), vp]
     L.wt_dlpack_file.argtypes = [C.c_char_p, C.c_int32, C.c_uint64, C.c_uint64, C.c_uint, C.POINTER(vp)]
     L.wt_dlpack_tensor.argtypes = [vp, sz, C.c_uint, C.POINTER(vp)]
     L.wt_dlpack_release.argtypes = [vp]
@@ -305,6 +346,26 @@ class Handle:
             rc = lib().wt_pass(self.ptr, (GemvDesc * max(1, n))(*descs), n, C.c_void_p(stream))
         if rc:
             _check(rc)
+
+    def adapt(self, descs, stream: int = 0):
+        """wt_adapt over a list of AdaptDesc, or a ctypes array of them (which a step that repeats
+        keeps: (AdaptDesc * n)(*descs) copies every descriptor)."""
+        n = len(descs)
+        if not isinstance(descs, C.Array):
+            descs = (AdaptDesc * max(1, n))(*descs)
+        _check(lib().wt_adapt(self.ptr, descs, n, stream))
+
+    def attend(self, desc: AttendDesc, stream: int = 0):
+        """wt_attend."""
+        _check(lib().wt_attend(self.ptr, C.byref(desc), stream))
+
+    def probs(self, desc: ProbsDesc, stream: int = 0):
+        """wt_probs."""
+        _check(lib().wt_probs(self.ptr, C.byref(desc), stream))
+
+    def verify(self, desc: VerifyDesc, stream: int = 0):
+        """wt_verify."""
+        _check(lib().wt_verify(self.ptr, C.byref(desc), stream))
 
     def checksum(self, ptrs: Sequence[int], nbytes: Sequence[int], out_dev: int, stream: int = 0,
                  plain: bool = False):
