@@ -325,20 +325,51 @@ __global__ void __launch_bounds__(256) attend_merge_kernel(const __grid_constant
   const int i = blockIdx.x * 8 + (threadIdx.x >> 5);
   if (i >= rq.n * d.heads) return;
   const int64_t row = (int64_t)rq.t0 * d.heads + i, rows = (int64_t)d.n_tokens * d.heads;
-  const int own = P.own_splits ? (rq.len + P.own_len - 1) / P.own_len : 0, all = own + P.pre_splits;
+  const int own = P.own_splits ? (rq.len + P.own_len - 1) / P.own_len : 0;
   const int D = d.head_dim;
-  auto part = [&](int k) { return (int64_t)(k < own ? k : P.own_splits + k - own) * rows + row; };
+  const float *o_of;
+  const float2 *ml_of;
+  // the parts: own splits, then the prefix's (those of the warp kernel, or the slots on tcgen05)
+  int all = own + P.pre_splits, x0 = 0, per = 1;
+  int64_t xrow = 0;
+  if (P.x.groups) {
+    const PrefixPlan &x = P.x;
+    const int hk = (int)(row % d.heads) / P.G;
+    const int r = (int)(row / d.heads) * P.G + (int)(row % d.heads) % P.G;
+    const int64_t total = (int64_t)x.kv_heads * x.tiles, start = (int64_t)hk * x.tiles;
+    int g0 = (int)(start * x.groups / total);
+    while (g0 + 1 < x.groups && total * (g0 + 1) / x.groups <= start) ++g0;
+    int g1 = g0 + 1;
+    while (g1 < x.groups && total * g1 / x.groups < start + x.tiles) ++g1;
+    per = x.apart ? 2 : 1;
+    all += (g1 - g0) * per;
+    x0 = (g0 + hk) * x.qtiles;
+    xrow = x.apart ? r : (int64_t)(r / x.tile_rows) * 128 + r % x.tile_rows;
+  }
+  auto find = [&](int k) -> int64_t {  // the part's row
+    o_of = P.o, ml_of = P.ml;
+    if (k < own) return (int64_t)k * rows + row;
+    k -= own;
+    if (k < P.pre_splits) return (int64_t)(P.own_splits + k) * rows + row;
+    o_of = P.x.o, ml_of = P.x.ml;
+    // apart: the two streams of a slot are tiles of their own; else a slot's tiles are row tiles
+    return ((int64_t)x0 + (int64_t)(k / per) * P.x.qtiles + k % per) * 128 + xrow;
+  };
   float m = -INFINITY;
-  for (int k = lane; k < all; k += 32) m = fmaxf(m, P.ml[part(k)].x);
+  for (int k = lane; k < all; k += 32) {
+    const int64_t at = find(k);
+    m = fmaxf(m, ml_of[at].x);
+  }
 #pragma unroll
   for (int s = 16; s; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
   float o[4] = {0, 0, 0, 0}, l = 0.0f;
   for (int k = 0; k < all; ++k) {
-    const float2 v = P.ml[part(k)];
+    const int64_t at = find(k);
+    const float2 v = ml_of[at];
     if (v.x == -INFINITY) continue;
     const float f = exp2_approx(v.x - m);
     l += f * v.y;
-    const float *src = P.o + part(k) * D;
+    const float *src = o_of + at * D;
     if (lane * 4 < D) {
       const float4 x = *reinterpret_cast<const float4 *>(src + lane * 4);
       o[0] += f * x.x, o[1] += f * x.y, o[2] += f * x.z, o[3] += f * x.w;

@@ -1,0 +1,490 @@
+// The shared prefix of wt_attend on the 5th-generation tensor cores (tcgen05): all queries of the
+// batch that use a kv head against that head's keys, as one matrix product after another,
+//
+//   S = Q K^T,   P = 2^(scale log2(e) S - m),   O += P V,   l += row sums of P,
+//
+// which reads the prefix once for the whole batch.  Rows are (token, head-in-group) pairs, 128 of
+// them (whole tokens) a tile; keys come in tiles of 128.  A CTA takes one contiguous range of the
+// key tiles of all kv heads (crossing from one head to the next where it must) for two row tiles, and
+// leaves O (fp32, not divided), m and l of each part for the merge.  CTAs that take the same keys for
+// other rows are neighbours in the grid, so a key tile crosses HBM once and is then found in L2.
+//
+//   producer warp    TMA boxes of Q (two tiles), and of K and V into a ring (128-byte swizzle)
+//   MMA thread       S_i = Q_i K^T for the two streams i, then O_i += P_i V as each P_i arrives
+//   two warpgroups   one per stream; a thread owns a row: it reads the row of S from tensor memory,
+//                    takes the exponentials and writes P (16-bit) back over S, where it is the next
+//                    product's A operand
+//
+// The two streams are two row tiles against the same keys, or, where there is one row tile only, the
+// even and the odd key tiles of the range, so that one stream's products run beside the other's
+// exponentials.  The reference m of a row moves only when its maximum has grown by more than 8 (in
+// log2): O is then rescaled in tensor memory; until then p stays below 2^8, which both 16-bit types
+// hold as precisely.  P is rounded to the caches' type (the MMA takes both operands in one type);
+// l is summed in fp32 from the unrounded values.
+//
+// Every mbarrier wait is bounded; a timeout records WT_ETIMEDOUT and every role stops.
+#include <cuda.h>
+
+#include "wt_device.cuh"
+#include "wt_serve.h"
+
+namespace wt {
+
+namespace {
+
+constexpr int kRowsT = 128;  // rows of a tile (UMMA M)
+constexpr int kKeysT = 128;  // keys of a tile
+constexpr int kThreads = 384;  // warps 0-3, 4-7: softmax of stream 0, 1; 8: producer; 9: MMA, TMEM; 10, 11: idle
+// Registers a thread after the split: 128 of S, and its exponentials, for softmax.  The launch gives
+// 3 x 168 to the three warpgroups together.
+constexpr int kRegsSoftmax = 224, kRegsRest = 56;
+static_assert(2 * kRegsSoftmax + kRegsRest <= 3 * 168, "what the launch has");
+constexpr uint32_t kHalf = 128 * 128;  // 128 rows of 64 elements
+constexpr uint32_t kTmemCols = 512;    // S_0, S_1 (128 columns each), O_0, O_1
+constexpr float kSlack = 8.0f;
+
+template <int DH>  // 64-element halves of head_dim
+struct Geo {
+  static constexpr uint32_t stage = DH * kHalf;
+  static constexpr int stages = DH == 2 ? 5 : 8;
+  static constexpr uint32_t ring = 2 * stage;  // after the two Q tiles
+  static constexpr uint32_t bars = ring + stages * stage;
+  static constexpr int nbars = 2 * stages + 9;
+  static constexpr size_t smem = bars + nbars * 8 + 16 + 1024;
+};
+static_assert(Geo<2>::smem <= 232448, "shared memory of one CTA");
+
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+
+// Shared-memory matrix descriptors in the 128-byte swizzled layout (version 1).  K-major: rows of
+// 128 bytes, groups of 8 rows 1024 bytes apart.  MN-major: 64 elements of N along a row, rows along
+// K; the stride offset leads from 8 rows to the next 8, the leading offset from 64 elements of N to
+// the next 64.
+__device__ __forceinline__ uint64_t desc_k(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
+         ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(kHalf >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+// kind::f16, fp32 accumulators, M = 128, A and B of one type; trans_b: B is MN-major.
+__host__ __device__ constexpr uint32_t idesc(uint32_t bf16, uint32_t n, uint32_t trans_b) {
+  return (1u << 4) | (bf16 << 7) | (bf16 << 10) | (trans_b << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+__device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(id), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(id), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+#define R4(v, o) "=r"(v[o]), "=r"(v[o + 1]), "=r"(v[o + 2]), "=r"(v[o + 3])
+#define W4(v, o) "r"(v[o]), "r"(v[o + 1]), "r"(v[o + 2]), "r"(v[o + 3])
+// 32 lanes x 32 columns of tensor memory: thread = lane.
+__device__ __forceinline__ void tmem_ld32(uint32_t a, uint32_t *r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : R4(r, 0), R4(r, 4), R4(r, 8), R4(r, 12), R4(r, 16), R4(r, 20), R4(r, 24), R4(r, 28)
+      : "r"(a));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t a, const uint32_t *r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(a),
+      W4(r, 0), W4(r, 4), W4(r, 8), W4(r, 12), W4(r, 16), W4(r, 20), W4(r, 24), W4(r, 28)
+      : "memory");
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// (x0, x1) * s + c
+__device__ __forceinline__ void fma_x2(float &x0, float &x1, float s, float c) {
+  asm("{\n\t.reg .b64 x, y, z;\n\t"
+      "mov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "+f"(x0), "+f"(x1)
+      : "f"(s), "f"(c));
+}
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if constexpr (DT == WT_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// A bounded wait of a whole warp: every lane gets the same answer, so a warp whose wait runs out
+// leaves together.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status) {
+  return __all_sync(0xffffffffu, bounded_wait(bar, parity, abort_flag, status));
+}
+
+// The segments of a CTA's range of key tiles: one for each kv head it meets.
+struct Segment {
+  int head, tile0, n;  // first key tile within the head, tiles
+};
+
+template <int DT, int DH>
+__global__ void __launch_bounds__(kThreads, 1)
+    attend_prefix_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+                         const __grid_constant__ CUtensorMap vmap, const __grid_constant__ PrefixPlan P, int *status) {
+  using X = Geo<DH>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t *gbase = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t full0 = base + X::bars, empty0 = full0 + X::stages * 8;
+  const uint32_t q_full = empty0 + X::stages * 8, q_empty = q_full + 8;
+  const uint32_t s_full = q_empty + 8, p_full = s_full + 16, o_full = p_full + 16;  // [2] each
+  const uint32_t fin = o_full + 16;
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gbase + X::bars + X::nbars * 8);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 2);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rb = blockIdx.x % P.row_blocks, grp = blockIdx.x / P.row_blocks;
+  const bool apart = P.apart != 0;  // one row tile; streams are the even and odd key tiles
+  const int64_t all = (int64_t)P.kv_heads * P.tiles;
+  const int w0 = (int)(all * grp / P.groups), w1 = (int)(all * (grp + 1) / P.groups);
+  auto segment = [&](int w) -> Segment {
+    const int head = w / P.tiles, t0 = w - head * P.tiles;
+    return {head, t0, min(P.tiles - t0, w1 - w)};
+  };
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < X::stages; ++s) {
+      mbar_init(full0 + 8 * s, 1);
+      mbar_init(empty0 + 8 * s, 1);
+    }
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
+    mbar_init(fin, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_full + 8 * i, 1);
+      mbar_init(p_full + 8 * i, 128);
+      mbar_init(o_full + 8 * i, 1);
+    }
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                 "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int lead = apart ? 2 : 1;  // key tiles whose K is loaded ahead of their V
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
+    // ---------------- producer
+    if (warp == 8 && lane == 0) {
+      uint32_t it = 0, seg = 0;
+      bool live = true;
+      auto load = [&](const CUtensorMap *map, int head, int tile) {
+        const uint32_t s = it % X::stages;
+        if (it >= X::stages && !bounded_wait(empty0 + 8 * s, ((it / X::stages) - 1) & 1, abort_flag, status)) return false;
+        const uint32_t bar = full0 + 8 * s, dst = base + X::ring + s * X::stage;
+        mbar_expect_tx(bar, X::stage);
+#pragma unroll
+        for (int hf = 0; hf < DH; ++hf) tma_3d(dst + hf * kHalf, map, hf * 64, head, tile * kKeysT, bar);
+        ++it;
+        return true;
+      };
+      uint32_t q_loads = 0;
+      for (int w = w0; w < w1 && live; ++seg) {
+        const Segment g = segment(w);
+        w += g.n;
+        if (seg && !bounded_wait(q_empty, (seg - 1) & 1, abort_flag, status)) break;
+        const int qtiles = apart ? 1 : 2;
+        mbar_expect_tx(q_full, (uint32_t)qtiles * DH * P.tile_rows * 128);
+        ++q_loads;
+        for (int i = 0; i < qtiles; ++i)
+#pragma unroll
+          for (int hf = 0; hf < DH; ++hf)
+            tma_3d(base + (i * DH + hf) * kHalf, &qmap, hf * 64, g.head * P.G, (rb * 2 + i) * P.tile_tokens, q_full);
+        for (int j = 0; j < min(lead, g.n) && live; ++j) live = load(&kmap, g.head, g.tile0 + j);
+        for (int j = 0; j < g.n && live; ++j) {
+          live = load(&vmap, g.head, g.tile0 + j);
+          if (live && j + lead < g.n) live = load(&kmap, g.head, g.tile0 + j + lead);
+        }
+      }
+      if (*abort_flag) {
+        // drain: copies of the last stages may still be landing
+        const uint32_t first = it > (uint32_t)X::stages ? it - X::stages : 0;
+        for (uint32_t j = first; j < it; ++j) {
+          const long long t0 = clock64();
+          while (!mbar_try_wait(full0 + 8 * (j % X::stages), (j / X::stages) & 1) && clock64() - t0 < kWaitCycles) {
+          }
+        }
+        if (q_loads) {
+          const long long t0 = clock64();
+          while (!mbar_try_wait(q_full, (q_loads - 1) & 1) && clock64() - t0 < kWaitCycles) {
+          }
+        }
+      }
+    }
+    // ---------------- MMA issuer
+    if (warp == 9 && lane == 0) {
+      constexpr uint32_t kBf = DT == WT_BF16 ? 1u : 0u;
+      constexpr uint32_t kIqk = idesc(kBf, kKeysT, 0), kIpv = idesc(kBf, DH * 64, 1);
+      uint32_t it = 0, seg = 0, np[2] = {0, 0};
+      bool live = true;
+      uint32_t stage = 0;
+      auto next = [&]() {  // the ring's next tile has landed
+        const uint32_t s = it % X::stages;
+        if (!bounded_wait(full0 + 8 * s, (it / X::stages) & 1, abort_flag, status)) return live = false;
+        fence_after();
+        stage = s;
+        ++it;
+        return true;
+      };
+      auto scores = [&](int i, uint32_t s) {
+        const uint32_t q = base + (apart ? 0 : i) * X::stage, k = base + X::ring + s * X::stage;
+        for (int e = 0; e < P.dim_steps; ++e) {
+          const uint32_t off = (e >> 2) * kHalf + (e & 3) * 32;
+          umma_ss(tmem + i * 128, desc_k(q + off), desc_k(k + off), kIqk, e != 0);
+        }
+        commit(s_full + 8 * i);
+      };
+      auto values = [&](int i, uint32_t s, bool first) {  // false: no P came
+        if (!bounded_wait(p_full + 8 * i, np[i] & 1, abort_flag, status)) return live = false;
+        ++np[i];
+        fence_after();
+        const uint32_t v = base + X::ring + s * X::stage;
+#pragma unroll
+        for (int e = 0; e < kKeysT / 16; ++e)
+          umma_ts(tmem + 256 + i * 128, tmem + i * 128 + e * 8, desc_mn(v + e * 2048), kIpv, !first || e != 0);
+        commit(o_full + 8 * i);
+        return true;
+      };
+      for (int w = w0; w < w1 && live; ++seg) {
+        const Segment g = segment(w);
+        w += g.n;
+        if (!bounded_wait(q_full, seg & 1, abort_flag, status)) break;
+        fence_after();
+        if (!apart) {
+          if (!next()) break;
+          scores(0, stage);
+          scores(1, stage);
+          commit(empty0 + 8 * stage);
+          if (g.n == 1) commit(q_empty);
+          for (int j = 0; j < g.n; ++j) {
+            if (!next()) break;
+            const uint32_t vs = stage;
+            const bool more = j + 1 < g.n;
+            if (!values(0, vs, j == 0)) break;
+            if (more) {
+              if (!next()) break;
+              scores(0, stage);
+            }
+            if (!values(1, vs, j == 0)) break;
+            commit(empty0 + 8 * vs);
+            if (more) {
+              scores(1, stage);
+              commit(empty0 + 8 * stage);
+              if (j + 2 == g.n) commit(q_empty);
+            }
+          }
+        } else {
+          for (int j = 0; j < min(2, g.n) && next(); ++j) {
+            scores(j, stage);
+            commit(empty0 + 8 * stage);
+          }
+          if (!live) break;
+          if (g.n <= 2) commit(q_empty);
+          for (int j = 0; j < g.n; ++j) {
+            if (!next()) break;
+            const uint32_t vs = stage;
+            if (!values(j & 1, vs, j < 2)) break;
+            commit(empty0 + 8 * vs);
+            if (j + 2 < g.n) {
+              if (!next()) break;
+              scores(j & 1, stage);
+              commit(empty0 + 8 * stage);
+              if (j + 3 == g.n) commit(q_empty);
+            }
+          }
+        }
+      }
+      // the last products must have finished before tensor memory is released
+      if (it > 0) {
+        commit(fin);
+        const long long t0 = clock64();
+        while (!mbar_try_wait(fin, 0) && clock64() - t0 < kWaitCycles) {
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    // ---------------- softmax: a thread owns row threadIdx.x % 128 of stream i
+    const int i = warp >> 2, r = threadIdx.x & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // 32 lanes of tensor memory per warp
+    const uint32_t S = tmem + lanes + i * 128, O = tmem + lanes + 256 + i * 128;
+    uint32_t done = 0;  // tiles of this stream over all segments
+    bool live = true;
+    for (int w = w0; w < w1 && live;) {
+      const Segment g = segment(w);
+      w += g.n;
+      const int n = apart ? (g.n + 1 - i) / 2 : g.n;
+      float m = 0.0f, l0 = 0.0f, l1 = 0.0f;
+      for (int j = 0; j < n; ++j) {
+        if (!warp_wait(s_full + 8 * i, (done + j) & 1, abort_flag, status)) {
+          live = false;
+          break;
+        }
+        fence_after();
+        float v[128];
+        {
+          uint32_t u[128];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(S + c * 32, u + c * 32);
+          wait_ld();
+#pragma unroll
+          for (int c = 0; c < 128; ++c) v[c] = __uint_as_float(u[c]);
+        }
+        const int keys = P.prefix_len - (g.tile0 + (apart ? 2 * j + i : j)) * kKeysT;
+        if (keys < kKeysT) {
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c >= keys) v[c] = -INFINITY;
+        }
+        float mx0 = v[0], mx1 = v[1], mx2 = v[2], mx3 = v[3];
+#pragma unroll
+        for (int c = 4; c < 128; c += 8) {
+          mx0 = fmaxf(fmaxf(mx0, v[c]), v[c + 4 < 128 ? c + 4 : c]);
+          mx1 = fmaxf(fmaxf(mx1, v[c + 1]), v[c + 5 < 128 ? c + 5 : c]);
+          mx2 = fmaxf(fmaxf(mx2, v[c + 2]), v[c + 6 < 128 ? c + 6 : c]);
+          mx3 = fmaxf(fmaxf(mx3, v[c + 3]), v[c + 7 < 128 ? c + 7 : c]);
+        }
+        const float top = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * P.scale_log2;
+        const bool grown = top > m + kSlack;
+        if (j == 0) {
+          m = top > -INFINITY ? top : 0.0f;
+        } else if (__any_sync(0xffffffffu, grown)) {
+          // O of this row, once the product before has been added to it, against the new reference
+          if (!warp_wait(o_full + 8 * i, (done + j - 1) & 1, abort_flag, status)) {
+            live = false;
+            break;
+          }
+          fence_after();
+          const float f = grown ? ex2(m - top) : 1.0f;
+          if (grown) m = top;
+          l0 *= f;
+          l1 *= f;
+#pragma unroll 1
+          for (int c = 0; c < DH * 64; c += 32) {
+            uint32_t o[32];
+            tmem_ld32(O + c, o);
+            wait_ld();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+            tmem_st32(O + c, o);
+          }
+        }
+        uint32_t u[64];
+#pragma unroll
+        for (int c = 0; c < 128; c += 2) {
+          fma_x2(v[c], v[c + 1], P.scale_log2, -m);
+          v[c] = ex2(v[c]);
+          v[c + 1] = ex2(v[c + 1]);
+          add_x2(l0, l1, v[c], v[c + 1]);
+          u[c / 2] = pack2<DT>(v[c], v[c + 1]);
+        }
+        tmem_st32(S, u);
+        tmem_st32(S + 32, u + 32);
+        wait_st();
+        fence_before();
+        mbar_arrive(p_full + 8 * i);
+      }
+      if (!live) break;
+      const int row = apart ? r : (rb * 2 + i) * P.tile_rows + r;
+      const bool mine = r < P.tile_rows && row < P.rows;
+      const int64_t at = ((int64_t)(grp + g.head) * P.qtiles + (apart ? i : rb * 2 + i)) * kRowsT + r;
+      if (n > 0) {
+        if (!warp_wait(o_full + 8 * i, (done + n - 1) & 1, abort_flag, status)) break;
+        fence_after();
+#pragma unroll 1
+        for (int c = 0; c < DH * 64; c += 32) {
+          uint32_t o[32];
+          tmem_ld32(O + c, o);
+          wait_ld();
+          if (mine) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 4)
+              if (c + k < P.head_dim)
+                *reinterpret_cast<uint4 *>(P.o + at * P.head_dim + c + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          }
+        }
+        fence_before();
+      }
+      if (mine) P.ml[at] = make_float2(n > 0 ? m : -INFINITY, l0 + l1);
+      done += n;
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+template <int DT, int DH>
+cudaError_t run(const PrefixPlan &P, const PrefixMaps &m, int *status, cudaStream_t s) {
+  attend_prefix_kernel<DT, DH><<<(unsigned)(P.row_blocks * P.groups), kThreads, Geo<DH>::smem, s>>>(
+      *reinterpret_cast<const CUtensorMap *>(m.q), *reinterpret_cast<const CUtensorMap *>(m.k),
+      *reinterpret_cast<const CUtensorMap *>(m.v), P, status);
+  return cudaGetLastError();
+}
+
+template <int DT, int DH>
+cudaError_t prepare_one() {
+  return cudaFuncSetAttribute(attend_prefix_kernel<DT, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)Geo<DH>::smem);
+}
+
+}  // namespace
+
+cudaError_t prefix_prepare() {
+  cudaError_t e = prepare_one<WT_BF16, 1>();
+  if (e == cudaSuccess) e = prepare_one<WT_BF16, 2>();
+  if (e == cudaSuccess) e = prepare_one<WT_F16, 1>();
+  if (e == cudaSuccess) e = prepare_one<WT_F16, 2>();
+  return e;
+}
+
+cudaError_t launch_attend_prefix(const PrefixPlan &P, const PrefixMaps &m, int dtype, int *status, cudaStream_t s) {
+  if (dtype == WT_BF16) return P.head_dim <= 64 ? run<WT_BF16, 1>(P, m, status, s) : run<WT_BF16, 2>(P, m, status, s);
+  return P.head_dim <= 64 ? run<WT_F16, 1>(P, m, status, s) : run<WT_F16, 2>(P, m, status, s);
+}
+
+}  // namespace wt

@@ -182,6 +182,50 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// The prefix goes to tcgen05 from 33 rows (token, head-in-group) on, which is where the warp kernel
+// would read it more than once, and from one key tile on.  Its reference only grows, so the scale has
+// to be positive; and a pitch has to fit a tensor map.
+bool prefix_on_tcgen05(const wt_attend_desc &d) {
+  const int64_t rows = (int64_t)d.n_tokens * (d.heads / d.kv_heads);
+  return rows > 32 && d.prefix_len >= 128 && d.scale > 0.0f && d.q_stride < (1ll << 38) && d.prefix_stride < (1ll << 38) &&
+         d.prefix_head < (1ll << 38);
+}
+
+// Rows in tiles of whole tokens, and as many ranges of key tiles as make the SMs' work come out even:
+// a range costs its tiles and about 3 more (first loads, the first and last product, the parts' stores).
+int plan_prefix(const wt_attend_desc &d, int G, wt::PrefixPlan *x, wt::PrefixMaps *maps) {
+  x->G = G;
+  x->kv_heads = d.kv_heads;
+  x->head_dim = d.head_dim;
+  x->dim_steps = (d.head_dim + 15) / 16;
+  x->prefix_len = (int)d.prefix_len;
+  x->scale_log2 = d.scale * 1.4426950408889634f;
+  x->tile_tokens = 128 / G;
+  x->tile_rows = x->tile_tokens * G;
+  x->rows = d.n_tokens * G;
+  x->tiles = (int)ceil_div(d.prefix_len, 128);
+  const int64_t row_tiles = ceil_div(d.n_tokens, x->tile_tokens);
+  x->apart = row_tiles == 1;
+  x->row_blocks = (int)ceil_div(row_tiles, 2);
+  x->qtiles = x->apart ? 2 : 2 * x->row_blocks;
+  const int64_t all = (int64_t)d.kv_heads * x->tiles, sms = wt::num_sms();
+  if (all > (1 << 30)) return serve_error(WT_EINVAL, "wt_attend: %lld key tiles", (long long)all);
+  int64_t best = INT64_MAX;
+  for (int64_t g = 1; g <= std::min<int64_t>(all, std::max<int64_t>(1, 2 * sms / x->row_blocks)); ++g) {
+    const int64_t cost = ceil_div(x->row_blocks * g, sms) * (ceil_div(all, g) + 3);
+    if (cost < best) best = cost, x->groups = (int)g;
+  }
+  const uint64_t D = d.head_dim;
+  const uint64_t qd[3] = {D, (uint64_t)d.heads, (uint64_t)d.n_tokens}, qs[2] = {2 * D, 2 * (uint64_t)d.q_stride};
+  const uint32_t qb[3] = {64, (uint32_t)G, (uint32_t)x->tile_tokens};
+  const uint64_t kd[3] = {D, (uint64_t)d.kv_heads, (uint64_t)d.prefix_len},
+                 ks[2] = {2 * (uint64_t)d.prefix_head, 2 * (uint64_t)d.prefix_stride};
+  const uint32_t kb[3] = {64, 1, 128};
+  CHECK(wt::serve_tensor_map(maps->q, d.q, 3, qd, qs, qb));
+  CHECK(wt::serve_tensor_map(maps->k, d.prefix_k, 3, kd, ks, kb));
+  return wt::serve_tensor_map(maps->v, d.prefix_v, 3, kd, ks, kb);
+}
+
 int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
   wt::ServeContext ctx;
   CHECK(wt::serve_context(h, "wt_attend", &ctx));
@@ -195,8 +239,12 @@ int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
   P.G = d.heads / d.kv_heads;
   P.status = ctx.status;
   const int64_t own_rows = (int64_t)d.max_new * P.G, pre_rows = (int64_t)d.n_tokens * P.G;
-  P.rows_tile = std::max(d.max_len ? own_rows : 0, d.prefix_len ? pre_rows : 0) <= 16 ? 16 : 32;
-  P.row_tiles = (int)ceil_div(std::max(d.max_len ? own_rows : 0, d.prefix_len ? pre_rows : 0), P.rows_tile);
+  wt::PrefixMaps maps;
+  if (d.prefix_len && prefix_on_tcgen05(d)) CHECK(plan_prefix(d, P.G, &P.x, &maps));
+  const bool pre_warp = d.prefix_len && !P.x.groups;
+  const int64_t most = std::max(d.max_len ? own_rows : 0, pre_warp ? pre_rows : 0);
+  P.rows_tile = most <= 16 ? 16 : 32;
+  P.row_tiles = (int)ceil_div(most, P.rows_tile);
   // Splits: 4 CTAs per SM over all of them, of at least 64 keys (one tile for each warp).
   const int64_t want = 4 * wt::num_sms();
   auto split = [&](int64_t keys, int64_t ctas, int &splits, int &len) {
@@ -205,21 +253,35 @@ int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
     splits = (int)ceil_div(keys, len);
   };
   if (d.max_len) split(d.max_len, (int64_t)d.n_req * d.kv_heads * ceil_div(own_rows, P.rows_tile), P.own_splits, P.own_len);
-  if (d.prefix_len) split(d.prefix_len, d.kv_heads * ceil_div(pre_rows, P.rows_tile), P.pre_splits, P.pre_len);
+  if (pre_warp) split(d.prefix_len, d.kv_heads * ceil_div(pre_rows, P.rows_tile), P.pre_splits, P.pre_len);
   const int64_t parts = P.own_splits + P.pre_splits, rows = (int64_t)d.n_tokens * d.heads;
   if ((int64_t)d.kv_heads * P.row_tiles * ((int64_t)d.n_req * P.own_splits + P.pre_splits) > 0x7fffffff)
     return serve_error(WT_EINVAL, "wt_attend: too many tokens, heads and keys for one launch");
-  const size_t ob = (size_t)(parts * rows * d.head_dim * 4 + 255) / 256 * 256;
+  // workspace: O and (m, l) of every part
+  auto take = [](size_t &at, size_t n) {
+    const size_t o = at;
+    at += (n + 255) / 256 * 256;
+    return o;
+  };
+  const int64_t xrows = P.x.groups ? (int64_t)(P.x.groups + d.kv_heads - 1) * P.x.qtiles * 128 : 0;
+  size_t bytes = 0;
+  const size_t o = take(bytes, (size_t)(parts * rows * d.head_dim) * 4), ml = take(bytes, (size_t)(parts * rows) * sizeof(float2));
+  const size_t xo = take(bytes, (size_t)(xrows * d.head_dim) * 4), xml = take(bytes, (size_t)xrows * sizeof(float2));
   Lock lock(h);
   wt::ServeWorkspace w;
-  CHECK(wt::serve_workspace(h, s, ob + (size_t)(parts * rows) * sizeof(float2), &w));
-  P.o = static_cast<float *>(w.p);
-  P.ml = reinterpret_cast<float2 *>(static_cast<uint8_t *>(w.p) + ob);
-  cudaError_t e = parts ? wt::launch_attend_warp(P, s) : cudaSuccess;
+  CHECK(wt::serve_workspace(h, s, bytes, &w));
+  uint8_t *ws = static_cast<uint8_t *>(w.p);
+  P.o = reinterpret_cast<float *>(ws + o);
+  P.ml = reinterpret_cast<float2 *>(ws + ml);
+  P.x.o = reinterpret_cast<float *>(ws + xo);
+  P.x.ml = reinterpret_cast<float2 *>(ws + xml);
+  cudaError_t e = cudaSuccess;
+  if (P.x.groups) e = wt::launch_attend_prefix(P.x, maps, d.dtype, ctx.status, s);
+  if (e == cudaSuccess && parts) e = wt::launch_attend_warp(P, s);
   if (e == cudaSuccess) e = wt::launch_attend_merge(P, s);
   const int rc = wt::serve_workspace_done(h, s, w);
   CU(e);
-  wt::serve_launched(h, parts ? 2 : 1);
+  wt::serve_launched(h, (P.x.groups != 0) + (parts != 0) + 1);
   return rc;
 }
 
@@ -273,6 +335,7 @@ int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {
 cudaError_t wt::serve_prepare() {
   cudaError_t e = adapt_prepare();
   if (e == cudaSuccess) e = attend_prepare();
+  if (e == cudaSuccess) e = prefix_prepare();
   return e;
 }
 

@@ -63,6 +63,30 @@ cudaError_t launch_verify(const wt_verify_desc &d, int *status, cudaStream_t s);
 // ---------------------------------------------------------------- wt_attend.cu
 // Partial results of one (token, head): O [head_dim] fp32 not yet divided by l, and (m, l) with m in
 // units of log2 (scores times scale log2 e).
+//
+// The shared prefix on tcgen05 (wt_prefix.cu): the key tiles (128 keys) of all kv heads in a row,
+// head after head, are cut into `groups` ranges of nearly equal length; each range is taken by
+// row_blocks CTAs of two row tiles each.  The part of range g that lies in head h is slot g + h.
+struct PrefixPlan {
+  int row_blocks, groups;
+  int apart;        // one row tile: the two streams take the even and the odd key tiles of a segment
+  int tiles;        // key tiles of a head
+  int tile_tokens, tile_rows;  // whole tokens of a row tile (up to 128 rows), and its rows
+  int qtiles;       // tiles of a slot: 2 row_blocks, or the 2 streams
+  int rows;         // n_tokens * G
+  int kv_heads, G, head_dim, dim_steps, prefix_len;
+  float scale_log2;
+  float *o;         // [groups + kv_heads - 1][qtiles][128][head_dim]
+  float2 *ml;       // [groups + kv_heads - 1][qtiles][128]
+};
+struct PrefixMaps {
+  alignas(64) uint8_t q[128];  // CUtensorMaps
+  alignas(64) uint8_t k[128];
+  alignas(64) uint8_t v[128];
+};
+cudaError_t prefix_prepare();
+cudaError_t launch_attend_prefix(const PrefixPlan &P, const PrefixMaps &m, int dtype, int *status, cudaStream_t s);
+
 struct AttendPlan {
   wt_attend_desc d;
   int G;          // heads / kv_heads
@@ -70,6 +94,7 @@ struct AttendPlan {
   int row_tiles;  // tiles that the longest request (or the prefix's rows) takes
   int own_splits, own_len;  // own keys per split
   int pre_splits, pre_len;  // prefix keys per split of the warp kernel (0: not taken there)
+  PrefixPlan x;             // the prefix on tcgen05 (x.groups 0: not taken there)
   float *o;                 // [own_splits + pre_splits][n_tokens * heads][head_dim]
   float2 *ml;               // [own_splits + pre_splits][n_tokens * heads]
   int *status;
