@@ -315,70 +315,101 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
   }
 }
 
-// out[t, h] = sum over the parts, one warp per (token, head).
-template <int DT>
-__global__ void __launch_bounds__(256) attend_merge_kernel(const __grid_constant__ AttendPlan P) {
+// out[t, h] = sum over the parts, WR warps (1 or 4) to a (token, head); with 4, each takes every
+// fourth part.  The references and sums of 32 parts are read at once, one by each lane, and the parts'
+// O eight at a time, so that few reads wait for one another (one part after another: 31 us for a
+// decode step of 24 requests with 37 parts each, this way 4).
+constexpr int kMergeParts = 8;
+template <int DT, int WR>
+__global__ void __launch_bounds__(kThreads) attend_merge_kernel(const __grid_constant__ AttendPlan P) {
+  __shared__ float4 so[kWarps][32];
   const wt_attend_desc &d = P.d;
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, warp = WR == 1 ? 0 : threadIdx.x >> 5;
   const int b = blockIdx.y;
   const Request rq = request_of(d, b, nullptr, false);
-  const int i = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int i = WR == 1 ? blockIdx.x * kWarps + (threadIdx.x >> 5) : blockIdx.x;
   if (i >= rq.n * d.heads) return;
+  const int h = i % d.heads, t = rq.t0 + i / d.heads;
   const int64_t row = (int64_t)rq.t0 * d.heads + i, rows = (int64_t)d.n_tokens * d.heads;
   const int own = P.own_splits ? (rq.len + P.own_len - 1) / P.own_len : 0;
   const int D = d.head_dim;
-  const float *o_of;
-  const float2 *ml_of;
   // the parts: own splits, then the prefix's (those of the warp kernel, or the slots on tcgen05)
-  int all = own + P.pre_splits, x0 = 0, per = 1;
-  int64_t xrow = 0;
+  int all = own + P.pre_splits, x0 = 0;
+  const int per = P.x.apart ? 2 : 1;
+  int xrow = 0;
   if (P.x.groups) {
     const PrefixPlan &x = P.x;
-    const int hk = (int)(row % d.heads) / P.G;
-    const int r = (int)(row / d.heads) * P.G + (int)(row % d.heads) % P.G;
-    const int64_t total = (int64_t)x.kv_heads * x.tiles, start = (int64_t)hk * x.tiles;
-    int g0 = (int)(start * x.groups / total);
-    while (g0 + 1 < x.groups && total * (g0 + 1) / x.groups <= start) ++g0;
-    int g1 = g0 + 1;
-    while (g1 < x.groups && total * g1 / x.groups < start + x.tiles) ++g1;
-    per = x.apart ? 2 : 1;
-    all += (g1 - g0) * per;
+    const int hk = h / P.G, r = t * P.G + h % P.G, start = hk * x.tiles;
+    const int g0 = start / x.len, g1 = (start + x.tiles - 1) / x.len;  // first and last range in the head
+    all += (g1 - g0 + 1) * per;
     x0 = (g0 + hk) * x.qtiles;
-    xrow = x.apart ? r : (int64_t)(r / x.tile_rows) * 128 + r % x.tile_rows;
+    xrow = x.apart ? r : r / x.tile_rows * 128 + r % x.tile_rows;
   }
-  auto find = [&](int k) -> int64_t {  // the part's row
-    o_of = P.o, ml_of = P.ml;
-    if (k < own) return (int64_t)k * rows + row;
-    k -= own;
-    if (k < P.pre_splits) return (int64_t)(P.own_splits + k) * rows + row;
-    o_of = P.x.o, ml_of = P.x.ml;
+  // part k: its O (of D numbers), and its m and l
+  auto find = [&](int k, const float2 *&ml) -> const float * {
+    int64_t at;
+    if (k < own + P.pre_splits) {
+      at = (int64_t)(k < own ? k : P.own_splits + k - own) * rows + row;
+      ml = P.ml + at;
+      return P.o + at * D;
+    }
+    k -= own + P.pre_splits;
     // apart: the two streams of a slot are tiles of their own; else a slot's tiles are row tiles
-    return ((int64_t)x0 + (int64_t)(k / per) * P.x.qtiles + k % per) * 128 + xrow;
+    at = (int64_t)(x0 + (per == 2 ? (k >> 1) * P.x.qtiles + (k & 1) : k * P.x.qtiles)) * 128 + xrow;
+    ml = P.x.ml + at;
+    return P.x.o + at * D;
   };
-  float m = -INFINITY;
-  for (int k = lane; k < all; k += 32) {
-    const int64_t at = find(k);
-    m = fmaxf(m, ml_of[at].x);
-  }
+  auto read = [&](int k) {
+    const float2 *ml;
+    find(k, ml);
+    return *ml;
+  };
+  float2 mine = lane < all ? read(lane) : make_float2(-INFINITY, 0.0f);
+  float m = mine.x;
+  for (int k = lane + 32; k < all; k += 32) m = fmaxf(m, read(k).x);
 #pragma unroll
   for (int s = 16; s; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
-  float o[4] = {0, 0, 0, 0}, l = 0.0f;
-  for (int k = 0; k < all; ++k) {
-    const int64_t at = find(k);
-    const float2 v = ml_of[at];
-    if (v.x == -INFINITY) continue;
-    const float f = exp2_approx(v.x - m);
-    l += f * v.y;
-    const float *src = o_of + at * D;
-    if (lane * 4 < D) {
-      const float4 x = *reinterpret_cast<const float4 *>(src + lane * 4);
-      o[0] += f * x.x, o[1] += f * x.y, o[2] += f * x.z, o[3] += f * x.w;
+  float4 o = make_float4(0, 0, 0, 0);
+  float l = 0.0f;
+  const bool cols = lane * 4 < D;
+  for (int k0 = 0; k0 < all; k0 += 32) {
+    if (k0) mine = k0 + lane < all ? read(k0 + lane) : make_float2(-INFINITY, 0.0f);
+    // a part without a key: its O was not written
+    const float f = mine.x > -INFINITY || mine.x != mine.x ? exp2_approx(mine.x - m) : 0.0f;
+    if (f != 0.0f) l += f * mine.y;
+    const unsigned some = __ballot_sync(0xffffffffu, f != 0.0f);
+    for (int k = k0 + warp; k < min(all, k0 + 32); k += WR * kMergeParts) {
+      float4 x[kMergeParts];
+      float w[kMergeParts];
+#pragma unroll
+      for (int u = 0; u < kMergeParts; ++u) {
+        const int kk = k + u * WR, at = kk - k0;
+        const bool there = at < 32 && (some >> at & 1) && cols;
+        const float2 *ml;
+        x[u] = there ? *reinterpret_cast<const float4 *>(find(kk, ml) + lane * 4) : make_float4(0, 0, 0, 0);
+        w[u] = __shfl_sync(0xffffffffu, f, at & 31);
+      }
+#pragma unroll
+      for (int u = 0; u < kMergeParts; ++u)
+        o.x += w[u] * x[u].x, o.y += w[u] * x[u].y, o.z += w[u] * x[u].z, o.w += w[u] * x[u].w;
     }
   }
-  if (lane * 4 < D) {
+#pragma unroll
+  for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+  if constexpr (WR > 1) {
+    so[warp][lane] = o;
+    __syncthreads();
+    if (warp) return;
+#pragma unroll
+    for (int w = 1; w < WR; ++w) {
+      const float4 x = so[w][lane];
+      o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
+    }
+  }
+  if (cols) {
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    uint16_t *dst = static_cast<uint16_t *>(d.out) + (row / d.heads) * d.out_stride + (row % d.heads) * D + lane * 4;
-    *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<DT>(o[0] * inv, o[1] * inv), pack2<DT>(o[2] * inv, o[3] * inv));
+    uint16_t *dst = static_cast<uint16_t *>(d.out) + (int64_t)t * d.out_stride + h * D + lane * 4;
+    *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<DT>(o.x * inv, o.y * inv), pack2<DT>(o.z * inv, o.w * inv));
   }
 }
 
@@ -429,11 +460,17 @@ cudaError_t launch_attend_warp(const AttendPlan &P, cudaStream_t s) {
   return P.d.dtype == WT_BF16 ? run_dim<WT_BF16>(P, s) : run_dim<WT_F16>(P, s);
 }
 
-cudaError_t launch_attend_merge(const AttendPlan &P, cudaStream_t s) {
-  const dim3 grid((unsigned)((P.d.max_new * P.d.heads + 7) / 8), (unsigned)P.d.n_req);
-  if (P.d.dtype == WT_BF16) attend_merge_kernel<WT_BF16><<<grid, 256, 0, s>>>(P);
-  else attend_merge_kernel<WT_F16><<<grid, 256, 0, s>>>(P);
+template <int DT>
+cudaError_t run_merge(const AttendPlan &P, cudaStream_t s) {
+  const unsigned rows = (unsigned)(P.d.max_new * P.d.heads), n = (unsigned)P.d.n_req;
+  // four warps to a row only where one to a row would leave SMs idle
+  if ((int64_t)P.d.n_tokens * P.d.heads >= 16ll * num_sms()) attend_merge_kernel<DT, 1><<<dim3((rows + kWarps - 1) / kWarps, n), kThreads, 0, s>>>(P);
+  else attend_merge_kernel<DT, kWarps><<<dim3(rows, n), kThreads, 0, s>>>(P);
   return cudaGetLastError();
+}
+
+cudaError_t launch_attend_merge(const AttendPlan &P, cudaStream_t s) {
+  return P.d.dtype == WT_BF16 ? run_merge<WT_BF16>(P, s) : run_merge<WT_F16>(P, s);
 }
 
 }  // namespace wt

@@ -168,8 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rb = blockIdx.x % P.row_blocks, grp = blockIdx.x / P.row_blocks;
   const bool apart = P.apart != 0;  // one row tile; streams are the even and odd key tiles
-  const int64_t all = (int64_t)P.kv_heads * P.tiles;
-  const int w0 = (int)(all * grp / P.groups), w1 = (int)(all * (grp + 1) / P.groups);
+  const int w0 = grp * P.len, w1 = min(P.kv_heads * P.tiles, w0 + P.len);
   auto segment = [&](int w) -> Segment {
     const int head = w / P.tiles, t0 = w - head * P.tiles;
     return {head, t0, min(P.tiles - t0, w1 - w)};

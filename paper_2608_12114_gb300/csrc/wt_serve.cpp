@@ -211,9 +211,10 @@ int plan_prefix(const wt_attend_desc &d, int G, wt::PrefixPlan *x, wt::PrefixMap
   const int64_t all = (int64_t)d.kv_heads * x->tiles, sms = wt::num_sms();
   if (all > (1 << 30)) return serve_error(WT_EINVAL, "wt_attend: %lld key tiles", (long long)all);
   int64_t best = INT64_MAX;
-  for (int64_t g = 1; g <= std::min<int64_t>(all, std::max<int64_t>(1, 2 * sms / x->row_blocks)); ++g) {
-    const int64_t cost = ceil_div(x->row_blocks * g, sms) * (ceil_div(all, g) + 3);
-    if (cost < best) best = cost, x->groups = (int)g;
+  for (int64_t g = std::min<int64_t>(all, std::max<int64_t>(1, 2 * sms / x->row_blocks)); g >= 1; --g) {
+    const int64_t len = ceil_div(all, g), n = ceil_div(all, len);
+    const int64_t cost = ceil_div(x->row_blocks * n, sms) * (len + 3);
+    if (cost < best) best = cost, x->len = (int)len, x->groups = (int)n;
   }
   const uint64_t D = d.head_dim;
   const uint64_t qd[3] = {D, (uint64_t)d.heads, (uint64_t)d.n_tokens}, qs[2] = {2 * D, 2 * (uint64_t)d.q_stride};
@@ -300,7 +301,7 @@ int probs_impl(wt_handle *h, const wt_probs_desc *d, cudaStream_t s) {
   if (d->p == d->logits ? d->ldp != d->ldl : overlap(d->p, pn, d->logits, ln))
     return serve_error(WT_EINVAL, "%s: p overlaps the logits", call);
   if (d->temp) CHECK(check_buffer(call, "temp", d->temp, 4 * (uint64_t)d->rows, 4));
-  CU(wt::launch_probs(*d, s));
+  CU(wt::launch_probs(*d, ctx.status, s));
   wt::serve_launched(h, 1);
   return WT_OK;
 }
@@ -336,6 +337,7 @@ cudaError_t wt::serve_prepare() {
   cudaError_t e = adapt_prepare();
   if (e == cudaSuccess) e = attend_prepare();
   if (e == cudaSuccess) e = prefix_prepare();
+  if (e == cudaSuccess) e = draw_prepare();
   return e;
 }
 

@@ -57,7 +57,8 @@ int adapt_tile(int max_T);  // tokens of one work item
 cudaError_t launch_adapt(const AdaptLaunch &L, int max_R, int max_T, int *status, cudaStream_t s);
 
 // ---------------------------------------------------------------- wt_draw.cu
-cudaError_t launch_probs(const wt_probs_desc &d, cudaStream_t s);
+cudaError_t draw_prepare();
+cudaError_t launch_probs(const wt_probs_desc &d, int *status, cudaStream_t s);
 cudaError_t launch_verify(const wt_verify_desc &d, int *status, cudaStream_t s);
 
 // ---------------------------------------------------------------- wt_attend.cu
@@ -65,10 +66,10 @@ cudaError_t launch_verify(const wt_verify_desc &d, int *status, cudaStream_t s);
 // units of log2 (scores times scale log2 e).
 //
 // The shared prefix on tcgen05 (wt_prefix.cu): the key tiles (128 keys) of all kv heads in a row,
-// head after head, are cut into `groups` ranges of nearly equal length; each range is taken by
-// row_blocks CTAs of two row tiles each.  The part of range g that lies in head h is slot g + h.
+// head after head, are cut into `groups` ranges of `len` tiles (the last may be shorter); each range
+// is taken by row_blocks CTAs of two row tiles each.  The part of range g that lies in head h is slot g + h.
 struct PrefixPlan {
-  int row_blocks, groups;
+  int row_blocks, groups, len;
   int apart;        // one row tile: the two streams take the even and the odd key tiles of a segment
   int tiles;        // key tiles of a head
   int tile_tokens, tile_rows;  // whole tokens of a row tile (up to 128 rows), and its rows
