@@ -1,13 +1,13 @@
 // Low-rank adapters of many requests beside a shared projection (include/wt_serve.h):
 // y[t] = base[t] + scale_s B_s (A_s x[t]), s = slot[t].
 //
-// One launch, one cluster of 8 CTAs per work item (projection, slot, up to kTile tokens of that
-// slot).  The cluster computes v = A x with each CTA taking an eighth of K, exchanges the partial
+// Few tokens (below 256): one launch, one cluster of 8 CTAs per work item (projection, slot, up to 16
+// tokens of that slot).  The cluster computes v = A x with each CTA taking an eighth of K, exchanges the partial
 // sums through distributed shared memory (always added in the order of the CTAs), and then each CTA
 // takes an eighth of the M outputs.  A and B are read once per item, B's lines being fetched into L2
 // while A is read; x and y cross once.  The slot map lies in device memory, so the items are found
-// there too: every CTA counts the tokens of each slot and picks its own.  Bound: HBM for prompts,
-// latency (two dependent reads and a cluster barrier) for decode steps.
+// there too: every CTA counts the tokens of each slot and picks its own.  Bound: latency
+// (two dependent reads and a cluster barrier).  More tokens: three launches, see below.
 //
 // Products run on the tensor cores.  A x: 16-bit operands, exact products, fp32 sums.  B v: B is
 // exact in tf32 (both 16-bit types fit), and v, held in fp32, is split into two tf32 numbers, so that
@@ -85,12 +85,35 @@ struct Item {
   int count;  // tokens
 };
 
-// MT: 16-row tiles of the rank (R <= 16 MT).  WT: groups of 16 tokens, each with 8 / WT warps.
-template <int DT, int MT, int WT>
+// Elements [k, k + 8) of a row of B of which the first r count, as 4 words; with EL 4, [k, k + 4) as 2.
+template <int EL>
+__device__ __forceinline__ void load_b(uint32_t (&w)[4], const uint16_t *row, int k, int r, bool vec) {
+  w[0] = w[1] = w[2] = w[3] = 0;
+  if (k >= r) return;
+  uint4 v;
+  if (!vec) {
+    v = load8<false>(row, k, min(r, k + EL));
+  } else if constexpr (EL == 8) {
+    v = keep8(__ldg(reinterpret_cast<const uint4 *>(row + k)), r - k);
+  } else {
+    const uint2 h = __ldg(reinterpret_cast<const uint2 *>(row + k));
+    v = keep8(make_uint4(h.x, h.y, 0, 0), r - k);
+  }
+  w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+}
+
+// v as two tf32 numbers; the lower of an infinite one means nothing.
+__device__ __forceinline__ void split(float v, uint32_t &hi, uint32_t &lo) {
+  hi = to_tf32(v);
+  lo = fabsf(__uint_as_float(hi)) < INFINITY ? to_tf32(v - __uint_as_float(hi)) : 0u;
+}
+
+// MT: 16-row tiles of the rank (R <= 16 MT).
+template <int DT, int MT>
 __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__ AdaptLaunch L, int *status) {
-  constexpr int kTile = 16 * WT;
+  constexpr int kTile = 16;  // tokens of an item
   constexpr int kR = 16 * MT;
-  constexpr int WK = kWarps / WT;  // warps that share a group of tokens
+  constexpr int WK = kWarps;
   extern __shared__ __align__(16) uint8_t smem[];
   float *part = reinterpret_cast<float *>(smem);          // [WK][kTile][kR] the warps' sums, then [kTile][kR] in part 0
   float *vfull = part + WK * kTile * kR;                  // [kTile][kR + 4] v of the whole cluster
@@ -173,7 +196,7 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
   }
 
   const int q = lane & 3, g = lane >> 2;
-  const int wt = warp / WK, wk = warp % WK;
+  const int wk = warp;
   // outputs of this CTA: whole groups of 16
   const int mper = ((M + 15) / 16 + kCluster - 1) / kCluster * 16;
   const int m0 = min(M, c * mper), m1 = min(M, m0 + mper);
@@ -212,7 +235,7 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
     bool xok[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int t = wt * 16 + j * 8 + g;
+      const int t = j * 8 + g;
       xok[j] = t < item.count;
       xr[j] = static_cast<const uint16_t *>(d.x) + (xok[j] ? (int64_t)tok[t] * d.ldx : 0);
     }
@@ -247,7 +270,7 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          mine[(wt * 16 + j * 8 + 2 * q + (e & 1)) * kR + i * 16 + g + (e >> 1) * 8] = acc[i][j][e];
+          mine[(j * 8 + 2 * q + (e & 1)) * kR + i * 16 + g + (e >> 1) * 8] = acc[i][j][e];
     __syncthreads();
     for (int i = tid; i < kTile * kR; i += kThreads) {
       float s = part[i];
@@ -276,14 +299,13 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
     for (int e = 0; e < 4; ++e) {
       // a0: (token g, k q), a1: (g + 8, q), a2: (g, q + 4), a3: (g + 8, q + 4); k = q and q + 4 of
       // step s stand for elements of the rank that B's lanes hold side by side
-      const int t = wt * 16 + g + (e & 1) * 8, k = (s >> 2) * 32 + q * 8 + (s & 3) * 2 + (e >> 1);
+      const int t = g + (e & 1) * 8, k = (s >> 2) * 32 + q * 8 + (s & 3) * 2 + (e >> 1);
       // kSteps below 4: the lane's 8 elements span the rank in chunks of 2 kSteps
       const int kk = kSteps >= 4 ? k : q * (2 * kSteps) + s * 2 + (e >> 1);
       const float v = r > 0 ? vfull[t * (kR + 4) + kk] : 0.0f;
-      vh[s][e] = to_tf32(v);
-      vl[s][e] = fabsf(__uint_as_float(vh[s][e])) < INFINITY ? to_tf32(v - __uint_as_float(vh[s][e])) : 0u;
+      split(v, vh[s][e], vl[s][e]);
     }
-  const int ta = wt * 16 + g, tb = ta + 8;
+  const int ta = g, tb = ta + 8;
   const bool oka = ta < item.count, okb = tb < item.count;
   const int64_t ia = oka ? tok[ta] : 0, ib = okb ? tok[tb] : 0;
   const bool yvec = (P.vec & 4) != 0;
@@ -304,23 +326,8 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
         for (int s4 = 0; s4 < (kSteps + 3) / 4; ++s4) {
           if (s4 * 32 >= r) break;
           constexpr int kEl = kSteps >= 4 ? 8 : 2 * kSteps;  // elements of a lane
-          const int k = kSteps >= 4 ? s4 * 32 + q * 8 : q * kEl;
-          uint32_t bw[4] = {0, 0, 0, 0};
-          if (ok && k < r) {
-            if (P.vec & 2) {
-              if constexpr (kEl == 8) {
-                const uint4 v = keep8(__ldg(reinterpret_cast<const uint4 *>(br + k)), r - k);
-                bw[0] = v.x, bw[1] = v.y, bw[2] = v.z, bw[3] = v.w;
-              } else {
-                const uint2 v = __ldg(reinterpret_cast<const uint2 *>(br + k));
-                const uint4 z = keep8(make_uint4(v.x, v.y, 0, 0), r - k);
-                bw[0] = z.x, bw[1] = z.y;
-              }
-            } else {
-              const uint4 v = load8<false>(br, k, min(r, k + kEl));
-              bw[0] = v.x, bw[1] = v.y, bw[2] = v.z, bw[3] = v.w;
-            }
-          }
+          uint32_t bw[4];
+          load_b<kEl>(bw, br, s4 * 32 + q * kEl, ok ? r : 0, (P.vec & 2) != 0);
 #pragma unroll
           for (int s = 0; s < (kSteps < 4 ? kSteps : 4); ++s) {
             uint32_t b0, b1;
@@ -353,76 +360,407 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
   }
 }
 
-template <int MT, int WT>
-size_t adapt_smem(int S) {
-  constexpr int kTile = 16 * WT, kR = 16 * MT, WK = kWarps / WT;
-  return sizeof(float) * (WK * kTile * kR + kTile * (kR + 4)) + sizeof(int) * (S + 1);
+
+// ------------------------------------------------------------------ prompts
+// Many tokens: x and y are most of the bytes, so the work is cut into three launches of many CTAs
+// each.  adapt_plan_kernel sorts the tokens by slot and cuts them into items of up to 64 tokens of one
+// slot.  adapt_shrink_kernel computes v = scale A x of an item, a cluster of 4 CTAs splitting K, with
+// x and A staged in shared memory by 16-byte cp.async; v goes to the workspace, fp32, in sorted order.
+// adapt_expand_kernel adds B v to 64 tokens x 128 outputs; every thread has its part of base in flight
+// before it turns to v and B, so the kernel runs as a copy of base to y does.  In one launch, as for
+// few tokens, each group of 16 outputs waited for its base: 350 us for the 4001 tokens of two
+// projections that take this 85 us.  Bound: HBM (base and y), then L2 (v and B, read once per tile).
+constexpr int kItem = 64;     // tokens of an item
+constexpr int kMTile = 128;   // outputs of a CTA of the expand kernel
+constexpr int kPlanThreads = 1024;
+constexpr int kSThreads = 128;
+constexpr int kSCluster = 4;
+constexpr int kSK = 64;       // elements of K of a stage
+constexpr int kSStages = 4;
+constexpr int kSPitch = kSK * 2 + 16;
+
+__device__ __forceinline__ int *plan_of(const AdaptWide &W, int plan) { return W.plans + (int64_t)plan * W.plan_ints; }
+// A plan: items (an int4 of slot, first place, tokens, 0), their number, then the tokens in order.
+__device__ __forceinline__ int4 item_of(const int *plan, int i) { return reinterpret_cast<const int4 *>(plan)[1 + i]; }
+
+__global__ void __launch_bounds__(kPlanThreads) adapt_plan_kernel(const __grid_constant__ AdaptLaunch L,
+                                                                  const __grid_constant__ AdaptWide W, int *status) {
+  extern __shared__ int cnt[];  // [S + 1] tokens, then the next place, of each slot
+  __shared__ int wsum[32][2];
+  const wt_adapt_desc &d = L.p[W.plan_proj[blockIdx.x]].d;
+  const int T = d.T, S = d.S, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool copy = d.base != d.y;
+  int *plan = plan_of(W, blockIdx.x);
+  int4 *items = reinterpret_cast<int4 *>(plan) + 1;
+  int *order = plan + W.order_at;
+  for (int s = tid; s <= S; s += kPlanThreads) cnt[s] = 0;
+  __syncthreads();
+  auto place = [&](int t) {  // a token's slot; -1: nothing to do
+    const int s = __ldg(d.slot + t);
+    return s >= 0 && s < S ? s : copy ? S : -1;
+  };
+  for (int t = tid; t < T; t += kPlanThreads) {
+    if (__ldg(d.slot + t) >= S && status) atomicCAS(status, 0, kStatusInvalid);
+    const int s = place(t);
+    if (s >= 0) atomicAdd(cnt + s, 1);
+  }
+  __syncthreads();
+  // places and items of the slots, by a scan over the slots
+  int tokens = 0, tiles = 0;
+  for (int s0 = 0; s0 <= S; s0 += kPlanThreads) {
+    const int s = s0 + tid, n = s <= S ? cnt[s] : 0, m = (n + kItem - 1) / kItem;
+    int a = n, b = m;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int ua = __shfl_up_sync(0xffffffffu, a, o), ub = __shfl_up_sync(0xffffffffu, b, o);
+      if (lane >= o) a += ua, b += ub;
+    }
+    if (lane == 31) wsum[warp][0] = a, wsum[warp][1] = b;
+    __syncthreads();
+    int ta = tokens, tb = tiles, at = tokens + a - n, it = tiles + b - m;
+    for (int w = 0; w < kPlanThreads / 32; ++w) {
+      if (w < warp) at += wsum[w][0], it += wsum[w][1];
+      ta += wsum[w][0], tb += wsum[w][1];
+    }
+    if (s <= S) cnt[s] = at;
+    for (int k = 0; k < m; ++k) items[it + k] = make_int4(s, at + k * kItem, min(kItem, n - k * kItem), 0);
+    tokens = ta, tiles = tb;
+    __syncthreads();
+  }
+  if (tid == 0) plan[0] = tiles;
+  // Which tokens share an item does not change their results, so their order within a slot is free.
+  for (int t = tid; t < T; t += kPlanThreads) {
+    const int s = place(t);
+    if (s >= 0) order[atomicAdd(cnt + s, 1)] = t;
+  }
 }
 
-template <int DT, int MT, int WT>
-cudaError_t run(const AdaptLaunch &L, int *status, cudaStream_t s) {
-  uint32_t items = 0;
-  int S = 0;
-  for (int i = 0; i < L.n; ++i) {
-    items += L.p[i].items;
-    S = std::max(S, L.p[i].d.S);
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t dst, const uint4 &v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+
+// MT: 16-row tiles of the rank, as for adapt_kernel.  A warp takes 16 tokens.
+template <int DT, int MT>
+__global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_constant__ AdaptLaunch L,
+                                                                 const __grid_constant__ AdaptWide W, int *status) {
+  constexpr int kR = 16 * MT;
+  constexpr int kStage = (kItem + kR) * kSPitch;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ int tok[kItem];
+  cg::cluster_group cl = cg::this_cluster();
+  const int c = cl.block_rank(), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
+  int pi = 0;
+  uint32_t w = blockIdx.x / kSCluster;
+  while (pi + 1 < L.n && w >= L.p[pi].items) w -= L.p[pi++].items;
+  const AdaptProj &P = L.p[pi];
+  const wt_adapt_desc &d = P.d;
+  const int *plan = plan_of(W, W.plan[pi]);
+  if ((int)w >= plan[0]) return;  // the whole cluster
+  const int4 item = item_of(plan, w);
+  const int slot = item.x, count = item.z, K = d.K, R = d.R;
+  if (slot >= d.S) return;
+  int r = d.rank ? __ldg(d.rank + slot) : R;
+  if (r < 0 || r > R) {
+    if (tid == 0 && c == 0 && status) atomicCAS(status, 0, kStatusInvalid);
+    r = min(max(r, 0), R);
   }
-  if (items == 0) return cudaSuccess;
+  if (r == 0) return;
+  if (tid < kItem) tok[tid] = tid < count ? plan[W.order_at + item.y + tid] : -1;
+  __syncthreads();
+
+  const uint16_t *A = static_cast<const uint16_t *>(d.A) + (int64_t)slot * d.a_slot;
+  const uint16_t *x = static_cast<const uint16_t *>(d.x);
+  const int steps = (K + kSK - 1) / kSK, per = (steps + kSCluster - 1) / kSCluster;
+  const int s0 = min(steps, c * per), s1 = min(steps, s0 + per);
+  const uint32_t base = smem_u32(smem);
+  const int rows = kItem + (r + 15) / 16 * 16;  // staged rows: tokens, then ranks
+  // Stage s: 8 vectors a row; absent tokens, ranks past the slot's and elements past K are zeros.
+  auto fetch = [&](int s) {
+    if (s < s1) {
+      const uint32_t st = base + (uint32_t)((s - s0) % kSStages) * kStage;
+      for (int i = tid; i < rows * 8; i += kSThreads) {
+        const int row = i >> 3, k = s * kSK + (i & 7) * 8;
+        const uint32_t dst = st + row * kSPitch + (i & 7) * 16;
+        const uint16_t *src = nullptr;
+        if (row < kItem) {
+          if (tok[row] >= 0) src = x + (int64_t)tok[row] * d.ldx;
+        } else if (row - kItem < r) {
+          src = A + (int64_t)(row - kItem) * K;
+        }
+        if (src && k < K && (P.vec & 1)) cp16(dst, src + k);
+        else sts128(dst, src ? load8<false>(src, k, K) : make_uint4(0, 0, 0, 0));
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < kSStages - 1; ++i) fetch(s0 + i);
+
+  float acc[MT][2][4];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.0f;
+  for (int s = s0; s < s1; ++s) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kSStages - 2) : "memory");
+    __syncthreads();
+    fetch(s + kSStages - 1);
+    const uint32_t xs = base + (uint32_t)((s - s0) % kSStages) * kStage, as = xs + kItem * kSPitch;
+#pragma unroll
+    for (int k = 0; k < kSK / 16; ++k) {
+      uint32_t xf[4];  // tokens 0-7 and 8-15 of the warp, each in two halves of 8 elements
+      ldsm4(xf, xs + (warp * 16 + (lane & 7) + (lane >> 4) * 8) * kSPitch + k * 32 + ((lane >> 3) & 1) * 16);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        if (i * 16 >= r) break;
+        uint32_t af[4];
+        ldsm4(af, as + (i * 16 + (lane & 15)) * kSPitch + k * 32 + (lane >> 4) * 16);
+        mma16816<DT>(acc[i][0], af[0], af[1], af[2], af[3], xf[0], xf[1]);
+        mma16816<DT>(acc[i][1], af[0], af[1], af[2], af[3], xf[2], xf[3]);
+      }
+    }
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
+  // this CTA's sums, [kItem][kR], over the stages
+  float *part = reinterpret_cast<float *>(smem);
+  static_assert(kItem * kR * 4 <= kSStages * kStage, "fits the stages");
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        part[(warp * 16 + j * 8 + 2 * q + (e & 1)) * kR + i * 16 + g + (e >> 1) * 8] = acc[i][j][e];
+  cl.sync();
+  // a quarter of the tokens each: the four CTAs' sums in their order; ranks past the slot's are zero
+  const float scale = d.scale ? __ldg(d.scale + slot) : 1.0f;
+  const float *from[kSCluster];
+#pragma unroll
+  for (int k = 0; k < kSCluster; ++k) from[k] = cl.map_shared_rank(part, k);
+  float *v = W.v + W.v_at[pi];
+  for (int i = tid; i < kItem / kSCluster * kR; i += kSThreads) {
+    const int t = c * (kItem / kSCluster) + i / kR, k = i % kR, at = t * kR + k;
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kSCluster; ++j) sum += from[j][at];
+    if (t < count) v[(int64_t)(item.y + t) * kR + k] = k < r ? sum * scale : 0.0f;
+  }
+  cl.sync();
+}
+
+template <int DT, int MT>
+__global__ void __launch_bounds__(kThreads, 2) adapt_expand_kernel(const __grid_constant__ AdaptLaunch L,
+                                                                   const __grid_constant__ AdaptWide W) {
+  constexpr int kR = 16 * MT, kEl = MT == 1 ? 4 : 8, kSub = kEl / 2;  // steps of 8 ranks in a lane's elements
+  __shared__ int tok[kItem];
+  int pi = 0;
+  uint32_t w = blockIdx.x;
+  while (pi + 1 < L.n && w >= L.p[pi].items * L.p[pi].m_tiles) {
+    w -= L.p[pi].items * L.p[pi].m_tiles;
+    ++pi;
+  }
+  const AdaptProj &P = L.p[pi];
+  const wt_adapt_desc &d = P.d;
+  const int *plan = plan_of(W, W.plan[pi]);
+  const int at_item = w / P.m_tiles, m_tile = w - at_item * P.m_tiles;
+  if (at_item >= plan[0]) return;
+  const int4 item = item_of(plan, at_item);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
+  const int slot = item.x, count = item.z, M = d.M;
+  if (tid < kItem) tok[tid] = tid < count ? plan[W.order_at + item.y + tid] : -1;
+  __syncthreads();
+  const int r = slot >= d.S ? 0 : min(max(d.rank ? __ldg(d.rank + slot) : d.R, 0), d.R);
+  // the warp's 16 tokens x 64 outputs: 4 groups of 16, in which a lane has 4 outputs of two tokens
+  const int t0 = (warp >> 1) * 16 + g, m0 = m_tile * kMTile + (warp & 1) * 64;
+  const int64_t tt[2] = {tok[t0], tok[t0 + 8]};
+  const bool yvec = (P.vec & 4) != 0;
+  float y[4][2][4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int m = m0 + j * 16 + 4 * q;
+      const float *bp = d.base + tt[e] * d.ldbase + m;
+      const bool ok = d.base && tt[e] >= 0;
+      if (yvec) {
+        const float4 b = ok && m + 4 <= M ? __ldcs(reinterpret_cast<const float4 *>(bp)) : make_float4(0, 0, 0, 0);
+        y[j][e][0] = b.x, y[j][e][1] = b.y, y[j][e][2] = b.z, y[j][e][3] = b.w;
+      }
+      if (!yvec || (m < M && m + 4 > M)) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[j][e][k] = ok && m + k < M ? bp[k] : 0.0f;
+      }
+    }
+  if (r > 0) {
+    const uint16_t *B = static_cast<const uint16_t *>(d.B) + (int64_t)slot * d.b_slot;
+    const float *v = W.v + W.v_at[pi] + (int64_t)item.y * kR;
+    float acc[4][2][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][n][e] = 0.0f;
+#pragma unroll 1
+    for (int k0 = 0; k0 < r; k0 += 4 * kEl) {
+      // the lane's elements of the rank: k0 + q kEl on, for both operands
+      uint32_t vh[kSub][4], vl[kSub][4];
+      float x[2][kEl];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int k = 0; k < kEl; k += 4) {
+          const float4 f = t0 + 8 * e < count ? __ldg(reinterpret_cast<const float4 *>(v + (t0 + 8 * e) * kR + k0 + q * kEl + k))
+                                              : make_float4(0, 0, 0, 0);
+          x[e][k] = f.x, x[e][k + 1] = f.y, x[e][k + 2] = f.z, x[e][k + 3] = f.w;
+        }
+#pragma unroll
+      for (int s = 0; s < kSub; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split(x[e & 1][2 * s + (e >> 1)], vh[s][e], vl[s][e]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          // column g of N tile n is output 4 (g / 2) + 2 n + g % 2 of the group
+          const int m = m0 + j * 16 + 4 * (g >> 1) + 2 * n + (g & 1);
+          uint32_t bw[4];
+          load_b<kEl>(bw, B + (int64_t)m * d.R, k0 + q * kEl, m < M ? r : 0, (P.vec & 2) != 0);
+#pragma unroll
+          for (int s = 0; s < kSub; ++s) {
+            uint32_t b0, b1;
+            widen<DT>(bw[s], b0, b1);
+            mma_tf32(acc[j][n], vl[s], b0, b1);
+            mma_tf32(acc[j][n], vh[s], b0, b1);
+          }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[j][e][k] += acc[j][k >> 1][2 * e + (k & 1)];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int m = m0 + j * 16 + 4 * q;
+      if (tt[e] < 0) continue;
+      float *yp = d.y + tt[e] * d.ldy + m;
+      if (yvec && m + 4 <= M) {
+        __stcs(reinterpret_cast<float4 *>(yp), make_float4(y[j][e][0], y[j][e][1], y[j][e][2], y[j][e][3]));
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (m + k < M) yp[k] = y[j][e][k];
+      }
+    }
+}
+
+template <typename... A>
+cudaError_t launch(void (*k)(A...), unsigned grid, int threads, int cluster, size_t smem, cudaStream_t s, const A &...args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(items * kCluster);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = adapt_smem<MT, WT>(S);
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = kCluster;
+  at[0].val.clusterDim.x = (unsigned)cluster;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, adapt_kernel<DT, MT, WT>, L, status);
+  cfg.numAttrs = cluster > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, k, args...);
 }
 
-template <int DT, int WT>
-cudaError_t run_rank(const AdaptLaunch &L, int max_R, int *status, cudaStream_t s) {
-  if (max_R <= 16) return run<DT, 1, WT>(L, status, s);
-  if (max_R <= 32) return run<DT, 2, WT>(L, status, s);
-  if (max_R <= 64) return run<DT, 4, WT>(L, status, s);
-  return run<DT, 8, WT>(L, status, s);
+int most_slots(const AdaptLaunch &L) {
+  int S = 0;
+  for (int i = 0; i < L.n; ++i) S = std::max(S, L.p[i].d.S);
+  return S;
 }
 
-template <int DT, int MT, int WT>
-cudaError_t prepare_one() {
-  return cudaFuncSetAttribute(adapt_kernel<DT, MT, WT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)adapt_smem<MT, WT>(WT_ADAPT_MAX_SLOTS));
+template <int MT>
+constexpr size_t few_smem(int S) {
+  return sizeof(float) * (kWarps * 16 * 16 * MT + 16 * (16 * MT + 4)) + sizeof(int) * (S + 1);
 }
-template <int DT, int WT>
-cudaError_t prepare_rank() {
-  cudaError_t e = prepare_one<DT, 1, WT>();
-  if (e == cudaSuccess) e = prepare_one<DT, 2, WT>();
-  if (e == cudaSuccess) e = prepare_one<DT, 4, WT>();
-  if (e == cudaSuccess) e = prepare_one<DT, 8, WT>();
+template <int MT>
+constexpr size_t shrink_smem() {
+  return (size_t)kSStages * (kItem + 16 * MT) * kSPitch;
+}
+
+template <int DT, int MT>
+cudaError_t run_few(const AdaptLaunch &L, int *status, cudaStream_t s) {
+  uint32_t items = 0;
+  for (int i = 0; i < L.n; ++i) items += L.p[i].items;
+  if (items == 0) return cudaSuccess;
+  return launch(adapt_kernel<DT, MT>, items * kCluster, kThreads, kCluster, few_smem<MT>(most_slots(L)), s, L, status);
+}
+
+template <int DT, int MT>
+cudaError_t run_wide(const AdaptLaunch &L, const AdaptWide &W, int *status, cudaStream_t s) {
+  uint32_t items = 0, tiles = 0;
+  for (int i = 0; i < L.n; ++i) {
+    items += L.p[i].items;
+    tiles += L.p[i].items * L.p[i].m_tiles;
+  }
+  if (items == 0) return cudaSuccess;
+  cudaError_t e = launch(adapt_plan_kernel, (unsigned)W.n_plans, kPlanThreads, 1, sizeof(int) * (most_slots(L) + 1), s, L, W, status);
+  if (e == cudaSuccess)
+    e = launch(adapt_shrink_kernel<DT, MT>, items * kSCluster, kSThreads, kSCluster, shrink_smem<MT>(), s, L, W, status);
+  if (e == cudaSuccess) e = launch(adapt_expand_kernel<DT, MT>, tiles, kThreads, 1, 0, s, L, W);
   return e;
+}
+
+template <int DT, int MT>
+cudaError_t prepare_one() {
+  cudaError_t e = cudaFuncSetAttribute(adapt_kernel<DT, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)few_smem<MT>(WT_ADAPT_MAX_SLOTS));
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(adapt_shrink_kernel<DT, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shrink_smem<MT>());
+  return e;
+}
+template <int DT>
+cudaError_t prepare_type() {
+  cudaError_t e = prepare_one<DT, 1>();
+  if (e == cudaSuccess) e = prepare_one<DT, 2>();
+  if (e == cudaSuccess) e = prepare_one<DT, 4>();
+  if (e == cudaSuccess) e = prepare_one<DT, 8>();
+  return e;
+}
+
+template <int DT>
+cudaError_t run_type(const AdaptLaunch &L, const AdaptWide *W, int max_R, int *status, cudaStream_t s) {
+  switch (adapt_rank_tiles(max_R)) {
+    case 1: return W ? run_wide<DT, 1>(L, *W, status, s) : run_few<DT, 1>(L, status, s);
+    case 2: return W ? run_wide<DT, 2>(L, *W, status, s) : run_few<DT, 2>(L, status, s);
+    case 4: return W ? run_wide<DT, 4>(L, *W, status, s) : run_few<DT, 4>(L, status, s);
+    default: return W ? run_wide<DT, 8>(L, *W, status, s) : run_few<DT, 8>(L, status, s);
+  }
 }
 
 }  // namespace
 
-// Tokens of one work item: 16, or 64 where there are so many tokens that reading a slot's A and B
-// once per 16 of them would cost more than x and y.
-int adapt_tile(int max_T) { return max_T >= 256 ? 64 : 16; }
-
 cudaError_t adapt_prepare() {
-  cudaError_t e = prepare_rank<WT_BF16, 1>();
-  if (e == cudaSuccess) e = prepare_rank<WT_BF16, 4>();
-  if (e == cudaSuccess) e = prepare_rank<WT_F16, 1>();
-  if (e == cudaSuccess) e = prepare_rank<WT_F16, 4>();
-  return e;
+  const cudaError_t e = prepare_type<WT_BF16>();
+  return e == cudaSuccess ? prepare_type<WT_F16>() : e;
 }
 
-cudaError_t launch_adapt(const AdaptLaunch &L, int max_R, int max_T, int *status, cudaStream_t s) {
-  const bool wide = adapt_tile(max_T) == 64;
-  if (L.p[0].d.dtype == WT_BF16)
-    return wide ? run_rank<WT_BF16, 4>(L, max_R, status, s) : run_rank<WT_BF16, 1>(L, max_R, status, s);
-  return wide ? run_rank<WT_F16, 4>(L, max_R, status, s) : run_rank<WT_F16, 1>(L, max_R, status, s);
+cudaError_t launch_adapt(const AdaptLaunch &L, const AdaptWide *W, int max_R, int *status, cudaStream_t s) {
+  return L.p[0].d.dtype == WT_BF16 ? run_type<WT_BF16>(L, W, max_R, status, s) : run_type<WT_F16>(L, W, max_R, status, s);
 }
 
 }  // namespace wt

@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(kPThreads, 3) probs_kernel(const wt_probs_desc
   const int held4 = held / 4;
   const float4 *sv4 = reinterpret_cast<const float4 *>(sv);
   float m = -INFINITY;
+#pragma unroll 4
   for (int i = tid; i < held4; i += kPThreads) {
     const float4 v = sv4[i];
     m = fmaxf(m, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
@@ -165,6 +166,7 @@ __global__ void __launch_bounds__(kPThreads, 3) probs_kernel(const wt_probs_desc
   // a logit of -infinity is no token, whatever the temperature
   auto e = [&](float x) { return x == -INFINITY ? 0.0f : exp2_full((x - mz) * k); };
   float s = 0.0f;
+#pragma unroll 4
   for (int i = tid; i < held4; i += kPThreads) {
     float4 v = sv4[i];
     v.x = e(v.x), v.y = e(v.y), v.z = e(v.z), v.w = e(v.w);
@@ -199,6 +201,7 @@ __global__ void __launch_bounds__(kPThreads, 3) probs_kernel(const wt_probs_desc
   // a row of -infinity alone has the sum 0: zeros.  NaN anywhere makes the sum NaN, and every element.
   const float f = sr == 0.0f ? 0.0f : scale(m) / sr;
   if (reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+#pragma unroll 4
     for (int i = tid; i < held4; i += kPThreads) {
       float4 v = sv4[i];
       v.x *= f, v.y *= f, v.z *= f, v.w *= f;

@@ -117,7 +117,8 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
       const wt_adapt_desc &e = P.d;
       const bool copy = e.base != e.y;
       P.items = (uint32_t)(std::min(e.S + (copy ? 1 : 0), e.T) + e.T / tile);
-      all += P.items;
+      P.m_tiles = (uint32_t)((e.M + 127) / 128);
+      all += (uint64_t)P.items * P.m_tiles;
       P.vec = 0;
       if (e.K % 8 == 0 && e.ldx % 8 == 0 && e.a_slot % 8 == 0 && aligned(e.x, 16) && aligned(e.A, 16)) P.vec |= 1;
       // a lane reads 4 elements of a row of B where no rank is above 16, else 8
@@ -125,9 +126,42 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
       if (e.R % el == 0 && e.b_slot % el == 0 && aligned(e.B, 2 * el)) P.vec |= 2;
       if (e.ldy % 4 == 0 && aligned(e.y, 16) && (!e.base || (e.ldbase % 4 == 0 && aligned(e.base, 16)))) P.vec |= 4;
     }
-    if (all > (1u << 27)) return serve_error(WT_EINVAL, "wt_adapt: %llu work items in one launch", (unsigned long long)all);
-    CU(wt::launch_adapt(L, max_R, max_T, ctx.status, s));
-    wt::serve_launched(h, 1);
+    if (all > (1u << 27)) return serve_error(WT_EINVAL, "wt_adapt: %llu tiles of work in one launch", (unsigned long long)all);
+    if (max_T < wt::kAdaptFew) {
+      CU(wt::launch_adapt(L, nullptr, max_R, ctx.status, s));
+      wt::serve_launched(h, 1);
+      continue;
+    }
+    // many tokens: a plan for each distinct slot map, and v of every projection, in the workspace
+    wt::AdaptWide W = {};
+    int64_t items = 0, v = 0;
+    for (int k = 0; k < L.n; ++k) {
+      const wt_adapt_desc &e = L.p[k].d;
+      auto same = [&](int q) {
+        const wt_adapt_desc &f = L.p[W.plan_proj[q]].d;
+        return f.slot == e.slot && f.T == e.T && f.S == e.S && (f.base == f.y) == (e.base == e.y);
+      };
+      int q = 0;
+      while (q < W.n_plans && !same(q)) ++q;
+      if (q == W.n_plans) W.plan_proj[W.n_plans++] = k;
+      W.plan[k] = q;
+      W.v_at[k] = v;
+      v += (int64_t)e.T * 16 * wt::adapt_rank_tiles(max_R);
+      items = std::max<int64_t>(items, L.p[k].items);
+    }
+    W.order_at = 4 * (items + 1);
+    W.plan_ints = (W.order_at + max_T + 63) / 64 * 64;
+    Lock lock(h);
+    wt::ServeWorkspace w;
+    const size_t plans = (size_t)(W.n_plans * W.plan_ints) * 4;
+    CHECK(wt::serve_workspace(h, s, plans + (size_t)v * 4, &w));
+    W.plans = static_cast<int *>(w.p);
+    W.v = reinterpret_cast<float *>(static_cast<uint8_t *>(w.p) + plans);
+    const cudaError_t e = wt::launch_adapt(L, &W, max_R, ctx.status, s);
+    const int rc = wt::serve_workspace_done(h, s, w);
+    CU(e);
+    wt::serve_launched(h, 3);
+    if (rc) return rc;
   }
   return WT_OK;
 }

@@ -43,18 +43,32 @@ cudaError_t serve_prepare();  // one-time function attributes of every kernel be
 
 // ---------------------------------------------------------------- wt_adapt.cu
 constexpr int kAdaptProjs = 8;  // projections of one launch
+constexpr int kAdaptFew = 256;  // tokens from which a launch's work is planned on the device first
+constexpr int adapt_tile(int max_T) { return max_T < kAdaptFew ? 16 : 64; }  // tokens of a work item
+// 16-row tiles of the rank that the kernels are built for
+constexpr int adapt_rank_tiles(int max_R) { return max_R <= 16 ? 1 : max_R <= 32 ? 2 : max_R <= 64 ? 4 : 8; }
 struct AdaptProj {
   wt_adapt_desc d;
-  uint32_t items;  // upper bound of (slot, token tile) work items
-  uint32_t vec;    // bit 0: A and x load in 16-byte vectors; bit 1: B does; bit 2: base and y do
+  uint32_t items;    // upper bound of (slot, token tile) work items
+  uint32_t m_tiles;  // tiles of 128 outputs
+  uint32_t vec;      // bit 0: A and x load in 16-byte vectors; bit 1: B does; bit 2: base and y do
 };
 struct AdaptLaunch {
   AdaptProj p[kAdaptProjs];
   int n;
 };
+// Workspace of a launch of many tokens: a plan for each distinct slot map, and v of each projection.
+struct AdaptWide {
+  int *plans;          // [n_plans][plan_ints]: {items, -, -, -}, items as int4, tokens from order_at on
+  float *v;
+  int64_t plan_ints, order_at;
+  int64_t v_at[kAdaptProjs];  // v [T, 16 adapt_rank_tiles], in the plan's token order
+  int plan[kAdaptProjs];      // a projection's plan
+  int plan_proj[kAdaptProjs]; // a plan's first projection
+  int n_plans;
+};
 cudaError_t adapt_prepare();
-int adapt_tile(int max_T);  // tokens of one work item
-cudaError_t launch_adapt(const AdaptLaunch &L, int max_R, int max_T, int *status, cudaStream_t s);
+cudaError_t launch_adapt(const AdaptLaunch &L, const AdaptWide *W, int max_R, int *status, cudaStream_t s);
 
 // ---------------------------------------------------------------- wt_draw.cu
 cudaError_t draw_prepare();
