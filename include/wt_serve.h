@@ -43,7 +43,8 @@ extern "C" {
  * a_slot and b_slot elements apart.  A slot of rank[s] < R uses the first rank[s] rows of A and
  * columns of B only; what lies in the others is never used (NaN there is harmless).  x is bf16 or
  * f16, as are A and B; base and y are fp32, as wt_pass leaves them.  A x is summed in fp32 and
- * enters the second product with at least 22 significant bits, which is summed in fp32.
+ * enters the second product with 22 bits or more (of the token's largest number), which is summed in
+ * fp32.
  * base may be y itself (then tokens without adapter cost nothing); otherwise the two must not
  * overlap.  base NULL stands for zeros.
  *

@@ -16,6 +16,8 @@
 #include <type_traits>
 
 #include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include "wt_device.cuh"
 #include "wt_serve.h"
@@ -365,18 +367,24 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
 // Many tokens: x and y are most of the bytes, so the work is cut into three launches of many CTAs
 // each.  adapt_plan_kernel sorts the tokens by slot and cuts them into items of up to 64 tokens of one
 // slot.  adapt_shrink_kernel computes v = scale A x of an item, a cluster of 4 CTAs splitting K, with
-// x and A staged in shared memory by 16-byte cp.async; v goes to the workspace, fp32, in sorted order.
-// adapt_expand_kernel adds B v to 64 tokens x 128 outputs; every thread has its part of base in flight
-// before it turns to v and B, so the kernel runs as a copy of base to y does.  In one launch, as for
-// few tokens, each group of 16 outputs waited for its base: 350 us for the 4001 tokens of two
-// projections that take this 85 us.  Bound: HBM (base and y), then L2 (v and B, read once per tile).
+// x and A staged in shared memory by 16-byte cp.async.  adapt_expand_kernel adds B v, a CTA taking
+// several tiles of 64 tokens x 128 outputs of an item, with the base and B of the next tiles always on
+// their way to shared memory (loading B into registers as it was needed, each tile waited for L2 twice:
+// 166 us for the expand kernel of 4001 tokens of two projections of 6912 outputs, against XXX).
+//
+// v crosses between the two as 16-bit parts that add up to it, so that the second product's operands
+// need no conversion: bf16 in three parts (24 bits); f16 in two (22 bits), after a power of two for
+// each token has brought its largest v to 2^14, far from f16's ends; the power is taken back in fp32.
+// Bound: HBM (base and y).
 constexpr int kItem = 64;     // tokens of an item
 constexpr int kMTile = 128;   // outputs of a CTA of the expand kernel
 constexpr int kPlanThreads = 1024;
 constexpr int kSThreads = 128;
 constexpr int kSCluster = 4;
 constexpr int kSK = 64;       // elements of K of a stage
-constexpr int kSStages = 4;
+constexpr int kSStages = 3;   // 55 KB at rank 64: four CTAs per SM
+template <int DT>
+constexpr int kParts = DT == WT_BF16 ? 3 : 2;
 constexpr int kSPitch = kSK * 2 + 16;
 
 __device__ __forceinline__ int *plan_of(const AdaptWide &W, int plan) { return W.plans + (int64_t)plan * W.plan_ints; }
@@ -544,68 +552,149 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
       for (int e = 0; e < 4; ++e)
         part[(warp * 16 + j * 8 + 2 * q + (e & 1)) * kR + i * 16 + g + (e >> 1) * 8] = acc[i][j][e];
   cl.sync();
-  // a quarter of the tokens each: the four CTAs' sums in their order; ranks past the slot's are zero
+  // a quarter of the tokens each, 8 lanes to a token: the four CTAs' sums in their order; ranks past
+  // the slot's are zero
   const float scale = d.scale ? __ldg(d.scale + slot) : 1.0f;
   const float *from[kSCluster];
 #pragma unroll
   for (int k = 0; k < kSCluster; ++k) from[k] = cl.map_shared_rank(part, k);
-  float *v = W.v + W.v_at[pi];
-  for (int i = tid; i < kItem / kSCluster * kR; i += kSThreads) {
-    const int t = c * (kItem / kSCluster) + i / kR, k = i % kR, at = t * kR + k;
+  static_assert(kItem / kSCluster * 8 == kSThreads, "8 lanes to a token");
+  const int t = c * (kItem / kSCluster) + (tid >> 3), k0 = (tid & 7) * (kR / 8);
+  float v[kR / 8], top = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kR / 8; ++k) {
     float sum = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kSCluster; ++j) sum += from[j][at];
-    if (t < count) v[(int64_t)(item.y + t) * kR + k] = k < r ? sum * scale : 0.0f;
+    for (int j = 0; j < kSCluster; ++j) sum += from[j][t * kR + k0 + k];
+    v[k] = k0 + k < r ? sum * scale : 0.0f;
+    top = fmaxf(top, fabsf(v[k]));
   }
   cl.sync();
+  uint16_t *out = W.v + W.v_at[pi] + (int64_t)(item.y + t) * kR + k0;
+  const int64_t part_at = (int64_t)d.T * kR;
+  if constexpr (DT == WT_F16) {
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    // 2^(14 - exponent of top), within what fp32 can take back; 1 for zeros, infinities and NaN
+    const int e = top > 0.0f && top < INFINITY ? min(max((int)(__float_as_uint(top) >> 23) - 127, -112), 127) : 14;
+    const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
+    if (t < count) {
+      if ((tid & 7) == 0) W.back[W.back_at[pi] + item.y + t] = __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+#pragma unroll
+      for (int k = 0; k < kR / 8; ++k) {
+        const float x = v[k] * up;
+        const __half h = __float2half_rn(x);
+        const float f = __half2float(h);
+        out[k] = __half_as_ushort(h);
+        out[part_at + k] = __half_as_ushort(__float2half_rn(fabsf(f) < INFINITY ? x - f : 0.0f));
+      }
+    }
+  } else if (t < count) {
+#pragma unroll
+    for (int k = 0; k < kR / 8; ++k) {
+      float x = v[k];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const __nv_bfloat16 h = __float2bfloat16_rn(x);
+        const float f = __bfloat162float(h);
+        out[i * part_at + k] = __bfloat16_as_ushort(h);
+        x = fabsf(f) < INFINITY ? x - f : 0.0f;
+      }
+    }
+  }
 }
 
+// Shared memory of the expand kernel: a ring of tiles (base, 8 vectors that only their thread reads;
+// then the 128 rows of B), and the item's v.
 template <int DT, int MT>
-__global__ void __launch_bounds__(kThreads, 2) adapt_expand_kernel(const __grid_constant__ AdaptLaunch L,
+struct Expand {
+  static constexpr int stages = MT == 8 ? 2 : 3;
+  static constexpr uint32_t pitch = 32 * MT + 16, base = kThreads * 128, stage = base + kMTile * pitch;
+  static constexpr uint32_t v = stages * stage, part = kItem * pitch;
+  static constexpr size_t smem = v + kParts<DT> * part;
+};
+static_assert(Expand<WT_BF16, 4>::smem <= 232448 && Expand<WT_BF16, 8>::smem <= 232448, "shared memory of one CTA");
+
+template <int DT, int MT>
+__global__ void __launch_bounds__(kThreads, 1) adapt_expand_kernel(const __grid_constant__ AdaptLaunch L,
                                                                    const __grid_constant__ AdaptWide W) {
-  constexpr int kR = 16 * MT, kEl = MT == 1 ? 4 : 8, kSub = kEl / 2;  // steps of 8 ranks in a lane's elements
-  __shared__ int tok[kItem];
+  using X = Expand<DT, MT>;
+  constexpr int kR = 16 * MT;
+  extern __shared__ __align__(16) uint8_t smem[];
   int pi = 0;
   uint32_t w = blockIdx.x;
-  while (pi + 1 < L.n && w >= L.p[pi].items * L.p[pi].m_tiles) {
-    w -= L.p[pi].items * L.p[pi].m_tiles;
+  while (pi + 1 < L.n && w >= L.p[pi].items * L.p[pi].m_groups) {
+    w -= L.p[pi].items * L.p[pi].m_groups;
     ++pi;
   }
   const AdaptProj &P = L.p[pi];
   const wt_adapt_desc &d = P.d;
   const int *plan = plan_of(W, W.plan[pi]);
-  const int at_item = w / P.m_tiles, m_tile = w - at_item * P.m_tiles;
+  const int at_item = w / P.m_groups, group = w - at_item * P.m_groups;
   if (at_item >= plan[0]) return;
   const int4 item = item_of(plan, at_item);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
   const int slot = item.x, count = item.z, M = d.M;
-  if (tid < kItem) tok[tid] = tid < count ? plan[W.order_at + item.y + tid] : -1;
-  __syncthreads();
+  // the warp's 16 tokens; in a tile it takes 64 outputs: 4 groups of 16, of which a lane has 4 outputs of
+  // two tokens
+  const int t0 = (warp >> 1) * 16 + g;
+  int64_t tt[2];
+  float back[2] = {1.0f, 1.0f};
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int t = t0 + 8 * e;
+    tt[e] = t < count ? plan[W.order_at + item.y + t] : -1;
+    if (DT == WT_F16 && t < count && slot < d.S) back[e] = W.back[W.back_at[pi] + item.y + t];
+  }
   const int r = slot >= d.S ? 0 : min(max(d.rank ? __ldg(d.rank + slot) : d.R, 0), d.R);
-  // the warp's 16 tokens x 64 outputs: 4 groups of 16, in which a lane has 4 outputs of two tokens
-  const int t0 = (warp >> 1) * 16 + g, m0 = m_tile * kMTile + (warp & 1) * 64;
-  const int64_t tt[2] = {tok[t0], tok[t0 + 8]};
-  const bool yvec = (P.vec & 4) != 0;
-  float y[4][2][4];
+  const int ksteps = (r + 15) / 16;
+  const bool yvec = (P.vec & 4) != 0, bvec = (P.vec & 2) != 0;
+  const int tiles = (M + kMTile - 1) / kMTile, tile0 = group * P.group_tiles, tile1 = min(tiles, tile0 + P.group_tiles);
+  const uint32_t base = smem_u32(smem);
+  const uint16_t *B = static_cast<const uint16_t *>(d.B) + (int64_t)slot * d.b_slot;
+  auto fetch = [&](int tile) {
+    if (tile < tile1) {
+      const uint32_t st = base + (uint32_t)((tile - tile0) % X::stages) * X::stage;
+      if (yvec && d.base) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int m = m0 + j * 16 + 4 * q;
-      const float *bp = d.base + tt[e] * d.ldbase + m;
-      const bool ok = d.base && tt[e] >= 0;
-      if (yvec) {
-        const float4 b = ok && m + 4 <= M ? __ldcs(reinterpret_cast<const float4 *>(bp)) : make_float4(0, 0, 0, 0);
-        y[j][e][0] = b.x, y[j][e][1] = b.y, y[j][e][2] = b.z, y[j][e][3] = b.w;
+          for (int e = 0; e < 2; ++e) {
+            const int m = tile * kMTile + (warp & 1) * 64 + j * 16 + 4 * q;
+            if (tt[e] >= 0 && m + 4 <= M)
+              cp16(st + (j * 2 + e) * (kThreads * 16) + tid * 16, d.base + tt[e] * d.ldbase + m);
+          }
       }
-      if (!yvec || (m < M && m + 4 > M)) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) y[j][e][k] = ok && m + k < M ? bp[k] : 0.0f;
+      // Output 4 a + 2 n + b of a group of 16 goes to row 8 n + 2 a + b: the rows of N tile n, in which a
+      // lane's four accumulators of two tiles are neighbouring outputs.  Absent ones are zeros.
+      for (int i = tid; i < kMTile * ksteps * 2; i += kThreads) {
+        const int row = i / (2 * ksteps), k = (i - row * 2 * ksteps) * 8, m = tile * kMTile + row;
+        const int to = (row & ~15) | (row & 2) << 2 | (row & 12) >> 1 | (row & 1);
+        const uint32_t dst = st + X::base + to * X::pitch + k * 2;
+        if (bvec && m < M && k + 8 <= r) cp16(dst, B + (int64_t)m * d.R + k);
+        else sts128(dst, m < M ? load8<false>(B + (int64_t)m * d.R, k, r) : make_uint4(0, 0, 0, 0));
       }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
   if (r > 0) {
-    const uint16_t *B = static_cast<const uint16_t *>(d.B) + (int64_t)slot * d.b_slot;
-    const float *v = W.v + W.v_at[pi] + (int64_t)item.y * kR;
+    // v of the item; absent tokens are zeros
+    const uint16_t *v = W.v + W.v_at[pi] + (int64_t)item.y * kR;
+    for (int i = tid; i < kParts<DT> * kItem * ksteps * 2; i += kThreads) {
+      const int pt = i / (kItem * 2 * ksteps), t = i / (2 * ksteps) % kItem, k = i % (2 * ksteps) * 8;
+      const uint32_t dst = base + X::v + pt * X::part + t * X::pitch + k * 2;
+      if (t < count) cp16(dst, v + pt * (int64_t)d.T * kR + (int64_t)t * kR + k);
+      else sts128(dst, make_uint4(0, 0, 0, 0));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < X::stages - 1; ++i) fetch(tile0 + i);
+
+  for (int tile = tile0; tile < tile1; ++tile) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(X::stages - 2) : "memory");
+    __syncthreads();
+    fetch(tile + X::stages - 1);  // where the tile before lay
+    const uint32_t st = base + (uint32_t)((tile - tile0) % X::stages) * X::stage;
     float acc[4][2][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -614,61 +703,45 @@ __global__ void __launch_bounds__(kThreads, 2) adapt_expand_kernel(const __grid_
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[j][n][e] = 0.0f;
 #pragma unroll 1
-    for (int k0 = 0; k0 < r; k0 += 4 * kEl) {
-      // the lane's elements of the rank: k0 + q kEl on, for both operands
-      uint32_t vh[kSub][4], vl[kSub][4];
-      float x[2][kEl];
+    for (int s = 0; s < ksteps; ++s) {
+      uint32_t a[kParts<DT>][4];
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int i = 0; i < kParts<DT>; ++i)
+        ldsm4(a[i], base + X::v + i * X::part + ((warp >> 1) * 16 + (lane & 15)) * X::pitch + s * 32 + (lane >> 4) * 16);
 #pragma unroll
-        for (int k = 0; k < kEl; k += 4) {
-          const float4 f = t0 + 8 * e < count ? __ldg(reinterpret_cast<const float4 *>(v + (t0 + 8 * e) * kR + k0 + q * kEl + k))
-                                              : make_float4(0, 0, 0, 0);
-          x[e][k] = f.x, x[e][k + 1] = f.y, x[e][k + 2] = f.z, x[e][k + 3] = f.w;
+      for (int j = 0; j < 4; ++j) {
+        uint32_t b[4];  // N tiles 0 and 1, each in two halves of 8 ranks
+        ldsm4(b, st + X::base + ((warp & 1) * 64 + j * 16 + (lane & 7) + (lane >> 4) * 8) * X::pitch + s * 32 + ((lane >> 3) & 1) * 16);
+#pragma unroll
+        for (int i = kParts<DT> - 1; i >= 0; --i) {  // the smallest part first
+          mma16816<DT>(acc[j][0], a[i][0], a[i][1], a[i][2], a[i][3], b[0], b[1]);
+          mma16816<DT>(acc[j][1], a[i][0], a[i][1], a[i][2], a[i][3], b[2], b[3]);
         }
-#pragma unroll
-      for (int s = 0; s < kSub; ++s)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) split(x[e & 1][2 * s + (e >> 1)], vh[s][e], vl[s][e]);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          // column g of N tile n is output 4 (g / 2) + 2 n + g % 2 of the group
-          const int m = m0 + j * 16 + 4 * (g >> 1) + 2 * n + (g & 1);
-          uint32_t bw[4];
-          load_b<kEl>(bw, B + (int64_t)m * d.R, k0 + q * kEl, m < M ? r : 0, (P.vec & 2) != 0);
-#pragma unroll
-          for (int s = 0; s < kSub; ++s) {
-            uint32_t b0, b1;
-            widen<DT>(bw[s], b0, b1);
-            mma_tf32(acc[j][n], vl[s], b0, b1);
-            mma_tf32(acc[j][n], vh[s], b0, b1);
-          }
-        }
+      }
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < 2; ++e) {
+        const int m = tile * kMTile + (warp & 1) * 64 + j * 16 + 4 * q;
+        if (tt[e] < 0) continue;
+        float o[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) y[j][e][k] += acc[j][k >> 1][2 * e + (k & 1)];
-  }
+        for (int k = 0; k < 4; ++k) o[k] = acc[j][k >> 1][2 * e + (k & 1)] * back[e];
+        float *yp = d.y + tt[e] * d.ldy + m;
+        if (yvec && m + 4 <= M) {
+          if (d.base) {
+            const uint4 b = lds128(st + (j * 2 + e) * (kThreads * 16) + tid * 16);
+            o[0] += __uint_as_float(b.x), o[1] += __uint_as_float(b.y), o[2] += __uint_as_float(b.z), o[3] += __uint_as_float(b.w);
+          }
+          __stcs(reinterpret_cast<float4 *>(yp), make_float4(o[0], o[1], o[2], o[3]));
+        } else {
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int m = m0 + j * 16 + 4 * q;
-      if (tt[e] < 0) continue;
-      float *yp = d.y + tt[e] * d.ldy + m;
-      if (yvec && m + 4 <= M) {
-        __stcs(reinterpret_cast<float4 *>(yp), make_float4(y[j][e][0], y[j][e][1], y[j][e][2], y[j][e][3]));
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (m + k < M) yp[k] = y[j][e][k];
+          for (int k = 0; k < 4; ++k)
+            if (m + k < M) yp[k] = (d.base ? d.base[tt[e] * d.ldbase + m + k] : 0.0f) + o[k];
+        }
       }
-    }
+  }
 }
 
 template <typename... A>
@@ -715,13 +788,13 @@ cudaError_t run_wide(const AdaptLaunch &L, const AdaptWide &W, int *status, cuda
   uint32_t items = 0, tiles = 0;
   for (int i = 0; i < L.n; ++i) {
     items += L.p[i].items;
-    tiles += L.p[i].items * L.p[i].m_tiles;
+    tiles += L.p[i].items * L.p[i].m_groups;
   }
   if (items == 0) return cudaSuccess;
   cudaError_t e = launch(adapt_plan_kernel, (unsigned)W.n_plans, kPlanThreads, 1, sizeof(int) * (most_slots(L) + 1), s, L, W, status);
   if (e == cudaSuccess)
     e = launch(adapt_shrink_kernel<DT, MT>, items * kSCluster, kSThreads, kSCluster, shrink_smem<MT>(), s, L, W, status);
-  if (e == cudaSuccess) e = launch(adapt_expand_kernel<DT, MT>, tiles, kThreads, 1, 0, s, L, W);
+  if (e == cudaSuccess) e = launch(adapt_expand_kernel<DT, MT>, tiles, kThreads, 1, Expand<DT, MT>::smem, s, L, W);
   return e;
 }
 
@@ -731,6 +804,8 @@ cudaError_t prepare_one() {
                                        (int)few_smem<MT>(WT_ADAPT_MAX_SLOTS));
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(adapt_shrink_kernel<DT, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shrink_smem<MT>());
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(adapt_expand_kernel<DT, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Expand<DT, MT>::smem);
   return e;
 }
 template <int DT>

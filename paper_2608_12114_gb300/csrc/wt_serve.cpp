@@ -18,6 +18,8 @@ using wt::serve_error;
     if (e_ != cudaSuccess) return wt::serve_cuda_error(e_, #call);  \
   } while (0)
 
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 struct Lock {
   wt_handle *h;
   explicit Lock(wt_handle *hh) : h(hh) { wt::serve_lock(h); }
@@ -117,8 +119,7 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
       const wt_adapt_desc &e = P.d;
       const bool copy = e.base != e.y;
       P.items = (uint32_t)(std::min(e.S + (copy ? 1 : 0), e.T) + e.T / tile);
-      P.m_tiles = (uint32_t)((e.M + 127) / 128);
-      all += (uint64_t)P.items * P.m_tiles;
+      all += (uint64_t)P.items * ((e.M + 127) / 128);
       P.vec = 0;
       if (e.K % 8 == 0 && e.ldx % 8 == 0 && e.a_slot % 8 == 0 && aligned(e.x, 16) && aligned(e.A, 16)) P.vec |= 1;
       // a lane reads 4 elements of a row of B where no rank is above 16, else 8
@@ -134,9 +135,15 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
     }
     // many tokens: a plan for each distinct slot map, and v of every projection, in the workspace
     wt::AdaptWide W = {};
-    int64_t items = 0, v = 0;
+    int64_t items = 0, v = 0, back = 0;
+    const int64_t row = 16 * wt::adapt_rank_tiles(max_R), parts = dtype == WT_BF16 ? 3 : 2;
+    // tiles of outputs that a CTA takes one after another: about three waves of one CTA per SM in all
+    const int64_t run = std::max<int64_t>(1, ceil_div((int64_t)all, 3 * wt::num_sms()));
     for (int k = 0; k < L.n; ++k) {
       const wt_adapt_desc &e = L.p[k].d;
+      const int64_t tiles = ceil_div(e.M, 128);
+      L.p[k].m_groups = (uint32_t)ceil_div(tiles, run);
+      L.p[k].group_tiles = (uint32_t)ceil_div(tiles, L.p[k].m_groups);
       auto same = [&](int q) {
         const wt_adapt_desc &f = L.p[W.plan_proj[q]].d;
         return f.slot == e.slot && f.T == e.T && f.S == e.S && (f.base == f.y) == (e.base == e.y);
@@ -146,7 +153,9 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
       if (q == W.n_plans) W.plan_proj[W.n_plans++] = k;
       W.plan[k] = q;
       W.v_at[k] = v;
-      v += (int64_t)e.T * 16 * wt::adapt_rank_tiles(max_R);
+      W.back_at[k] = back;
+      v += parts * e.T * row;
+      back += e.T;
       items = std::max<int64_t>(items, L.p[k].items);
     }
     W.order_at = 4 * (items + 1);
@@ -154,9 +163,10 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
     Lock lock(h);
     wt::ServeWorkspace w;
     const size_t plans = (size_t)(W.n_plans * W.plan_ints) * 4;
-    CHECK(wt::serve_workspace(h, s, plans + (size_t)v * 4, &w));
+    CHECK(wt::serve_workspace(h, s, plans + (size_t)v * 2 + (size_t)back * 4, &w));
     W.plans = static_cast<int *>(w.p);
-    W.v = reinterpret_cast<float *>(static_cast<uint8_t *>(w.p) + plans);
+    W.v = reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(w.p) + plans);
+    W.back = reinterpret_cast<float *>(W.v + v);
     const cudaError_t e = wt::launch_adapt(L, &W, max_R, ctx.status, s);
     const int rc = wt::serve_workspace_done(h, s, w);
     CU(e);
@@ -213,8 +223,6 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
   }
   return WT_OK;
 }
-
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // The prefix goes to tcgen05 from 33 rows (token, head-in-group) on, which is where the warp kernel
 // would read it more than once, and from one key tile on.  Its reference only grows, so the scale has

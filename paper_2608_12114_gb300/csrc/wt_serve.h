@@ -50,7 +50,7 @@ constexpr int adapt_rank_tiles(int max_R) { return max_R <= 16 ? 1 : max_R <= 32
 struct AdaptProj {
   wt_adapt_desc d;
   uint32_t items;    // upper bound of (slot, token tile) work items
-  uint32_t m_tiles;  // tiles of 128 outputs
+  uint32_t m_groups, group_tiles;  // many tokens: CTAs of an item, and the tiles of 128 outputs that each takes
   uint32_t vec;      // bit 0: A and x load in 16-byte vectors; bit 1: B does; bit 2: base and y do
 };
 struct AdaptLaunch {
@@ -60,9 +60,10 @@ struct AdaptLaunch {
 // Workspace of a launch of many tokens: a plan for each distinct slot map, and v of each projection.
 struct AdaptWide {
   int *plans;          // [n_plans][plan_ints]: {items, -, -, -}, items as int4, tokens from order_at on
-  float *v;
+  uint16_t *v;         // 16-bit parts of v, [2 or 3][T][16 adapt_rank_tiles] a projection, in the plan's token order
+  float *back;         // [T] a projection: what its token's v was divided by (f16)
   int64_t plan_ints, order_at;
-  int64_t v_at[kAdaptProjs];  // v [T, 16 adapt_rank_tiles], in the plan's token order
+  int64_t v_at[kAdaptProjs], back_at[kAdaptProjs];
   int plan[kAdaptProjs];      // a projection's plan
   int plan_proj[kAdaptProjs]; // a plan's first projection
   int n_plans;
