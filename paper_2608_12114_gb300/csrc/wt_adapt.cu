@@ -16,8 +16,6 @@
 #include <type_traits>
 
 #include <cooperative_groups.h>
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
 
 #include "wt_device.cuh"
 #include "wt_serve.h"
@@ -379,6 +377,7 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
 constexpr int kItem = 64;     // tokens of an item
 constexpr int kMTile = 128;   // outputs of a CTA of the expand kernel
 constexpr int kPlanThreads = 1024;
+constexpr int kEThreads = 512;  // the expand kernel: 16 warps cover the latency of its products (8: 125 us for 99)
 constexpr int kSThreads = 128;
 constexpr int kSCluster = 4;
 constexpr int kSK = 64;       // elements of K of a stage
@@ -490,22 +489,29 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
   const int steps = (K + kSK - 1) / kSK, per = (steps + kSCluster - 1) / kSCluster;
   const int s0 = min(steps, c * per), s1 = min(steps, s0 + per);
   const uint32_t base = smem_u32(smem);
-  const int rows = kItem + (r + 15) / 16 * 16;  // staged rows: tokens, then ranks
-  // Stage s: 8 vectors a row; absent tokens, ranks past the slot's and elements past K are zeros.
+  // Stage s: 8 vectors a row; a thread takes vector tid % 8 of rows tid / 8 + 16 i, tokens first, then
+  // ranks.  Absent tokens, ranks past the slot's and elements past K are zeros.
+  const int row = tid >> 3, col = (tid & 7) * 8;
+  const uint16_t *xp[kItem / 16];
+#pragma unroll
+  for (int i = 0; i < kItem / 16; ++i) xp[i] = tok[row + 16 * i] >= 0 ? x + (int64_t)tok[row + 16 * i] * d.ldx : nullptr;
+  const bool vec = (P.vec & 1) != 0;
   auto fetch = [&](int s) {
     if (s < s1) {
-      const uint32_t st = base + (uint32_t)((s - s0) % kSStages) * kStage;
-      for (int i = tid; i < rows * 8; i += kSThreads) {
-        const int row = i >> 3, k = s * kSK + (i & 7) * 8;
-        const uint32_t dst = st + row * kSPitch + (i & 7) * 16;
-        const uint16_t *src = nullptr;
-        if (row < kItem) {
-          if (tok[row] >= 0) src = x + (int64_t)tok[row] * d.ldx;
-        } else if (row - kItem < r) {
-          src = A + (int64_t)(row - kItem) * K;
+      const uint32_t dst = base + (uint32_t)((s - s0) % kSStages) * kStage + row * kSPitch + col * 2;
+      const int k = s * kSK + col;
+#pragma unroll
+      for (int i = 0; i < kItem / 16 + MT; ++i) {
+        const uint16_t *src;
+        if (i < kItem / 16) {
+          src = xp[i];
+        } else {
+          const int a = row + 16 * (i - kItem / 16);
+          if (16 * (i - kItem / 16) >= r) break;
+          src = a < r ? A + (int64_t)a * K : nullptr;
         }
-        if (src && k < K && (P.vec & 1)) cp16(dst, src + k);
-        else sts128(dst, src ? load8<false>(src, k, K) : make_uint4(0, 0, 0, 0));
+        if (src && k < K && vec) cp16(dst + i * 16 * kSPitch, src + k);
+        else sts128(dst + i * 16 * kSPitch, src ? load8<false>(src, k, K) : make_uint4(0, 0, 0, 0));
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -562,11 +568,20 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
   const int t = c * (kItem / kSCluster) + (tid >> 3), k0 = (tid & 7) * (kR / 8);
   float v[kR / 8], top = 0.0f;
 #pragma unroll
-  for (int k = 0; k < kR / 8; ++k) {
-    float sum = 0.0f;
+  for (int k = 0; k < kR / 8; ++k) v[k] = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kSCluster; ++j) sum += from[j][t * kR + k0 + k];
-    v[k] = k0 + k < r ? sum * scale : 0.0f;
+  for (int j = 0; j < kSCluster; ++j) {
+    const float2 *src = reinterpret_cast<const float2 *>(from[j] + t * kR + k0);
+#pragma unroll
+    for (int k = 0; k < kR / 8; k += 2) {
+      const float2 f = src[k / 2];
+      v[k] += f.x;
+      v[k + 1] += f.y;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kR / 8; ++k) {
+    v[k] = k0 + k < r ? v[k] * scale : 0.0f;
     top = fmaxf(top, fabsf(v[k]));
   }
   cl.sync();
@@ -578,45 +593,45 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
     // 2^(14 - exponent of top), within what fp32 can take back; 1 for zeros, infinities and NaN
     const int e = top > 0.0f && top < INFINITY ? min(max((int)(__float_as_uint(top) >> 23) - 127, -112), 127) : 14;
     const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
-    if (t < count) {
-      if ((tid & 7) == 0) W.back[W.back_at[pi] + item.y + t] = __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+    if (t < count && (tid & 7) == 0) W.back[W.back_at[pi] + item.y + t] = __uint_as_float((uint32_t)(127 - 14 + e) << 23);
 #pragma unroll
-      for (int k = 0; k < kR / 8; ++k) {
-        const float x = v[k] * up;
-        const __half h = __float2half_rn(x);
-        const float f = __half2float(h);
-        out[k] = __half_as_ushort(h);
-        out[part_at + k] = __half_as_ushort(__float2half_rn(fabsf(f) < INFINITY ? x - f : 0.0f));
-      }
-    }
-  } else if (t < count) {
-#pragma unroll
-    for (int k = 0; k < kR / 8; ++k) {
-      float x = v[k];
-#pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        const __nv_bfloat16 h = __float2bfloat16_rn(x);
-        const float f = __bfloat162float(h);
-        out[i * part_at + k] = __bfloat16_as_ushort(h);
-        x = fabsf(f) < INFINITY ? x - f : 0.0f;
-      }
-    }
+    for (int k = 0; k < kR / 8; ++k) v[k] *= up;
   }
+  if (t >= count) return;
+#pragma unroll
+  for (int i = 0; i < kParts<DT>; ++i)
+#pragma unroll
+    for (int k = 0; k < kR / 8; k += 2) {
+      uint32_t w;
+      float f0, f1;
+      if constexpr (DT == WT_BF16) {
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(v[k + 1]), "f"(v[k]));
+      } else {
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(v[k + 1]), "f"(v[k]));
+      }
+      uint32_t b0, b1;
+      widen<DT>(w, b0, b1);
+      f0 = __uint_as_float(b0), f1 = __uint_as_float(b1);
+      // what the next part holds; nothing after an infinite one
+      v[k] = fabsf(f0) < INFINITY ? v[k] - f0 : 0.0f;
+      v[k + 1] = fabsf(f1) < INFINITY ? v[k + 1] - f1 : 0.0f;
+      *reinterpret_cast<uint32_t *>(out + i * part_at + k) = w;
+    }
 }
 
-// Shared memory of the expand kernel: a ring of tiles (base, 8 vectors that only their thread reads;
+// Shared memory of the expand kernel: a ring of tiles (base, 4 vectors that only their thread reads;
 // then the 128 rows of B), and the item's v.
 template <int DT, int MT>
 struct Expand {
   static constexpr int stages = MT == 8 ? 2 : 3;
-  static constexpr uint32_t pitch = 32 * MT + 16, base = kThreads * 128, stage = base + kMTile * pitch;
+  static constexpr uint32_t pitch = 32 * MT + 16, base = kEThreads * 64, stage = base + kMTile * pitch;
   static constexpr uint32_t v = stages * stage, part = kItem * pitch;
   static constexpr size_t smem = v + kParts<DT> * part;
 };
 static_assert(Expand<WT_BF16, 4>::smem <= 232448 && Expand<WT_BF16, 8>::smem <= 232448, "shared memory of one CTA");
 
 template <int DT, int MT>
-__global__ void __launch_bounds__(kThreads, 1) adapt_expand_kernel(const __grid_constant__ AdaptLaunch L,
+__global__ void __launch_bounds__(kEThreads, 1) adapt_expand_kernel(const __grid_constant__ AdaptLaunch L,
                                                                    const __grid_constant__ AdaptWide W) {
   using X = Expand<DT, MT>;
   constexpr int kR = 16 * MT;
@@ -635,9 +650,9 @@ __global__ void __launch_bounds__(kThreads, 1) adapt_expand_kernel(const __grid_
   const int4 item = item_of(plan, at_item);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
   const int slot = item.x, count = item.z, M = d.M;
-  // the warp's 16 tokens; in a tile it takes 64 outputs: 4 groups of 16, of which a lane has 4 outputs of
+  // the warp's 16 tokens; in a tile it takes 32 outputs: 2 groups of 16, of which a lane has 4 outputs of
   // two tokens
-  const int t0 = (warp >> 1) * 16 + g;
+  const int t0 = (warp >> 2) * 16 + g;
   int64_t tt[2];
   float back[2] = {1.0f, 1.0f};
 #pragma unroll
@@ -657,22 +672,24 @@ __global__ void __launch_bounds__(kThreads, 1) adapt_expand_kernel(const __grid_
       const uint32_t st = base + (uint32_t)((tile - tile0) % X::stages) * X::stage;
       if (yvec && d.base) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int m = tile * kMTile + (warp & 1) * 64 + j * 16 + 4 * q;
+            const int m = tile * kMTile + (warp & 3) * 32 + j * 16 + 4 * q;
             if (tt[e] >= 0 && m + 4 <= M)
-              cp16(st + (j * 2 + e) * (kThreads * 16) + tid * 16, d.base + tt[e] * d.ldbase + m);
+              cp16(st + (j * 2 + e) * (kEThreads * 16) + tid * 16, d.base + tt[e] * d.ldbase + m);
           }
       }
       // Output 4 a + 2 n + b of a group of 16 goes to row 8 n + 2 a + b: the rows of N tile n, in which a
       // lane's four accumulators of two tiles are neighbouring outputs.  Absent ones are zeros.
-      for (int i = tid; i < kMTile * ksteps * 2; i += kThreads) {
-        const int row = i / (2 * ksteps), k = (i - row * 2 * ksteps) * 8, m = tile * kMTile + row;
-        const int to = (row & ~15) | (row & 2) << 2 | (row & 12) >> 1 | (row & 1);
-        const uint32_t dst = st + X::base + to * X::pitch + k * 2;
-        if (bvec && m < M && k + 8 <= r) cp16(dst, B + (int64_t)m * d.R + k);
-        else sts128(dst, m < M ? load8<false>(B + (int64_t)m * d.R, k, r) : make_uint4(0, 0, 0, 0));
+      // Two neighbouring lanes take 32 bytes of a row.
+      const int row = (tid >> 1) & (kMTile - 1), m = tile * kMTile + row;
+      const int to = (row & ~15) | (row & 2) << 2 | (row & 12) >> 1 | (row & 1);
+      const uint16_t *src = B + (int64_t)m * d.R;
+      const uint32_t dst = st + X::base + to * X::pitch;
+      for (int k = ((tid & 1) + (tid >> 8) * 2) * 8; k < ksteps * 16; k += 32) {
+        if (bvec && m < M && k + 8 <= r) cp16(dst + k * 2, src + k);
+        else sts128(dst + k * 2, m < M ? load8<false>(src, k, r) : make_uint4(0, 0, 0, 0));
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -680,7 +697,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapt_expand_kernel(const __grid_
   if (r > 0) {
     // v of the item; absent tokens are zeros
     const uint16_t *v = W.v + W.v_at[pi] + (int64_t)item.y * kR;
-    for (int i = tid; i < kParts<DT> * kItem * ksteps * 2; i += kThreads) {
+    for (int i = tid; i < kParts<DT> * kItem * ksteps * 2; i += kEThreads) {
       const int pt = i / (kItem * 2 * ksteps), t = i / (2 * ksteps) % kItem, k = i % (2 * ksteps) * 8;
       const uint32_t dst = base + X::v + pt * X::part + t * X::pitch + k * 2;
       if (t < count) cp16(dst, v + pt * (int64_t)d.T * kR + (int64_t)t * kR + k);
@@ -695,9 +712,9 @@ __global__ void __launch_bounds__(kThreads, 1) adapt_expand_kernel(const __grid_
     __syncthreads();
     fetch(tile + X::stages - 1);  // where the tile before lay
     const uint32_t st = base + (uint32_t)((tile - tile0) % X::stages) * X::stage;
-    float acc[4][2][4];
+    float acc[2][2][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -707,11 +724,11 @@ __global__ void __launch_bounds__(kThreads, 1) adapt_expand_kernel(const __grid_
       uint32_t a[kParts<DT>][4];
 #pragma unroll
       for (int i = 0; i < kParts<DT>; ++i)
-        ldsm4(a[i], base + X::v + i * X::part + ((warp >> 1) * 16 + (lane & 15)) * X::pitch + s * 32 + (lane >> 4) * 16);
+        ldsm4(a[i], base + X::v + i * X::part + ((warp >> 2) * 16 + (lane & 15)) * X::pitch + s * 32 + (lane >> 4) * 16);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 2; ++j) {
         uint32_t b[4];  // N tiles 0 and 1, each in two halves of 8 ranks
-        ldsm4(b, st + X::base + ((warp & 1) * 64 + j * 16 + (lane & 7) + (lane >> 4) * 8) * X::pitch + s * 32 + ((lane >> 3) & 1) * 16);
+        ldsm4(b, st + X::base + ((warp & 3) * 32 + j * 16 + (lane & 7) + (lane >> 4) * 8) * X::pitch + s * 32 + ((lane >> 3) & 1) * 16);
 #pragma unroll
         for (int i = kParts<DT> - 1; i >= 0; --i) {  // the smallest part first
           mma16816<DT>(acc[j][0], a[i][0], a[i][1], a[i][2], a[i][3], b[0], b[1]);
@@ -720,10 +737,10 @@ __global__ void __launch_bounds__(kThreads, 1) adapt_expand_kernel(const __grid_
       }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int m = tile * kMTile + (warp & 1) * 64 + j * 16 + 4 * q;
+        const int m = tile * kMTile + (warp & 3) * 32 + j * 16 + 4 * q;
         if (tt[e] < 0) continue;
         float o[4];
 #pragma unroll
@@ -731,7 +748,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapt_expand_kernel(const __grid_
         float *yp = d.y + tt[e] * d.ldy + m;
         if (yvec && m + 4 <= M) {
           if (d.base) {
-            const uint4 b = lds128(st + (j * 2 + e) * (kThreads * 16) + tid * 16);
+            const uint4 b = lds128(st + (j * 2 + e) * (kEThreads * 16) + tid * 16);
             o[0] += __uint_as_float(b.x), o[1] += __uint_as_float(b.y), o[2] += __uint_as_float(b.z), o[3] += __uint_as_float(b.w);
           }
           __stcs(reinterpret_cast<float4 *>(yp), make_float4(o[0], o[1], o[2], o[3]));
@@ -794,7 +811,7 @@ cudaError_t run_wide(const AdaptLaunch &L, const AdaptWide &W, int *status, cuda
   cudaError_t e = launch(adapt_plan_kernel, (unsigned)W.n_plans, kPlanThreads, 1, sizeof(int) * (most_slots(L) + 1), s, L, W, status);
   if (e == cudaSuccess)
     e = launch(adapt_shrink_kernel<DT, MT>, items * kSCluster, kSThreads, kSCluster, shrink_smem<MT>(), s, L, W, status);
-  if (e == cudaSuccess) e = launch(adapt_expand_kernel<DT, MT>, tiles, kThreads, 1, Expand<DT, MT>::smem, s, L, W);
+  if (e == cudaSuccess) e = launch(adapt_expand_kernel<DT, MT>, tiles, kEThreads, 1, Expand<DT, MT>::smem, s, L, W);
   return e;
 }
 

@@ -122,8 +122,8 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
       all += (uint64_t)P.items * ((e.M + 127) / 128);
       P.vec = 0;
       if (e.K % 8 == 0 && e.ldx % 8 == 0 && e.a_slot % 8 == 0 && aligned(e.x, 16) && aligned(e.A, 16)) P.vec |= 1;
-      // a lane reads 4 elements of a row of B where no rank is above 16, else 8
-      const int el = max_R <= 16 ? 4 : 8;
+      // vectors of B: 8 elements; 4 for a launch of few tokens where no rank is above 16
+      const int el = max_T < wt::kAdaptFew && max_R <= 16 ? 4 : 8;
       if (e.R % el == 0 && e.b_slot % el == 0 && aligned(e.B, 2 * el)) P.vec |= 2;
       if (e.ldy % 4 == 0 && aligned(e.y, 16) && (!e.base || (e.ldbase % 4 == 0 && aligned(e.base, 16)))) P.vec |= 4;
     }

@@ -210,3 +210,27 @@ def test_refusals(torch, h):
         serving.adapters(x, y, slot, A, B, base=base[:1].expand(4, 32))
     with pytest.raises(ValueError):
         serving.adapters(x.cpu(), y, slot, A, B)
+
+
+@pytest.mark.parametrize("T", [40, 300])
+@pytest.mark.parametrize("R", [4, 10, 12, 16, 20, 24, 40, 72, 100])
+def test_ranks_off_the_vectors(torch, h, T, R):
+    """Rows of B whose length is no multiple of a 16-byte vector, in both forms."""
+    x, y, slot, A, B, scale, base = make(torch, T, 72, 150, 4, R, torch.float16)
+    h.adapt([serving.adapters(x, y, slot, A, B, scale, base=base)])
+    torch.cuda.synchronize()
+    close(torch, y, _serve.adapt(x, slot, A, B, scale, None, base), 72, R)
+
+
+@pytest.mark.parametrize("dt", ["bfloat16", "float16"])
+def test_updates_of_any_size(torch, h, dt):
+    """Tokens whose A x lies far apart, in one launch of many tokens."""
+    x, y, slot, A, B, scale, base = make(torch, 280, 64, 96, 2, 16, getattr(torch, dt))
+    slot.clamp_(min=0)
+    size = 10.0 ** (torch.arange(280, device="cuda") % 9 - 4.0)
+    x.copy_(x.float() * size.view(-1, 1))
+    x[7] = 0
+    base.zero_()
+    h.adapt([serving.adapters(x, y, slot, A, B, scale, base=base)])
+    torch.cuda.synchronize()
+    close(torch, y, _serve.adapt(x, slot, A, B, scale, None, base), 64, 16)
