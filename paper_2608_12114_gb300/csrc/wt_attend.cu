@@ -9,9 +9,11 @@
 //
 // attend_warp_kernel takes a CTA per (rows, kv head, keys of one request): rows are the (token,
 // head) pairs that share a kv head, 16 or 32 of them, and each of 4 warps streams its own tiles of
-// 16 keys through a ring of its own in shared memory (16-byte cp.async, absent keys zero-filled, so
-// what a page holds past its last key never reaches a product), with m16n8k16 MMAs on them.  No warp
-// waits for another before the end.  Bound: HBM (or L2) for up to 32 rows.
+// 16 keys through a ring of its own in shared memory (16-byte cp.async; one bulk copy a row, of 256
+// bytes, was slower: 56 us against 47 for the own keys of 64 requests' drafts), with m16n8k16 MMAs on
+// them.  The rows of absent keys arrive as zeros and their scores are masked, so what a page holds past
+// its last key never reaches a product.  No warp waits for another before the end.  Bound: HBM (or
+// L2) for up to 32 rows, latency for few keys.
 #include <algorithm>
 
 #include "wt_device.cuh"
@@ -24,8 +26,9 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kKeys = 16;    // keys of a tile
-constexpr int kStages = 3;   // tiles of a warp's ring
+constexpr int kStages = 2;   // tiles of a warp's ring: three CTAs per SM at head_dim 128
 constexpr int kStatusInvalid = -1;
+constexpr float kSlack = 8.0f;
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
@@ -81,8 +84,7 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
   constexpr int kPitch = ND * 32 + 16;              // bytes of a staged row: 8 rows hit 8 different bank groups
   constexpr int kTileBytes = 2 * kKeys * kPitch;    // K rows, then V rows
   constexpr int kRows = 16 * MT;
-  __shared__ uint32_t there[kWarps][kStages];  // bit r: key r of the staged tile exists
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ __align__(128) uint8_t smem[];
   const wt_attend_desc &d = P.d;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
   const int hk = blockIdx.x % d.kv_heads, rt = blockIdx.x / d.kv_heads % P.row_tiles;
@@ -93,28 +95,108 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
   const int b = pre ? 0 : keys_of / P.own_splits;
   const int split = pre ? keys_of - d.n_req * P.own_splits : keys_of % P.own_splits;
   Request rq;
-  int64_t k0, k1;
+  int k0, k1;
   if (pre) {
     rq = {0, d.n_tokens, 0};
-    k0 = (int64_t)split * P.pre_len;
-    k1 = min(d.prefix_len, k0 + P.pre_len);
+    k0 = split * P.pre_len;
+    k1 = (int)min(d.prefix_len, (int64_t)k0 + P.pre_len);
   } else {
     rq = request_of(d, b, P.status, hk == 0 && rt == 0 && split == 0 && tid == 0);
-    k0 = (int64_t)split * P.own_len;
-    k1 = min((int64_t)rq.len, k0 + P.own_len);
+    k0 = split * P.own_len;
+    k1 = (int)min((int64_t)rq.len, (int64_t)k0 + P.own_len);
   }
   const int rows = rq.n * G, row0 = rt * kRows;
   if (row0 >= rows) return;
   const int part = (pre ? P.own_splits : 0) + split;
   if (k0 >= k1) return;  // the merge knows from the length that there is nothing
 
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * kStages * kTileBytes;
-  // columns past head_dim stay zero: no copy touches them
-  for (int i = tid; i < kWarps * kStages * kTileBytes / 16; i += kThreads)
-    reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
-  __syncthreads();
+  const uint32_t ring = smem_u32(smem) + warp * kStages * kTileBytes;
+  if (D % 16) {
+    // the last 8 columns stay zero: no copy touches them
+    for (int i = tid; i < kWarps * kStages * 2 * kKeys; i += kThreads)
+      *reinterpret_cast<uint4 *>(smem + i * kPitch + D * 2) = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+  }
+
+  const int tiles = (k1 - k0 + kKeys - 1) / kKeys;
+  const int chunks = D / 8;  // 16-byte pieces of a row
+  const int row_lane = lane / chunks, in_lane = lane - row_lane * chunks, row_step = 32 / chunks, in_step = 32 - row_step * chunks;
+  const uint8_t *k_of = static_cast<const uint8_t *>(pre ? d.prefix_k : d.k_pages) + 2 * (pre ? hk * d.prefix_head : (int64_t)hk * D);
+  const uint8_t *v_of = static_cast<const uint8_t *>(pre ? d.prefix_v : d.v_pages) + 2 * (pre ? hk * d.prefix_head : (int64_t)hk * D);
+  const int64_t key_bytes = 2 * (pre ? d.prefix_stride : (int64_t)d.kv_heads * D);  // from a key to the next, within a page
+  // Tiles start at multiples of 16 keys, so in pages of 16, 32, ... keys a tile lies in one page, its rows
+  // evenly apart, and rows of 64 or 128 elements (8 or 16 lanes) keep each lane in its column.
+  const bool even = (pre || d.page % kKeys == 0) && in_step == 0;
+  // Tile i of this warp (tiles warp, warp + 4, ...) into its ring; bit r of `there`: key r exists.
+  uint32_t there[kStages];
+  auto fetch = [&](int i, uint32_t &found) {
+    const int tile = warp + i * kWarps;
+    if (tile < tiles) {
+      const int key0 = k0 + tile * kKeys;
+      const uint32_t dst = ring + (i % kStages) * kTileBytes;
+      if (even) {
+        int64_t first = key0;
+        int n = min(kKeys, k1 - key0);
+        if (!pre) {
+          const int pg = key0 / d.page;
+          const int page = __ldg(d.table + (int64_t)b * d.table_stride + pg);
+          if (page >= 0 && page < d.n_pages) {
+            first = (int64_t)page * d.page + (key0 - pg * d.page);
+          } else {
+            first = n = 0;
+            if (P.status && lane == 0) atomicCAS(P.status, 0, kStatusInvalid);
+          }
+        }
+        found = (1u << n) - 1;
+        const int64_t off = first * key_bytes + row_lane * key_bytes + in_lane * 16;
+        const uint8_t *ks = k_of + off, *vs = v_of + off;
+        uint32_t to = dst + row_lane * kPitch + in_lane * 16;
+        const int64_t by = row_step * key_bytes;
+#pragma unroll 4
+        for (int r = row_lane; r < kKeys; r += row_step) {
+          const bool ok = r < n;
+          cp16(to, ok ? ks : d.q, ok);
+          cp16(to + kKeys * kPitch, ok ? vs : d.q, ok);
+          to += row_step * kPitch;
+          ks += by;
+          vs += by;
+        }
+      } else {
+        // lane r knows where row r lies (rows 0-15: K, 16-31: V), and the lanes copy whole rows together
+        const int key = key0 + (lane & 15);
+        uint64_t src = 0;  // 0: an absent key
+        if (key < k1) {
+          const uint8_t *base = lane < 16 ? k_of : v_of;
+          if (pre) {
+            src = reinterpret_cast<uint64_t>(base + key * key_bytes);
+          } else {
+            const int pg = key / d.page;
+            const int page = __ldg(d.table + (int64_t)b * d.table_stride + pg);
+            if (page >= 0 && page < d.n_pages)
+              src = reinterpret_cast<uint64_t>(base + ((int64_t)page * d.page + (key - pg * d.page)) * key_bytes);
+            else if (P.status)
+              atomicCAS(P.status, 0, kStatusInvalid);
+          }
+        }
+        found = __ballot_sync(0xffffffffu, src != 0) & 0xffffu;
+        int row = row_lane, in = in_lane;
+#pragma unroll 4
+        for (int c = 0; c < chunks; ++c) {
+          const uint64_t a = __shfl_sync(0xffffffffu, src, row);
+          cp16(dst + row * kPitch + in * 16, a ? reinterpret_cast<const void *>(a + in * 16) : d.q, a != 0);
+          row += row_step;
+          in += in_step;
+          if (in >= chunks) in -= chunks, ++row;
+        }
+      }
+    }
+    cp_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) fetch(i, there[i]);
 
   // queries as A operands
+  const int ksteps = (D + 15) / 16;
   uint32_t qf[MT][ND][4];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -145,60 +227,23 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
   }
   const float sl = d.scale * 1.4426950408889634f;
 
-  const int tiles = (int)((k1 - k0 + kKeys - 1) / kKeys);
-  const int chunks = D / 8;  // 16-byte pieces of a row
-  // Tile i of this warp (tiles warp, warp + 4, ...) into its ring: lane r (r < 16) knows the row of
-  // key r, and the lanes copy whole rows together.
-  auto fetch = [&](int i) {
-    const int tile = warp + i * kWarps;
-    if (tile < tiles) {
-      const int64_t key = k0 + (int64_t)tile * kKeys + (lane & 15);
-      uint64_t src = 0;  // 0: an absent key
-      if (key < k1) {
-        const uint8_t *base = static_cast<const uint8_t *>(lane < 16 ? (pre ? d.prefix_k : d.k_pages)
-                                                                     : (pre ? d.prefix_v : d.v_pages));
-        if (pre) {
-          src = reinterpret_cast<uint64_t>(base + 2 * (key * d.prefix_stride + hk * d.prefix_head));
-        } else {
-          const int pg = (int)key / d.page, in = (int)key - pg * d.page;
-          const int page = __ldg(d.table + (int64_t)b * d.table_stride + pg);
-          if (page >= 0 && page < d.n_pages)
-            src = reinterpret_cast<uint64_t>(base + 2 * (((int64_t)page * d.page + in) * d.kv_heads + hk) * D);
-          else if (P.status)
-            atomicCAS(P.status, 0, kStatusInvalid);
-        }
-      }
-      const uint32_t dst = ring + (i % kStages) * kTileBytes;
-      const uint32_t found = __ballot_sync(0xffffffffu, src != 0);
-      if (lane == 0) there[warp][i % kStages] = found;
-      for (int c0 = 0; c0 < 32 * chunks; c0 += 32) {
-        const int c = c0 + lane, row = c / chunks, in = c - row * chunks;  // rows 0..15: K, 16..31: V
-        const uint64_t a = __shfl_sync(0xffffffffu, src, row);
-        cp16(dst + row * kPitch + in * 16, reinterpret_cast<const void *>(a ? a + in * 16 : reinterpret_cast<uint64_t>(d.q)), a != 0);
-      }
-    }
-    cp_commit();
-  };
-#pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) fetch(i);
-
   // keys a row may see: all but the tail for own keys
-  int64_t sees[MT][2];
+  int sees[MT][2];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int r = row0 + i * 16 + g + e * 8;
-      sees[i][e] = pre ? k1 : min(k1, (int64_t)rq.len - rq.n + 1 + r / G);
+      sees[i][e] = pre ? k1 : min(k1, rq.len - rq.n + 1 + r / G);
     }
 
-  for (int i = 0; warp + i * kWarps < tiles; ++i) {
-    fetch(i + kStages - 1);
+  const int sees_all = pre ? k1 : min(k1, rq.len - rq.n + 1 + row0 / G);
+  auto step = [&](int i, uint32_t found) {
+    const int slot = i % kStages;
     cp_wait<kStages - 1>();
     __syncwarp();
-    const uint32_t kt = ring + (i % kStages) * kTileBytes, vt = kt + kKeys * kPitch;
-    const int64_t key0 = k0 + (int64_t)(warp + i * kWarps) * kKeys;
-    const uint32_t found = there[warp][i % kStages];
+    const uint32_t kt = ring + slot * kTileBytes, vt = kt + kKeys * kPitch;
+    const int key0 = k0 + (warp + i * kWarps) * kKeys;
     float s[MT][2][4];
 #pragma unroll
     for (int a = 0; a < MT; ++a)
@@ -208,6 +253,7 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
         for (int e = 0; e < 4; ++e) s[a][j][e] = 0.0f;
 #pragma unroll
     for (int k = 0; k < ND; ++k) {
+      if (k >= ksteps) break;
       uint32_t kf[4];  // keys 0-7 and 8-15, each in two halves of 8 elements
       ldsm4(kf, kt + ((lane & 7) + (lane >> 4) * 8) * kPitch + k * 32 + ((lane >> 3) & 1) * 16);
 #pragma unroll
@@ -216,31 +262,48 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
         mma16816<DT>(s[a][1], qf[a][k][0], qf[a][k][1], qf[a][k][2], qf[a][k][3], kf[2], kf[3]);
       }
     }
+    // every row sees every key of the tile, but at the end of a request
+    const bool whole = found == 0xffffu && key0 + kKeys <= sees_all;
     uint32_t pf[MT][4];
 #pragma unroll
     for (int a = 0; a < MT; ++a) {
-      float mx[2] = {m[a][0], m[a][1]};
+      float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int r = j * 8 + q * 2 + (e & 1);
-          s[a][j][e] = (found >> r & 1) && key0 + r < sees[a][e >> 1] ? s[a][j][e] * sl : -INFINITY;
+          s[a][j][e] *= sl;
+          if (!whole) {
+            const int r = j * 8 + q * 2 + (e & 1);
+            if (!(found >> r & 1) || key0 + r >= sees[a][e >> 1]) s[a][j][e] = -INFINITY;
+          }
           mx[e >> 1] = fmaxf(mx[e >> 1], s[a][j][e]);
         }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
         mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
-        const float ref = mx[e] > -INFINITY ? mx[e] : 0.0f;
-        const float f = exp2_approx(m[a][e] - ref);
-        m[a][e] = mx[e];
-        l[a][e] *= f;
+      }
+      // The reference moves when a row's maximum passes it by more than 2^8; p then stays within what
+      // both 16-bit types hold as precisely.  It starts at -infinity, so the first key seen sets it.
+      const bool grown0 = mx[0] > m[a][0] + kSlack, grown1 = mx[1] > m[a][1] + kSlack;
+      if (__any_sync(0xffffffffu, grown0 || grown1)) {
 #pragma unroll
-        for (int j = 0; j < 2 * ND; ++j) {
-          o[a][j][2 * e] *= f;
-          o[a][j][2 * e + 1] *= f;
+        for (int e = 0; e < 2; ++e) {
+          const float to = (e ? grown1 : grown0) ? mx[e] : m[a][e];
+          const float f = to > -INFINITY ? exp2_approx(m[a][e] - to) : 1.0f;
+          m[a][e] = to;
+          l[a][e] *= f;
+#pragma unroll
+          for (int j = 0; j < 2 * ND; ++j) {
+            o[a][j][2 * e] *= f;
+            o[a][j][2 * e + 1] *= f;
+          }
         }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float ref = m[a][e] > -INFINITY ? m[a][e] : 0.0f;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -258,6 +321,7 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
     }
 #pragma unroll
     for (int k = 0; k < ND; ++k) {
+      if (k >= ksteps) break;
       uint32_t vf[4];  // 16 keys x 16 elements
       ldsm4t(vf, vt + (lane & 15) * kPitch + k * 32 + (lane >> 4) * 16);
 #pragma unroll
@@ -267,7 +331,15 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
       }
     }
     __syncwarp();  // every lane has read the tile before a later fetch overwrites it
-  }
+  };
+  const int mine = (tiles - warp + kWarps - 1) / kWarps;  // tiles of this warp
+  for (int i = 0; i < mine; i += kStages)
+#pragma unroll
+    for (int u = 0; u < kStages; ++u)  // unrolled: the ring's slots and `there` are constants
+      if (i + u < mine) {
+        fetch(i + u + kStages - 1, there[(u + kStages - 1) % kStages]);
+        step(i + u, there[u]);
+      }
   cp_wait<0>();
   __syncthreads();
 

@@ -181,8 +181,8 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
   if (d.dtype != WT_BF16 && d.dtype != WT_F16)
     return serve_error(d.dtype >= WT_F32 && d.dtype <= WT_U8 ? WT_ENOTSUP : WT_EINVAL,
                        "%s: dtype %d: queries and caches are bf16 or f16", call, d.dtype);
-  if (d.n_req < 0 || d.n_req > 65535 || d.n_tokens < 0 || d.max_new < 0 || d.prefix_len < 0 || d.prefix_len > 0x7fffffff ||
-      d.max_len < 0 || d.n_pages < 0)
+  if (d.n_req < 0 || d.n_req > 65535 || d.n_tokens < 0 || d.max_new < 0 || d.prefix_len < 0 || d.prefix_len > (1 << 30) ||
+      d.max_len < 0 || d.max_len > (1 << 30) || d.n_pages < 0)
     return serve_error(WT_EINVAL, "%s: n_req %d, n_tokens %d, max_new %d, prefix_len %lld, max_len %d or n_pages %d out of range",
                        call, d.n_req, d.n_tokens, d.max_new, (long long)d.prefix_len, d.max_len, d.n_pages);
   if (d.heads < 1 || d.kv_heads < 1 || d.heads > 65536 || d.heads % d.kv_heads || d.heads / d.kv_heads > 128)
