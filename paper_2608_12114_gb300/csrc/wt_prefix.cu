@@ -62,36 +62,39 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, int
       : "memory");
 }
 
-// Shared-memory matrix descriptors in the 128-byte swizzled layout (version 1).  K-major: rows of
-// 128 bytes, groups of 8 rows 1024 bytes apart.  MN-major: 64 elements of N along a row, rows along
-// K; the stride offset leads from 8 rows to the next 8, the leading offset from 64 elements of N to
-// the next 64.
-__device__ __forceinline__ uint64_t desc_k(uint32_t addr) {
-  return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
-         ((uint64_t)2 << 61);
-}
-__device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
-  return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(kHalf >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
-         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
+// Shared-memory matrix descriptors in the 128-byte swizzled layout (version 1), in two words; the low
+// one starts with the address in units of 16 bytes, so steps are additions.  K-major: rows of 128
+// bytes, groups of 8 rows 1024 bytes apart.  MN-major: 64 elements of N along a row, rows along K; the
+// stride offset leads from 8 rows to the next 8, the leading offset from 64 elements of N to the next.
+constexpr uint32_t kDescHi = (1024 >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t desc_k(uint32_t addr) { return (addr >> 4) | 1u << 16; }
+__device__ __forceinline__ uint32_t desc_mn(uint32_t addr) { return (addr >> 4) | (kHalf >> 4) << 16; }
 // kind::f16, fp32 accumulators, M = 128, A and B of one type; trans_b: B is MN-major.
 __host__ __device__ constexpr uint32_t idesc(uint32_t bf16, uint32_t n, uint32_t trans_b) {
   return (1u << 4) | (bf16 << 7) | (bf16 << 10) | (trans_b << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
-__device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) {
+__device__ __forceinline__ void umma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(id), "r"(acc)
+      "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(id), "r"(acc), "r"(kDescHi)
       : "memory");
 }
-__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(id), "r"(acc)
+      "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(id), "r"(acc), "r"(kDescHi)
       : "memory");
+}
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
 }
 __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -251,8 +254,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-    // ---------------- MMA issuer
-    if (warp == 9 && lane == 0) {
+    // ---------------- MMA issuer: the warp keeps together, so that addresses stay in uniform registers
+    // (one thread alone, with its descriptors built at each product, spent twice the products' time on
+    // issuing them: 113 us against XXX)
+    if (warp == 9) {
       constexpr uint32_t kBf = DT == WT_BF16 ? 1u : 0u;
       constexpr uint32_t kIqk = idesc(kBf, kKeysT, 0), kIpv = idesc(kBf, DH * 64, 1);
       uint32_t it = 0, seg = 0, np[2] = {0, 0};
@@ -260,42 +265,53 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t stage = 0;
       auto next = [&]() {  // the ring's next tile has landed
         const uint32_t s = it % X::stages;
-        if (!bounded_wait(full0 + 8 * s, (it / X::stages) & 1, abort_flag, status)) return live = false;
+        if (!warp_wait(full0 + 8 * s, (it / X::stages) & 1, abort_flag, status)) return live = false;
         fence_after();
         stage = s;
         ++it;
         return true;
       };
+      auto release = [&](uint32_t bar) {
+        if (elect_one()) commit(bar);
+        __syncwarp();
+      };
       auto scores = [&](int i, uint32_t s) {
-        const uint32_t q = base + (apart ? 0 : i) * X::stage, k = base + X::ring + s * X::stage;
-        for (int e = 0; e < P.dim_steps; ++e) {
-          const uint32_t off = (e >> 2) * kHalf + (e & 3) * 32;
-          umma_ss(tmem + i * 128, desc_k(q + off), desc_k(k + off), kIqk, e != 0);
+        const uint32_t q = desc_k(base + (apart ? 0 : i) * X::stage), k = desc_k(base + X::ring + s * X::stage);
+        if (elect_one()) {
+#pragma unroll
+          for (int e = 0; e < DH * 4; ++e) {
+            const uint32_t off = ((e >> 2) * kHalf + (e & 3) * 32) >> 4;
+            if (e < P.dim_steps) umma_ss(tmem + i * 128, q + off, k + off, kIqk, e != 0);
+          }
+          commit(s_full + 8 * i);
         }
-        commit(s_full + 8 * i);
+        __syncwarp();
       };
       auto values = [&](int i, uint32_t s, bool first) {  // false: no P came
-        if (!bounded_wait(p_full + 8 * i, np[i] & 1, abort_flag, status)) return live = false;
+        if (!warp_wait(p_full + 8 * i, np[i] & 1, abort_flag, status)) return live = false;
         ++np[i];
         fence_after();
-        const uint32_t v = base + X::ring + s * X::stage;
+        const uint32_t v = desc_mn(base + X::ring + s * X::stage);
+        if (elect_one()) {
 #pragma unroll
-        for (int e = 0; e < kKeysT / 16; ++e)
-          umma_ts(tmem + 256 + i * 128, tmem + i * 128 + e * 8, desc_mn(v + e * 2048), kIpv, !first || e != 0);
-        commit(o_full + 8 * i);
+          for (int e = 0; e < kKeysT / 16; ++e)
+            umma_ts(tmem + 256 + i * 128, tmem + i * 128 + e * 8, v + e * (2048 >> 4), kIpv, !first || e != 0);
+          commit(o_full + 8 * i);
+        }
+        __syncwarp();
         return true;
       };
       for (int w = w0; w < w1 && live; ++seg) {
         const Segment g = segment(w);
         w += g.n;
-        if (!bounded_wait(q_full, seg & 1, abort_flag, status)) break;
+        if (!warp_wait(q_full, seg & 1, abort_flag, status)) break;
         fence_after();
         if (!apart) {
           if (!next()) break;
           scores(0, stage);
           scores(1, stage);
-          commit(empty0 + 8 * stage);
-          if (g.n == 1) commit(q_empty);
+          release(empty0 + 8 * stage);
+          if (g.n == 1) release(q_empty);
           for (int j = 0; j < g.n; ++j) {
             if (!next()) break;
             const uint32_t vs = stage;
@@ -306,37 +322,37 @@ __global__ void __launch_bounds__(kThreads, 1)
               scores(0, stage);
             }
             if (!values(1, vs, j == 0)) break;
-            commit(empty0 + 8 * vs);
+            release(empty0 + 8 * vs);
             if (more) {
               scores(1, stage);
-              commit(empty0 + 8 * stage);
-              if (j + 2 == g.n) commit(q_empty);
+              release(empty0 + 8 * stage);
+              if (j + 2 == g.n) release(q_empty);
             }
           }
         } else {
           for (int j = 0; j < min(2, g.n) && next(); ++j) {
             scores(j, stage);
-            commit(empty0 + 8 * stage);
+            release(empty0 + 8 * stage);
           }
           if (!live) break;
-          if (g.n <= 2) commit(q_empty);
+          if (g.n <= 2) release(q_empty);
           for (int j = 0; j < g.n; ++j) {
             if (!next()) break;
             const uint32_t vs = stage;
             if (!values(j & 1, vs, j < 2)) break;
-            commit(empty0 + 8 * vs);
+            release(empty0 + 8 * vs);
             if (j + 2 < g.n) {
               if (!next()) break;
               scores(j & 1, stage);
-              commit(empty0 + 8 * stage);
-              if (j + 3 == g.n) commit(q_empty);
+              release(empty0 + 8 * stage);
+              if (j + 3 == g.n) release(q_empty);
             }
           }
         }
       }
       // the last products must have finished before tensor memory is released
       if (it > 0) {
-        commit(fin);
+        release(fin);
         const long long t0 = clock64();
         while (!mbar_try_wait(fin, 0) && clock64() - t0 < kWaitCycles) {
         }
