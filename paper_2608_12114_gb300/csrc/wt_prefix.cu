@@ -49,7 +49,7 @@ struct Geo {
   static constexpr int stages = DH == 2 ? 5 : 8;
   static constexpr uint32_t ring = 2 * stage;  // after the two Q tiles
   static constexpr uint32_t bars = ring + stages * stage;
-  static constexpr int nbars = 2 * stages + 9;
+  static constexpr int nbars = 2 * stages + 11;
   static constexpr size_t smem = bars + nbars * 8 + 16 + 1024;
 };
 static_assert(Geo<2>::smem <= 232448, "shared memory of one CTA");
@@ -146,6 +146,7 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 // A bounded wait of a whole warp: every lane gets the same answer, so a warp whose wait runs out
 // leaves together.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
   return __all_sync(0xffffffffu, bounded_wait(bar, parity, abort_flag, status));
 }
 
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t full0 = base + X::bars, empty0 = full0 + X::stages * 8;
   const uint32_t q_full = empty0 + X::stages * 8, q_empty = q_full + 8;
   const uint32_t s_full = q_empty + 8, p_full = s_full + 16, o_full = p_full + 16;  // [2] each
-  const uint32_t fin = o_full + 16;
+  const uint32_t p_half = o_full + 16, fin = p_half + 16;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gbase + X::bars + X::nbars * 8);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -188,6 +189,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + 8 * i, 1);
       mbar_init(p_full + 8 * i, 128);
+      mbar_init(p_half + 8 * i, 128);
       mbar_init(o_full + 8 * i, 1);
     }
     *abort_flag = 0;
@@ -288,17 +290,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
       };
       auto values = [&](int i, uint32_t s, bool first) {  // false: no P came
-        if (!warp_wait(p_full + 8 * i, np[i] & 1, abort_flag, status)) return live = false;
-        ++np[i];
-        fence_after();
         const uint32_t v = desc_mn(base + X::ring + s * X::stage);
-        if (elect_one()) {
+        // the first half of the keys as soon as its P is there
 #pragma unroll
-          for (int e = 0; e < kKeysT / 16; ++e)
-            umma_ts(tmem + 256 + i * 128, tmem + i * 128 + e * 8, v + e * (2048 >> 4), kIpv, !first || e != 0);
-          commit(o_full + 8 * i);
+        for (int hf = 0; hf < 2; ++hf) {
+          if (!warp_wait((hf ? p_full : p_half) + 8 * i, np[i] & 1, abort_flag, status)) return live = false;
+          fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int e = hf * 4; e < hf * 4 + 4; ++e)
+              umma_ts(tmem + 256 + i * 128, tmem + i * 128 + e * 8, v + e * (2048 >> 4), kIpv, !first || e != 0);
+            if (hf) commit(o_full + 8 * i);
+          }
+          __syncwarp();
         }
-        __syncwarp();
+        ++np[i];
         return true;
       };
       for (int w = w0; w < w1 && live; ++seg) {
@@ -425,20 +431,23 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_st32(O + c, o);
           }
         }
-        uint32_t u[64];
 #pragma unroll
-        for (int c = 0; c < 128; c += 2) {
-          fma_x2(v[c], v[c + 1], P.scale_log2, -m);
-          v[c] = ex2(v[c]);
-          v[c + 1] = ex2(v[c + 1]);
-          add_x2(l0, l1, v[c], v[c + 1]);
-          u[c / 2] = pack2<DT>(v[c], v[c + 1]);
+        for (int hf = 0; hf < 2; ++hf) {
+          uint32_t u[32];
+#pragma unroll
+          for (int k = 0; k < 64; k += 2) {
+            const int c = hf * 64 + k;
+            fma_x2(v[c], v[c + 1], P.scale_log2, -m);
+            v[c] = ex2(v[c]);
+            v[c + 1] = ex2(v[c + 1]);
+            add_x2(l0, l1, v[c], v[c + 1]);
+            u[k / 2] = pack2<DT>(v[c], v[c + 1]);
+          }
+          tmem_st32(S + hf * 32, u);
+          wait_st();
+          fence_before();
+          mbar_arrive((hf ? p_full : p_half) + 8 * i);
         }
-        tmem_st32(S, u);
-        tmem_st32(S + 32, u + 32);
-        wait_st();
-        fence_before();
-        mbar_arrive(p_full + 8 * i);
       }
       if (!live) break;
       const int row = apart ? r : (rb * 2 + i) * P.tile_rows + r;
