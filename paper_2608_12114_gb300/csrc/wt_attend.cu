@@ -148,15 +148,13 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
           }
         }
         found = (1u << n) - 1;
-        const int64_t off = first * key_bytes + row_lane * key_bytes + in_lane * 16;
+        const int64_t off = (first + row_lane) * key_bytes + in_lane * 16, by = row_step * key_bytes;
         const uint8_t *ks = k_of + off, *vs = v_of + off;
         uint32_t to = dst + row_lane * kPitch + in_lane * 16;
-        const int64_t by = row_step * key_bytes;
 #pragma unroll 4
         for (int r = row_lane; r < kKeys; r += row_step) {
-          const bool ok = r < n;
-          cp16(to, ok ? ks : d.q, ok);
-          cp16(to + kKeys * kPitch, ok ? vs : d.q, ok);
+          cp16(to, ks, r < n);  // an absent row is not read, wherever its address leads
+          cp16(to + kKeys * kPitch, vs, r < n);
           to += row_step * kPitch;
           ks += by;
           vs += by;
@@ -375,11 +373,14 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
         ll += f[w] * v.y;
       }
       const int64_t at = (int64_t)part * d.n_tokens * d.heads + (int64_t)(rq.t0 + row / G) * d.heads + hk * G + row % G;
-      for (int c = lane; c < D; c += 32) {
-        float v = 0.0f;
+      if (lane * 4 < D) {
+        float4 v = make_float4(0, 0, 0, 0);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) v += f[w] * so[(w * 16 + r) * kCols + c];
-        P.o[at * D + c] = v;
+        for (int w = 0; w < kWarps; ++w) {
+          const float4 x = *reinterpret_cast<const float4 *>(so + (w * 16 + r) * kCols + lane * 4);
+          v.x += f[w] * x.x, v.y += f[w] * x.y, v.z += f[w] * x.z, v.w += f[w] * x.w;
+        }
+        *reinterpret_cast<float4 *>(P.o + at * D + lane * 4) = v;
       }
       if (lane == 0) P.ml[at] = make_float2(mm, ll);
     }

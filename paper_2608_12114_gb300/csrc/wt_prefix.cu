@@ -127,6 +127,11 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 // (x0, x1) * s + c
 __device__ __forceinline__ void fma_x2(float &x0, float &x1, float s, float c) {
   asm("{\n\t.reg .b64 x, y, z;\n\t"
@@ -400,13 +405,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         float mx0 = v[0], mx1 = v[1], mx2 = v[2], mx3 = v[3];
 #pragma unroll
-        for (int c = 4; c < 128; c += 8) {
-          mx0 = fmaxf(fmaxf(mx0, v[c]), v[c + 4 < 128 ? c + 4 : c]);
-          mx1 = fmaxf(fmaxf(mx1, v[c + 1]), v[c + 5 < 128 ? c + 5 : c]);
-          mx2 = fmaxf(fmaxf(mx2, v[c + 2]), v[c + 6 < 128 ? c + 6 : c]);
-          mx3 = fmaxf(fmaxf(mx3, v[c + 3]), v[c + 7 < 128 ? c + 7 : c]);
+        for (int c = 4; c < 124; c += 8) {
+          mx0 = max3(mx0, v[c], v[c + 4]);
+          mx1 = max3(mx1, v[c + 1], v[c + 5]);
+          mx2 = max3(mx2, v[c + 2], v[c + 6]);
+          mx3 = max3(mx3, v[c + 3], v[c + 7]);
         }
-        const float top = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * P.scale_log2;
+        mx0 = max3(mx0, v[124], v[125]);
+        mx1 = max3(mx1, v[126], v[127]);
+        const float top = max3(max3(mx0, mx1, mx2), mx3, mx3) * P.scale_log2;
         const bool grown = top > m + kSlack;
         if (j == 0) {
           m = top > -INFINITY ? top : 0.0f;
