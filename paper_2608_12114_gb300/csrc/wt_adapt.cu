@@ -471,6 +471,7 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
   const AdaptProj &P = L.p[pi];
   const wt_adapt_desc &d = P.d;
   const int *plan = plan_of(W, W.plan[pi]);
+  griddep_wait();
   if ((int)w >= plan[0]) return;  // the whole cluster
   const int4 item = item_of(plan, w);
   const int slot = item.x, count = item.z, K = d.K, R = d.R;
@@ -646,6 +647,7 @@ __global__ void __launch_bounds__(kEThreads, 1) adapt_expand_kernel(const __grid
   const wt_adapt_desc &d = P.d;
   const int *plan = plan_of(W, W.plan[pi]);
   const int at_item = w / P.m_groups, group = w - at_item * P.m_groups;
+  griddep_wait();
   if (at_item >= plan[0]) return;
   const int4 item = item_of(plan, at_item);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
@@ -761,19 +763,31 @@ __global__ void __launch_bounds__(kEThreads, 1) adapt_expand_kernel(const __grid
   }
 }
 
+// `after`: the kernel waits on the device for the one before it in this call, so it may be launched
+// while that one ends.
 template <typename... A>
-cudaError_t launch(void (*k)(A...), unsigned grid, int threads, int cluster, size_t smem, cudaStream_t s, const A &...args) {
+cudaError_t launch(void (*k)(A...), unsigned grid, int threads, int cluster, size_t smem, bool after, cudaStream_t s,
+                   const A &...args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)cluster;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute at[2];
+  int n = 0;
+  if (cluster > 1) {
+    at[n].id = cudaLaunchAttributeClusterDimension;
+    at[n].val.clusterDim.x = (unsigned)cluster;
+    at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (after) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
   cfg.attrs = at;
-  cfg.numAttrs = cluster > 1 ? 1 : 0;
+  cfg.numAttrs = (unsigned)n;
   return cudaLaunchKernelEx(&cfg, k, args...);
 }
 
@@ -797,7 +811,7 @@ cudaError_t run_few(const AdaptLaunch &L, int *status, cudaStream_t s) {
   uint32_t items = 0;
   for (int i = 0; i < L.n; ++i) items += L.p[i].items;
   if (items == 0) return cudaSuccess;
-  return launch(adapt_kernel<DT, MT>, items * kCluster, kThreads, kCluster, few_smem<MT>(most_slots(L)), s, L, status);
+  return launch(adapt_kernel<DT, MT>, items * kCluster, kThreads, kCluster, few_smem<MT>(most_slots(L)), false, s, L, status);
 }
 
 template <int DT, int MT>
@@ -808,10 +822,10 @@ cudaError_t run_wide(const AdaptLaunch &L, const AdaptWide &W, int *status, cuda
     tiles += L.p[i].items * L.p[i].m_groups;
   }
   if (items == 0) return cudaSuccess;
-  cudaError_t e = launch(adapt_plan_kernel, (unsigned)W.n_plans, kPlanThreads, 1, sizeof(int) * (most_slots(L) + 1), s, L, W, status);
+  cudaError_t e = launch(adapt_plan_kernel, (unsigned)W.n_plans, kPlanThreads, 1, sizeof(int) * (most_slots(L) + 1), false, s, L, W, status);
   if (e == cudaSuccess)
-    e = launch(adapt_shrink_kernel<DT, MT>, items * kSCluster, kSThreads, kSCluster, shrink_smem<MT>(), s, L, W, status);
-  if (e == cudaSuccess) e = launch(adapt_expand_kernel<DT, MT>, tiles, kEThreads, 1, Expand<DT, MT>::smem, s, L, W);
+    e = launch(adapt_shrink_kernel<DT, MT>, items * kSCluster, kSThreads, kSCluster, shrink_smem<MT>(), true, s, L, W, status);
+  if (e == cudaSuccess) e = launch(adapt_expand_kernel<DT, MT>, tiles, kEThreads, 1, Expand<DT, MT>::smem, true, s, L, W);
   return e;
 }
 
