@@ -1,10 +1,11 @@
 // Low-rank adapters of many requests beside a shared projection (include/wt_serve.h):
 // y[t] = base[t] + scale_s B_s (A_s x[t]), s = slot[t].
 //
-// Few tokens (below 256): one launch, one cluster of 8 CTAs per work item (projection, slot, up to 16
-// tokens of that slot).  The cluster computes v = A x with each CTA taking an eighth of K, exchanges the partial
+// Few tokens (below 256): one launch, one cluster of C = 8 CTAs (4 or 2 where there are more items than
+// SMs can hold at 8) per work item (projection, slot, up to 16 tokens of that slot).  The cluster
+// computes v = A x with each CTA taking a C-th of K, exchanges the partial
 // sums through distributed shared memory (always added in the order of the CTAs), and then each CTA
-// takes an eighth of the M outputs.  A and B are read once per item, B's lines being fetched into L2
+// takes a C-th of the M outputs.  A and B are read once per item, B's lines being fetched into L2
 // while A is read; x and y cross once.  The slot map lies in device memory, so the items are found
 // there too: every CTA counts the tokens of each slot and picks its own.  Bound: latency
 // (two dependent reads and a cluster barrier).  More tokens: three launches, see below.
@@ -28,7 +29,7 @@ namespace cg = cooperative_groups;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = 8;
-constexpr int kCluster = 8;
+constexpr int kMostCluster = 8;
 constexpr int kStatusInvalid = -1;
 
 __device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -110,7 +111,7 @@ __device__ __forceinline__ void split(float v, uint32_t &hi, uint32_t &lo) {
 
 // MT: 16-row tiles of the rank (R <= 16 MT).
 template <int DT, int MT>
-__global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__ AdaptLaunch L, int *status) {
+__global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const __grid_constant__ AdaptLaunch L, int *status) {
   constexpr int kTile = 16;  // tokens of an item
   constexpr int kR = 16 * MT;
   constexpr int WK = kWarps;
@@ -123,12 +124,12 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
   __shared__ int tok[kTile];
   __shared__ int wsum[kWarps];
   cg::cluster_group cl = cg::this_cluster();
-  const int c = cl.block_rank();
+  const int c = cl.block_rank(), C = cl.num_blocks();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   // the projection and the item of this cluster
   int pi = 0;
-  uint32_t w = blockIdx.x / kCluster;
+  uint32_t w = blockIdx.x / C;
   while (pi + 1 < L.n && w >= L.p[pi].items) w -= L.p[pi++].items;
   const AdaptProj &P = L.p[pi];
   const wt_adapt_desc &d = P.d;
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
   const int q = lane & 3, g = lane >> 2;
   const int wk = warp;
   // outputs of this CTA: whole groups of 16
-  const int mper = ((M + 15) / 16 + kCluster - 1) / kCluster * 16;
+  const int mper = ((M + 15) / 16 + C - 1) / C * 16;
   const int m0 = min(M, c * mper), m1 = min(M, m0 + mper);
   int r = 0;  // the slot's rank
   const uint16_t *A = nullptr, *B = nullptr;
@@ -211,6 +212,43 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
     A = static_cast<const uint16_t *>(d.A) + (int64_t)item.slot * d.a_slot;
     B = static_cast<const uint16_t *>(d.B) + (int64_t)item.slot * d.b_slot;
   }
+
+  constexpr int kSteps = 2 * MT, kEl = kSteps >= 4 ? 8 : 2 * kSteps;  // steps of 8 ranks; a lane's neighbouring elements
+  const int ta = g, tb = ta + 8;
+  const bool oka = ta < item.count, okb = tb < item.count;
+  const int64_t ia = tok[oka ? ta : 0], ib = tok[okb ? tb : 0];
+  // Where all of base, y and B load in vectors, a warp's first kHold groups of 16 outputs have their base
+  // (and B, at ranks up to 32) on its way before v is computed, by loads without a branch: each group
+  // waiting for its own took 1820 cycles, half of a call for one token.
+  constexpr int kHold = MT == 1 ? 4 : 2;
+  constexpr bool kHoldB = MT <= 2;
+  const bool fast = d.base && r > 0 && (P.vec & 6) == 6 && M % 16 == 0;
+  float4 held[kHold][2];
+  uint32_t heldb[kHoldB ? kHold : 1][2][kEl / 2];
+  const uint16_t *brow = B + (int64_t)(4 * (g >> 1) + (g & 1)) * R;  // column g of N tile j: output 4 (g / 2) + 2 j + g % 2
+  auto hold = [&](int mb) {
+#pragma unroll
+    for (int u = 0; u < kHold; ++u) {
+      const int m = min(mb + u * WK * 16, m1 - 16);
+      held[u][0] = *reinterpret_cast<const float4 *>(d.base + ia * d.ldbase + m + 4 * q);
+      held[u][1] = *reinterpret_cast<const float4 *>(d.base + ib * d.ldbase + m + 4 * q);
+      if constexpr (kHoldB) {
+        const int k = q * kEl < R ? q * kEl : 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint16_t *src = brow + (int64_t)(m + 2 * j) * R + k;
+          if constexpr (kEl == 8) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(src));
+            heldb[u][j][0] = v.x, heldb[u][j][1] = v.y, heldb[u][j][2] = v.z, heldb[u][j][3] = v.w;
+          } else {
+            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(src));
+            heldb[u][j][0] = v.x, heldb[u][j][1] = v.y;
+          }
+        }
+      }
+    }
+  };
+  if (fast && m0 < m1) hold(m0 + wk * 16);
 
   if (r > 0) {
     // B's rows of this CTA on their way into L2
@@ -229,7 +267,7 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.0f;
-    const int steps = (K + 31) / 32, per = (steps + kCluster - 1) / kCluster;
+    const int steps = (K + 31) / 32, per = (steps + C - 1) / C;
     const int s0 = min(steps, c * per), s1 = min(steps, s0 + per);
     const uint16_t *xr[2];
     bool xok[2];
@@ -282,16 +320,16 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
     for (int i = tid; i < kTile * kR; i += kThreads) {
       float s = 0.0f;
 #pragma unroll
-      for (int k = 0; k < kCluster; ++k) s += cl.map_shared_rank(part, k)[i];
+      for (int k = 0; k < kMostCluster; ++k)
+        if (k < C) s += cl.map_shared_rank(part, k)[i];
       // ranks past the slot's: zero, also where x is infinite
       vfull[i / kR * (kR + 4) + i % kR] = i % kR < r ? s * scale : 0.0f;
     }
     cl.sync();
   }
 
-  // y^T: M = tokens (16 of this warp), N = outputs.  A lane's eight accumulators of two N tiles are
-  // four consecutive outputs of two tokens, so y moves in 16-byte vectors.
-  constexpr int kSteps = 2 * MT;  // 8 elements of the rank each
+  // y^T: M = tokens (16), N = outputs.  A lane's eight accumulators of two N tiles are four consecutive
+  // outputs of two tokens, so y moves in 16-byte vectors.
   uint32_t vh[kSteps][4], vl[kSteps][4];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s)
@@ -305,9 +343,52 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
       const float v = r > 0 ? vfull[t * (kR + 4) + kk] : 0.0f;
       split(v, vh[s][e], vl[s][e]);
     }
-  const int ta = g, tb = ta + 8;
-  const bool oka = ta < item.count, okb = tb < item.count;
-  const int64_t ia = oka ? tok[ta] : 0, ib = okb ? tok[tb] : 0;
+  if (fast) {
+    for (int mb = m0 + wk * 16; mb < m1; mb += kHold * WK * 16) {
+      if (mb != m0 + wk * 16) hold(mb);
+#pragma unroll
+      for (int u = 0; u < kHold; ++u) {
+        const int m = mb + u * WK * 16;
+        float acc[2][4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[j][e] = 0.0f;
+#pragma unroll
+        for (int s4 = 0; s4 < (kSteps + 3) / 4; ++s4) {
+          if (s4 * 32 >= r) break;
+          const int k = s4 * 32 + q * kEl;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint32_t bw[4];
+            if constexpr (kHoldB) {
+              const uint4 v = keep8(make_uint4(heldb[u][j][0], heldb[u][j][1], kEl == 8 ? heldb[u][j][kEl / 2 - 2] : 0,
+                                               kEl == 8 ? heldb[u][j][kEl / 2 - 1] : 0), max(r - k, 0));
+              bw[0] = v.x, bw[1] = v.y, bw[2] = v.z, bw[3] = v.w;
+            } else {
+              load_b<kEl>(bw, brow + (int64_t)(min(m, m1 - 16) + 2 * j) * R, k, r, true);
+            }
+#pragma unroll
+            for (int s = 0; s < (kSteps < 4 ? kSteps : 4); ++s) {
+              uint32_t b0, b1;
+              widen<DT>(bw[s], b0, b1);
+              mma_tf32(acc[j], vl[s4 * 4 + s], b0, b1);
+              mma_tf32(acc[j], vh[s4 * 4 + s], b0, b1);
+            }
+          }
+        }
+        // acc[j][0, 1]: token g, outputs m + 4 q + 2 j, + 1; acc[j][2, 3]: token g + 8
+        if (m < m1) {
+          float4 y0 = held[u][0], y1 = held[u][1];
+          y0.x += acc[0][0], y0.y += acc[0][1], y0.z += acc[1][0], y0.w += acc[1][1];
+          y1.x += acc[0][2], y1.y += acc[0][3], y1.z += acc[1][2], y1.w += acc[1][3];
+          if (oka) *reinterpret_cast<float4 *>(d.y + ia * d.ldy + m + 4 * q) = y0;
+          if (okb) *reinterpret_cast<float4 *>(d.y + ib * d.ldy + m + 4 * q) = y1;
+        }
+      }
+    }
+    return;
+  }
   const bool yvec = (P.vec & 4) != 0;
   for (int m = m0 + wk * 16; m < m1; m += WK * 16) {
     float acc[2][4];
@@ -325,7 +406,6 @@ __global__ void __launch_bounds__(kThreads) adapt_kernel(const __grid_constant__
 #pragma unroll
         for (int s4 = 0; s4 < (kSteps + 3) / 4; ++s4) {
           if (s4 * 32 >= r) break;
-          constexpr int kEl = kSteps >= 4 ? 8 : 2 * kSteps;  // elements of a lane
           uint32_t bw[4];
           load_b<kEl>(bw, br, s4 * 32 + q * kEl, ok ? r : 0, (P.vec & 2) != 0);
 #pragma unroll
@@ -811,7 +891,11 @@ cudaError_t run_few(const AdaptLaunch &L, int *status, cudaStream_t s) {
   uint32_t items = 0;
   for (int i = 0; i < L.n; ++i) items += L.p[i].items;
   if (items == 0) return cudaSuccess;
-  return launch(adapt_kernel<DT, MT>, items * kCluster, kThreads, kCluster, few_smem<MT>(most_slots(L)), false, s, L, status);
+  // 48 tokens of 24 adapters through three projections: 11.7 us in clusters of 4 (432 CTAs), 18.4 in
+  // clusters of 8; one token 5.8 us in a cluster of 8, 7.2 in one of 4
+  int c = kMostCluster;
+  while (c > 2 && (int64_t)items * c > 3 * num_sms()) c /= 2;
+  return launch(adapt_kernel<DT, MT>, items * (unsigned)c, kThreads, c, few_smem<MT>(most_slots(L)), false, s, L, status);
 }
 
 template <int DT, int MT>
