@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const 
 // each.  adapt_plan_kernel sorts the tokens by slot and cuts them into items of up to 64 tokens of one
 // slot.  adapt_shrink_kernel computes v = scale A x of an item, a cluster of 4 CTAs splitting K, with
 // x and A staged in shared memory by 16-byte cp.async.  adapt_expand_kernel adds B v, a CTA taking
-// several tiles of 64 tokens x 128 outputs of an item, with the base and B of the next tiles always on
+// several tiles of 64 tokens x 64 outputs of an item, with the base and B of the next tiles always on
 // their way to shared memory (loading B into registers as it was needed, each tile waited for L2 twice:
 // 166 us for the expand kernel of 4001 tokens of two projections of 6912 outputs, against XXX).
 //
@@ -455,9 +455,10 @@ __global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const 
 // each token has brought its largest v to 2^14, far from f16's ends; the power is taken back in fp32.
 // Bound: HBM (base and y).
 constexpr int kItem = 64;     // tokens of an item
-constexpr int kMTile = 128;   // outputs of a CTA of the expand kernel
+constexpr int kMTile = kAdaptMTile;   // outputs of a tile of the expand kernel
 constexpr int kPlanThreads = 1024;
-constexpr int kEThreads = 512;  // the expand kernel: 16 warps cover the latency of its products (8: 125 us for 99)
+constexpr int kEThreads = 256;  // the expand kernel, twice on an SM: one CTA's products run while the other waits for a tile
+constexpr int kEAcross = kMTile / 32;  // warps side by side in a tile
 constexpr int kSThreads = 128;
 constexpr int kSCluster = 4;
 constexpr int kSK = 64;       // elements of K of a stage
@@ -712,7 +713,7 @@ struct Expand {
 static_assert(Expand<WT_BF16, 4>::smem <= 232448 && Expand<WT_BF16, 8>::smem <= 232448, "shared memory of one CTA");
 
 template <int DT, int MT>
-__global__ void __launch_bounds__(kEThreads, 1) adapt_expand_kernel(const __grid_constant__ AdaptLaunch L,
+__global__ void __launch_bounds__(kEThreads, MT == 8 ? 1 : 2) adapt_expand_kernel(const __grid_constant__ AdaptLaunch L,
                                                                    const __grid_constant__ AdaptWide W) {
   using X = Expand<DT, MT>;
   constexpr int kR = 16 * MT;
@@ -734,7 +735,7 @@ __global__ void __launch_bounds__(kEThreads, 1) adapt_expand_kernel(const __grid
   const int slot = item.x, count = item.z, M = d.M;
   // the warp's 16 tokens; in a tile it takes 32 outputs: 2 groups of 16, of which a lane has 4 outputs of
   // two tokens
-  const int t0 = (warp >> 2) * 16 + g;
+  const int t0 = warp / kEAcross * 16 + g;
   int64_t tt[2];
   float back[2] = {1.0f, 1.0f};
 #pragma unroll
@@ -757,7 +758,7 @@ __global__ void __launch_bounds__(kEThreads, 1) adapt_expand_kernel(const __grid
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int m = tile * kMTile + (warp & 3) * 32 + j * 16 + 4 * q;
+            const int m = tile * kMTile + warp % kEAcross * 32 + j * 16 + 4 * q;
             if (tt[e] >= 0 && m + 4 <= M)
               cp16(st + (j * 2 + e) * (kEThreads * 16) + tid * 16, d.base + tt[e] * d.ldbase + m);
           }
@@ -769,7 +770,7 @@ __global__ void __launch_bounds__(kEThreads, 1) adapt_expand_kernel(const __grid
       const int to = (row & ~15) | (row & 2) << 2 | (row & 12) >> 1 | (row & 1);
       const uint16_t *src = B + (int64_t)m * d.R;
       const uint32_t dst = st + X::base + to * X::pitch;
-      for (int k = ((tid & 1) + (tid >> 8) * 2) * 8; k < ksteps * 16; k += 32) {
+      for (int k = ((tid & 1) + tid / (2 * kMTile) * 2) * 8; k < ksteps * 16; k += kEThreads / kMTile * 8) {
         if (bvec && m < M && k + 8 <= r) cp16(dst + k * 2, src + k);
         else sts128(dst + k * 2, m < M ? load8<false>(src, k, r) : make_uint4(0, 0, 0, 0));
       }
@@ -806,11 +807,11 @@ __global__ void __launch_bounds__(kEThreads, 1) adapt_expand_kernel(const __grid
       uint32_t a[kParts<DT>][4];
 #pragma unroll
       for (int i = 0; i < kParts<DT>; ++i)
-        ldsm4(a[i], base + X::v + i * X::part + ((warp >> 2) * 16 + (lane & 15)) * X::pitch + s * 32 + (lane >> 4) * 16);
+        ldsm4(a[i], base + X::v + i * X::part + (warp / kEAcross * 16 + (lane & 15)) * X::pitch + s * 32 + (lane >> 4) * 16);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         uint32_t b[4];  // N tiles 0 and 1, each in two halves of 8 ranks
-        ldsm4(b, st + X::base + ((warp & 3) * 32 + j * 16 + (lane & 7) + (lane >> 4) * 8) * X::pitch + s * 32 + ((lane >> 3) & 1) * 16);
+        ldsm4(b, st + X::base + (warp % kEAcross * 32 + j * 16 + (lane & 7) + (lane >> 4) * 8) * X::pitch + s * 32 + ((lane >> 3) & 1) * 16);
 #pragma unroll
         for (int i = kParts<DT> - 1; i >= 0; --i) {  // the smallest part first
           mma16816<DT>(acc[j][0], a[i][0], a[i][1], a[i][2], a[i][3], b[0], b[1]);
@@ -822,7 +823,7 @@ __global__ void __launch_bounds__(kEThreads, 1) adapt_expand_kernel(const __grid
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int m = tile * kMTile + (warp & 3) * 32 + j * 16 + 4 * q;
+        const int m = tile * kMTile + warp % kEAcross * 32 + j * 16 + 4 * q;
         if (tt[e] < 0) continue;
         float o[4];
 #pragma unroll

@@ -119,7 +119,7 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
       const wt_adapt_desc &e = P.d;
       const bool copy = e.base != e.y;
       P.items = (uint32_t)(std::min(e.S + (copy ? 1 : 0), e.T) + e.T / tile);
-      all += (uint64_t)P.items * ((e.M + 127) / 128);
+      all += (uint64_t)P.items * ((e.M + wt::kAdaptMTile - 1) / wt::kAdaptMTile);
       P.vec = 0;
       if (e.K % 8 == 0 && e.ldx % 8 == 0 && e.a_slot % 8 == 0 && aligned(e.x, 16) && aligned(e.A, 16)) P.vec |= 1;
       // vectors of B: 8 elements; 4 for a launch of few tokens where no rank is above 16
@@ -137,11 +137,11 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
     wt::AdaptWide W = {};
     int64_t items = 0, v = 0, back = 0;
     const int64_t row = 16 * wt::adapt_rank_tiles(max_R), parts = dtype == WT_BF16 ? 3 : 2;
-    // tiles of outputs that a CTA takes one after another: about three waves of one CTA per SM in all
-    const int64_t run = std::max<int64_t>(1, ceil_div((int64_t)all, 3 * wt::num_sms()));
+    // tiles of outputs that a CTA takes one after another: about three waves of two CTAs per SM in all
+    const int64_t run = std::max<int64_t>(1, ceil_div((int64_t)all, 6 * wt::num_sms()));
     for (int k = 0; k < L.n; ++k) {
       const wt_adapt_desc &e = L.p[k].d;
-      const int64_t tiles = ceil_div(e.M, 128);
+      const int64_t tiles = ceil_div(e.M, wt::kAdaptMTile);
       L.p[k].m_groups = (uint32_t)ceil_div(tiles, run);
       L.p[k].group_tiles = (uint32_t)ceil_div(tiles, L.p[k].m_groups);
       auto same = [&](int q) {

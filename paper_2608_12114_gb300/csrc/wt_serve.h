@@ -43,6 +43,7 @@ cudaError_t serve_prepare();  // one-time function attributes of every kernel be
 
 // ---------------------------------------------------------------- wt_adapt.cu
 constexpr int kAdaptProjs = 8;  // projections of one launch
+constexpr int kAdaptMTile = 64;
 constexpr int kAdaptFew = 256;  // tokens from which a launch's work is planned on the device first
 constexpr int adapt_tile(int max_T) { return max_T < kAdaptFew ? 16 : 64; }  // tokens of a work item
 // 16-row tiles of the rank that the kernels are built for
@@ -50,7 +51,7 @@ constexpr int adapt_rank_tiles(int max_R) { return max_R <= 16 ? 1 : max_R <= 32
 struct AdaptProj {
   wt_adapt_desc d;
   uint32_t items;    // upper bound of (slot, token tile) work items
-  uint32_t m_groups, group_tiles;  // many tokens: CTAs of an item, and the tiles of 128 outputs that each takes
+  uint32_t m_groups, group_tiles;  // many tokens: CTAs of an item, and the tiles of kAdaptMTile outputs that each takes
   uint32_t vec;      // bit 0: A and x load in 16-byte vectors; bit 1: B does; bit 2: base and y do
 };
 struct AdaptLaunch {
