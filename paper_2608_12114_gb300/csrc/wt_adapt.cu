@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const 
 constexpr int kItem = 64;     // tokens of an item
 constexpr int kMTile = kAdaptMTile;   // outputs of a tile of the expand kernel
 constexpr int kPlanThreads = 1024;
-constexpr int kEThreads = 256;  // the expand kernel, twice on an SM: one CTA's products run while the other waits for a tile
+constexpr int kEThreads = 256;  // the expand kernel, three to an SM: products run while other CTAs wait for a tile
 constexpr int kEAcross = kMTile / 32;  // warps side by side in a tile
 constexpr int kSThreads = 128;
 constexpr int kSCluster = 4;
@@ -705,7 +705,7 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
 // then the 128 rows of B), and the item's v.
 template <int DT, int MT>
 struct Expand {
-  static constexpr int stages = MT == 8 ? 2 : 3;
+  static constexpr int stages = 2;
   static constexpr uint32_t pitch = 32 * MT + 16, base = kEThreads * 64, stage = base + kMTile * pitch;
   static constexpr uint32_t v = stages * stage, part = kItem * pitch;
   static constexpr size_t smem = v + kParts<DT> * part;
@@ -713,7 +713,7 @@ struct Expand {
 static_assert(Expand<WT_BF16, 4>::smem <= 232448 && Expand<WT_BF16, 8>::smem <= 232448, "shared memory of one CTA");
 
 template <int DT, int MT>
-__global__ void __launch_bounds__(kEThreads, MT == 8 ? 1 : 2) adapt_expand_kernel(const __grid_constant__ AdaptLaunch L,
+__global__ void __launch_bounds__(kEThreads, MT == 8 ? 1 : 3) adapt_expand_kernel(const __grid_constant__ AdaptLaunch L,
                                                                    const __grid_constant__ AdaptWide W) {
   using X = Expand<DT, MT>;
   constexpr int kR = 16 * MT;
