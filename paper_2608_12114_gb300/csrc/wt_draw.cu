@@ -66,10 +66,11 @@ struct RowPart {
   int first;  // first index of m
 };
 
-__device__ __forceinline__ float exp2_full(float x) {  // subnormal results are kept
+// 2^(2 x): the square keeps subnormal results, without the tests that the function's own way takes.
+__device__ __forceinline__ float exp2_twice(float x) {
   float y;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y * y;
 }
 
 __global__ void __launch_bounds__(kPThreads, 3) probs_kernel(const wt_probs_desc d, const int held_most, int *status) {
@@ -155,16 +156,17 @@ __global__ void __launch_bounds__(kPThreads, 3) probs_kernel(const wt_probs_desc
       const RowPart r = *cl.map_shared_rank(&part, q);
       if (r.m > mr) mr = r.m, at = r.first;
     }
+    cluster_arrive();
     for (int i = tid; i < n; i += kPThreads) p[i] = i + lo == at ? 1.0f : 0.0f;
-    cl.sync();
+    cluster_wait();
     return;
   }
 
-  // 1 / t beyond the largest number: any such factor sends every logit but the largest to 0
-  const float k = fminf(1.4426950408889634f / t, 3.4028234e38f);
+  // log2(e) / 2 t.  Beyond the largest number any factor sends every logit but the largest to 0, and one
+  // above 0 a logit of -infinity, whatever the temperature.
+  const float k = fmaxf(fminf(0.72134752044448170f / t, 3.4028234e38f), 1.1754944e-38f);
   const float mz = m > -INFINITY ? m : 0.0f;
-  // a logit of -infinity is no token, whatever the temperature
-  auto e = [&](float x) { return x == -INFINITY ? 0.0f : exp2_full((x - mz) * k); };
+  auto e = [&](float x) { return exp2_twice((x - mz) * k); };
   float s = 0.0f;
 #pragma unroll 4
   for (int i = tid; i < held4; i += kPThreads) {
@@ -194,7 +196,8 @@ __global__ void __launch_bounds__(kPThreads, 3) probs_kernel(const wt_probs_desc
     all[q] = q < C ? *cl.map_shared_rank(&part, q) : RowPart{-INFINITY, 0.0f, 0};
     mr = fmaxf(mr, all[q].m);
   }
-  auto scale = [&](float mc) { return mc == mr ? 1.0f : mc > -INFINITY ? exp2_full((mc - mr) * k) : 0.0f; };
+  cluster_arrive();  // before the stores: a barrier after them would wait for them to be done
+  auto scale = [&](float mc) { return mc == mr ? 1.0f : mc > -INFINITY ? exp2_twice((mc - mr) * k) : 0.0f; };
 #pragma unroll
   for (int q = 0; q < kMaxCluster; ++q)
     if (all[q].s != 0.0f) sr += all[q].s * scale(all[q].m);
@@ -212,7 +215,7 @@ __global__ void __launch_bounds__(kPThreads, 3) probs_kernel(const wt_probs_desc
     for (int i = tid; i < held; i += kPThreads) p[i] = sv[i] * f;
   }
   for (int i = held + tid; i < n; i += kPThreads) p[i] = e(l[i]) * f;
-  cl.sync();  // no CTA leaves while another may still read its part
+  cluster_wait();  // no CTA leaves while another may still read its part
 }
 
 // ------------------------------------------------------------------ verification
