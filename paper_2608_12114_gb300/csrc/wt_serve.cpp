@@ -286,12 +286,17 @@ int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
   if (d.prefix_len && prefix_on_tcgen05(d)) CHECK(plan_prefix(d, P.G, &P.x, &maps));
   const bool pre_warp = d.prefix_len && !P.x.groups;
   const int64_t most = std::max(d.max_len ? own_rows : 0, pre_warp ? pre_rows : 0);
-  P.rows_tile = most <= 16 ? 16 : 32;
+  // tiles of 32 rows where a request has more than 16; a prefix beside shorter ones is read once for each 16
+  P.rows_tile = (d.max_len ? own_rows : most) <= 16 ? 16 : 32;
   P.row_tiles = (int)ceil_div(most, P.rows_tile);
-  // Splits: 4 CTAs per SM over all of them, of at least 64 keys (one tile for each warp).
-  const int64_t want = 4 * wt::num_sms();
+  // Splits, of at least 64 keys (one tile for each warp): own keys alone take 4 CTAs per SM (lengths differ,
+  // and CTAs without keys end at once); own keys and prefix in one launch take one each, and up to 4
+  // where splits stay at 512 keys (7 requests with a head for every query behind 1021 keys: 13.6 us,
+  // with 4 throughout 17.1; 24 requests' own keys alone, 4: 30.4, 2: 33.6).
+  const int64_t sms = wt::num_sms(), few = pre_warp ? 1 : 4;
   auto split = [&](int64_t keys, int64_t ctas, int &splits, int &len) {
-    const int64_t n = std::max<int64_t>(1, std::min(ceil_div(keys, 64), ceil_div(want, ctas)));
+    const int64_t n = std::max(std::min(ceil_div(keys, 64), ceil_div(few * sms, ctas)),
+                               std::min(ceil_div(keys, 512), ceil_div(4 * sms, ctas)));
     len = (int)(ceil_div(ceil_div(keys, n), 64) * 64);
     splits = (int)ceil_div(keys, len);
   };
