@@ -2365,9 +2365,17 @@ bool wt::serve_inside_mapping(const wt_handle *h, const void *p, uint64_t n) {
   return !h->by_base.empty() && inside_mapping(h, p, n);
 }
 
-bool wt::serve_range_ok(const void *p, uint64_t n) {
+bool wt::serve_range_ok(const void *p, uint64_t n, ServeRanges *seen) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+  for (int i = 0; i < seen->n; ++i)
+    if (a >= seen->lo[i] && a < seen->hi[i]) return a + n <= seen->hi[i] && a + n >= a;
   RangeCache c;
-  return device_range_ok(p, n, c);
+  const bool ok = device_range_ok(p, n, c);
+  if (c.hi && seen->n < ServeRanges::kMost) {
+    seen->lo[seen->n] = c.lo;
+    seen->hi[seen->n++] = c.hi;
+  }
+  return ok;
 }
 
 void wt::serve_lock(wt_handle *h) { h->mu.lock(); }

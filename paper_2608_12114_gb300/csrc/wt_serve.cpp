@@ -35,16 +35,16 @@ uint64_t extent(uint64_t rows, uint64_t pitch, uint64_t row, uint64_t elem) {
 }
 constexpr int64_t kMaxPitch = 1ll << 40;
 
-int check_buffer(const char *call, const char *name, const void *p, uint64_t n, uintptr_t align) {
+int check_buffer(wt::ServeRanges *seen, const char *call, const char *name, const void *p, uint64_t n, uintptr_t align) {
   if (n == 0) return WT_OK;
   if (!p) return serve_error(WT_EINVAL, "%s: %s is NULL", call, name);
   if (!aligned(p, align)) return serve_error(WT_EINVAL, "%s: %s is not on a %d-byte boundary", call, name, (int)align);
-  if (!wt::serve_range_ok(p, n)) return serve_error(WT_EINVAL, "%s: %s runs past the end of its device allocation", call, name);
+  if (!wt::serve_range_ok(p, n, seen)) return serve_error(WT_EINVAL, "%s: %s runs past the end of its device allocation", call, name);
   return WT_OK;
 }
 
-int check_output(wt_handle *h, const char *call, const char *name, const void *p, uint64_t n, uintptr_t align) {
-  int rc = check_buffer(call, name, p, n, align);
+int check_output(wt_handle *h, wt::ServeRanges *seen, const char *call, const char *name, const void *p, uint64_t n, uintptr_t align) {
+  int rc = check_buffer(seen, call, name, p, n, align);
   if (rc == WT_OK && n && wt::serve_inside_mapping(h, p, n))
     rc = serve_error(WT_EINVAL, "%s: %s lies inside a read-only mapping", call, name);
   return rc;
@@ -61,7 +61,7 @@ bool overlap(const void *a, uint64_t na, const void *b, uint64_t nb) {
     if (rc_) return rc_;     \
   } while (0)
 
-int check_adapt(wt_handle *h, const wt_adapt_desc &d, size_t i) {
+int check_adapt(wt_handle *h, wt::ServeRanges &seen, const wt_adapt_desc &d, size_t i) {
   const char *call = "wt_adapt";
   if (d.dtype != WT_BF16 && d.dtype != WT_F16)
     return serve_error(d.dtype >= WT_F32 && d.dtype <= WT_U8 ? WT_ENOTSUP : WT_EINVAL,
@@ -75,20 +75,20 @@ int check_adapt(wt_handle *h, const wt_adapt_desc &d, size_t i) {
     return serve_error(WT_EINVAL, "%s: desc %zu: a pitch is shorter than its row, or not below 2^40", call, i);
   if (T == 0 || M == 0) return WT_OK;
   const uint64_t yn = extent(T, d.ldy, M, 4), bn = d.base ? extent(T, d.ldbase, M, 4) : 0;
-  CHECK(check_output(h, call, "y", d.y, yn, 4));
-  CHECK(check_buffer(call, "base", d.base, bn, 4));
+  CHECK(check_output(h, &seen, call, "y", d.y, yn, 4));
+  CHECK(check_buffer(&seen, call, "base", d.base, bn, 4));
   if (d.base == d.y) {
     if (d.ldbase != d.ldy) return serve_error(WT_EINVAL, "%s: desc %zu: base is y, with another pitch", call, i);
   } else if (overlap(d.y, yn, d.base, bn)) {
     return serve_error(WT_EINVAL, "%s: desc %zu: base overlaps y", call, i);
   }
-  CHECK(check_buffer(call, "slot", d.slot, 4 * T, 4));
+  CHECK(check_buffer(&seen, call, "slot", d.slot, 4 * T, 4));
   if (S == 0 || R == 0) return WT_OK;
-  CHECK(check_buffer(call, "x", d.x, extent(T, d.ldx, K, 2), 2));
-  CHECK(check_buffer(call, "A", d.A, extent(S, d.a_slot, R * K, 2), 2));
-  CHECK(check_buffer(call, "B", d.B, extent(S, d.b_slot, M * R, 2), 2));
-  if (d.rank) CHECK(check_buffer(call, "rank", d.rank, 4 * S, 4));
-  if (d.scale) CHECK(check_buffer(call, "scale", d.scale, 4 * S, 4));
+  CHECK(check_buffer(&seen, call, "x", d.x, extent(T, d.ldx, K, 2), 2));
+  CHECK(check_buffer(&seen, call, "A", d.A, extent(S, d.a_slot, R * K, 2), 2));
+  CHECK(check_buffer(&seen, call, "B", d.B, extent(S, d.b_slot, M * R, 2), 2));
+  if (d.rank) CHECK(check_buffer(&seen, call, "rank", d.rank, 4 * S, 4));
+  if (d.scale) CHECK(check_buffer(&seen, call, "scale", d.scale, 4 * S, 4));
   return WT_OK;
 }
 
@@ -96,7 +96,8 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
   wt::ServeContext ctx;
   CHECK(wt::serve_context(h, "wt_adapt", &ctx));
   if (n && !d) return serve_error(WT_EINVAL, "wt_adapt: NULL descriptors");
-  for (size_t i = 0; i < n; ++i) CHECK(check_adapt(h, d[i], i));
+  wt::ServeRanges seen;
+  for (size_t i = 0; i < n; ++i) CHECK(check_adapt(h, seen, d[i], i));
   for (size_t i = 0; i < n;) {
     // up to 8 descriptors of one type a launch
     wt::AdaptLaunch L;
@@ -178,6 +179,7 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
 
 int check_attend(wt_handle *h, const wt_attend_desc &d) {
   const char *call = "wt_attend";
+  wt::ServeRanges seen;
   if (d.dtype != WT_BF16 && d.dtype != WT_F16)
     return serve_error(d.dtype >= WT_F32 && d.dtype <= WT_U8 ? WT_ENOTSUP : WT_EINVAL,
                        "%s: dtype %d: queries and caches are bf16 or f16", call, d.dtype);
@@ -198,9 +200,9 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
                        (long long)d.q_stride, (long long)d.out_stride);
   if ((int64_t)d.n_tokens * d.heads > 0x7fffffff) return serve_error(WT_EINVAL, "%s: n_tokens * heads above 2^31-1", call);
   if (d.n_req == 0 || d.n_tokens == 0 || d.max_new == 0) return WT_OK;
-  CHECK(check_buffer(call, "q", d.q, extent(d.n_tokens, d.q_stride, row, 2), 16));
-  CHECK(check_output(h, call, "out", d.out, extent(d.n_tokens, d.out_stride, row, 2), 16));
-  CHECK(check_buffer(call, "begin", d.begin, 4 * ((uint64_t)d.n_req + 1), 4));
+  CHECK(check_buffer(&seen, call, "q", d.q, extent(d.n_tokens, d.q_stride, row, 2), 16));
+  CHECK(check_output(h, &seen, call, "out", d.out, extent(d.n_tokens, d.out_stride, row, 2), 16));
+  CHECK(check_buffer(&seen, call, "begin", d.begin, 4 * ((uint64_t)d.n_req + 1), 4));
   if (d.prefix_len) {
     if (d.prefix_head < D || d.prefix_head % 8 || d.prefix_stride < D || d.prefix_stride % 8 || d.prefix_head > kMaxPitch ||
         d.prefix_stride > kMaxPitch)
@@ -208,18 +210,18 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
                          (long long)d.prefix_stride, (long long)d.prefix_head);
     // dense either way round: [key, head, dim] or [head, key, dim]
     const uint64_t n = 2 * ((uint64_t)(d.prefix_len - 1) * d.prefix_stride + (uint64_t)(d.kv_heads - 1) * d.prefix_head + D);
-    CHECK(check_buffer(call, "prefix_k", d.prefix_k, n, 16));
-    CHECK(check_buffer(call, "prefix_v", d.prefix_v, n, 16));
+    CHECK(check_buffer(&seen, call, "prefix_k", d.prefix_k, n, 16));
+    CHECK(check_buffer(&seen, call, "prefix_v", d.prefix_v, n, 16));
   }
   if (d.max_len) {
     if (d.page < 1 || d.table_stride < 0 || d.table_stride > 0x7fffffff || (int64_t)d.max_len > d.table_stride * d.page)
       return serve_error(WT_EINVAL, "%s: max_len %d does not fit %lld pages of %d keys", call, d.max_len,
                          (long long)d.table_stride, d.page);
     const uint64_t n = (uint64_t)d.n_pages * d.page * d.kv_heads * D * 2;
-    CHECK(check_buffer(call, "k_pages", d.k_pages, n, 16));
-    CHECK(check_buffer(call, "v_pages", d.v_pages, n, 16));
-    CHECK(check_buffer(call, "table", d.table, extent(d.n_req, d.table_stride, d.table_stride, 4), 4));
-    CHECK(check_buffer(call, "len", d.len, 4 * (uint64_t)d.n_req, 4));
+    CHECK(check_buffer(&seen, call, "k_pages", d.k_pages, n, 16));
+    CHECK(check_buffer(&seen, call, "v_pages", d.v_pages, n, 16));
+    CHECK(check_buffer(&seen, call, "table", d.table, extent(d.n_req, d.table_stride, d.table_stride, 4), 4));
+    CHECK(check_buffer(&seen, call, "len", d.len, 4 * (uint64_t)d.n_req, 4));
   }
   return WT_OK;
 }
@@ -335,6 +337,7 @@ int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
 
 int probs_impl(wt_handle *h, const wt_probs_desc *d, cudaStream_t s) {
   const char *call = "wt_probs";
+  wt::ServeRanges seen;
   wt::ServeContext ctx;
   CHECK(wt::serve_context(h, call, &ctx));
   if (!d) return serve_error(WT_EINVAL, "%s: NULL descriptor", call);
@@ -343,11 +346,11 @@ int probs_impl(wt_handle *h, const wt_probs_desc *d, cudaStream_t s) {
     return serve_error(WT_EINVAL, "%s: rows %d, vocab %d or a pitch out of range", call, d->rows, d->vocab);
   if (d->rows == 0 || d->vocab == 0) return WT_OK;
   const uint64_t ln = extent(d->rows, d->ldl, d->vocab, 4), pn = extent(d->rows, d->ldp, d->vocab, 4);
-  CHECK(check_buffer(call, "logits", d->logits, ln, 4));
-  CHECK(check_output(h, call, "p", d->p, pn, 4));
+  CHECK(check_buffer(&seen, call, "logits", d->logits, ln, 4));
+  CHECK(check_output(h, &seen, call, "p", d->p, pn, 4));
   if (d->p == d->logits ? d->ldp != d->ldl : overlap(d->p, pn, d->logits, ln))
     return serve_error(WT_EINVAL, "%s: p overlaps the logits", call);
-  if (d->temp) CHECK(check_buffer(call, "temp", d->temp, 4 * (uint64_t)d->rows, 4));
+  if (d->temp) CHECK(check_buffer(&seen, call, "temp", d->temp, 4 * (uint64_t)d->rows, 4));
   CU(wt::launch_probs(*d, ctx.status, s));
   wt::serve_launched(h, 1);
   return WT_OK;
@@ -355,6 +358,7 @@ int probs_impl(wt_handle *h, const wt_probs_desc *d, cudaStream_t s) {
 
 int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {
   const char *call = "wt_verify";
+  wt::ServeRanges seen;
   wt::ServeContext ctx;
   CHECK(wt::serve_context(h, call, &ctx));
   if (!d) return serve_error(WT_EINVAL, "%s: NULL descriptor", call);
@@ -365,14 +369,14 @@ int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {
                        d->n_req, d->n_drafted, d->max_draft, d->vocab, WT_VERIFY_MAX_VOCAB);
   if (d->n_req == 0) return WT_OK;
   const uint64_t B = d->n_req, n = d->n_drafted;
-  CHECK(check_buffer(call, "p", d->p, extent(n + B, d->ldp, d->vocab, 4), 4));
-  if (d->q) CHECK(check_buffer(call, "q", d->q, extent(n, d->ldq, d->vocab, 4), 4));
-  CHECK(check_buffer(call, "drafted", d->drafted, 4 * n, 4));
-  CHECK(check_buffer(call, "begin", d->begin, 4 * (B + 1), 4));
-  CHECK(check_buffer(call, "u", d->u, 4 * n, 4));
-  CHECK(check_buffer(call, "u_draw", d->u_draw, 4 * B, 4));
-  CHECK(check_output(h, call, "accepted", d->accepted, 4 * B, 4));
-  CHECK(check_output(h, call, "tokens", d->tokens, 4 * B * ((uint64_t)d->max_draft + 1), 4));
+  CHECK(check_buffer(&seen, call, "p", d->p, extent(n + B, d->ldp, d->vocab, 4), 4));
+  if (d->q) CHECK(check_buffer(&seen, call, "q", d->q, extent(n, d->ldq, d->vocab, 4), 4));
+  CHECK(check_buffer(&seen, call, "drafted", d->drafted, 4 * n, 4));
+  CHECK(check_buffer(&seen, call, "begin", d->begin, 4 * (B + 1), 4));
+  CHECK(check_buffer(&seen, call, "u", d->u, 4 * n, 4));
+  CHECK(check_buffer(&seen, call, "u_draw", d->u_draw, 4 * B, 4));
+  CHECK(check_output(h, &seen, call, "accepted", d->accepted, 4 * B, 4));
+  CHECK(check_output(h, &seen, call, "tokens", d->tokens, 4 * B * ((uint64_t)d->max_draft + 1), 4));
   CU(wt::launch_verify(*d, ctx.status, s));
   wt::serve_launched(h, 1);
   return WT_OK;

@@ -19,8 +19,15 @@ struct ServeContext {
 // Refuses NULL and host-only handles.
 int serve_context(wt_handle *h, const char *call, ServeContext *out);
 bool serve_inside_mapping(const wt_handle *h, const void *p, uint64_t n);
+// Device allocations that a call has met: its small buffers often share one, and each look-up costs
+// the driver's time.
+struct ServeRanges {
+  static constexpr int kMost = 8;
+  uintptr_t lo[kMost], hi[kMost];
+  int n = 0;
+};
 // false only when [p, p + n) starts inside a device allocation and runs past its end
-bool serve_range_ok(const void *p, uint64_t n);
+bool serve_range_ok(const void *p, uint64_t n, ServeRanges *seen);
 void serve_launched(wt_handle *h, int kernels);
 // The handle's mutex, held from serve_workspace to serve_workspace_done.
 void serve_lock(wt_handle *h);

@@ -351,21 +351,31 @@ class Handle:
         """wt_adapt over a list of AdaptDesc, or a ctypes array of them (which a step that repeats
         keeps: (AdaptDesc * n)(*descs) copies every descriptor)."""
         n = len(descs)
-        if not isinstance(descs, C.Array):
+        if n == 1:
+            descs = C.byref(descs[0])
+        elif not isinstance(descs, C.Array):
             descs = (AdaptDesc * max(1, n))(*descs)
-        _check(lib().wt_adapt(self.ptr, descs, n, stream))
+        rc = lib().wt_adapt(self.ptr, descs, n, stream)
+        if rc:
+            _check(rc)
 
     def attend(self, desc: AttendDesc, stream: int = 0):
         """wt_attend."""
-        _check(lib().wt_attend(self.ptr, C.byref(desc), stream))
+        rc = lib().wt_attend(self.ptr, C.byref(desc), stream)
+        if rc:
+            _check(rc)
 
     def probs(self, desc: ProbsDesc, stream: int = 0):
         """wt_probs."""
-        _check(lib().wt_probs(self.ptr, C.byref(desc), stream))
+        rc = lib().wt_probs(self.ptr, C.byref(desc), stream)
+        if rc:
+            _check(rc)
 
     def verify(self, desc: VerifyDesc, stream: int = 0):
         """wt_verify."""
-        _check(lib().wt_verify(self.ptr, C.byref(desc), stream))
+        rc = lib().wt_verify(self.ptr, C.byref(desc), stream)
+        if rc:
+            _check(rc)
 
     def checksum(self, ptrs: Sequence[int], nbytes: Sequence[int], out_dev: int, stream: int = 0,
                  plain: bool = False):
