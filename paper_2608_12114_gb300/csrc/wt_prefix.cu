@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(empty0 + 8 * s, 1);
     }
     mbar_init(q_full, 1);
-    mbar_init(q_empty, 1);
+    mbar_init(q_empty, 256);
     mbar_init(fin, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + 8 * i, 1);
@@ -322,7 +322,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           scores(0, stage);
           scores(1, stage);
           release(empty0 + 8 * stage);
-          if (g.n == 1) release(q_empty);
           for (int j = 0; j < g.n; ++j) {
             if (!next()) break;
             const uint32_t vs = stage;
@@ -337,7 +336,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (more) {
               scores(1, stage);
               release(empty0 + 8 * stage);
-              if (j + 2 == g.n) release(q_empty);
             }
           }
         } else {
@@ -346,7 +344,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             release(empty0 + 8 * stage);
           }
           if (!live) break;
-          if (g.n <= 2) release(q_empty);
           for (int j = 0; j < g.n; ++j) {
             if (!next()) break;
             const uint32_t vs = stage;
@@ -356,7 +353,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (!next()) break;
               scores(j & 1, stage);
               release(empty0 + 8 * stage);
-              if (j + 3 == g.n) release(q_empty);
             }
           }
         }
@@ -457,27 +453,43 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (!live) break;
-      const int row = apart ? r : (rb * 2 + i) * P.tile_rows + r;
-      const bool mine = r < P.tile_rows && row < P.rows;
-      const int64_t at = ((int64_t)(grp + g.head) * P.qtiles + (apart ? i : rb * 2 + i)) * kRowsT + r;
+      // This stream's rows to the workspace, 32 columns at a time, turned in shared memory so that 8 lanes
+      // write 128 bytes of a row (a lane writing its own row touched 32 lines with each store: 3.3 us of a
+      // decode step's 8).  The queries have been read by then, and their place is this stream's until
+      // q_empty.
+      const int row0 = apart ? 0 : (rb * 2 + i) * P.tile_rows;
+      const int rows = min(P.tile_rows, P.rows - row0);  // of the tile; may be none
+      const int64_t tile_at = ((int64_t)(grp + g.head) * P.qtiles + (apart ? i : rb * 2 + i)) * kRowsT;
       if (n > 0) {
         if (!warp_wait(o_full + 8 * i, (done + n - 1) & 1, abort_flag, status)) break;
         fence_after();
+        const uint32_t turn = base + i * X::stage + (warp & 3) * (X::stage / 4);
+        static_assert(32 * 128 <= X::stage / 4, "32 rows of 32 columns");
 #pragma unroll 1
         for (int c = 0; c < DH * 64; c += 32) {
           uint32_t o[32];
           tmem_ld32(O + c, o);
           wait_ld();
-          if (mine) {
 #pragma unroll
-            for (int k = 0; k < 32; k += 4)
-              if (c + k < P.head_dim)
-                *reinterpret_cast<uint4 *>(P.o + at * P.head_dim + c + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          for (int k = 0; k < 8; ++k)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(turn + lane * 128 + (k ^ (lane & 7)) * 16), "r"(o[4 * k]),
+                         "r"(o[4 * k + 1]), "r"(o[4 * k + 2]), "r"(o[4 * k + 3])
+                         : "memory");
+          __syncwarp();
+          const int col = c + (lane & 7) * 4;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int t = k * 4 + (lane >> 3), at = (warp & 3) * 32 + t;
+            const uint4 v = lds128(turn + t * 128 + ((lane ^ t) & 7) * 16);
+            if (at < rows && col < P.head_dim) *reinterpret_cast<uint4 *>(P.o + (tile_at + at) * P.head_dim + col) = v;
           }
+          __syncwarp();
         }
         fence_before();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the next queries land there
       }
-      if (mine) P.ml[at] = make_float2(n > 0 ? m : -INFINITY, l0 + l1);
+      mbar_arrive(q_empty);
+      if (r < rows) P.ml[tile_at + r] = make_float2(n > 0 ? m : -INFINITY, l0 + l1);
       done += n;
     }
   }
