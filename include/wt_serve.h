@@ -18,6 +18,7 @@
  *     largest call.  A call captured into a CUDA graph takes a workspace of its own, which stays
  *     until wt_close; every replay must complete before wt_close, and two replays of one graph must
  *     not overlap.  No warm-up call is needed before a capture.
+ *   - wt_close waits for the device to go idle if the handle made any of these calls.
  *   - Descriptors are read during the call and not kept.
  *   - Lengths, slots, page numbers and tokens that lie in device memory cannot be checked on the
  *     host.  Where one contradicts its descriptor, the kernel clamps it (an offset, a length, a

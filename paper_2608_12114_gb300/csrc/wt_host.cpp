@@ -475,6 +475,7 @@ struct wt_handle {
   std::vector<cudaEvent_t> events;
   std::list<Plan *> plans;
   std::vector<Workspace *> workspaces;  // of the serving calls (wt_serve.h), one per stream
+  std::atomic<bool> served{false};      // a serving call was made: its kernels may write the status word
   std::atomic<uint64_t> kernel_launches{0};
   wt_open_phases open_times{};
   std::mutex mu;
@@ -2300,6 +2301,9 @@ int close_impl(wt_handle *h) {
     h->trace.clear();
     for (Plan *P : h->plans) destroy_plan(P);
     h->plans.clear();
+    // serving calls leave no event behind, nor do replays of graphs that hold them: the device goes idle
+    // before another handle may get the status word and the workspaces
+    if (h->served) cudaDeviceSynchronize();
     for (Workspace *w : h->workspaces) destroy_workspace(h->device, w);
     h->workspaces.clear();
     for (cudaEvent_t e : h->events) ev_destroy(e);
@@ -2357,6 +2361,7 @@ int wt::serve_cuda_error(cudaError_t e, const char *what) { return cuda_err(e, w
 int wt::serve_context(wt_handle *h, const char *call, ServeContext *out) {
   if (!h) return set_err(WT_EINVAL, "%s: NULL handle", call);
   if (h->host_only) return set_err(WT_ENOTSUP, "%s: handle was opened host-only", call);
+  h->served = true;
   *out = {h->device, h->status};
   return WT_OK;
 }
