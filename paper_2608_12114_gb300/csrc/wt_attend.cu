@@ -85,7 +85,11 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
   constexpr int kTileBytes = 2 * kKeys * kPitch;    // K rows, then V rows
   constexpr int kRows = 16 * MT;
   extern __shared__ __align__(128) uint8_t smem[];
-  griddep_wait();  // the prefix before it: launched while that ends
+  // Nothing here needs the prefix's parts, so this kernel may start while that one still runs; but it
+  // must not end before it, because the merge waits for this kernel alone.
+  struct AtEnd {
+    __device__ ~AtEnd() { griddep_wait(); }
+  } at_end;
   const wt_attend_desc &d = P.d;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
   const int hk = blockIdx.x % d.kv_heads, rt = blockIdx.x / d.kv_heads % P.row_tiles;
@@ -397,11 +401,11 @@ constexpr int kMergeParts = 8;
 template <int DT, int WR>
 __global__ void __launch_bounds__(kThreads) attend_merge_kernel(const __grid_constant__ AttendPlan P) {
   __shared__ float4 so[kWarps][32];
-  griddep_wait();  // launched while the kernel before it ends
   const wt_attend_desc &d = P.d;
   const int lane = threadIdx.x & 31, warp = WR == 1 ? 0 : threadIdx.x >> 5;
   const int b = blockIdx.y;
   const Request rq = request_of(d, b, nullptr, false);
+  griddep_wait();  // launched while the kernel before it ends
   const int i = WR == 1 ? blockIdx.x * kWarps + (threadIdx.x >> 5) : blockIdx.x;
   if (i >= rq.n * d.heads) return;
   const int h = i % d.heads, t = rq.t0 + i / d.heads;

@@ -209,6 +209,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   fence_before();
   __syncthreads();
   fence_after();
+  griddep_launch();  // the own keys' kernel may take SMs as they come free
   const uint32_t tmem = *tmem_slot;
   const int lead = apart ? 2 : 1;  // key tiles whose K is loaded ahead of their V
 
