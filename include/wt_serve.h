@@ -49,7 +49,8 @@ extern "C" {
  * base may be y itself (then tokens without adapter cost nothing); otherwise the two must not
  * overlap.  base NULL stands for zeros.
  *
- * All descriptors of a call share one launch per 8 of them.  Any K, M >= 0, 0 <= R <= 128, any T
+ * All descriptors of a call share one launch per 8 of them (three launches from 256 tokens on); no y of
+ * a call may overlap another descriptor's operands.  Any K, M >= 0, 0 <= R <= 128, any T
  * and any element alignment; rows that lie on 16-byte boundaries load faster. */
 #define WT_ADAPT_MAX_RANK 128
 #define WT_ADAPT_MAX_SLOTS 4096

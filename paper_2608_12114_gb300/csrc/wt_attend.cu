@@ -92,13 +92,16 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
   } at_end;
   const wt_attend_desc &d = P.d;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
-  const int hk = blockIdx.x % d.kv_heads, rt = blockIdx.x / d.kv_heads % P.row_tiles;
-  const int keys_of = blockIdx.x / (d.kv_heads * P.row_tiles);  // (request, split), then the prefix's splits
   const int G = P.G, D = d.head_dim;
-  // the last "request" is the shared prefix with every token of the batch, where it is taken here
-  const bool pre = keys_of >= d.n_req * P.own_splits;
+  // CTAs of own keys by (request, split, row tile, kv head), then those of the prefix, where it is taken
+  // here, by (split, row tile, kv head): it is a request of its own with every token of the batch.
+  const int own_ctas = d.n_req * P.own_splits * P.own_tiles * d.kv_heads;
+  const bool pre = (int)blockIdx.x >= own_ctas;
+  const int at = pre ? blockIdx.x - own_ctas : blockIdx.x, hk = at % d.kv_heads;
+  const int row_tiles = pre ? P.pre_tiles : P.own_tiles, rt = at / d.kv_heads % row_tiles;
+  const int keys_of = at / (d.kv_heads * row_tiles);
   const int b = pre ? 0 : keys_of / P.own_splits;
-  const int split = pre ? keys_of - d.n_req * P.own_splits : keys_of % P.own_splits;
+  const int split = pre ? keys_of : keys_of % P.own_splits;
   Request rq;
   int k0, k1;
   if (pre) {
@@ -156,13 +159,18 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
         const int64_t off = (first + row_lane) * key_bytes + in_lane * 16, by = row_step * key_bytes;
         const uint8_t *ks = k_of + off, *vs = v_of + off;
         uint32_t to = dst + row_lane * kPitch + in_lane * 16;
+        if (n == kKeys) {
 #pragma unroll 4
-        for (int r = row_lane; r < kKeys; r += row_step) {
-          cp16(to, ks, r < n);  // an absent row is not read, wherever its address leads
-          cp16(to + kKeys * kPitch, vs, r < n);
-          to += row_step * kPitch;
-          ks += by;
-          vs += by;
+          for (int r = row_lane; r < kKeys; r += row_step, to += row_step * kPitch, ks += by, vs += by) {
+            cp16(to, ks, true);
+            cp16(to + kKeys * kPitch, vs, true);
+          }
+        } else {
+#pragma unroll 1
+          for (int r = row_lane; r < kKeys; r += row_step, to += row_step * kPitch, ks += by, vs += by) {
+            cp16(to, r < n ? ks : d.q, r < n);
+            cp16(to + kKeys * kPitch, r < n ? vs : d.q, r < n);
+          }
         }
       } else {
         // lane r knows where row r lies (rows 0-15: K, 16-31: V), and the lanes copy whole rows together
@@ -515,7 +523,7 @@ cudaError_t launch(void (*k)(AttendPlan), dim3 grid, size_t smem, bool after, cu
 
 template <int DT, int ND>
 cudaError_t run_warp(const AttendPlan &P, cudaStream_t s) {
-  const unsigned grid = (unsigned)(P.d.kv_heads * P.row_tiles * (P.d.n_req * P.own_splits + P.pre_splits));
+  const unsigned grid = (unsigned)(P.d.kv_heads * (P.d.n_req * P.own_splits * P.own_tiles + P.pre_splits * P.pre_tiles));
   if (grid == 0) return cudaSuccess;
   return launch(P.rows_tile == 16 ? attend_warp_kernel<DT, ND, 1> : attend_warp_kernel<DT, ND, 2>, dim3(grid), warp_smem<ND>(),
                 P.x.groups != 0, s, P);

@@ -226,12 +226,12 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
   return WT_OK;
 }
 
-// The prefix goes to tcgen05 from 33 rows (token, head-in-group) on, which is where the warp kernel
-// would read it more than once, and from one key tile on.  Its reference only grows, so the scale has
-// to be positive; and a pitch has to fit a tensor map.
+// The prefix goes to tcgen05 from 33 rows (token, head-in-group) on, where the warp kernel would read
+// it more than twice.  Its softmax takes the largest product for the largest score, so the scale has to
+// be positive; and a pitch has to fit a tensor map.
 bool prefix_on_tcgen05(const wt_attend_desc &d) {
   const int64_t rows = (int64_t)d.n_tokens * (d.heads / d.kv_heads);
-  return rows > 32 && d.prefix_len >= 128 && d.scale > 0.0f && d.q_stride < (1ll << 38) && d.prefix_stride < (1ll << 38) &&
+  return rows > 32 && d.scale > 0.0f && d.q_stride < (1ll << 38) && d.prefix_stride < (1ll << 38) &&
          d.prefix_head < (1ll << 38);
 }
 
@@ -255,7 +255,8 @@ int plan_prefix(const wt_attend_desc &d, int G, wt::PrefixPlan *x, wt::PrefixMap
   const int64_t all = (int64_t)d.kv_heads * x->tiles, sms = wt::num_sms();
   if (all > (1 << 30)) return serve_error(WT_EINVAL, "wt_attend: %lld key tiles", (long long)all);
   int64_t best = INT64_MAX;
-  for (int64_t g = std::min<int64_t>(all, std::max<int64_t>(1, 2 * sms / x->row_blocks)); g >= 1; --g) {
+  for (int64_t waves = 1; waves <= 4; ++waves) {
+    const int64_t g = std::min(all, std::max<int64_t>(1, waves * sms / x->row_blocks));
     const int64_t len = ceil_div(all, g), n = ceil_div(all, len);
     const int64_t cost = ceil_div(x->row_blocks * n, sms) * (len + 3);
     if (cost < best) best = cost, x->len = (int)len, x->groups = (int)n;
@@ -287,10 +288,10 @@ int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
   wt::PrefixMaps maps;
   if (d.prefix_len && prefix_on_tcgen05(d)) CHECK(plan_prefix(d, P.G, &P.x, &maps));
   const bool pre_warp = d.prefix_len && !P.x.groups;
-  const int64_t most = std::max(d.max_len ? own_rows : 0, pre_warp ? pre_rows : 0);
   // tiles of 32 rows where a request has more than 16; a prefix beside shorter ones is read once for each 16
-  P.rows_tile = (d.max_len ? own_rows : most) <= 16 ? 16 : 32;
-  P.row_tiles = (int)ceil_div(most, P.rows_tile);
+  P.rows_tile = (d.max_len ? own_rows : pre_rows) <= 16 ? 16 : 32;
+  P.own_tiles = (int)ceil_div(own_rows, P.rows_tile);
+  P.pre_tiles = (int)ceil_div(pre_rows, P.rows_tile);
   // Splits, of at least 64 keys (one tile for each warp): own keys alone take 4 CTAs per SM (lengths differ,
   // and CTAs without keys end at once); own keys and prefix in one launch take one each, and up to 4
   // where splits stay at 512 keys (7 requests with a head for every query behind 1021 keys: 13.6 us,
@@ -302,10 +303,10 @@ int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
     len = (int)(ceil_div(ceil_div(keys, n), 64) * 64);
     splits = (int)ceil_div(keys, len);
   };
-  if (d.max_len) split(d.max_len, (int64_t)d.n_req * d.kv_heads * ceil_div(own_rows, P.rows_tile), P.own_splits, P.own_len);
-  if (pre_warp) split(d.prefix_len, d.kv_heads * ceil_div(pre_rows, P.rows_tile), P.pre_splits, P.pre_len);
+  if (d.max_len) split(d.max_len, (int64_t)d.n_req * d.kv_heads * P.own_tiles, P.own_splits, P.own_len);
+  if (pre_warp) split(d.prefix_len, (int64_t)d.kv_heads * P.pre_tiles, P.pre_splits, P.pre_len);
   const int64_t parts = P.own_splits + P.pre_splits, rows = (int64_t)d.n_tokens * d.heads;
-  if ((int64_t)d.kv_heads * P.row_tiles * ((int64_t)d.n_req * P.own_splits + P.pre_splits) > 0x7fffffff)
+  if ((double)d.kv_heads * ((double)d.n_req * P.own_splits * P.own_tiles + (double)P.pre_splits * P.pre_tiles) > 0x7fffffff)
     return serve_error(WT_EINVAL, "wt_attend: too many tokens, heads and keys for one launch");
   // workspace: O and (m, l) of every part
   auto take = [](size_t &at, size_t n) {

@@ -115,7 +115,7 @@ struct AttendPlan {
   wt_attend_desc d;
   int G;          // heads / kv_heads
   int rows_tile;  // rows (token, head-in-group) of one CTA of the warp kernel: 16 or 32
-  int row_tiles;  // tiles that the longest request (or the prefix's rows) takes
+  int own_tiles, pre_tiles;  // tiles of the longest request's rows, and of all rows (for the prefix)
   int own_splits, own_len;  // own keys per split
   int pre_splits, pre_len;  // prefix keys per split of the warp kernel (0: not taken there)
   PrefixPlan x;             // the prefix on tcgen05 (x.groups 0: not taken there)

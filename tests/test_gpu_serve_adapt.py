@@ -234,3 +234,16 @@ def test_updates_of_any_size(torch, h, dt):
     h.adapt([serving.adapters(x, y, slot, A, B, scale, base=base)])
     torch.cuda.synchronize()
     close(torch, y, _serve.adapt(x, slot, A, B, scale, None, base), 64, 16)
+
+
+@pytest.mark.parametrize("T", [3, 260])
+def test_offsets_past_32_bits(torch, h, T):
+    x, y, slot, A, B, scale, base = make(torch, T, 64, 32, 2, 8, torch.bfloat16)
+    far = torch.empty((1 << 31) + 8 * 64, dtype=torch.bfloat16, device="cuda")
+    A2 = far.as_strided((2, 8, 64), (1 << 31, 64, 1))
+    A2.copy_(A)
+    big = torch.empty((1 << 31) + 32 * T, device="cuda")
+    y2 = big[-32 * T:].view(T, 32) if T > 3 else big.as_strided((3, 32), (1 << 30, 1))
+    h.adapt([serving.adapters(x, y2, slot, A2, B, scale, base=base)])
+    torch.cuda.synchronize()
+    close(torch, y2, _serve.adapt(x, slot, A, B, scale, None, base), 64, 8)

@@ -300,3 +300,42 @@ def test_refusals(torch, h):
             s.desc(**bad)
     with pytest.raises(ValueError):
         serving.attention(s.q, s.out[:, :2], s.begin, max_new=2)
+
+
+@pytest.mark.parametrize("P", [1, 5, 100, 127, 128, 129, 255, 257])
+@pytest.mark.parametrize("G,D", [(1, 128), (4, 64), (5, 96), (128, 128)])
+def test_batches_behind_short_prefixes(torch, h, P, G, D):
+    """Many rows, few keys: key tiles and row tiles that are hardly filled."""
+    new = [2, 0, 3, 1] * (12 if G < 128 else 1)
+    s = Set(torch, new, [n + 3 for n in new], P, 2 * G, 2, D, seed=P)
+    h.attend(s.desc())
+    torch.cuda.synchronize()
+    s.check(torch)
+
+
+@pytest.mark.parametrize("scale", [0.3, -0.3, 0.0])
+def test_batches_at_any_scale(torch, h, scale):
+    s = Set(torch, [3] * 16, [20] * 16, 300, 8, 2, 64)
+    s.scale = scale
+    h.attend(s.desc())
+    torch.cuda.synchronize()
+    s.check(torch)
+
+
+def test_offsets_past_32_bits(torch, h):
+    """A pool of more than 2^31 elements, and a prefix whose keys lie as far apart."""
+    s = Set(torch, [1, 2], [40, 33], 3, 4, 2, 128)
+    total = (1 << 31) // (16 * 2 * 128) + 40
+    k, v = (torch.empty(total, 16, 2, 128, dtype=s.k.dtype, device="cuda") for _ in range(2))
+    far = s.k.shape[0]
+    k[-far:], v[-far:] = s.k, s.v
+    s.k, s.v = k, v
+    s.table += total - far
+    pk, pv = (torch.empty((1 << 31) + 4096, dtype=k.dtype, device="cuda").as_strided((3, 2, 128), (1 << 30, 128, 1))
+              for _ in range(2))
+    pk.copy_(s.pk), pv.copy_(s.pv)
+    s.pk, s.pv = pk, pv
+    near = Set(torch, [1, 2], [40, 33], 3, 4, 2, 128)
+    h.attend(s.desc())
+    torch.cuda.synchronize()
+    s.check(torch, near.want())

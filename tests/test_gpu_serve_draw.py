@@ -274,3 +274,16 @@ def test_verify_refusals(torch, h):
         args.update(bad)
         with pytest.raises(ValueError):
             serving.verification(**args)
+
+
+def test_offsets_past_32_bits(torch, h):
+    far = torch.empty((1 << 31) + 5000, device="cuda")
+    l = far.as_strided((3, 4999), (1 << 30, 1))
+    l.copy_(torch.randn(3, 4999, device="cuda"))
+    near = l.contiguous()
+    h.probs(serving.probabilities(l, l))
+    torch.cuda.synchronize()
+    close(torch, l, near, None)
+    p, q, d, begin, u, w = drafts(torch, [2], 4999, 2.0, False)
+    l.copy_(p)
+    assert run(torch, h, l, q, d, begin, u, w, 2) == _serve.verify(p, q, d, begin, u, w, 2)
