@@ -81,6 +81,9 @@ __device__ __forceinline__ uint4 keep8(const uint4 &v, int keep) {
   return keep >= 8 ? v : and4(v, byte_mask(0, 2 * keep));
 }
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
 struct Item {
   int slot;   // S: tokens without an adapter
   int count;  // tokens
@@ -310,14 +313,15 @@ __global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const 
         for (int e = 0; e < 4; ++e)
           mine[(j * 8 + 2 * q + (e & 1)) * kR + i * 16 + g + (e >> 1) * 8] = acc[i][j][e];
     __syncthreads();
-    for (int i = tid; i < kTile * kR; i += kThreads) {
+    const int sums = item.count * kR;  // rows of absent tokens mean nothing
+    for (int i = tid; i < sums; i += kThreads) {
       float s = part[i];
       for (int k = 1; k < WK; ++k) s += part[k * kTile * kR + i];
       part[i] = s;
     }
     cl.sync();
     const float scale = d.scale ? __ldg(d.scale + item.slot) : 1.0f;
-    for (int i = tid; i < kTile * kR; i += kThreads) {
+    for (int i = tid; i < sums; i += kThreads) {
       float s = 0.0f;
 #pragma unroll
       for (int k = 0; k < kMostCluster; ++k)
@@ -325,7 +329,8 @@ __global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const 
       // ranks past the slot's: zero, also where x is infinite
       vfull[i / kR * (kR + 4) + i % kR] = i % kR < r ? s * scale : 0.0f;
     }
-    cl.sync();
+    cluster_arrive();  // the other CTAs' sums have been read; each waits for this before it leaves
+    __syncthreads();
   }
 
   // y^T: M = tokens (16), N = outputs.  A lane's eight accumulators of two N tiles are four consecutive
@@ -387,6 +392,7 @@ __global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const 
         }
       }
     }
+    cluster_wait();
     return;
   }
   const bool yvec = (P.vec & 4) != 0;
@@ -438,6 +444,7 @@ __global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const 
       }
     }
   }
+  if (r > 0) cluster_wait();
 }
 
 
@@ -446,9 +453,12 @@ __global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const 
 // each.  adapt_plan_kernel sorts the tokens by slot and cuts them into items of up to 64 tokens of one
 // slot.  adapt_shrink_kernel computes v = scale A x of an item, a cluster of 4 CTAs splitting K, with
 // x and A staged in shared memory by 16-byte cp.async.  adapt_expand_kernel adds B v, a CTA taking
-// several tiles of 64 tokens x 64 outputs of an item, with the base and B of the next tiles always on
-// their way to shared memory (loading B into registers as it was needed, each tile waited for L2 twice:
-// 166 us for the expand kernel of 4001 tokens of two projections of 6912 outputs, against XXX).
+// several tiles of 64 tokens x 64 outputs of an item, with the base and B of the next tile always on
+// their way to shared memory.  Measured for 4001 tokens of two projections of 6912 outputs, ranks up to
+// 64: in one launch, as for few tokens, 350 us; three launches 175, of which the expand kernel took 152
+// (each tile waited for its base) or 166 (base ahead, B into registers as needed: each tile waited for
+// L2 twice); both ahead through shared memory, 8 warps 124, 16 warps 107, three CTAs of 8 warps 82 of
+// 111 in all.  Base to y alone, as torch copies it, takes 85.
 //
 // v crosses between the two as 16-bit parts that add up to it, so that the second product's operands
 // need no conversion: bf16 in three parts (24 bits); f16 in two (22 bits), after a power of two for
