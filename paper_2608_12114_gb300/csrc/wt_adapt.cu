@@ -76,6 +76,16 @@ __device__ __forceinline__ uint4 load8(const uint16_t *row, int k, int n) {
   }
 }
 
+// The same off the 16-byte grid: with 8 elements of the row on either side, from the two vectors that hold
+// them (rows of 2731 elements, 463 tokens: 26 us with 8 loads of an element each, 21 so).  The kernel
+// for few tokens keeps the 8 loads, which are in flight together and take less code.
+__device__ __forceinline__ uint4 load8_shifted(const uint16_t *row, int k, int n) {
+  if (k < 8 || k + 16 > n) return load8<false>(row, k, n);
+  const uint64_t at = reinterpret_cast<uint64_t>(row + k), lo = at & ~(uint64_t)15;
+  const uint4 *v = reinterpret_cast<const uint4 *>(lo);
+  return shift_bytes(__ldg(v), __ldg(v + 1), (uint32_t)(at - lo));
+}
+
 // The first `keep` elements of 8, zeros for the others.
 __device__ __forceinline__ uint4 keep8(const uint4 &v, int keep) {
   return keep >= 8 ? v : and4(v, byte_mask(0, 2 * keep));
@@ -451,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const 
 // ------------------------------------------------------------------ prompts
 // Many tokens: x and y are most of the bytes, so the work is cut into three launches of many CTAs
 // each.  adapt_plan_kernel sorts the tokens by slot and cuts them into items of up to 64 tokens of one
-// slot.  adapt_shrink_kernel computes v = scale A x of an item, a cluster of 4 CTAs splitting K, with
+// slot.  adapt_shrink_kernel computes v = scale A x of an item, a cluster of 4 or 8 CTAs splitting K, with
 // x and A staged in shared memory by 16-byte cp.async.  adapt_expand_kernel adds B v, a CTA taking
 // several tiles of 64 tokens x 64 outputs of an item, with the base and B of the next tile always on
 // their way to shared memory.  Measured for 4001 tokens of two projections of 6912 outputs, ranks up to
@@ -471,7 +481,6 @@ static_assert(kPlanThreads == 32 * 32, "a lane for each warp");
 constexpr int kEThreads = 256;  // the expand kernel, three to an SM: products run while other CTAs wait for a tile
 constexpr int kEAcross = kMTile / 32;  // warps side by side in a tile
 constexpr int kSThreads = 128;
-constexpr int kSCluster = 4;
 constexpr int kSK = 64;       // elements of K of a stage
 constexpr int kSStages = 3;   // 55 KB at rank 64: four CTAs per SM
 template <int DT>
@@ -566,9 +575,9 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ int tok[kItem];
   cg::cluster_group cl = cg::this_cluster();
-  const int c = cl.block_rank(), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
+  const int c = cl.block_rank(), C = cl.num_blocks(), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
   int pi = 0;
-  uint32_t w = blockIdx.x / kSCluster;
+  uint32_t w = blockIdx.x / C;
   while (pi + 1 < L.n && w >= L.p[pi].items) w -= L.p[pi++].items;
   const AdaptProj &P = L.p[pi];
   const wt_adapt_desc &d = P.d;
@@ -589,7 +598,7 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
 
   const uint16_t *A = static_cast<const uint16_t *>(d.A) + (int64_t)slot * d.a_slot;
   const uint16_t *x = static_cast<const uint16_t *>(d.x);
-  const int steps = (K + kSK - 1) / kSK, per = (steps + kSCluster - 1) / kSCluster;
+  const int steps = (K + kSK - 1) / kSK, per = (steps + C - 1) / C;
   const int s0 = min(steps, c * per), s1 = min(steps, s0 + per);
   const uint32_t base = smem_u32(smem);
   // Stage s: 8 vectors a row; a thread takes vector tid % 8 of rows tid / 8 + 16 i, tokens first, then
@@ -614,7 +623,7 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
           src = a < r ? A + (int64_t)a * K : nullptr;
         }
         if (src && k < K && vec) cp16(dst + i * 16 * kSPitch, src + k);
-        else sts128(dst + i * 16 * kSPitch, src ? load8<false>(src, k, K) : make_uint4(0, 0, 0, 0));
+        else sts128(dst + i * 16 * kSPitch, src ? load8_shifted(src, k, K) : make_uint4(0, 0, 0, 0));
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -661,27 +670,28 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
       for (int e = 0; e < 4; ++e)
         part[(warp * 16 + j * 8 + 2 * q + (e & 1)) * kR + i * 16 + g + (e >> 1) * 8] = acc[i][j][e];
   cl.sync();
-  // a quarter of the tokens each, 8 lanes to a token: the four CTAs' sums in their order; ranks past
-  // the slot's are zero
+  // a C-th of the tokens each, 8 lanes to a token: the CTAs' sums in their order; ranks past the slot's
+  // are zero
   const float scale = d.scale ? __ldg(d.scale + slot) : 1.0f;
-  const float *from[kSCluster];
-#pragma unroll
-  for (int k = 0; k < kSCluster; ++k) from[k] = cl.map_shared_rank(part, k);
-  static_assert(kItem / kSCluster * 8 == kSThreads, "8 lanes to a token");
-  const int t = c * (kItem / kSCluster) + (tid >> 3), k0 = (tid & 7) * (kR / 8);
+  const int own = kItem / C, t = min(c * own + (tid >> 3), kItem - 1), k0 = (tid & 7) * (kR / 8);
+  const bool mine = (tid >> 3) < own;  // with 8 CTAs half the threads have a token
   float v[kR / 8], top = 0.0f;
 #pragma unroll
   for (int k = 0; k < kR / 8; ++k) v[k] = 0.0f;
+  auto gather = [&](auto n) {
 #pragma unroll
-  for (int j = 0; j < kSCluster; ++j) {
-    const float2 *src = reinterpret_cast<const float2 *>(from[j] + t * kR + k0);
+    for (int j = 0; j < decltype(n)::value; ++j) {
+      const float2 *src = reinterpret_cast<const float2 *>(cl.map_shared_rank(part, j) + t * kR + k0);
 #pragma unroll
-    for (int k = 0; k < kR / 8; k += 2) {
-      const float2 f = src[k / 2];
-      v[k] += f.x;
-      v[k + 1] += f.y;
+      for (int k = 0; k < kR / 8; k += 2) {
+        const float2 f = src[k / 2];
+        v[k] += f.x;
+        v[k + 1] += f.y;
+      }
     }
-  }
+  };
+  if (C == 8) gather(std::integral_constant<int, 8>{});
+  else gather(std::integral_constant<int, 4>{});
 #pragma unroll
   for (int k = 0; k < kR / 8; ++k) {
     v[k] = k0 + k < r ? v[k] * scale : 0.0f;
@@ -696,11 +706,11 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
     // 2^(14 - exponent of top), within what fp32 can take back; 1 for zeros, infinities and NaN
     const int e = top > 0.0f && top < INFINITY ? min(max((int)(__float_as_uint(top) >> 23) - 127, -112), 127) : 14;
     const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
-    if (t < count && (tid & 7) == 0) W.back[W.back_at[pi] + item.y + t] = __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+    if (mine && t < count && (tid & 7) == 0) W.back[W.back_at[pi] + item.y + t] = __uint_as_float((uint32_t)(127 - 14 + e) << 23);
 #pragma unroll
     for (int k = 0; k < kR / 8; ++k) v[k] *= up;
   }
-  if (t >= count) return;
+  if (!mine || t >= count) return;
 #pragma unroll
   for (int i = 0; i < kParts<DT>; ++i)
 #pragma unroll
@@ -913,10 +923,14 @@ cudaError_t run_few(const AdaptLaunch &L, int *status, cudaStream_t s) {
   uint32_t items = 0;
   for (int i = 0; i < L.n; ++i) items += L.p[i].items;
   if (items == 0) return cudaSuccess;
-  // 48 tokens of 24 adapters through three projections: 11.7 us in clusters of 4 (432 CTAs), 18.4 in
-  // clusters of 8; one token 5.8 us in a cluster of 8, 7.2 in one of 4
+  // 48 tokens of 24 adapters through three projections: 11.7 us in clusters of 4 (432 CTAs), 18.4 of 8;
+  // one token 5.8 us in a cluster of 8, 7.2 of 4.  Above rank 32 an SM holds one CTA, but the number of
+  // items is a bound, which is near only where slots have several tokens each (106 tokens of 4 adapters
+  // of rank 64: 18 us in clusters of 4, 26 of 8; 34 tokens of up to 38 adapters, in fact 4: 20 and 14).
+  const wt_adapt_desc &d = L.p[0].d;
+  const int per_sm = MT <= 2 ? 3 : d.T >= 4 * d.S ? 1 : 2;
   int c = kMostCluster;
-  while (c > 2 && (int64_t)items * c > 3 * num_sms()) c /= 2;
+  while (c > 2 && (int64_t)items * c > per_sm * num_sms()) c /= 2;
   return launch(adapt_kernel<DT, MT>, items * (unsigned)c, kThreads, c, few_smem<MT>(most_slots(L)), false, s, L, status);
 }
 
@@ -929,8 +943,11 @@ cudaError_t run_wide(const AdaptLaunch &L, const AdaptWide &W, int *status, cuda
   }
   if (items == 0) return cudaSuccess;
   cudaError_t e = launch(adapt_plan_kernel, (unsigned)W.n_plans, kPlanThreads, 1, sizeof(int) * (most_slots(L) + 1), false, s, L, W, status);
-  if (e == cudaSuccess)
-    e = launch(adapt_shrink_kernel<DT, MT>, items * kSCluster, kSThreads, kSCluster, shrink_smem<MT>(), true, s, L, W, status);
+  if (e == cudaSuccess) {
+    // 8 CTAs to an item while all of them are resident: long rows of few items
+    const int c = (int64_t)items * 8 <= 4 * num_sms() ? 8 : 4;
+    e = launch(adapt_shrink_kernel<DT, MT>, items * (unsigned)c, kSThreads, c, shrink_smem<MT>(), true, s, L, W, status);
+  }
   if (e == cudaSuccess) e = launch(adapt_expand_kernel<DT, MT>, tiles, kEThreads, 1, Expand<DT, MT>::smem, true, s, L, W);
   return e;
 }

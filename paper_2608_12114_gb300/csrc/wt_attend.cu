@@ -117,7 +117,14 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
   const int rows = rq.n * G, row0 = rt * kRows;
   if (row0 >= rows) return;
   const int part = (pre ? P.own_splits : 0) + split;
-  if (k0 >= k1) return;  // the merge knows from the length that there is nothing
+  if (k0 >= k1) {  // the merge knows from the length that there is nothing
+    if (P.direct)
+      for (int r = row0 + (tid >> 5); r < min(rows, row0 + kRows); r += kWarps)
+        if (lane * 4 < D)
+          *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(d.out) + (int64_t)(rq.t0 + r / G) * d.out_stride +
+                                     (hk * G + r % G) * D + lane * 4) = make_uint2(0, 0);
+    return;
+  }
 
   const uint32_t ring = smem_u32(smem) + warp * kStages * kTileBytes;
   if (D % 16) {
@@ -394,9 +401,16 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
           const float4 x = *reinterpret_cast<const float4 *>(so + (w * 16 + r) * kCols + lane * 4);
           v.x += f[w] * x.x, v.y += f[w] * x.y, v.z += f[w] * x.z, v.w += f[w] * x.w;
         }
-        *reinterpret_cast<float4 *>(P.o + at * D + lane * 4) = v;
+        if (P.direct) {
+          const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+          *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(d.out) + (int64_t)(rq.t0 + row / G) * d.out_stride +
+                                     (hk * G + row % G) * D + lane * 4) =
+              make_uint2(pack2<DT>(v.x * inv, v.y * inv), pack2<DT>(v.z * inv, v.w * inv));
+        } else {
+          *reinterpret_cast<float4 *>(P.o + at * D + lane * 4) = v;
+        }
       }
-      if (lane == 0) P.ml[at] = make_float2(mm, ll);
+      if (lane == 0 && !P.direct) P.ml[at] = make_float2(mm, ll);
     }
     __syncthreads();
   }

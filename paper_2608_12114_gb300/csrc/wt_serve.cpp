@@ -114,7 +114,8 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
     i = j;
     if (L.n == 0) continue;
     uint64_t all = 0;
-    const int tile = wt::adapt_tile(max_T);
+    const bool planned = wt::adapt_planned(max_T);
+    const int tile = planned ? 64 : 16;  // tokens of a work item
     for (int k = 0; k < L.n; ++k) {
       wt::AdaptProj &P = L.p[k];
       const wt_adapt_desc &e = P.d;
@@ -123,13 +124,13 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
       all += (uint64_t)P.items * ((e.M + wt::kAdaptMTile - 1) / wt::kAdaptMTile);
       P.vec = 0;
       if (e.K % 8 == 0 && e.ldx % 8 == 0 && e.a_slot % 8 == 0 && aligned(e.x, 16) && aligned(e.A, 16)) P.vec |= 1;
-      // vectors of B: 8 elements; 4 for a launch of few tokens where no rank is above 16
-      const int el = max_T < wt::kAdaptFew && max_R <= 16 ? 4 : 8;
+      // vectors of B: 8 elements; 4 in the one-launch kernel where no rank is above 16
+      const int el = !planned && max_R <= 16 ? 4 : 8;
       if (e.R % el == 0 && e.b_slot % el == 0 && aligned(e.B, 2 * el)) P.vec |= 2;
       if (e.ldy % 4 == 0 && aligned(e.y, 16) && (!e.base || (e.ldbase % 4 == 0 && aligned(e.base, 16)))) P.vec |= 4;
     }
     if (all > (1u << 27)) return serve_error(WT_EINVAL, "wt_adapt: %llu tiles of work in one launch", (unsigned long long)all);
-    if (max_T < wt::kAdaptFew) {
+    if (!planned) {
       CU(wt::launch_adapt(L, nullptr, max_R, ctx.status, s));
       wt::serve_launched(h, 1);
       continue;
@@ -227,11 +228,12 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
 }
 
 // The prefix goes to tcgen05 from 33 rows (token, head-in-group) on, where the warp kernel would read
-// it more than twice.  Its softmax takes the largest product for the largest score, so the scale has to
+// it more than twice, and from 17 where it is long (10 tokens of 4 heads a group behind 10475 keys: 23 us
+// on the warp kernel, under 20; 42 tokens of one behind 50: 13.4 against 18.6).  Its softmax takes the largest product for the largest score, so the scale has to
 // be positive; and a pitch has to fit a tensor map.
 bool prefix_on_tcgen05(const wt_attend_desc &d) {
   const int64_t rows = (int64_t)d.n_tokens * (d.heads / d.kv_heads);
-  return rows > 32 && d.scale > 0.0f && d.q_stride < (1ll << 38) && d.prefix_stride < (1ll << 38) &&
+  return (rows > 32 || (rows > 16 && d.prefix_len >= 2048)) && d.scale > 0.0f && d.q_stride < (1ll << 38) && d.prefix_stride < (1ll << 38) &&
          d.prefix_head < (1ll << 38);
 }
 
@@ -292,20 +294,22 @@ int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
   P.rows_tile = (d.max_len ? own_rows : pre_rows) <= 16 ? 16 : 32;
   P.own_tiles = (int)ceil_div(own_rows, P.rows_tile);
   P.pre_tiles = (int)ceil_div(pre_rows, P.rows_tile);
-  // Splits, of at least 64 keys (one tile for each warp): own keys alone take 4 CTAs per SM (lengths differ,
-  // and CTAs without keys end at once); own keys and prefix in one launch take one each, and up to 4
-  // where splits stay at 512 keys (7 requests with a head for every query behind 1021 keys: 13.6 us,
-  // with 4 throughout 17.1; 24 requests' own keys alone, 4: 30.4, 2: 33.6).
-  const int64_t sms = wt::num_sms(), few = pre_warp ? 1 : 4;
-  auto split = [&](int64_t keys, int64_t ctas, int &splits, int &len) {
-    const int64_t n = std::max(std::min(ceil_div(keys, 64), ceil_div(few * sms, ctas)),
-                               std::min(ceil_div(keys, 512), ceil_div(4 * sms, ctas)));
+  // Splits, of at least 64 keys (one tile for each warp).  Own keys alone take 4 CTAs per SM, as lengths
+  // differ and CTAs without keys end at once (24 requests: 30.4 us, with 2 CTAs 33.6).  Own keys and prefix
+  // in one launch take one CTA per SM each (7 requests with a head for every query behind 1021 keys:
+  // 13.6 us, with 4 17.1), and more where splits stay at 512 keys: 4, or for the prefix what an SM holds.
+  const int64_t sms = wt::num_sms(), few = pre_warp ? 1 : 4, resident = P.rows_tile == 16 ? 3 : 2;
+  auto split = [&](int64_t keys, int64_t ctas, int64_t most, int &splits, int &len) {
+    const int64_t n = std::max(std::min(ceil_div(keys, 64), ceil_div(few * sms, ctas)), std::min(ceil_div(keys, 512), most));
     len = (int)(ceil_div(ceil_div(keys, n), 64) * 64);
     splits = (int)ceil_div(keys, len);
   };
-  if (d.max_len) split(d.max_len, (int64_t)d.n_req * d.kv_heads * P.own_tiles, P.own_splits, P.own_len);
-  if (pre_warp) split(d.prefix_len, (int64_t)d.kv_heads * P.pre_tiles, P.pre_splits, P.pre_len);
+  const int64_t own_ctas = (int64_t)d.n_req * d.kv_heads * P.own_tiles, pre_ctas = (int64_t)d.kv_heads * P.pre_tiles;
+  if (d.max_len) split(d.max_len, own_ctas, ceil_div(4 * sms, own_ctas), P.own_splits, P.own_len);
+  if (pre_warp) split(d.prefix_len, pre_ctas, std::max<int64_t>(1, resident * sms / pre_ctas), P.pre_splits, P.pre_len);
   const int64_t parts = P.own_splits + P.pre_splits, rows = (int64_t)d.n_tokens * d.heads;
+  // a token's only part is its result
+  P.direct = P.own_splits == 1 && !d.prefix_len;
   if ((double)d.kv_heads * ((double)d.n_req * P.own_splits * P.own_tiles + (double)P.pre_splits * P.pre_tiles) > 0x7fffffff)
     return serve_error(WT_EINVAL, "wt_attend: too many tokens, heads and keys for one launch");
   // workspace: O and (m, l) of every part
@@ -316,7 +320,8 @@ int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
   };
   const int64_t xrows = P.x.groups ? (int64_t)(P.x.groups + d.kv_heads - 1) * P.x.qtiles * 128 : 0;
   size_t bytes = 0;
-  const size_t o = take(bytes, (size_t)(parts * rows * d.head_dim) * 4), ml = take(bytes, (size_t)(parts * rows) * sizeof(float2));
+  const size_t o = take(bytes, P.direct ? 0 : (size_t)(parts * rows * d.head_dim) * 4),
+               ml = take(bytes, P.direct ? 0 : (size_t)(parts * rows) * sizeof(float2));
   const size_t xo = take(bytes, (size_t)(xrows * d.head_dim) * 4), xml = take(bytes, (size_t)xrows * sizeof(float2));
   Lock lock(h);
   wt::ServeWorkspace w;
@@ -329,10 +334,10 @@ int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
   if (P.x.groups) e = wt::launch_attend_prefix(P.x, maps, d.dtype, ctx.status, s);
   if (e == cudaSuccess && parts) e = wt::launch_attend_warp(P, s);
-  if (e == cudaSuccess) e = wt::launch_attend_merge(P, s);
+  if (e == cudaSuccess && !P.direct) e = wt::launch_attend_merge(P, s);
   const int rc = wt::serve_workspace_done(h, s, w);
   CU(e);
-  wt::serve_launched(h, (P.x.groups != 0) + (parts != 0) + 1);
+  wt::serve_launched(h, (P.x.groups != 0) + (parts != 0) + !P.direct);
   return rc;
 }
 

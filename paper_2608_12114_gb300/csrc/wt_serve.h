@@ -51,8 +51,10 @@ cudaError_t serve_prepare();  // one-time function attributes of every kernel be
 // ---------------------------------------------------------------- wt_adapt.cu
 constexpr int kAdaptProjs = 8;  // projections of one launch
 constexpr int kAdaptMTile = 64;
-constexpr int kAdaptFew = 256;  // tokens from which a launch's work is planned on the device first
-constexpr int adapt_tile(int max_T) { return max_T < kAdaptFew ? 16 : 64; }  // tokens of a work item
+// Whether a launch's work is planned on the device first: from 256 tokens on, as the one-launch kernel
+// looks at each token in every CTA and reads a slot again for each 16 of its tokens.  (Earlier only
+// where slots have many: 106 tokens of 4 adapters of rank 64, three projections: 28 us planned, 26 not.)
+constexpr bool adapt_planned(int max_T) { return max_T >= 256; }
 // 16-row tiles of the rank that the kernels are built for
 constexpr int adapt_rank_tiles(int max_R) { return max_R <= 16 ? 1 : max_R <= 32 ? 2 : max_R <= 64 ? 4 : 8; }
 struct AdaptProj {
@@ -118,6 +120,7 @@ struct AttendPlan {
   int own_tiles, pre_tiles;  // tiles of the longest request's rows, and of all rows (for the prefix)
   int own_splits, own_len;  // own keys per split
   int pre_splits, pre_len;  // prefix keys per split of the warp kernel (0: not taken there)
+  bool direct;              // one split of own keys and no prefix: the warp kernel writes the result
   PrefixPlan x;             // the prefix on tcgen05 (x.groups 0: not taken there)
   float *o;                 // [own_splits + pre_splits][n_tokens * heads][head_dim]
   float2 *ml;               // [own_splits + pre_splits][n_tokens * heads]
