@@ -58,6 +58,17 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+template <int DT>
+__device__ __forceinline__ void unpack2(uint32_t w, float &lo, float &hi) {
+  if constexpr (DT == WT_BF16) {
+    lo = __uint_as_float(w << 16);
+    hi = __uint_as_float(w & 0xffff0000u);
+  } else {
+    asm("{\n\t.reg .f16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.f32.f16 %0, x;\n\tcvt.f32.f16 %1, y;\n\t}"
+        : "=f"(lo), "=f"(hi)
+        : "r"(w));
+  }
+}
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -329,14 +340,18 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
           for (int z = 0; z < 2; ++z) {
             float &p = s[a][j][2 * e + z];
             p = exp2_approx(p - ref);
-            l[a][e] += p;
           }
       }
+      // l from the rounded weights: what their roundings have in common cancels
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        pf[a][2 * j] = pack2<DT>(s[a][j][0], s[a][j][1]);
-        pf[a][2 * j + 1] = pack2<DT>(s[a][j][2], s[a][j][3]);
-      }
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          pf[a][2 * j + e] = pack2<DT>(s[a][j][2 * e], s[a][j][2 * e + 1]);
+          float lo, hi;
+          unpack2<DT>(pf[a][2 * j + e], lo, hi);
+          l[a][e] += lo + hi;
+        }
     }
 #pragma unroll
     for (int k = 0; k < ND; ++k) {

@@ -20,7 +20,8 @@
 // exponentials.  The reference m of a row moves only when its maximum has grown by more than 8 (in
 // log2): O is then rescaled in tensor memory; until then p stays below 2^8, which both 16-bit types
 // hold as precisely.  P is rounded to the caches' type (the MMA takes both operands in one type);
-// l is summed in fp32 from the unrounded values.
+// l is summed in fp32 from the rounded values, so that what all keys' roundings have in common cancels
+// (equal scores give the mean of the values, whatever the reference).
 //
 // Bound: the products.  768 rows against 32768 keys of 8 heads of 128: 68 us, 1.5 PFLOP/s of the 1.86
 // that a large library product reaches, P crossing in two halves (74 us as one, when the parts also
@@ -151,6 +152,18 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   if constexpr (DT == WT_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+
+template <int DT>
+__device__ __forceinline__ void unpack2(uint32_t w, float &lo, float &hi) {
+  if constexpr (DT == WT_BF16) {
+    lo = __uint_as_float(w << 16);
+    hi = __uint_as_float(w & 0xffff0000u);
+  } else {
+    asm("{\n\t.reg .f16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.f32.f16 %0, x;\n\tcvt.f32.f16 %1, y;\n\t}"
+        : "=f"(lo), "=f"(hi)
+        : "r"(w));
+  }
 }
 
 // A bounded wait of a whole warp: every lane gets the same answer, so a warp whose wait runs out
@@ -449,8 +462,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             fma_x2(v[c], v[c + 1], P.scale_log2, -m);
             v[c] = ex2(v[c]);
             v[c + 1] = ex2(v[c + 1]);
-            add_x2(l0, l1, v[c], v[c + 1]);
             u[k / 2] = pack2<DT>(v[c], v[c + 1]);
+            float r0, r1;
+            unpack2<DT>(u[k / 2], r0, r1);
+            add_x2(l0, l1, r0, r1);
           }
           tmem_st32(S + hf * 32, u);
           wait_st();

@@ -339,3 +339,24 @@ def test_offsets_past_32_bits(torch, h):
     h.attend(s.desc())
     torch.cuda.synchronize()
     s.check(torch, near.want())
+
+
+@pytest.mark.parametrize("dt", ["bfloat16", "float16"])
+@pytest.mark.parametrize("rise", [0.0, 1.3, 5.2])
+def test_roundings_that_weights_share_cancel(torch, h, dt, rise):
+    """Scores of two kinds, so that most weights are one number and share its rounding: it must not show in
+    the result, which then errs to both sides alike (128 columns and more: a mean error of 0.2 u would be
+    four standard deviations of roundings alone)."""
+    for new in ([1, 2], [2] * 20):  # on the warp kernel and on tcgen05
+        s = Set(torch, new, [40] * len(new), 4000, 4, 2, 128, dt=dt, sharp=0.0)
+        s.q[:, :, 0] = 1.0
+        s.scale = 1.0
+        s.pk[:, :, 0] = rise * (torch.arange(4000, device="cuda") // 128 % 2).view(-1, 1).to(s.pk.dtype)
+        s.k[:, :, :, 0] = 0.0
+        for v in (s.pv, s.v):
+            v += torch.linspace(1, 8, 128, device="cuda").to(v.dtype)
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        o, _, _ = s.want()
+        off = (s.out.double().cpu() - o) / o
+        assert off.abs().max() <= 1.1 * s.u and off.mean().abs() <= 0.2 * s.u
