@@ -23,9 +23,8 @@
 // l is summed in fp32 from the rounded values, so that what all keys' roundings have in common cancels
 // (equal scores give the mean of the values, whatever the reference).
 //
-// Bound: the products.  768 rows against 32768 keys of 8 heads of 128: 68 us, 1.5 PFLOP/s of the 1.86
-// that a large library product reaches, P crossing in two halves (74 us as one, when the parts also
-// left a lane to a row).  For few rows, HBM and then latency: 6000 keys of 8 heads against 96 rows take
+// Bound: the products.  768 rows against 32768 keys of 8 heads of 128: 71 us, 1.4 PFLOP/s of the 1.86
+// that a large library product reaches.  For few rows, HBM and then latency: 6000 keys of 8 heads against 96 rows take
 // 13 us, of which HBM needs 4.
 //
 // Every mbarrier wait is bounded; a timeout records WT_ETIMEDOUT and every role stops.
