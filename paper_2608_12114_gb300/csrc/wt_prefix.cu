@@ -390,10 +390,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // 32 lanes of tensor memory per warp
     const uint32_t S = tmem + lanes + i * 128, O = tmem + lanes + 256 + i * 128;
     uint32_t done = 0;  // tiles of this stream over all segments
+    uint32_t seg = 0;
     bool live = true;
-    for (int w = w0; w < w1 && live;) {
+    for (int w = w0; w < w1 && live; ++seg) {
       const Segment g = segment(w);
       w += g.n;
+      // The segment's queries have landed, so every thread has released those before (q_empty).  A stream
+      // without a tile here waits for nothing else: ahead of the other it would release queries that are
+      // still in use, and the producer would announce the next ones in a phase that has its arrival.
+      if (!warp_wait(q_full, seg & 1, abort_flag, status)) break;
       const int n = apart ? (g.n + 1 - i) / 2 : g.n;
       float m = 0.0f, l0 = 0.0f, l1 = 0.0f;
       for (int j = 0; j < n; ++j) {

@@ -313,6 +313,20 @@ def test_batches_behind_short_prefixes(torch, h, P, G, D):
     s.check(torch)
 
 
+@pytest.mark.parametrize("P,H,D,dt", [(100, 160, 8, "bfloat16"), (300, 160, 64, "float16"), (1595, 20, 128, "float16"),
+                                     (1595, 40, 128, "bfloat16"), (600, 75, 72, "bfloat16")])
+def test_ranges_of_few_tiles_over_many_heads(torch, h, P, H, D, dt):
+    """One row tile, and ranges of key tiles that meet several heads with one tile of some of them: the
+    stream of the odd tiles then has none, and must not run ahead of the stream of the even ones."""
+    s = Set(torch, [2] * 20, [12] * 20, P, H, H, D, dt=dt)
+    want = s.want()
+    for _ in range(20):
+        s.out.fill_(_serve.NAN)
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        s.check(torch, want)
+
+
 @pytest.mark.parametrize("scale", [0.3, -0.3, 0.0])
 def test_batches_at_any_scale(torch, h, scale):
     s = Set(torch, [3] * 16, [20] * 16, 300, 8, 2, 64)
