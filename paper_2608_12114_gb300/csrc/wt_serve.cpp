@@ -229,8 +229,9 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
 
 // The prefix goes to tcgen05 from 33 rows (token, head-in-group) on, where the warp kernel would read
 // it more than twice, and from 17 where it is long (10 tokens of 4 heads a group behind 10475 keys: 23 us
-// on the warp kernel, under 20; 42 tokens of one behind 50: 13.4 against 18.6).  Its softmax takes the largest product for the largest score, so the scale has to
-// be positive; and a pitch has to fit a tensor map.
+// on the warp kernel, under 20; 42 tokens of one behind 50: 13.4 against 18.6).  Its softmax takes the
+// largest product for the largest score, so the scale has to be positive; and a pitch has to fit a
+// tensor map.
 bool prefix_on_tcgen05(const wt_attend_desc &d) {
   const int64_t rows = (int64_t)d.n_tokens * (d.heads / d.kv_heads);
   return (rows > 32 || (rows > 16 && d.prefix_len >= 2048)) && d.scale > 0.0f && d.q_stride < (1ll << 38) && d.prefix_stride < (1ll << 38) &&
