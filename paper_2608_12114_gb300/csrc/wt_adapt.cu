@@ -769,13 +769,14 @@ __global__ void __launch_bounds__(kEThreads, MT == 8 ? 1 : 3) adapt_expand_kerne
   const int t0 = warp / kEAcross * 16 + g;
   int64_t tt[2];
   float back[2] = {1.0f, 1.0f};
+  const int r = slot >= d.S ? 0 : min(max(d.rank ? __ldg(d.rank + slot) : d.R, 0), d.R);
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int t = t0 + 8 * e;
     tt[e] = t < count ? plan[W.order_at + item.y + t] : -1;
-    if (DT == WT_F16 && t < count && slot < d.S) back[e] = W.back[W.back_at[pi] + item.y + t];
+    // the shrink kernel leaves v and what it was divided by only where there are ranks
+    if (DT == WT_F16 && t < count && r > 0) back[e] = W.back[W.back_at[pi] + item.y + t];
   }
-  const int r = slot >= d.S ? 0 : min(max(d.rank ? __ldg(d.rank + slot) : d.R, 0), d.R);
   const int ksteps = (r + 15) / 16;
   const bool yvec = (P.vec & 4) != 0, bvec = (P.vec & 2) != 0;
   const int tiles = (M + kMTile - 1) / kMTile, tile0 = group * P.group_tiles, tile1 = min(tiles, tile0 + P.group_tiles);
