@@ -5,7 +5,8 @@
 // sum O of p v, the sum l of p and the reference m the p were taken against, p = 2^(s - m) with
 // s = scale log2(e) q.k.  Parts are joined exactly as softmax splits: O = sum_i 2^(m_i - m) O_i,
 // l = sum_i 2^(m_i - m) l_i, m = max m_i, out = O / l; a part without a key has m = -infinity, and
-// a token without any gets zeros.
+// a token without any gets zeros.  The maximum passes over NaN scores, so a part whose sum is NaN says so
+// in its m: a NaN query or key makes the token NaN on every route.
 //
 // attend_warp_kernel takes a CTA per (rows, kv head, keys of one request): rows are the (token,
 // head) pairs that share a kv head, 16 or 32 of them, and each of 4 warps streams its own tiles of
@@ -425,7 +426,7 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
           *reinterpret_cast<float4 *>(P.o + at * D + lane * 4) = v;
         }
       }
-      if (lane == 0 && !P.direct) P.ml[at] = make_float2(mm, ll);
+      if (lane == 0 && !P.direct) P.ml[at] = make_float2(ll == ll ? mm : ll, ll);
     }
     __syncthreads();
   }
@@ -491,10 +492,12 @@ __global__ void __launch_bounds__(kThreads) attend_merge_kernel(const __grid_con
   const bool cols = lane * 4 < D;
   for (int k0 = 0; k0 < all; k0 += 32) {
     if (k0) mine = k0 + lane < all ? read(k0 + lane) : make_float2(-INFINITY, 0.0f);
-    // a part without a key: its O was not written
-    const float f = mine.x > -INFINITY || mine.x != mine.x ? exp2_approx(mine.x - m) : 0.0f;
-    if (f != 0.0f) l += f * mine.y;
-    const unsigned some = __ballot_sync(0xffffffffu, f != 0.0f);
+    // A part without a key: its O was not written.  One whose factor is 0 still counts: what is not finite in
+    // it has to show.
+    const bool keys = mine.x > -INFINITY || mine.x != mine.x;
+    const float f = keys ? exp2_approx(mine.x - m) : 0.0f;
+    if (keys) l += f * mine.y;
+    const unsigned some = __ballot_sync(0xffffffffu, keys);
     for (int k = k0 + warp; k < min(all, k0 + 32); k += WR * kMergeParts) {
       float4 x[kMergeParts];
       float w[kMergeParts];

@@ -514,7 +514,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the next queries land there
       }
       mbar_arrive(q_empty);
-      if (r < rows) P.ml[tile_at + r] = make_float2(n > 0 ? m : -INFINITY, l0 + l1);
+      const float l = l0 + l1;
+      if (r < rows) P.ml[tile_at + r] = make_float2(n == 0 ? -INFINITY : l == l ? m : l, l);
       done += n;
     }
   }

@@ -46,3 +46,77 @@ def test_slots_of_rank_zero_among_many_tokens(torch, dt, R, rank):
         h.adapt([serving.adapters(x, y, slot, A, B, scale, rank=rk, base=base)])
         torch.cuda.synchronize()
         close(torch, y, _serve.adapt(x, slot, A, B, scale, rk, base), 96, R)
+
+
+ROUTES = {  # new, lens, P, H, Hkv, D
+    "one split": ([1, 3], [30, 9], 0, 8, 2, 64), "own splits": ([1, 2], [700, 40], 0, 8, 2, 64),
+    "prefix by warps": ([1, 2], [37, 20], 500, 8, 2, 128), "prefix alone by warps": ([2], None, 300, 8, 8, 128),
+    "tcgen05, one row tile": ([1] * 12, [20] * 12, 900, 4, 1, 128), "tcgen05": ([4] * 20, [20] * 20, 900, 8, 2, 64),
+    "tcgen05 alone": ([4] * 20, None, 900, 8, 2, 64)}
+
+
+def non_finite_where(torch, s, want):
+    """Rows the 64-bit form leaves NaN are NaN, the others within the usual tolerance."""
+    o = want[0]
+    got = s.out.double().cpu()
+    bad = torch.isnan(o)
+    assert bad.any() and not torch.isfinite(got[bad]).any()
+    if not bad.all():
+        s.check(torch, want)
+
+
+@pytest.mark.parametrize("route", ROUTES)
+@pytest.mark.parametrize("dt", ["bfloat16", "float16"])
+def test_a_query_of_nan(torch, h, route, dt):
+    s = Set(torch, *ROUTES[route], dt=dt)
+    s.q[1, 3] = NAN
+    s.q[0, 0, 0] = NAN
+    h.attend(s.desc())
+    torch.cuda.synchronize()
+    non_finite_where(torch, s, s.want())
+
+
+@pytest.mark.parametrize("route", [r for r in ROUTES if ROUTES[r][2]])
+@pytest.mark.parametrize("keys", [(0, 128), (130, 131), (256, 300)])
+def test_prefix_keys_of_nan(torch, h, route, keys):
+    """A whole part of them, and one beside parts that weigh 2^200 times as much."""
+    s = Set(torch, *ROUTES[route])
+    s.pk[keys[0]:keys[1], 0] = NAN
+    h.attend(s.desc())
+    torch.cuda.synchronize()
+    non_finite_where(torch, s, s.want())
+    s = Set(torch, *ROUTES[route], sharp=0.0)
+    s.q[:, :, 0] = 8.0
+    s.scale = 1.0
+    s.pk[:, :, 0] = 0.0
+    s.pk[200:220, :, 0] = 20.0
+    s.pk[keys[0]:keys[1], 0] = NAN
+    h.attend(s.desc())
+    torch.cuda.synchronize()
+    non_finite_where(torch, s, s.want())
+
+
+@pytest.mark.parametrize("route", [r for r in ROUTES if ROUTES[r][2]])
+@pytest.mark.parametrize("what", [NAN, INF])
+def test_prefix_values_that_are_not_finite(torch, h, route, what):
+    """Beside keys that weigh 2^200 times as much, too."""
+    for heavy in (0.0, 20.0):
+        s = Set(torch, *ROUTES[route], sharp=0.0)
+        s.q[:, :, 0] = 8.0
+        s.scale = 1.0
+        s.pk[:, :, 0] = 0.0
+        s.pk[200:220, :, 0] = heavy
+        s.pv[70, 0, 5] = what
+        clean = s.pv.clone()
+        clean[70, 0, 5] = 0
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        got = s.out.double().cpu()
+        G = s.q.shape[1] // s.pk.shape[1]
+        assert not torch.isfinite(got[:, :G, 5]).any()
+        s.pv = clean
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        keep = torch.ones_like(got, dtype=torch.bool)
+        keep[:, :G, 5] = False
+        assert torch.equal(got[keep], s.out.double().cpu()[keep])
