@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float top = max3(max3(mx0, mx1, mx2), mx3, mx3) * P.scale_log2;
         const bool grown = top > m + kSlack;
         if (j == 0) {
-          m = top > -INFINITY ? top : 0.0f;
+          m = top > -INFINITY ? top : -INFINITY;  // also where all are NaN: their p are NaN against any reference
         } else if (__any_sync(0xffffffffu, grown)) {
           // O of this row, once the product before has been added to it, against the new reference
           if (!warp_wait(o_full + 8 * i, (done + j - 1) & 1, abort_flag, status)) {
@@ -457,13 +457,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_st32(O + c, o);
           }
         }
+        const float ref = m > -INFINITY ? m : 0.0f;  // no score above -infinity yet
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
           uint32_t u[32];
 #pragma unroll
           for (int k = 0; k < 64; k += 2) {
             const int c = hf * 64 + k;
-            fma_x2(v[c], v[c + 1], P.scale_log2, -m);
+            fma_x2(v[c], v[c + 1], P.scale_log2, -ref);
             v[c] = ex2(v[c]);
             v[c + 1] = ex2(v[c + 1]);
             u[k / 2] = pack2<DT>(v[c], v[c + 1]);

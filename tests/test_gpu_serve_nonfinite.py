@@ -120,3 +120,32 @@ def test_prefix_values_that_are_not_finite(torch, h, route, what):
         keep = torch.ones_like(got, dtype=torch.bool)
         keep[:, :G, 5] = False
         assert torch.equal(got[keep], s.out.double().cpu()[keep])
+
+
+@pytest.mark.parametrize("route", ROUTES)
+def test_scores_of_minus_infinity(torch, h, route):
+    """A key whose score is -infinity has no weight; a token with no other key gets zeros; a part that has
+    no other key leaves the others as they are, however small their scores."""
+    new, lens, P, H, Hkv, D = ROUTES[route]
+    for dt in ("bfloat16", "float16"):
+        s = Set(torch, *ROUTES[route], dt=dt, sharp=0.0)
+        s.q[:, :, 0] = 8.0
+        s.scale = 1.0
+        for t in (s.pk, s.k):
+            if t is not None:
+                t[..., 0] = -25.0  # scores of -200
+                t[..., 1:] = 0.0
+        if P:
+            s.pk[:192, :, 0] = -INF
+        if lens:
+            s.k[s.table[0, 0], ::2, :, 0] = -INF
+        want = s.want()
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        s.check(torch, (want[0], want[1], torch.full_like(want[2], 200.0)))
+        for t in (s.pk, s.k):
+            if t is not None:
+                t[..., 0] = -INF
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        assert (s.out[:int(s.begin[-1])] == 0).all()
