@@ -30,7 +30,6 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kKeys = 16;    // keys of a tile
 constexpr int kStages = 2;   // tiles of a warp's ring: three CTAs per SM at head_dim 128
 constexpr int kStatusInvalid = -1;
-constexpr float kSlack = 8.0f;
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
@@ -315,13 +314,14 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
         mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
         mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
       }
-      // The reference moves when a row's maximum passes it by more than 2^8; p then stays within what
+      // The reference moves when a row's maximum has grown by more than 2^8; p then stays within what
       // both 16-bit types hold as precisely.  It starts at -infinity, so the first key seen sets it.
-      const bool grown0 = mx[0] > m[a][0] + kSlack, grown1 = mx[1] > m[a][1] + kSlack;
+      constexpr float kGrow = kSlack + kBelow<DT>;
+      const bool grown0 = mx[0] > m[a][0] + kGrow, grown1 = mx[1] > m[a][1] + kGrow;
       if (__any_sync(0xffffffffu, grown0 || grown1)) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float to = (e ? grown1 : grown0) ? mx[e] : m[a][e];
+          const float to = (e ? grown1 : grown0) ? mx[e] - kBelow<DT> : m[a][e];
           const float f = to > -INFINITY ? exp2_approx(m[a][e] - to) : 1.0f;
           m[a][e] = to;
           l[a][e] *= f;

@@ -17,9 +17,9 @@
 //
 // The two streams are two row tiles against the same keys, or, where there is one row tile only, the
 // even and the odd key tiles of the range, so that one stream's products run beside the other's
-// exponentials.  The reference m of a row moves only when its maximum has grown by more than 8 (in
-// log2): O is then rescaled in tensor memory; until then p stays below 2^8, which both 16-bit types
-// hold as precisely.  P is rounded to the caches' type (the MMA takes both operands in one type);
+// exponentials.  The reference m of a row (set below its maximum for f16: kBelow) moves only when the
+// maximum has grown by more than 8 (in log2): O is then rescaled in tensor memory; until then p stays
+// where both 16-bit types hold it as precisely.  P is rounded to the caches' type (the MMA takes both operands in one type);
 // l is summed in fp32 from the rounded values, so that what all keys' roundings have in common cancels
 // (equal scores give the mean of the values, whatever the reference).
 //
@@ -46,7 +46,6 @@ constexpr int kRegsSoftmax = 224, kRegsRest = 56;
 static_assert(2 * kRegsSoftmax + kRegsRest <= 3 * 168, "what the launch has");
 constexpr uint32_t kHalf = 128 * 128;  // 128 rows of 64 elements
 constexpr uint32_t kTmemCols = 512;    // S_0, S_1 (128 columns each), O_0, O_1
-constexpr float kSlack = 8.0f;
 
 template <int DH>  // 64-element halves of head_dim
 struct Geo {
@@ -433,9 +432,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         mx0 = max3(mx0, v[124], v[125]);
         mx1 = max3(mx1, v[126], v[127]);
         const float top = max3(max3(mx0, mx1, mx2), mx3, mx3) * P.scale_log2;
-        const bool grown = top > m + kSlack;
+        const bool grown = top > m + (kSlack + kBelow<DT>);
         if (j == 0) {
-          m = top > -INFINITY ? top : -INFINITY;  // also where all are NaN: their p are NaN against any reference
+          m = top > -INFINITY ? top - kBelow<DT> : -INFINITY;  // also where all are NaN: their p are NaN against any reference
         } else if (__any_sync(0xffffffffu, grown)) {
           // O of this row, once the product before has been added to it, against the new reference
           if (!warp_wait(o_full + 8 * i, (done + j - 1) & 1, abort_flag, status)) {
@@ -443,8 +442,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
           fence_after();
-          const float f = grown ? ex2(m - top) : 1.0f;
-          if (grown) m = top;
+          const float f = grown ? ex2(m - (top - kBelow<DT>)) : 1.0f;
+          if (grown) m = top - kBelow<DT>;
           l0 *= f;
           l1 *= f;
 #pragma unroll 1

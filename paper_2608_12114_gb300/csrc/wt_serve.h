@@ -86,7 +86,16 @@ cudaError_t draw_prepare();
 cudaError_t launch_probs(const wt_probs_desc &d, int *status, cudaStream_t s);
 cudaError_t launch_verify(const wt_verify_desc &d, int *status, cudaStream_t s);
 
-// ---------------------------------------------------------------- wt_attend.cu
+// ---------------------------------------------------------------- wt_attend.cu, wt_prefix.cu
+// Weights p = 2^(s - m) are rounded to the caches' type.  The reference m lies kBelow under the largest
+// score (in log2) that set it, and follows a larger one when that is kSlack above it: p reaches 2^15 for
+// f16 and 2^8 for bf16.  f16 rounds p below 2^-14 to multiples of 2^-24.  Without the seven bits of
+// kBelow, 65535 keys of weight 2^-26 in one part gave 0 in place of 2^-10; with them even 2^20 keys that
+// are lost weigh less together than the result's own rounding.
+constexpr float kSlack = 8.0f;
+template <int DT>
+constexpr float kBelow = DT == WT_F16 ? 7.0f : 0.0f;
+
 // Partial results of one (token, head): O [head_dim] fp32 not yet divided by l, and (m, l) with m in
 // units of log2 (scores times scale log2 e).
 //

@@ -149,3 +149,24 @@ def test_scores_of_minus_infinity(torch, h, route):
         h.attend(s.desc())
         torch.cuda.synchronize()
         assert (s.out[:int(s.begin[-1])] == 0).all()
+
+
+@pytest.mark.parametrize("dt", ["bfloat16", "float16"])
+@pytest.mark.parametrize("new", [[1], [1] * 12, [500] * 8])  # parts of few keys and, behind many rows, of many
+def test_many_small_weights(torch, h, new, dt):
+    """65,535 keys of weight 2^-26 beside one of weight 1 add up to 2^-10.  An f16 weight is rounded to a
+    multiple of 2^-24 of its reference, which lies 2^7 below the largest: 2^-32 a key."""
+    P = 65536
+    s = Set(torch, new, None, P, 8, 1, 64, dt=dt, sharp=0.0)
+    s.q[:, :, 0] = 1.0
+    s.scale = 1.0
+    s.pk.zero_(), s.pv.fill_(1.0)
+    s.pk[1:, :, 0] = -18.0
+    s.pv[0] = 0.0
+    h.attend(s.desc())
+    torch.cuda.synchronize()
+    crowd = (P - 1) * 2.718281828459045 ** -18
+    want = crowd / (1 + crowd)
+    got = s.out.double().cpu()
+    tol = (0 if dt == "bfloat16" else P * 2.0 ** -32) + (2 * s.u + 2.0 ** -15) * want
+    assert (got - want).abs().max() <= tol, (float(got.min()), float(got.max()), want)
