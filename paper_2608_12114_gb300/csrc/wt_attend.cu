@@ -69,6 +69,17 @@ __device__ __forceinline__ void unpack2(uint32_t w, float &lo, float &hi) {
         : "r"(w));
   }
 }
+// Whether one of a word's two numbers is NaN or infinite.
+template <int DT>
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+  constexpr uint32_t kExp = DT == WT_BF16 ? 0x7f80u : 0x7c00u;
+  return (w & kExp) == kExp || (w >> 16 & kExp) == kExp;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t r;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r) : "r"(a));
+  return r;
+}
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -90,9 +101,10 @@ __device__ __forceinline__ Request request_of(const wt_attend_desc &d, int b, in
   return {t0, t1 - t0, len};
 }
 
-// ND: 16-element groups of head_dim (rounded up).  MT: tiles of 16 rows.
+// ND: 16-element groups of head_dim (rounded up).  MT: tiles of 16 rows.  Short heads keep four CTAs to an
+// SM (their rows beside later tokens' keys would take 160 registers, and three).
 template <int DT, int ND, int MT>
-__global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_constant__ AttendPlan P) {
+__global__ void __launch_bounds__(kThreads, ND == 4 && MT == 1 ? 4 : 0) attend_warp_kernel(const __grid_constant__ AttendPlan P) {
   constexpr int kPitch = ND * 32 + 16;              // bytes of a staged row: 8 rows hit 8 different bank groups
   constexpr int kTileBytes = 2 * kKeys * kPitch;    // K rows, then V rows
   constexpr int kRows = 16 * MT;
@@ -294,6 +306,8 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
     }
     // every row sees every key of the tile, but at the end of a request
     const bool whole = found == 0xffffu && key0 + kKeys <= sees_all;
+    // some row does not see a key that is there: a later token's
+    const bool hides = key0 + kKeys > sees_all && sees_all < k1;
     uint32_t pf[MT][4];
 #pragma unroll
     for (int a = 0; a < MT; ++a) {
@@ -353,6 +367,39 @@ __global__ void __launch_bounds__(kThreads) attend_warp_kernel(const __grid_cons
           unpack2<DT>(pf[a][2 * j + e], lo, hi);
           l[a][e] += lo + hi;
         }
+    }
+    // A weight of 0 does not hide a value that is not finite (0 * infinity), so where a tile has such a
+    // value and not all rows see all its keys, each row adds those that it sees one by one.
+    bool odd = false;
+    if (hides)
+      for (int i = lane; i < kKeys * chunks; i += 32) {
+        const uint4 w = lds128(vt + i / chunks * kPitch + i % chunks * 16);
+        odd |= not_finite<DT>(w.x) || not_finite<DT>(w.y) || not_finite<DT>(w.z) || not_finite<DT>(w.w);
+      }
+    if (__any_sync(0xffffffffu, odd)) {
+#pragma unroll 1
+      for (int r = 0; r < kKeys; ++r) {
+        if (!(found >> r & 1)) continue;
+#pragma unroll
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t w = __shfl_sync(0xffffffffu, r < 8 ? pf[a][e] : pf[a][2 + e], (lane & 28) | (r & 7) >> 1);
+            float p0, p1;
+            unpack2<DT>(w, p0, p1);
+            const float p = r & 1 ? p1 : p0;
+            if (key0 + r < sees[a][e])
+#pragma unroll
+              for (int j = 0; j < 2 * ND; ++j) {
+                float v0, v1;
+                unpack2<DT>(lds32(vt + r * kPitch + j * 16 + q * 4), v0, v1);
+                o[a][j][2 * e] += p * v0;
+                o[a][j][2 * e + 1] += p * v1;
+              }
+          }
+      }
+      __syncwarp();
+      return;
     }
 #pragma unroll
     for (int k = 0; k < ND; ++k) {

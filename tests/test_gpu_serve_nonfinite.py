@@ -170,3 +170,35 @@ def test_many_small_weights(torch, h, new, dt):
     got = s.out.double().cpu()
     tol = (0 if dt == "bfloat16" else P * 2.0 ** -32) + (2 * s.u + 2.0 ** -15) * want
     assert (got - want).abs().max() <= tol, (float(got.min()), float(got.max()), want)
+
+
+@pytest.mark.parametrize("what", [NAN, INF, -INF])
+@pytest.mark.parametrize("case", [([6], [50], 40, 4, 2, 64), ([6, 1, 9], [50, 9, 33], 0, 8, 2, 128), ([40], [61], 0, 3, 1, 72),
+                                  ([3] * 20, [18] * 20, 300, 4, 1, 128)])
+@pytest.mark.parametrize("dt", ["bfloat16", "float16"])
+def test_later_drafts_that_are_not_finite(torch, h, case, what, dt):
+    """What a token may not see does not reach it, in keys and in values."""
+    s = Set(torch, *case, dt=dt)
+    new, lens = case[0], case[1]
+    for b in (0, len(new) - 1):
+        j = lens[b] - 1 - new[b] // 2  # one of the new tokens' keys
+        at = s.table[b, j // 16]
+        s.v[at, j % 16] = what
+        want = s.want()
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        seen = torch.zeros(len(s.q), dtype=torch.bool)
+        for c in (0, len(new) - 1)[:1 if b == 0 else 2]:
+            t1 = sum(new[:c + 1])
+            seen[t1 - new[c] // 2 - 1:t1] = True
+        assert not torch.isfinite(s.out.double().cpu()[seen]).any()
+        fine = (torch.where(seen.view(-1, 1, 1), torch.full_like(want[0], NAN), want[0]), want[1], want[2])
+        s.check(torch, fine)
+    j = lens[0] - 1
+    s = Set(torch, *case, dt=dt)
+    s.k[s.table[0, j // 16], j % 16] = what
+    want = s.want()
+    want[0][new[0] - 1] = NAN
+    h.attend(s.desc())
+    torch.cuda.synchronize()
+    s.check(torch, want)
