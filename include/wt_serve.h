@@ -84,8 +84,9 @@ int wt_adapt(wt_handle *h, const wt_adapt_desc *d, size_t n, void *stream);
  * a key has no weight.  A NaN in its query or in a key that it sees makes a token's head NaN, and a
  * value that is not finite makes its column so, however small its weight.  Own keys live in pages: key
  * j of request b is row j % page of page table[b, j / page].  Rows of a page past len[b] are never
- * used, and a later token's key and value never reach an earlier one (NaN and infinity are harmless there).  q, caches and out are bf16 or f16; scores, softmax
- * statistics and sums are fp32, and the weights p enter the second product rounded to the caches' type.
+ * used, and a later token's key and value never reach an earlier one (NaN and infinity there are
+ * harmless).  q, caches and out are bf16 or f16; scores, softmax statistics and sums are fp32, and the
+ * weights p enter the second product rounded to the caches' type.
  *
  * head_dim is a multiple of 8 up to 128; heads a multiple of kv_heads, heads / kv_heads <= 128.
  * Pointers lie on 16-byte boundaries and strides are multiples of 8 elements.  prefix_len 0 or

@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const 
 //
 // v crosses between the two as 16-bit parts that add up to it, so that the second product's operands
 // need no conversion: bf16 in three parts (24 bits); f16 in two (22 bits), after a power of two for
-// each token has brought its largest v to 2^14, far from f16's ends; the power is taken back in fp32.
+// each token has brought its largest finite v to 2^14, far from f16's ends; the power is taken back in fp32.
 // Bound: HBM (base and y).
 constexpr int kItem = 64;     // tokens of an item
 constexpr int kMTile = kAdaptMTile;   // outputs of a tile of the expand kernel
@@ -695,7 +695,7 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
 #pragma unroll
   for (int k = 0; k < kR / 8; ++k) {
     v[k] = k0 + k < r ? v[k] * scale : 0.0f;
-    top = fmaxf(top, fabsf(v[k]));
+    if (fabsf(v[k]) < INFINITY) top = fmaxf(top, fabsf(v[k]));
   }
   cl.sync();
   uint16_t *out = W.v + W.v_at[pi] + (int64_t)(item.y + t) * kR + k0;
@@ -703,8 +703,9 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
   if constexpr (DT == WT_F16) {
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    // 2^(14 - exponent of top), within what fp32 can take back; 1 for zeros, infinities and NaN
-    const int e = top > 0.0f && top < INFINITY ? min(max((int)(__float_as_uint(top) >> 23) - 127, -112), 127) : 14;
+    // 2^(14 - exponent of the largest finite one), within what fp32 can take back; 1 where all are zeros,
+    // infinities or NaN
+    const int e = top > 0.0f ? min(max((int)(__float_as_uint(top) >> 23) - 127, -112), 127) : 14;
     const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
     if (mine && t < count && (tid & 7) == 0) W.back[W.back_at[pi] + item.y + t] = __uint_as_float((uint32_t)(127 - 14 + e) << 23);
 #pragma unroll

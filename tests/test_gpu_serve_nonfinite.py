@@ -202,3 +202,18 @@ def test_later_drafts_that_are_not_finite(torch, h, case, what, dt):
     h.attend(s.desc())
     torch.cuda.synchronize()
     s.check(torch, want)
+
+
+@pytest.mark.parametrize("T", [3, 280])
+@pytest.mark.parametrize("dt", ["bfloat16", "float16"])
+def test_an_infinite_update_beside_a_large_one(torch, h, T, dt):
+    x, y, slot, A, B, scale, base = make(torch, T, 64, 32, 1, 2, getattr(torch, dt))
+    slot.zero_(), scale.fill_(1.0)
+    A.zero_(), B.zero_(), x.zero_()
+    A[0, 0, 0], A[0, 1, 1] = INF, 2.0
+    x[:, 0], x[:, 1] = 1.0, 60000.0
+    x[1, 0] = -1.0
+    B[0, :, 0], B[0, :, 1] = 1.0, -1.0
+    h.adapt([serving.adapters(x, y, slot, A, B, scale, base=base)])
+    torch.cuda.synchronize()
+    assert (y[0] == INF).all() and (y[1] == -INF).all()
