@@ -28,10 +28,25 @@ struct Lock {
 
 bool aligned(const void *p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+// Bytes of memory, which stay at the largest number where a product or a sum would pass 64 bits (rows of
+// 2^31 at a pitch of 2^40 do): such a range runs past the end of any allocation.
+struct Bytes {
+  uint64_t n;
+  Bytes(uint64_t v) : n(v) {}
+  Bytes operator*(Bytes o) const {
+    uint64_t r;
+    return __builtin_mul_overflow(n, o.n, &r) ? UINT64_MAX : r;
+  }
+  Bytes operator+(Bytes o) const {
+    uint64_t r;
+    return __builtin_add_overflow(n, o.n, &r) ? UINT64_MAX : r;
+  }
+};
+
 // Bytes from the first to one past the last element of `rows` rows of `row` elements, `pitch`
-// elements apart.  Sizes are below 2^31 and pitches below 2^40, so nothing overflows.
+// elements apart.
 uint64_t extent(uint64_t rows, uint64_t pitch, uint64_t row, uint64_t elem) {
-  return rows == 0 || row == 0 ? 0 : ((rows - 1) * pitch + row) * elem;
+  return rows == 0 || row == 0 ? 0 : ((Bytes(rows - 1) * pitch + row) * elem).n;
 }
 constexpr int64_t kMaxPitch = 1ll << 40;
 
@@ -210,7 +225,7 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
       return serve_error(WT_EINVAL, "%s: prefix pitches %lld and %lld are not multiples of 8 of at least head_dim", call,
                          (long long)d.prefix_stride, (long long)d.prefix_head);
     // dense either way round: [key, head, dim] or [head, key, dim]
-    const uint64_t n = 2 * ((uint64_t)(d.prefix_len - 1) * d.prefix_stride + (uint64_t)(d.kv_heads - 1) * d.prefix_head + D);
+    const uint64_t n = (Bytes(2) * (Bytes(d.prefix_len - 1) * d.prefix_stride + Bytes(d.kv_heads - 1) * d.prefix_head + D)).n;
     CHECK(check_buffer(&seen, call, "prefix_k", d.prefix_k, n, 16));
     CHECK(check_buffer(&seen, call, "prefix_v", d.prefix_v, n, 16));
   }
@@ -218,7 +233,7 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
     if (d.page < 1 || d.table_stride < 0 || d.table_stride > 0x7fffffff || (int64_t)d.max_len > d.table_stride * d.page)
       return serve_error(WT_EINVAL, "%s: max_len %d does not fit %lld pages of %d keys", call, d.max_len,
                          (long long)d.table_stride, d.page);
-    const uint64_t n = (uint64_t)d.n_pages * d.page * d.kv_heads * D * 2;
+    const uint64_t n = (Bytes(d.n_pages) * d.page * d.kv_heads * D * 2).n;
     CHECK(check_buffer(&seen, call, "k_pages", d.k_pages, n, 16));
     CHECK(check_buffer(&seen, call, "v_pages", d.v_pages, n, 16));
     CHECK(check_buffer(&seen, call, "table", d.table, extent(d.n_req, d.table_stride, d.table_stride, 4), 4));
