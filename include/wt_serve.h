@@ -50,8 +50,8 @@ extern "C" {
  * overlap.  base NULL stands for zeros.
  *
  * All descriptors of a call share one launch per 8 of them (three launches from 256 tokens on); no y of
- * a call may overlap another descriptor's operands.  Any K, M >= 0, 0 <= R <= 128, any T
- * and any element alignment; rows that lie on 16-byte boundaries load faster. */
+ * a call may overlap another descriptor's operands.  T, K and M up to 2^30,
+ * R up to 128, any element alignment; rows that lie on 16-byte boundaries load faster. */
 #define WT_ADAPT_MAX_RANK 128
 #define WT_ADAPT_MAX_SLOTS 4096
 typedef struct {
@@ -88,7 +88,8 @@ int wt_adapt(wt_handle *h, const wt_adapt_desc *d, size_t n, void *stream);
  * harmless).  q, caches and out are bf16 or f16; scores, softmax statistics and sums are fp32, and the
  * weights p enter the second product rounded to the caches' type.
  *
- * head_dim is a multiple of 8 up to 128; heads a multiple of kv_heads, heads / kv_heads <= 128.
+ * head_dim is a multiple of 8 up to 128; heads a multiple of kv_heads, heads / kv_heads <= 128; n_req
+ * is below 65536, n_tokens, prefix_len and max_len go up to 2^30, n_tokens * heads to 2^31 - 1.
  * Pointers lie on 16-byte boundaries and strides are multiples of 8 elements.  prefix_len 0 or
  * max_len 0 leave that part out (its pointers may be NULL). */
 typedef struct {
@@ -150,7 +151,7 @@ int wt_probs(wt_handle *h, const wt_probs_desc *d, void *stream);
  * token drawn is the first whose running sum exceeds floor(floor(u_draw 2^24) S / 2^24).  Where
  * S = 0 at a refused position (p <= q everywhere: equal up to rounding) the token is drawn from p;
  * where that has S = 0 too, it is -1.  A drafted token outside 0 .. vocab - 1 is refused.  u and
- * u_draw lie in [0, 1). */
+ * u_draw lie in [0, 1).  n_drafted goes up to 2^30, n_req to 2^24, max_draft to 2^20. */
 #define WT_VERIFY_MAX_VOCAB (1 << 18)
 typedef struct {
   const float *p;          /* [n_drafted + n_req, vocab], row pitch ldp */

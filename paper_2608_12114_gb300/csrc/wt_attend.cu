@@ -95,7 +95,7 @@ __device__ __forceinline__ Request request_of(const wt_attend_desc &d, int b, in
   if (t0 < 0 || t1 < t0 || t1 > d.n_tokens || t1 - t0 > d.max_new || len < 0 || len > d.max_len) {
     if (tell && status) atomicCAS(status, 0, kStatusInvalid);
     t0 = min(max(t0, 0), d.n_tokens);
-    t1 = min(max(t1, t0), min(d.n_tokens, t0 + d.max_new));
+    t1 = min(max(t1, t0), t0 + min(d.max_new, d.n_tokens - t0));
     len = min(max(len, 0), d.max_len);
   }
   return {t0, t1 - t0, len};

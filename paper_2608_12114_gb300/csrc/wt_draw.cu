@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kVThreads, 2) verify_kernel(const wt_verify_de
   if (n0 < 0 || n1 < n0 || n1 > d.n_drafted || n1 - n0 > d.max_draft) {
     if (tid == 0) note_invalid(status);
     n0 = min(max(n0, 0), d.n_drafted);
-    n1 = min(max(n1, n0), min(d.n_drafted, n0 + d.max_draft));
+    n1 = min(max(n1, n0), n0 + min(d.max_draft, d.n_drafted - n0));
   }
   const int n = n1 - n0;
   // Every warp finds the first refused draft for itself: lane i looks at draft i.

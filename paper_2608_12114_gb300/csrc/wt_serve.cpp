@@ -49,6 +49,8 @@ uint64_t extent(uint64_t rows, uint64_t pitch, uint64_t row, uint64_t elem) {
   return rows == 0 || row == 0 ? 0 : ((Bytes(rows - 1) * pitch + row) * elem).n;
 }
 constexpr int64_t kMaxPitch = 1ll << 40;
+// Tokens and lengths of rows: what a kernel adds to one (a stride over threads, a tile) stays below 2^31.
+constexpr int32_t kMaxSize = 1 << 30;
 
 int check_buffer(wt::ServeRanges *seen, const char *call, const char *name, const void *p, uint64_t n, uintptr_t align) {
   if (n == 0) return WT_OK;
@@ -81,8 +83,10 @@ int check_adapt(wt_handle *h, wt::ServeRanges &seen, const wt_adapt_desc &d, siz
   if (d.dtype != WT_BF16 && d.dtype != WT_F16)
     return serve_error(d.dtype >= WT_F32 && d.dtype <= WT_U8 ? WT_ENOTSUP : WT_EINVAL,
                        "%s: desc %zu: dtype %d: x, A and B are bf16 or f16", call, i, d.dtype);
-  if (d.T < 0 || d.K < 0 || d.M < 0 || d.S < 0 || d.R < 0 || d.S > WT_ADAPT_MAX_SLOTS || d.R > WT_ADAPT_MAX_RANK)
-    return serve_error(WT_EINVAL, "%s: desc %zu: T %d, K %d, M %d, S %d (up to %d) or R %d (up to %d) out of range", call, i,
+  if (d.T < 0 || d.K < 0 || d.M < 0 || d.S < 0 || d.R < 0 || d.T > kMaxSize || d.K > kMaxSize || d.M > kMaxSize ||
+      d.S > WT_ADAPT_MAX_SLOTS || d.R > WT_ADAPT_MAX_RANK)
+    return serve_error(WT_EINVAL,
+                       "%s: desc %zu: T %d, K %d, M %d (up to 2^30), S %d (up to %d) or R %d (up to %d) out of range", call, i,
                        d.T, d.K, d.M, d.S, WT_ADAPT_MAX_SLOTS, d.R, WT_ADAPT_MAX_RANK);
   const uint64_t T = d.T, K = d.K, M = d.M, S = d.S, R = d.R;
   if (d.ldx < d.K || d.ldy < d.M || (d.base && d.ldbase < d.M) || d.a_slot < (int64_t)(R * K) || d.b_slot < (int64_t)(M * R) ||
@@ -199,7 +203,7 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
   if (d.dtype != WT_BF16 && d.dtype != WT_F16)
     return serve_error(d.dtype >= WT_F32 && d.dtype <= WT_U8 ? WT_ENOTSUP : WT_EINVAL,
                        "%s: dtype %d: queries and caches are bf16 or f16", call, d.dtype);
-  if (d.n_req < 0 || d.n_req > 65535 || d.n_tokens < 0 || d.max_new < 0 || d.prefix_len < 0 || d.prefix_len > (1 << 30) ||
+  if (d.n_req < 0 || d.n_req > 65535 || d.n_tokens < 0 || d.n_tokens > kMaxSize || d.max_new < 0 || d.prefix_len < 0 || d.prefix_len > (1 << 30) ||
       d.max_len < 0 || d.max_len > (1 << 30) || d.n_pages < 0)
     return serve_error(WT_EINVAL, "%s: n_req %d, n_tokens %d, max_new %d, prefix_len %lld, max_len %d or n_pages %d out of range",
                        call, d.n_req, d.n_tokens, d.max_new, (long long)d.prefix_len, d.max_len, d.n_pages);
@@ -384,7 +388,7 @@ int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {
   wt::ServeContext ctx;
   CHECK(wt::serve_context(h, call, &ctx));
   if (!d) return serve_error(WT_EINVAL, "%s: NULL descriptor", call);
-  if (d->n_req < 0 || d->n_req > (1 << 24) || d->n_drafted < 0 || d->max_draft < 0 || d->max_draft > (1 << 20) || d->vocab < 1 ||
+  if (d->n_req < 0 || d->n_req > (1 << 24) || d->n_drafted < 0 || d->n_drafted > kMaxSize || d->max_draft < 0 || d->max_draft > (1 << 20) || d->vocab < 1 ||
       d->vocab > WT_VERIFY_MAX_VOCAB || d->ldp < d->vocab || d->ldp > kMaxPitch ||
       (d->q && (d->ldq < d->vocab || d->ldq > kMaxPitch)))
     return serve_error(WT_EINVAL, "%s: n_req %d, n_drafted %d, max_draft %d, vocab %d (up to %d) or a pitch out of range", call,

@@ -58,3 +58,20 @@ def test_sizes_whose_bytes_pass_64_bits(torch, h):
     d = s.desc()
     d.n_tokens, d.q_stride, d.heads, d.kv_heads = (1 << 23) + 1, 1 << 40, 2, 2
     refused(h.attend, d, "q runs past")
+
+
+def test_sizes_near_32_bits(torch, h):
+    x, y, slot, A, B, scale, base = make(torch, 4, 64, 32, 2, 8, torch.bfloat16)
+    for name in ("T", "K", "M"):
+        d = serving.adapters(x, y, slot, A, B, scale, base=base)
+        d.ldx = d.ldy = d.ldbase = d.a_slot = d.b_slot = 1 << 39
+        setattr(d, name, (1 << 30) + 1)
+        refused(lambda e: h.adapt([e]), d, "out of range")
+    d = Set(torch, [2, 1], [40, 33], 100, 1, 1, 64).desc()
+    d.n_tokens = (1 << 30) + 1
+    refused(h.attend, d, "out of range")
+    a = drafts(torch, [2, 1], 64, 1.0, False)
+    acc, tok = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(2, 3, dtype=torch.int32, device="cuda")
+    d = serving.verification(a[0], a[2], a[3], a[4], a[5], acc, tok, q=a[1])
+    d.n_drafted = (1 << 30) + 1
+    refused(h.verify, d, "out of range")
