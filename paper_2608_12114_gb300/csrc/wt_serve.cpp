@@ -102,11 +102,12 @@ int check_adapt(wt_handle *h, wt::ServeRanges &seen, const wt_adapt_desc &d, siz
     return serve_error(WT_EINVAL, "%s: desc %zu: base overlaps y", call, i);
   }
   CHECK(check_buffer(&seen, call, "slot", d.slot, 4 * T, 4));
-  if (S == 0 || R == 0) return WT_OK;
+  if (S == 0) return WT_OK;
+  if (d.rank) CHECK(check_buffer(&seen, call, "rank", d.rank, 4 * S, 4));  // read where R is 0, too
+  if (R == 0) return WT_OK;
   CHECK(check_buffer(&seen, call, "x", d.x, extent(T, d.ldx, K, 2), 2));
   CHECK(check_buffer(&seen, call, "A", d.A, extent(S, d.a_slot, R * K, 2), 2));
   CHECK(check_buffer(&seen, call, "B", d.B, extent(S, d.b_slot, M * R, 2), 2));
-  if (d.rank) CHECK(check_buffer(&seen, call, "rank", d.rank, 4 * S, 4));
   if (d.scale) CHECK(check_buffer(&seen, call, "scale", d.scale, 4 * S, 4));
   return WT_OK;
 }

@@ -75,3 +75,12 @@ def test_sizes_near_32_bits(torch, h):
     d = serving.verification(a[0], a[2], a[3], a[4], a[5], acc, tok, q=a[1])
     d.n_drafted = (1 << 30) + 1
     refused(h.verify, d, "out of range")
+
+
+def test_ranks_of_slots_without_rows(torch, h):
+    """R = 0 still reads rank."""
+    x, y, slot, A, B, scale, base = make(torch, 4, 64, 32, 2, 0, torch.bfloat16)
+    rank = torch.zeros(2, dtype=torch.int32, device="cuda")
+    d = serving.adapters(x, y, slot, A, B, scale, rank=rank, base=base)
+    d.rank += 2
+    refused(lambda e: h.adapt([e]), d, "rank")
