@@ -46,12 +46,13 @@ extern "C" {
  * f16, as are A and B; base and y are fp32, as wt_pass leaves them.  A x is summed in fp32 and
  * enters the second product with 22 bits or more (of the token's largest number), which is summed in
  * fp32.
- * base may be y itself (then tokens without adapter cost nothing); otherwise the two must not
- * overlap.  base NULL stands for zeros.
+ * base may be y itself (then tokens without adapter cost nothing).  base NULL stands for zeros.
  *
- * All descriptors of a call share one launch per 8 of them (three launches from 256 tokens on); no y of
- * a call may overlap another descriptor's operands.  T, K and M up to 2^30,
- * R up to 128, any element alignment; rows that lie on 16-byte boundaries load faster. */
+ * All descriptors of a call share one launch per 8 of them (three launches from 256 tokens on).
+ * No y may overlap what its own or another descriptor reads, or another's y; a call refuses that where
+ * the two share a launch.  (Rows count, not the bytes between them: columns of one buffer are fine.)
+ * T, K and M go up to 2^30, R up to 128, at any element alignment; rows that lie on 16-byte boundaries
+ * load faster. */
 #define WT_ADAPT_MAX_RANK 128
 #define WT_ADAPT_MAX_SLOTS 4096
 typedef struct {
@@ -91,7 +92,8 @@ int wt_adapt(wt_handle *h, const wt_adapt_desc *d, size_t n, void *stream);
  * head_dim is a multiple of 8 up to 128; heads a multiple of kv_heads, heads / kv_heads <= 128; n_req
  * is below 65536, n_tokens, prefix_len and max_len go up to 2^30, n_tokens * heads to 2^31 - 1.
  * Pointers lie on 16-byte boundaries and strides are multiples of 8 elements.  prefix_len 0 or
- * max_len 0 leave that part out (its pointers may be NULL). */
+ * max_len 0 leave that part out (its pointers may be NULL).  out may be q itself (at its pitch);
+ * otherwise it must not overlap any input, as rows of tokens. */
 typedef struct {
   const void *q;            /* [n_tokens, heads, head_dim], token pitch q_stride elements */
   void *out;                /* [n_tokens, heads, head_dim], token pitch out_stride */
@@ -122,7 +124,7 @@ int wt_attend(wt_handle *h, const wt_attend_desc *d, void *stream);
  * temp[r] that is not above zero draws greedily: p is 1 at the first of the row's largest logits and
  * 0 elsewhere.  A logit of -infinity has probability 0; a row of nothing else is all zeros.  NaN or
  * +infinity in a row with temp > 0 makes the row NaN; a greedy row ignores NaN.  p may be the logits
- * themselves (ldp == ldl), otherwise the two must not overlap. */
+ * themselves (ldp == ldl), otherwise p must not overlap logits or temp (as rows). */
 typedef struct {
   const float *logits;  /* [rows, vocab], row pitch ldl */
   float *p;             /* [rows, vocab], row pitch ldp */
@@ -151,7 +153,8 @@ int wt_probs(wt_handle *h, const wt_probs_desc *d, void *stream);
  * token drawn is the first whose running sum exceeds floor(floor(u_draw 2^24) S / 2^24).  Where
  * S = 0 at a refused position (p <= q everywhere: equal up to rounding) the token is drawn from p;
  * where that has S = 0 too, it is -1.  A drafted token outside 0 .. vocab - 1 is refused.  u and
- * u_draw lie in [0, 1).  n_drafted goes up to 2^30, n_req to 2^24, max_draft to 2^20. */
+ * u_draw lie in [0, 1).  n_drafted goes up to 2^30, n_req to 2^24, max_draft to 2^20.
+ * accepted and tokens must not overlap the inputs or each other. */
 #define WT_VERIFY_MAX_VOCAB (1 << 18)
 typedef struct {
   const float *p;          /* [n_drafted + n_req, vocab], row pitch ldp */

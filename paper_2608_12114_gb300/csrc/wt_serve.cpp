@@ -67,9 +67,34 @@ int check_output(wt_handle *h, wt::ServeRanges *seen, const char *call, const ch
   return rc;
 }
 
-bool overlap(const void *a, uint64_t na, const void *b, uint64_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return na && nb && x < y + nb && y < x + na;
+// Rows of a buffer, in bytes; its extent has been checked.
+struct Rows {
+  const char *name;
+  uintptr_t p;
+  uint64_t n, pitch, row;
+  Rows(const char *what, const void *at, uint64_t rows, uint64_t pitch_bytes, uint64_t row_bytes)
+      : name(what), p(reinterpret_cast<uintptr_t>(at)), n(row_bytes ? rows : 0), pitch(pitch_bytes), row(row_bytes) {}
+  Rows(const char *what, const void *at, uint64_t bytes) : Rows(what, at, 1, bytes, bytes) {}
+  uintptr_t end() const { return p + (n - 1) * pitch + row; }
+  // whether one of the rows meets [lo, hi)
+  bool meets(uintptr_t lo, uintptr_t hi) const {
+    const uint64_t k = lo < p + row ? 0 : (lo - p - row) / pitch + 1;  // the first row that ends past lo
+    return k < n && p + k * pitch < hi;
+  }
+};
+
+// Whether a byte belongs to rows of both: columns of one buffer, which only interleave, do not overlap.
+bool overlap(const Rows &a, const Rows &b) {
+  if (a.n == 0 || b.n == 0 || a.p >= b.end() || b.p >= a.end()) return false;
+  if (a.pitch == b.pitch && a.n > 1 && b.n > 1) {
+    const Rows &lo = a.p <= b.p ? a : b, &hi = a.p <= b.p ? b : a;
+    const uint64_t off = (hi.p - lo.p) % a.pitch;
+    return off < lo.row || a.pitch - off < hi.row;
+  }
+  const Rows &few = a.n <= b.n ? a : b, &many = a.n <= b.n ? b : a;
+  for (uint64_t i = 0; i < few.n; ++i)
+    if (many.meets(few.p + i * few.pitch, few.p + i * few.pitch + few.row)) return true;
+  return false;
 }
 
 #define CHECK(expr)          \
@@ -93,14 +118,10 @@ int check_adapt(wt_handle *h, wt::ServeRanges &seen, const wt_adapt_desc &d, siz
       d.ldx > kMaxPitch || d.ldy > kMaxPitch || d.ldbase > kMaxPitch || d.a_slot > kMaxPitch || d.b_slot > kMaxPitch)
     return serve_error(WT_EINVAL, "%s: desc %zu: a pitch is shorter than its row, or not below 2^40", call, i);
   if (T == 0 || M == 0) return WT_OK;
-  const uint64_t yn = extent(T, d.ldy, M, 4), bn = d.base ? extent(T, d.ldbase, M, 4) : 0;
-  CHECK(check_output(h, &seen, call, "y", d.y, yn, 4));
-  CHECK(check_buffer(&seen, call, "base", d.base, bn, 4));
-  if (d.base == d.y) {
-    if (d.ldbase != d.ldy) return serve_error(WT_EINVAL, "%s: desc %zu: base is y, with another pitch", call, i);
-  } else if (overlap(d.y, yn, d.base, bn)) {
-    return serve_error(WT_EINVAL, "%s: desc %zu: base overlaps y", call, i);
-  }
+  CHECK(check_output(h, &seen, call, "y", d.y, extent(T, d.ldy, M, 4), 4));
+  CHECK(check_buffer(&seen, call, "base", d.base, d.base ? extent(T, d.ldbase, M, 4) : 0, 4));
+  if (d.base == d.y && d.ldbase != d.ldy)
+    return serve_error(WT_EINVAL, "%s: desc %zu: base is y, with another pitch", call, i);
   CHECK(check_buffer(&seen, call, "slot", d.slot, 4 * T, 4));
   if (S == 0) return WT_OK;
   if (d.rank) CHECK(check_buffer(&seen, call, "rank", d.rank, 4 * S, 4));  // read where R is 0, too
@@ -112,27 +133,62 @@ int check_adapt(wt_handle *h, wt::ServeRanges &seen, const wt_adapt_desc &d, siz
   return WT_OK;
 }
 
+// The descriptors of one launch run at once: no y of them may meet anything that one of them reads or
+// another writes.  (Those of different launches follow one another.)
+int check_adapt_overlap(const wt::AdaptLaunch &L) {
+  for (int j = 0; j < L.n; ++j) {
+    const wt_adapt_desc &d = L.p[j].d;
+    const uint64_t T = d.T, K = d.K, M = d.M, R = d.R, S = R ? d.S : 0;
+    const Rows y("y", d.y, T, 4 * d.ldy, 4 * M);
+    const Rows reads[] = {{"base", d.base, d.base ? T : 0, 4 * (uint64_t)d.ldbase, 4 * M},
+                          {"x", d.x, S ? T : 0, 2 * (uint64_t)d.ldx, 2 * K},
+                          {"A", d.A, S, 2 * (uint64_t)d.a_slot, 2 * R * K},
+                          {"B", d.B, S, 2 * (uint64_t)d.b_slot, 2 * M * R},
+                          {"slot", d.slot, 4 * T},
+                          {"rank", d.rank, d.rank ? 4 * (uint64_t)d.S : 0},
+                          {"scale", d.scale, d.scale ? 4 * S : 0}};
+    for (int i = 0; i < L.n; ++i) {
+      const wt_adapt_desc &e = L.p[i].d;
+      const Rows out("y", e.y, e.T, 4 * (uint64_t)e.ldy, 4 * (uint64_t)e.M);
+      if (i < j && overlap(out, y)) return serve_error(WT_EINVAL, "wt_adapt: the y of two descriptors overlap");
+      for (const Rows &r : reads) {
+        if (i == j && &r == &reads[0] && d.base == d.y) continue;
+        if (overlap(out, r))
+          return serve_error(WT_EINVAL, "wt_adapt: y overlaps %s of %s descriptor", r.name, i == j ? "its" : "another");
+      }
+    }
+  }
+  return WT_OK;
+}
+
 int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
   wt::ServeContext ctx;
   CHECK(wt::serve_context(h, "wt_adapt", &ctx));
   if (n && !d) return serve_error(WT_EINVAL, "wt_adapt: NULL descriptors");
   wt::ServeRanges seen;
   for (size_t i = 0; i < n; ++i) CHECK(check_adapt(h, seen, d[i], i));
-  for (size_t i = 0; i < n;) {
-    // up to 8 descriptors of one type a launch
-    wt::AdaptLaunch L;
-    L.n = 0;
-    int max_R = 0, max_T = 0;
+  wt::AdaptLaunch L;
+  // up to 8 descriptors of one type a launch; the index of the first of the next one
+  auto take = [&](size_t i) {
     const int dtype = d[i].dtype;
-    size_t j = i;
-    for (; j < n && L.n < wt::kAdaptProjs && d[j].dtype == dtype; ++j) {
-      if (d[j].T == 0 || d[j].M == 0) continue;
-      L.p[L.n++].d = d[j];
-      max_R = std::max(max_R, d[j].R);
-      max_T = std::max(max_T, d[j].T);
-    }
-    i = j;
+    L.n = 0;
+    for (; i < n && L.n < wt::kAdaptProjs && d[i].dtype == dtype; ++i)
+      if (d[i].T && d[i].M) L.p[L.n++].d = d[i];
+    return i;
+  };
+  for (size_t i = 0; i < n;) {
+    i = take(i);
+    CHECK(check_adapt_overlap(L));
+  }
+  for (size_t i = 0; i < n;) {
+    const int dtype = d[i].dtype;
+    i = take(i);
     if (L.n == 0) continue;
+    int max_R = 0, max_T = 0;
+    for (int k = 0; k < L.n; ++k) {
+      max_R = std::max(max_R, L.p[k].d.R);
+      max_T = std::max(max_T, L.p[k].d.T);
+    }
     uint64_t all = 0;
     const bool planned = wt::adapt_planned(max_T);
     const int tile = planned ? 64 : 16;  // tokens of a work item
@@ -224,6 +280,14 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
   CHECK(check_buffer(&seen, call, "q", d.q, extent(d.n_tokens, d.q_stride, row, 2), 16));
   CHECK(check_output(h, &seen, call, "out", d.out, extent(d.n_tokens, d.out_stride, row, 2), 16));
   CHECK(check_buffer(&seen, call, "begin", d.begin, 4 * ((uint64_t)d.n_req + 1), 4));
+  const Rows out("out", d.out, d.n_tokens, 2 * (uint64_t)d.out_stride, 2 * (uint64_t)row);
+  auto apart = [&](const Rows &r) {
+    return overlap(out, r) ? serve_error(WT_EINVAL, "%s: out overlaps %s", call, r.name) : WT_OK;
+  };
+  // out may be q: a token's head is written once all that reads it has been read
+  if (d.out != d.q || d.out_stride != d.q_stride)
+    CHECK(apart({"q", d.q, (uint64_t)d.n_tokens, 2 * (uint64_t)d.q_stride, 2 * (uint64_t)row}));
+  CHECK(apart({"begin", d.begin, 4 * ((uint64_t)d.n_req + 1)}));
   if (d.prefix_len) {
     if (d.prefix_head < D || d.prefix_head % 8 || d.prefix_stride < D || d.prefix_stride % 8 || d.prefix_head > kMaxPitch ||
         d.prefix_stride > kMaxPitch)
@@ -233,6 +297,13 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
     const uint64_t n = (Bytes(2) * (Bytes(d.prefix_len - 1) * d.prefix_stride + Bytes(d.kv_heads - 1) * d.prefix_head + D)).n;
     CHECK(check_buffer(&seen, call, "prefix_k", d.prefix_k, n, 16));
     CHECK(check_buffer(&seen, call, "prefix_v", d.prefix_v, n, 16));
+    // as rows of whole keys where those lie apart, else of whole heads, or one
+    const uint64_t P = d.prefix_len, H = d.kv_heads, key = 2 * ((H - 1) * d.prefix_head + D), head = 2 * ((P - 1) * d.prefix_stride + D);
+    const bool keys = P > 1 && 2 * (uint64_t)d.prefix_stride >= key, heads = H > 1 && 2 * (uint64_t)d.prefix_head >= head;
+    for (const void *p : {d.prefix_k, d.prefix_v})
+      CHECK(apart(keys    ? Rows("the prefix", p, P, 2 * d.prefix_stride, key)
+                  : heads ? Rows("the prefix", p, H, 2 * d.prefix_head, head)
+                          : Rows("the prefix", p, n)));
   }
   if (d.max_len) {
     if (d.page < 1 || d.table_stride < 0 || d.table_stride > 0x7fffffff || (int64_t)d.max_len > d.table_stride * d.page)
@@ -243,6 +314,10 @@ int check_attend(wt_handle *h, const wt_attend_desc &d) {
     CHECK(check_buffer(&seen, call, "v_pages", d.v_pages, n, 16));
     CHECK(check_buffer(&seen, call, "table", d.table, extent(d.n_req, d.table_stride, d.table_stride, 4), 4));
     CHECK(check_buffer(&seen, call, "len", d.len, 4 * (uint64_t)d.n_req, 4));
+    CHECK(apart({"k_pages", d.k_pages, n}));
+    CHECK(apart({"v_pages", d.v_pages, n}));
+    CHECK(apart({"table", d.table, (uint64_t)d.n_req, 4 * (uint64_t)d.table_stride, 4 * (uint64_t)d.table_stride}));
+    CHECK(apart({"len", d.len, 4 * (uint64_t)d.n_req}));
   }
   return WT_OK;
 }
@@ -372,12 +447,14 @@ int probs_impl(wt_handle *h, const wt_probs_desc *d, cudaStream_t s) {
       d->ldl > kMaxPitch || d->ldp > kMaxPitch)
     return serve_error(WT_EINVAL, "%s: rows %d, vocab %d or a pitch out of range", call, d->rows, d->vocab);
   if (d->rows == 0 || d->vocab == 0) return WT_OK;
-  const uint64_t ln = extent(d->rows, d->ldl, d->vocab, 4), pn = extent(d->rows, d->ldp, d->vocab, 4);
-  CHECK(check_buffer(&seen, call, "logits", d->logits, ln, 4));
-  CHECK(check_output(h, &seen, call, "p", d->p, pn, 4));
-  if (d->p == d->logits ? d->ldp != d->ldl : overlap(d->p, pn, d->logits, ln))
+  const uint64_t rows = d->rows, V = d->vocab;
+  CHECK(check_buffer(&seen, call, "logits", d->logits, extent(rows, d->ldl, V, 4), 4));
+  CHECK(check_output(h, &seen, call, "p", d->p, extent(rows, d->ldp, V, 4), 4));
+  const Rows p("p", d->p, rows, 4 * d->ldp, 4 * V);
+  if (d->p == d->logits ? d->ldp != d->ldl : overlap(p, {"logits", d->logits, rows, 4 * (uint64_t)d->ldl, 4 * V}))
     return serve_error(WT_EINVAL, "%s: p overlaps the logits", call);
-  if (d->temp) CHECK(check_buffer(&seen, call, "temp", d->temp, 4 * (uint64_t)d->rows, 4));
+  if (d->temp) CHECK(check_buffer(&seen, call, "temp", d->temp, 4 * rows, 4));
+  if (d->temp && overlap(p, {"temp", d->temp, 4 * rows})) return serve_error(WT_EINVAL, "%s: p overlaps temp", call);
   CU(wt::launch_probs(*d, ctx.status, s));
   wt::serve_launched(h, 1);
   return WT_OK;
@@ -404,6 +481,15 @@ int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {
   CHECK(check_buffer(&seen, call, "u_draw", d->u_draw, 4 * B, 4));
   CHECK(check_output(h, &seen, call, "accepted", d->accepted, 4 * B, 4));
   CHECK(check_output(h, &seen, call, "tokens", d->tokens, 4 * B * ((uint64_t)d->max_draft + 1), 4));
+  const uint64_t V = d->vocab;
+  const Rows accepted("accepted", d->accepted, 4 * B), tokens("tokens", d->tokens, 4 * B * ((uint64_t)d->max_draft + 1));
+  const Rows reads[] = {{"p", d->p, n + B, 4 * (uint64_t)d->ldp, 4 * V}, {"q", d->q, d->q ? n : 0, 4 * (uint64_t)d->ldq, 4 * V},
+                        {"drafted", d->drafted, 4 * n},                  {"begin", d->begin, 4 * (B + 1)},
+                        {"u", d->u, 4 * n},                              {"u_draw", d->u_draw, 4 * B}};
+  for (const Rows &r : reads)
+    for (const Rows *o : {&accepted, &tokens})
+      if (overlap(*o, r)) return serve_error(WT_EINVAL, "%s: %s overlaps %s", call, o->name, r.name);
+  if (overlap(accepted, tokens)) return serve_error(WT_EINVAL, "%s: accepted overlaps tokens", call);
   CU(wt::launch_verify(*d, ctx.status, s));
   wt::serve_launched(h, 1);
   return WT_OK;

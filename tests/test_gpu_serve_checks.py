@@ -84,3 +84,98 @@ def test_ranks_of_slots_without_rows(torch, h):
     d = serving.adapters(x, y, slot, A, B, scale, rank=rank, base=base)
     d.rank += 2
     refused(lambda e: h.adapt([e]), d, "rank")
+
+
+def test_overlapping_buffers_are_refused(torch, h):
+    x, y, slot, A, B, scale, base = make(torch, 4, 64, 32, 2, 8, torch.bfloat16)
+    rank = torch.full((2,), 8, dtype=torch.int32, device="cuda")
+
+    def adapt(**change):
+        d = serving.adapters(x, y, slot, A, B, scale, rank=rank, base=base)
+        for k, v in change.items():
+            setattr(d, k, v)
+        return d
+
+    one = lambda d: h.adapt([d])  # noqa: E731
+    big = torch.zeros(1 << 16, device="cuda")
+    at = big.data_ptr()
+    for name in ("x", "A", "B", "slot", "rank", "scale", "base"):
+        refused(one, adapt(y=at, ldy=32, **{name: at + 256}), "overlap")
+    refused(one, adapt(base=y.data_ptr() + 16), "overlap")
+    for name in ("x", "A", "B", "slot", "rank", "scale", "base"):
+        d = adapt(**{name: at + 256})
+        other = adapt(y=at, ldy=32)
+        refused(h.adapt, [d, other], "overlap"), refused(h.adapt, [other, d], "overlap")
+    refused(h.adapt, [adapt(y=at, ldy=32), adapt(y=at + 64, ldy=40)], "overlap")
+
+    s = Set(torch, [2, 1], [40, 33], 100, 4, 2, 64)
+    n = s.out.numel() * 2
+    for name in ("q", "begin", "prefix_k", "prefix_v", "k_pages", "v_pages", "table", "len"):
+        d = s.desc()
+        setattr(d, name, at + n - 16)
+        d.out = at
+        refused(h.attend, d, "overlap")
+    d = s.desc()
+    d.out, d.out_stride = d.q, d.q_stride + 8
+    refused(h.attend, d, "overlap")
+
+    l, p = torch.randn(3, 64, device="cuda"), torch.empty(3, 64, device="cuda")
+    t = torch.ones(3, device="cuda")
+    d = serving.probabilities(l, p, temperature=t)
+    d.temp = p.data_ptr() + 4
+    refused(h.probs, d, "overlap")
+
+    a = drafts(torch, [2, 1], 64, 1.0, False)
+    acc, tok = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(2, 3, dtype=torch.int32, device="cuda")
+
+    def verify(**change):
+        d = serving.verification(a[0], a[2], a[3], a[4], a[5], acc, tok, q=a[1])
+        for k, v in change.items():
+            setattr(d, k, v)
+        return d
+
+    for name in ("p", "q", "drafted", "begin", "u", "u_draw", "accepted"):
+        refused(h.verify, verify(tokens=at, **{name: at + 4}), "overlap")
+    for name in ("p", "q", "drafted", "begin", "u", "u_draw"):
+        refused(h.verify, verify(accepted=at, **{name: at + 4}), "overlap")
+
+
+def test_buffers_that_interleave_are_accepted(torch, h):
+    """Columns of one buffer, as fused projections and gathered outputs leave them."""
+    x, y, slot, A, B, scale, base = make(torch, 40, 64, 32, 2, 8, torch.bfloat16)
+    one = torch.full((40, 100), _serve.NAN, device="cuda")
+    one[:, 32:64] = base
+    want = _serve.adapt(x, slot, A, B, scale, None, base)
+    h.adapt([serving.adapters(x, one[:, :32], slot, A, B, scale, base=one[:, 32:64]),
+             serving.adapters(x, one[:, 64:96], slot, A, B, scale, base=one[:, 32:64])])
+    torch.cuda.synchronize()
+    close(torch, one[:, :32], want, 64, 8), close(torch, one[:, 64:96], want, 64, 8)
+    assert torch.isnan(one[:, 96:]).all()
+    # rows of other pitches between one another's: y in the gaps of every second row of base
+    wide = torch.full((80, 100), _serve.NAN, device="cuda")
+    pairs = wide.view(40, 200)
+    pairs[:, 140:172] = base
+    h.adapt([serving.adapters(x, wide[:40, :32], slot, A, B, scale, base=pairs[:, 140:172])])
+    torch.cuda.synchronize()
+    close(torch, wide[:40, :32], want, 64, 8)
+
+    l = torch.randn(9, 1003, device="cuda")
+    both = torch.full((9, 2100), _serve.NAN, device="cuda")
+    both[:, 1050:2053] = l
+    h.probs(serving.probabilities(both[:, 1050:2053], both[:, 3:1006]))
+    torch.cuda.synchronize()
+    want = torch.softmax(l.double(), dim=1)
+    assert ((both[:, 3:1006].double() - want).abs() <= 1e-5 * want + 1e-12).all()
+
+    for new, lens, P in (([2, 1], [40, 33], 0), ([2, 1], [40, 33], 100), ([2] * 20, [9] * 20, 300)):
+        s = Set(torch, new, lens, P, 4, 2, 64)
+        want = s.want()
+        fused = torch.cat([s.q, torch.full_like(s.q, _serve.NAN)], dim=1)
+        s.q, s.out = fused[:, :4], fused[:, 4:]
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        s.check(torch, want)
+        s.out = s.q  # in place
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        s.check(torch, want)
