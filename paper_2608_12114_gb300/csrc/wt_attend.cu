@@ -101,10 +101,10 @@ __device__ __forceinline__ Request request_of(const wt_attend_desc &d, int b, in
   return {t0, t1 - t0, len};
 }
 
-// ND: 16-element groups of head_dim (rounded up).  MT: tiles of 16 rows.  Short heads keep four CTAs to an
-// SM (their rows beside later tokens' keys would take 160 registers, and three).
+// ND: 16-element groups of head_dim (rounded up).  MT: tiles of 16 rows.  With one, three CTAs to an SM, and
+// four of short heads (which the rows beside later tokens' keys would else bring to 160 registers and three).
 template <int DT, int ND, int MT>
-__global__ void __launch_bounds__(kThreads, ND == 4 && MT == 1 ? 4 : 0) attend_warp_kernel(const __grid_constant__ AttendPlan P) {
+__global__ void __launch_bounds__(kThreads, MT > 1 ? 0 : ND == 4 ? 4 : 3) attend_warp_kernel(const __grid_constant__ AttendPlan P) {
   constexpr int kPitch = ND * 32 + 16;              // bytes of a staged row: 8 rows hit 8 different bank groups
   constexpr int kTileBytes = 2 * kKeys * kPitch;    // K rows, then V rows
   constexpr int kRows = 16 * MT;
@@ -372,8 +372,9 @@ __global__ void __launch_bounds__(kThreads, ND == 4 && MT == 1 ? 4 : 0) attend_w
     // value and not all rows see all its keys, each row adds those that it sees one by one.
     bool odd = false;
     if (hides)
-      for (int i = lane; i < kKeys * chunks; i += 32) {
-        const uint4 w = lds128(vt + i / chunks * kPitch + i % chunks * 16);
+#pragma unroll 1
+      for (int c = lane & 1; c < chunks; c += 2) {  // two lanes a row
+        const uint4 w = lds128(vt + (lane >> 1) * kPitch + c * 16);
         odd |= not_finite<DT>(w.x) || not_finite<DT>(w.y) || not_finite<DT>(w.z) || not_finite<DT>(w.w);
       }
     if (__any_sync(0xffffffffu, odd)) {
