@@ -102,7 +102,7 @@ typedef struct {
   const void *prefix_v;     /* the same pitches */
   const void *k_pages;      /* [n_pages, page, kv_heads, head_dim], dense */
   const void *v_pages;
-  const int32_t *table;     /* [n_req, table_stride] page numbers */
+  const int32_t *table;     /* [n_req, pages of max_len keys] page numbers, row pitch table_stride */
   const int32_t *len;       /* [n_req] own keys, the new tokens' included; <= max_len */
   int64_t q_stride, out_stride, prefix_stride, prefix_head, table_stride;
   int64_t prefix_len;

@@ -179,3 +179,17 @@ def test_buffers_that_interleave_are_accepted(torch, h):
         h.attend(s.desc())
         torch.cuda.synchronize()
         s.check(torch, want)
+
+
+def test_a_table_that_is_part_of_a_wider_one(torch, h):
+    """Its last row ends with its allocation."""
+    torch.cuda.empty_cache()
+    s = Set(torch, [2, 1], [40, 33], 100, 4, 2, 64)
+    wide = torch.full((8, 1 << 20), -1, dtype=torch.int32, device="cuda")  # a 32 MB allocation of its own
+    part = wide[6:, (1 << 20) - s.table.shape[1]:]
+    part.copy_(s.table)
+    want = s.want()
+    s.table = part
+    h.attend(s.desc())
+    torch.cuda.synchronize()
+    s.check(torch, want)
