@@ -109,8 +109,9 @@ def attention(q, out, begin, k_pages=None, v_pages=None, table=None, lens=None, 
         _is(prefix_k, "prefix_k", q.dtype, 3), _is(prefix_v, "prefix_v", q.dtype, 3)
         P, Hkv, Dk = prefix_k.shape
         _need(Dk == D and prefix_v.shape == prefix_k.shape, "prefix_k and prefix_v are [keys, kv_heads, %d]" % D)
-        _need(prefix_k.stride() == prefix_v.stride() and prefix_k.stride(2) == 1,
-              "prefix_k and prefix_v have the same strides and contiguous head rows")
+        # the stride of a dimension of one says nothing
+        _need(all(n == 1 or a == b for n, a, b in zip(prefix_k.shape, prefix_k.stride(), prefix_v.stride())) and
+              prefix_k.stride(2) == 1, "prefix_k and prefix_v have the same strides and contiguous head rows")
         d.prefix_k, d.prefix_v, d.prefix_len = _ptr(prefix_k), _ptr(prefix_v), P
         d.prefix_stride = prefix_k.stride(0) if P > 1 else Hkv * D
         d.prefix_head = prefix_k.stride(1) if Hkv > 1 else D

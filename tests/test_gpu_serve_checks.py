@@ -193,3 +193,19 @@ def test_a_table_that_is_part_of_a_wider_one(torch, h):
     h.attend(s.desc())
     torch.cuda.synchronize()
     s.check(torch, want)
+
+
+def test_strides_of_dimensions_of_one(torch, h):
+    """They say nothing: two prefixes that differ in them alone are alike."""
+    for P, Hkv in ((1, 2), (60, 1), (1, 1)):
+        s = Set(torch, [2, 1], [40, 33], P, 4, Hkv, 64)
+        want = s.want()
+        st = list(s.pv.stride())
+        if P == 1:
+            st[0] = 8 * 64 * Hkv
+        if Hkv == 1:
+            st[1] = 8 * 64
+        s.pv = torch.as_strided(s.pv, s.pv.shape, st)
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        s.check(torch, want)
