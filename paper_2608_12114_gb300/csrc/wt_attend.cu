@@ -491,7 +491,8 @@ __global__ void __launch_bounds__(kThreads) attend_merge_kernel(const __grid_con
   const wt_attend_desc &d = P.d;
   const int lane = threadIdx.x & 31, warp = WR == 1 ? 0 : threadIdx.x >> 5;
   const int b = blockIdx.y;
-  const Request rq = request_of(d, b, nullptr, false);
+  // without own keys no CTA before has looked at the requests
+  const Request rq = request_of(d, b, P.status, P.own_splits == 0 && blockIdx.x == 0 && threadIdx.x == 0);
   griddep_wait();  // launched while the kernel before it ends
   const int i = WR == 1 ? blockIdx.x * kWarps + (threadIdx.x >> 5) : blockIdx.x;
   if (i >= rq.n * d.heads) return;

@@ -209,3 +209,22 @@ def test_strides_of_dimensions_of_one(torch, h):
         h.attend(s.desc())
         torch.cuda.synchronize()
         s.check(torch, want)
+
+
+@pytest.mark.parametrize("new", [[2, 1], [2] * 30])
+@pytest.mark.parametrize("P", [0, 100])
+def test_offsets_that_contradict_a_call_without_own_keys(torch, new, P):
+    """On the warp kernel, on tcgen05 and with no key at all."""
+    B, n = len(new), sum(new)
+    for at, bad in ((1, 9), (0, -4), (B, 2 ** 31 - 1), (1, -2 ** 31)):
+        s = Set(torch, new, None, P, 4, 2, 64)
+        s.begin[at] = bad
+        with wt.Handle([]) as h:
+            h.attend(s.desc())
+            torch.cuda.synchronize()
+            assert h.device_status() == wt.WT_EINVAL
+    s = Set(torch, new, None, P, 4, 2, 64)
+    with wt.Handle([]) as h:
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        assert h.device_status() == 0
