@@ -588,7 +588,8 @@ constexpr size_t warp_smem() {
 }
 
 // `after`: the kernel waits on the device for the one before it in this call, so it may be launched
-// while that one ends (measured a call: 1 to 4 us less, from one token to 64 requests).
+// while that one ends (measured a call: 1 to 4 us less, from one token to 64 requests).  Never a call's first
+// kernel: it reads the caller's memory before it waits.
 cudaError_t launch(void (*k)(AttendPlan), dim3 grid, size_t smem, bool after, cudaStream_t s, const AttendPlan &P) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
@@ -650,7 +651,8 @@ cudaError_t run_merge(const AttendPlan &P, cudaStream_t s) {
   // four warps to a row only where one to a row would leave SMs idle
   const bool one = (int64_t)P.d.n_tokens * P.d.heads >= 16ll * num_sms();
   return launch(one ? attend_merge_kernel<DT, 1> : attend_merge_kernel<DT, kWarps>,
-                dim3(one ? (rows + kWarps - 1) / kWarps : rows, (unsigned)P.d.n_req), 0, true, s, P);
+                dim3(one ? (rows + kWarps - 1) / kWarps : rows, (unsigned)P.d.n_req), 0,
+                P.x.groups || P.own_splits || P.pre_splits, s, P);
 }
 
 cudaError_t launch_attend_merge(const AttendPlan &P, cudaStream_t s) {
