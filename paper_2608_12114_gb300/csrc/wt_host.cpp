@@ -2361,6 +2361,15 @@ int wt::serve_cuda_error(cudaError_t e, const char *what) { return cuda_err(e, w
 int wt::serve_context(wt_handle *h, const char *call, ServeContext *out) {
   if (!h) return set_err(WT_EINVAL, "%s: NULL handle", call);
   if (h->host_only) return set_err(WT_ENOTSUP, "%s: handle was opened host-only", call);
+  // A thread that has made no runtime call yet has no current context.  The driver's own calls need one: the
+  // allocation look-ups, which else pass every range, and the tensor maps.
+  static thread_local bool bound = false;
+  if (!bound) {
+    int dev = 0;
+    CU(cudaGetDevice(&dev));
+    CU(cudaSetDevice(dev));
+    bound = true;
+  }
   h->served = true;
   *out = {h->device, h->status};
   return WT_OK;

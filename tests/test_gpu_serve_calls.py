@@ -1,10 +1,12 @@
 """How a program makes the serving calls: from threads and streams, into graphs, many at a time, again and again."""
 import ctypes as C
+import threading
 
 import pytest
 
 from paper_2608_12114_gb300 import build, serving, wt
-from tests.test_gpu_serve_adapt import make
+from tests import _serve
+from tests.test_gpu_serve_adapt import close, make
 from tests.test_gpu_serve_attend import Set
 
 pytestmark = pytest.mark.gpu
@@ -60,3 +62,48 @@ def test_the_first_kernel_of_a_call_waits_for_the_stream(torch, h):
         kinds = [data[8 * i + 2] for i in range(n.value) if frm[i] in first]
         assert kinds == [0], kinds
         rt.cudaGraphDestroy(g)
+
+
+def test_threads_on_one_handle(torch, h):
+    """Two threads, each with its stream, its calls of every kind and its sizes."""
+    sets = [Set(torch, [1 + i] * 6, [40] * 6, 900 + 700 * i, 8, 2, 128, seed=i) for i in range(2)]
+    ads = [make(torch, 280 + 40 * i, 96, 64, 3, 16, torch.float16, seed=i) for i in range(2)]
+    wants = [s.want() for s in sets]
+    wad = [_serve.adapt(x, s, A, B, c, None, b) for x, y, s, A, B, c, b in ads]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    failed = []
+
+    def body(i):
+        try:
+            x, y, s, A, B, c, b = ads[i]
+            da, dd = sets[i].desc(), [serving.adapters(x, y, s, A, B, c, base=b)]
+            for _ in range(200):
+                h.attend(da, streams[i].cuda_stream)
+                h.adapt(dd, streams[i].cuda_stream)
+        except Exception as e:
+            failed.append(e)
+
+    threads = [threading.Thread(target=body, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed
+    for i in range(2):
+        sets[i].check(torch, wants[i])
+        close(torch, ads[i][1], wad[i], 96, 16)
+
+
+def test_the_first_call_of_a_thread_is_checked(torch, h):
+    """Before any other use of the GPU on it: the range of every buffer, as on other threads."""
+    torch.cuda.empty_cache()
+    l, p = (torch.zeros(8, 1 << 20, device="cuda") for _ in range(2))  # allocations of their own
+    d = serving.probabilities(l, p)
+    d.rows = 1 << 16
+    got = []
+    t = threading.Thread(target=lambda: got.append((wt.lib().wt_probs(h.ptr, C.byref(d), None), wt.lib().wt_last_error())))
+    t.start()
+    t.join()
+    assert got[0][0] == wt.WT_EINVAL and b"runs past" in got[0][1]
