@@ -13,11 +13,13 @@
  * Conventions are those of wt.h: int status codes and wt_last_error, void* streams, caller-owned
  * device memory, no C++ exception across the boundary.  Besides:
  *   - A handle supplies the device, the status word and the workspaces; wt_open with no path gives
- *     one.  A call enqueues its kernels on `stream` and returns; nothing waits on the host.
- *   - Workspaces belong to the handle, one per stream the calls were made on, and grow to the
- *     largest call.  A call captured into a CUDA graph takes a workspace of its own, which stays
- *     until wt_close; every replay must complete before wt_close, and two replays of one graph must
- *     not overlap.  No warm-up call is needed before a capture.
+ *     one.  A call enqueues its kernels on `stream` and returns; nothing waits on the host for the
+ *     device (a call larger than those before it on its stream allocates).
+ *   - Workspaces belong to the handle and stay until wt_close.  Each stream has its own; from the
+ *     ninth stream on a new one takes over those of a stream whose calls have completed.  A call
+ *     captured into a CUDA graph takes a workspace of its own; every replay must complete before
+ *     wt_close, and two replays of one graph must not overlap.  No warm-up call is needed before a
+ *     capture.
  *   - wt_close waits for the device to go idle if the handle made any of these calls.
  *   - Descriptors are read during the call and not kept.
  *   - Lengths, slots, page numbers and tokens that lie in device memory cannot be checked on the

@@ -432,15 +432,28 @@ struct Ring {
 
 Ring g_ring[64];
 
-// Scratch memory of the serving calls on one stream.  `done` follows its latest use outside a
-// capture; one taken for a capture belongs to that graph until the handle closes.
-struct Workspace {
-  unsigned long long capture_id = 0;  // nonzero: of that stream capture
-  unsigned long long stream_id = 0;   // the stream's number; its address in a capture
+// Scratch memory of serving calls.
+struct ServeBlock {
   void *p = nullptr;
   size_t n = 0;
+  unsigned long long capture = 0, stream = 0;  // one taken in a capture: which, and the stream's address
+};
+
+// The serving calls made outside a capture on one stream: `done` follows the latest, and the blocks are
+// theirs in turn.  A block that a larger call outgrew stays, since the stream may still be busy with it.
+struct StreamUse {
+  unsigned long long id = 0;  // the stream's number
   cudaEvent_t done = nullptr;
-  bool used = false;
+  std::vector<ServeBlock> blocks;
+  size_t largest() const { return blocks.empty() ? 0 : blocks.back().n; }
+};
+
+// While it lives, this thread's calls are allowed beside captures: its own, and those of other threads, which
+// an event query or an allocation would else end with an error.
+struct Relax {
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  Relax() { cudaThreadExchangeStreamCaptureMode(&mode); }
+  ~Relax() { cudaThreadExchangeStreamCaptureMode(&mode); }
 };
 
 }  // namespace
@@ -474,8 +487,9 @@ struct wt_handle {
   int *status = nullptr;
   std::vector<cudaEvent_t> events;
   std::list<Plan *> plans;
-  std::vector<Workspace *> workspaces;  // of the serving calls (wt_serve.h), one per stream
-  std::atomic<bool> served{false};      // a serving call was made: its kernels may write the status word
+  std::atomic<bool> served{false};   // a serving call was made: its kernels may write the status word
+  std::list<StreamUse> uses;         // the serving calls (wt_serve.h), by stream
+  std::vector<ServeBlock> captured;  // blocks of calls in captures: their graphs may be replayed until wt_close
   std::atomic<uint64_t> kernel_launches{0};
   wt_open_phases open_times{};
   std::mutex mu;
@@ -2275,15 +2289,6 @@ int run_plan(wt_handle *h, Plan *P, const wt_gemv_desc *d, cudaStream_t s, bool 
   return WT_OK;
 }
 
-void destroy_workspace(int dev, Workspace *w) {
-  if (w->done) {
-    if (w->used) cudaEventSynchronize(w->done);
-    ev_destroy(w->done);
-  }
-  cached_free(false, dev, w->p, w->n);
-  delete w;
-}
-
 int close_impl(wt_handle *h) {
   int rc = WT_OK;
   if (!h->host_only && h->device >= 0) {
@@ -2301,11 +2306,17 @@ int close_impl(wt_handle *h) {
     h->trace.clear();
     for (Plan *P : h->plans) destroy_plan(P);
     h->plans.clear();
-    // serving calls leave no event behind, nor do replays of graphs that hold them: the device goes idle
-    // before another handle may get the status word and the workspaces
+    // calls without a workspace leave no event behind, nor do replays of graphs: the device goes idle before
+    // another handle may get the status word and the blocks
     if (h->served) cudaDeviceSynchronize();
-    for (Workspace *w : h->workspaces) destroy_workspace(h->device, w);
-    h->workspaces.clear();
+    for (StreamUse &u : h->uses) cudaEventSynchronize(u.done);
+    for (StreamUse &u : h->uses) {
+      for (const ServeBlock &b : u.blocks) cached_free(false, h->device, b.p, b.n);
+      ev_destroy(u.done);
+    }
+    for (const ServeBlock &b : h->captured) cached_free(false, h->device, b.p, b.n);
+    h->uses.clear();
+    h->captured.clear();
     for (cudaEvent_t e : h->events) ev_destroy(e);
     h->events.clear();
     status_give(h->device, h->status);
@@ -2418,83 +2429,101 @@ int wt::serve_tensor_map(void *out, const void *base, int rank, const uint64_t *
   return WT_OK;
 }
 
-int wt::serve_workspace(wt_handle *h, cudaStream_t s, size_t n, ServeWorkspace *out) {
-  *out = {};
-  cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
-  unsigned long long capture = 0, id = 0;
-  if (cudaStreamGetCaptureInfo(s, &cs, &capture) != cudaSuccess) {
-    cudaGetLastError();
-    cs = cudaStreamCaptureStatusNone;
-  }
-  if (cs != cudaStreamCaptureStatusActive) capture = 0;
-  // a stream's number is its own for good, unlike its address, but cannot be asked for in a capture
-  if (capture) id = reinterpret_cast<uintptr_t>(s);
-  else CU(cudaStreamGetId(s, &id));
-  // a capture forbids allocations that might synchronise, unless the thread allows them
-  struct Relax {
-    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
-    bool on;
-    explicit Relax(bool b) : on(b) {
-      if (on) cudaThreadExchangeStreamCaptureMode(&mode);
+// The record of stream s: its own, or one whose stream's work has completed once there are kServeStreams,
+// with a block of n bytes where one of those has it.  Nothing here waits.
+static int serve_use(wt_handle *h, unsigned long long id, size_t n, StreamUse **out) {
+  constexpr size_t kServeStreams = 8;
+  for (StreamUse &u : h->uses)
+    if (u.id == id) {
+      *out = &u;
+      return WT_OK;
     }
-    ~Relax() {
-      if (on) cudaThreadExchangeStreamCaptureMode(&mode);
+  const Relax relax;
+  StreamUse *idle = nullptr;
+  if (h->uses.size() >= kServeStreams)
+    for (StreamUse &u : h->uses) {
+      const cudaError_t e = cudaEventQuery(u.done);
+      if (e == cudaErrorNotReady) cudaGetLastError();
+      if (e != cudaSuccess) continue;
+      if (!idle || u.largest() >= n) idle = &u;
+      if (u.largest() >= n) break;
     }
-  };
-  Workspace *w = nullptr;
-  size_t eager = 0;
-  for (Workspace *q : h->workspaces) {
-    if (q->capture_id == capture && q->stream_id == id && q->n >= n) w = q;
-    eager += q->capture_id == 0;
-  }
-  if (w) {
-    *out = {w->p, w};
-    return WT_OK;
-  }
-  Relax relax(capture != 0);
-  if (!capture) {
-    // a smaller one of this stream, or the oldest of too many streams, goes once its work is done
-    constexpr size_t kStreams = 8;
-    for (size_t i = 0; i < h->workspaces.size();) {
-      Workspace *q = h->workspaces[i];
-      if (q->capture_id == 0 && (q->stream_id == id || eager >= kStreams)) {
-        h->workspaces.erase(h->workspaces.begin() + (long)i);
-        destroy_workspace(h->device, q);
-        --eager;
-      } else {
-        ++i;
-      }
+  if (!idle) {
+    StreamUse u;
+    CU(ev_create(&u.done, cudaEventDisableTiming));
+    try {
+      h->uses.push_back(std::move(u));
+    } catch (const std::bad_alloc &) {
+      ev_destroy(u.done);
+      return set_err(WT_ENOMEM, "out of host memory");
     }
+    idle = &h->uses.back();
   }
-  try {
-    size_t cap = 1 << 16;
-    while (cap < n) cap *= 2;
-    std::unique_ptr<Workspace> own(new Workspace);
-    h->workspaces.reserve(h->workspaces.size() + 1);
-    own->stream_id = id;
-    own->capture_id = capture;
-    if (!capture) CU(ev_create(&own->done, cudaEventDisableTiming));
-    const cudaError_t e = wt::fault_injected("alloc") ? cudaErrorMemoryAllocation : cached_alloc(false, h->device, &own->p, cap);
-    if (e != cudaSuccess) {
-      cudaGetLastError();
-      ev_destroy(own->done);
-      return set_err(WT_ENOMEM, "a workspace of %zu bytes: %s", cap, cudaGetErrorString(e));
-    }
-    own->n = cap;
-    w = own.release();
-    h->workspaces.push_back(w);
-  } catch (const std::bad_alloc &) {
-    return set_err(WT_ENOMEM, "out of host memory");
-  }
-  *out = {w->p, w};
+  idle->id = id;
+  *out = idle;
   return WT_OK;
 }
 
-int wt::serve_workspace_done(wt_handle *h, cudaStream_t s, const ServeWorkspace &sw) {
-  Workspace *w = static_cast<Workspace *>(sw.entry);
-  if (!w || w->capture_id) return WT_OK;
-  CU(cudaEventRecord(w->done, s));
-  w->used = true;
+// A block of at least n bytes into `blocks`.
+static int serve_block(wt_handle *h, std::vector<ServeBlock> &blocks, size_t n, unsigned long long capture, unsigned long long id) {
+  const Relax relax;  // a capture, this thread's or another's, forbids allocations that might synchronise
+  ServeBlock b;
+  b.n = 1 << 16;
+  while (b.n < n) b.n *= 2;
+  b.capture = capture;
+  b.stream = id;
+  try {
+    blocks.reserve(blocks.size() + 1);
+  } catch (const std::bad_alloc &) {
+    return set_err(WT_ENOMEM, "out of host memory");
+  }
+  const cudaError_t e = wt::fault_injected("alloc") ? cudaErrorMemoryAllocation : cached_alloc(false, h->device, &b.p, b.n);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return set_err(WT_ENOMEM, "a workspace of %zu bytes: %s", b.n, cudaGetErrorString(e));
+  }
+  blocks.push_back(b);
+  return WT_OK;
+}
+
+// The capture that s is in (0: none), and what tells it from other streams: its number, which is its own for
+// good, unlike its address, but cannot be asked for in a capture.
+static int serve_stream(cudaStream_t s, unsigned long long *capture, unsigned long long *id) {
+  cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+  if (cudaStreamGetCaptureInfo(s, &cs, capture) != cudaSuccess) {
+    cudaGetLastError();
+    cs = cudaStreamCaptureStatusNone;
+  }
+  if (cs != cudaStreamCaptureStatusActive) *capture = 0;
+  if (*capture) *id = reinterpret_cast<uintptr_t>(s);
+  else CU(cudaStreamGetId(s, id));
+  return WT_OK;
+}
+
+int wt::serve_workspace(wt_handle *h, cudaStream_t s, size_t n, ServeWorkspace *out) {
+  *out = {};
+  unsigned long long capture = 0, id = 0;
+  int rc = serve_stream(s, &capture, &id);
+  if (rc) return rc;
+  StreamUse *use = nullptr;
+  if (!capture && (rc = serve_use(h, id, n, &use))) return rc;
+  out->entry = use;
+  if (n == 0) return WT_OK;
+  std::vector<ServeBlock> &blocks = use ? use->blocks : h->captured;
+  for (int made = 0; made < 2; ++made) {
+    for (const ServeBlock &b : blocks)
+      if (b.n >= n && (use || (b.capture == capture && b.stream == id))) {
+        out->p = b.p;
+        return WT_OK;
+      }
+    if (!made && (rc = serve_block(h, blocks, n, capture, id))) return rc;
+  }
+  return WT_OK;
+}
+
+int wt::serve_done(wt_handle *, cudaStream_t s, const ServeWorkspace &w) {
+  StreamUse *use = static_cast<StreamUse *>(w.entry);
+  if (use) CU(cudaEventRecord(use->done, s));
   return WT_OK;
 }
 

@@ -246,7 +246,7 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
     W.v = reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(w.p) + plans);
     W.back = reinterpret_cast<float *>(W.v + v);
     const cudaError_t e = wt::launch_adapt(L, &W, max_R, ctx.status, s);
-    const int rc = wt::serve_workspace_done(h, s, w);
+    const int rc = wt::serve_done(h, s, w);
     CU(e);
     wt::serve_launched(h, 3);
     if (rc) return rc;
@@ -433,7 +433,7 @@ int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
   if (P.x.groups) e = wt::launch_attend_prefix(P.x, maps, d.dtype, ctx.status, s);
   if (e == cudaSuccess && parts) e = wt::launch_attend_warp(P, s);
   if (e == cudaSuccess && !P.direct) e = wt::launch_attend_merge(P, s);
-  const int rc = wt::serve_workspace_done(h, s, w);
+  const int rc = wt::serve_done(h, s, w);
   CU(e);
   wt::serve_launched(h, (P.x.groups != 0) + (parts != 0) + !P.direct);
   return rc;

@@ -29,17 +29,17 @@ struct ServeRanges {
 // false only when [p, p + n) starts inside a device allocation and runs past its end
 bool serve_range_ok(const void *p, uint64_t n, ServeRanges *seen);
 void serve_launched(wt_handle *h, int kernels);
-// The handle's mutex, held from serve_workspace to serve_workspace_done.
+// The handle's mutex, held from serve_workspace to serve_done.
 void serve_lock(wt_handle *h);
 void serve_unlock(wt_handle *h);
-// A workspace of at least n bytes for calls on stream s (256-byte aligned).  The caller makes the
-// matching serve_workspace_done after its last launch (also after a failed one).
+// A workspace of at least n bytes for calls on stream s (256-byte aligned; none for 0).  The caller makes
+// the matching serve_done after its last launch (also after a failed one): wt_close waits for it.
 struct ServeWorkspace {
   void *p = nullptr;
   void *entry = nullptr;
 };
 int serve_workspace(wt_handle *h, cudaStream_t s, size_t n, ServeWorkspace *out);
-int serve_workspace_done(wt_handle *h, cudaStream_t s, const ServeWorkspace &w);
+int serve_done(wt_handle *h, cudaStream_t s, const ServeWorkspace &w);
 // cuTensorMapEncodeTiled of a 16-bit tensor with the 128-byte swizzle; strides in bytes for dims 1..
 int serve_tensor_map(void *out, const void *base, int rank, const uint64_t *dims, const uint64_t *strides,
                      const uint32_t *box);

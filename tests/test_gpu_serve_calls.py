@@ -1,6 +1,7 @@
 """How a program makes the serving calls: from threads and streams, into graphs, many at a time, again and again."""
 import ctypes as C
 import threading
+import time
 
 import pytest
 
@@ -107,3 +108,54 @@ def test_the_first_call_of_a_thread_is_checked(torch, h):
     t.start()
     t.join()
     assert got[0][0] == wt.WT_EINVAL and b"runs past" in got[0][1]
+
+
+SECOND = 2_000_000_000  # cycles, about
+
+
+def test_a_larger_call_does_not_wait_for_the_stream(torch, h):
+    """Its stream is busy for a second with work the smaller call's workspace waits for."""
+    a, b = Set(torch, [1], [60], 2000, 8, 2, 128), Set(torch, [2] * 30, [60] * 30, 4000, 8, 2, 128)
+    other = torch.cuda.Stream()
+    with wt.Handle([]) as warm:
+        warm.attend(b.desc()), warm.attend(a.desc())
+        torch.cuda.synchronize()
+    wa, wb = a.want(), b.want()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        torch.cuda._sleep(SECOND)
+        t0 = time.perf_counter()
+        h.attend(a.desc(), other.cuda_stream)
+        h.attend(b.desc(), other.cuda_stream)
+        took, busy = time.perf_counter() - t0, not other.query()
+    assert busy and took < 0.2, took
+    other.synchronize()
+    a.check(torch, wa), b.check(torch, wb)
+    h.attend(a.desc(), other.cuda_stream)
+    other.synchronize()
+    a.check(torch, wa)
+
+
+def test_many_streams_do_not_wait_for_one_another(torch, h):
+    s = Set(torch, [1] * 8, [60] * 8, 2000, 8, 2, 128)
+    want = s.want()
+    h.attend(s.desc())
+    streams = [torch.cuda.Stream() for _ in range(20)]
+    torch.cuda.synchronize()
+    for st in streams[:1]:
+        with torch.cuda.stream(st):
+            torch.cuda._sleep(SECOND)
+    t0 = time.perf_counter()
+    for st in streams:
+        h.attend(s.desc(), st.cuda_stream)
+    took, busy = time.perf_counter() - t0, not streams[0].query()
+    assert busy and took < 0.3, took
+    torch.cuda.synchronize()
+    s.check(torch, want)
+    # finished streams' workspaces serve later ones: no more of them however many streams come
+    before = wt.live()["device_bytes"]
+    for _ in range(40):
+        st = torch.cuda.Stream()
+        h.attend(s.desc(), st.cuda_stream)
+        st.synchronize()
+    assert wt.live()["device_bytes"] == before
