@@ -20,7 +20,8 @@
  *     captured into a CUDA graph takes a workspace of its own; every replay must complete before
  *     wt_close, and two replays of one graph must not overlap.  No warm-up call is needed before a
  *     capture.
- *   - wt_close waits for the device to go idle if the handle made any of these calls.
+ *   - wt_close waits for the last call on each stream, and for nothing else on the device.  Calls
+ *     and wt_close may be made while another thread captures.
  *   - Descriptors are read during the call and not kept.
  *   - Lengths, slots, page numbers and tokens that lie in device memory cannot be checked on the
  *     host.  Where one contradicts its descriptor, the kernel clamps it (an offset, a length, a

@@ -487,7 +487,6 @@ struct wt_handle {
   int *status = nullptr;
   std::vector<cudaEvent_t> events;
   std::list<Plan *> plans;
-  std::atomic<bool> served{false};   // a serving call was made: its kernels may write the status word
   std::list<StreamUse> uses;         // the serving calls (wt_serve.h), by stream
   std::vector<ServeBlock> captured;  // blocks of calls in captures: their graphs may be replayed until wt_close
   std::atomic<uint64_t> kernel_launches{0};
@@ -2292,6 +2291,7 @@ int run_plan(wt_handle *h, Plan *P, const wt_gemv_desc *d, cudaStream_t s, bool 
 int close_impl(wt_handle *h) {
   int rc = WT_OK;
   if (!h->host_only && h->device >= 0) {
+    const Relax relax;
     int cur = -1;
     cudaGetDevice(&cur);
     if (cur != h->device) cudaSetDevice(h->device);
@@ -2306,9 +2306,8 @@ int close_impl(wt_handle *h) {
     h->trace.clear();
     for (Plan *P : h->plans) destroy_plan(P);
     h->plans.clear();
-    // calls without a workspace leave no event behind, nor do replays of graphs: the device goes idle before
-    // another handle may get the status word and the blocks
-    if (h->served) cudaDeviceSynchronize();
+    // another handle may get the status word and the blocks once the last call on every stream has completed
+    // (replays of captured ones have, by the contract)
     for (StreamUse &u : h->uses) cudaEventSynchronize(u.done);
     for (StreamUse &u : h->uses) {
       for (const ServeBlock &b : u.blocks) cached_free(false, h->device, b.p, b.n);
@@ -2381,7 +2380,6 @@ int wt::serve_context(wt_handle *h, const char *call, ServeContext *out) {
     CU(cudaSetDevice(dev));
     bound = true;
   }
-  h->served = true;
   *out = {h->device, h->status};
   return WT_OK;
 }

@@ -26,6 +26,19 @@ struct Lock {
   ~Lock() { wt::serve_unlock(h); }
 };
 
+// One kernel that needs no workspace.
+template <typename F>
+int launch_alone(wt_handle *h, cudaStream_t s, F launch) {
+  Lock lock(h);
+  wt::ServeWorkspace w;
+  if (int rc = wt::serve_workspace(h, s, 0, &w)) return rc;
+  const cudaError_t e = launch();
+  const int rc = wt::serve_done(h, s, w);
+  CU(e);
+  wt::serve_launched(h, 1);
+  return rc;
+}
+
 bool aligned(const void *p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 // Bytes of memory, which stay at the largest number where a product or a sum would pass 64 bits (rows of
@@ -207,8 +220,7 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
     }
     if (all > (1u << 27)) return serve_error(WT_EINVAL, "wt_adapt: %llu tiles of work in one launch", (unsigned long long)all);
     if (!planned) {
-      CU(wt::launch_adapt(L, nullptr, max_R, ctx.status, s));
-      wt::serve_launched(h, 1);
+      CHECK(launch_alone(h, s, [&] { return wt::launch_adapt(L, nullptr, max_R, ctx.status, s); }));
       continue;
     }
     // many tokens: a plan for each distinct slot map, and v of every projection, in the workspace
@@ -457,9 +469,7 @@ int probs_impl(wt_handle *h, const wt_probs_desc *d, cudaStream_t s) {
     return serve_error(WT_EINVAL, "%s: p overlaps the logits", call);
   if (d->temp) CHECK(check_buffer(&seen, call, "temp", d->temp, 4 * rows, 4));
   if (d->temp && overlap(p, {"temp", d->temp, 4 * rows})) return serve_error(WT_EINVAL, "%s: p overlaps temp", call);
-  CU(wt::launch_probs(*d, ctx.status, s));
-  wt::serve_launched(h, 1);
-  return WT_OK;
+  return launch_alone(h, s, [&] { return wt::launch_probs(*d, ctx.status, s); });
 }
 
 int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {
@@ -492,9 +502,7 @@ int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {
     for (const Rows *o : {&accepted, &tokens})
       if (overlap(*o, r)) return serve_error(WT_EINVAL, "%s: %s overlaps %s", call, o->name, r.name);
   if (overlap(accepted, tokens)) return serve_error(WT_EINVAL, "%s: accepted overlaps tokens", call);
-  CU(wt::launch_verify(*d, ctx.status, s));
-  wt::serve_launched(h, 1);
-  return WT_OK;
+  return launch_alone(h, s, [&] { return wt::launch_verify(*d, ctx.status, s); });
 }
 
 }  // namespace

@@ -9,6 +9,7 @@ from paper_2608_12114_gb300 import build, serving, wt
 from tests import _serve
 from tests.test_gpu_serve_adapt import close, make
 from tests.test_gpu_serve_attend import Set
+from tests.test_gpu_serve_draw import drafts
 
 pytestmark = pytest.mark.gpu
 
@@ -159,3 +160,63 @@ def test_many_streams_do_not_wait_for_one_another(torch, h):
         h.attend(s.desc(), st.cuda_stream)
         st.synchronize()
     assert wt.live()["device_bytes"] == before
+
+
+
+def capturing(torch, mode):
+    """A capture open on another thread: (start it, end it and say whether it held)."""
+    begun, end, ok = threading.Event(), threading.Event(), []
+
+    def body():
+        st, x = torch.cuda.Stream(), torch.zeros(8, device="cuda")
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        try:
+            with torch.cuda.stream(st):
+                g.capture_begin(capture_error_mode=mode)
+                x += 1
+                begun.set()
+                end.wait(60)
+                x += 1
+                g.capture_end()
+            g.replay()
+            torch.cuda.synchronize()
+            ok.append(x.tolist() == [2.0] * 8)
+        except Exception as e:
+            ok.append(str(e))
+        finally:
+            begun.set()
+
+    t = threading.Thread(target=body)
+    t.start()
+    begun.wait(60)
+
+    def finish():
+        end.set()
+        t.join(60)
+        return ok
+
+    return finish
+
+
+@pytest.mark.parametrize("mode", ["global", "thread_local"])
+def test_a_handle_used_and_closed_while_another_thread_captures(torch, mode):
+    p, q, d, begin, u, w = drafts(torch, [3, 0, 2], 5003, 2.0, False)
+    acc, tok = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(3, 4, dtype=torch.int32, device="cuda")
+    a = Set(torch, [1] * 8, [60] * 8, 2000, 8, 2, 128)
+    want, wa = _serve.verify(p, q, d, begin, u, w, 3), a.want()
+    desc, da = serving.verification(p, d, begin, u, w, acc, tok, q=q), a.desc()
+    st = torch.cuda.Stream()
+    h = wt.Handle([])
+    torch.cuda.synchronize()
+    finish = capturing(torch, mode)
+    try:
+        h.verify(desc, st.cuda_stream)
+        h.attend(da, st.cuda_stream)
+        h.close()
+    finally:
+        ok = finish()
+    assert ok == [True]
+    torch.cuda.synchronize()
+    assert (acc.tolist(), tok.tolist()) == want
+    a.check(torch, wa)
