@@ -653,7 +653,6 @@ int prepare_device(int dev) {
     CU(wt::gemm_cols_umma_prepare());
     CU(wt::gemm_q8_rows_prepare());
     CU(wt::gemm_short_prepare());
-    CU(wt::serve_prepare());
     g_prepared[dev] = true;
   }
   return WT_OK;
@@ -2366,9 +2365,24 @@ int wt::serve_error(int code, const char *fmt, ...) {
   return set_err(code, "%s", buf);
 }
 
+int wt::serve_prepare(int device, ServeKernels k) {
+  static std::atomic<bool> ready[64][kServeKernels];
+  if (device < 64 && ready[device][k].load(std::memory_order_acquire)) return WT_OK;
+  std::lock_guard<std::mutex> g(g_prep_mu);
+  const Relax relax;  // the first call may be in a capture
+  if (k == kServeAdapt) CU(adapt_prepare());
+  if (k == kServeAttend) {
+    CU(attend_prepare());
+    CU(prefix_prepare());
+  }
+  if (k == kServeDraw) CU(draw_prepare());
+  if (device < 64) ready[device][k].store(true, std::memory_order_release);
+  return WT_OK;
+}
+
 int wt::serve_cuda_error(cudaError_t e, const char *what) { return cuda_err(e, what); }
 
-int wt::serve_context(wt_handle *h, const char *call, ServeContext *out) {
+int wt::serve_context(wt_handle *h, const char *call, ServeKernels kernels, ServeContext *out) {
   if (!h) return set_err(WT_EINVAL, "%s: NULL handle", call);
   if (h->host_only) return set_err(WT_ENOTSUP, "%s: handle was opened host-only", call);
   // A thread that has made no runtime call yet has no current context.  The driver's own calls need one: the
@@ -2381,7 +2395,7 @@ int wt::serve_context(wt_handle *h, const char *call, ServeContext *out) {
     bound = true;
   }
   *out = {h->device, h->status};
-  return WT_OK;
+  return serve_prepare(h->device, kernels);
 }
 
 bool wt::serve_inside_mapping(const wt_handle *h, const void *p, uint64_t n) {

@@ -176,7 +176,7 @@ int check_adapt_overlap(const wt::AdaptLaunch &L) {
 
 int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
   wt::ServeContext ctx;
-  CHECK(wt::serve_context(h, "wt_adapt", &ctx));
+  CHECK(wt::serve_context(h, "wt_adapt", wt::kServeAdapt, &ctx));
   if (n && !d) return serve_error(WT_EINVAL, "wt_adapt: NULL descriptors");
   wt::ServeRanges seen;
   for (size_t i = 0; i < n; ++i) CHECK(check_adapt(h, seen, d[i], i));
@@ -386,7 +386,7 @@ int plan_prefix(const wt_attend_desc &d, int G, wt::PrefixPlan *x, wt::PrefixMap
 
 int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
   wt::ServeContext ctx;
-  CHECK(wt::serve_context(h, "wt_attend", &ctx));
+  CHECK(wt::serve_context(h, "wt_attend", wt::kServeAttend, &ctx));
   if (!dp) return serve_error(WT_EINVAL, "wt_attend: NULL descriptor");
   CHECK(check_attend(h, *dp));
   wt::AttendPlan P = {};
@@ -455,7 +455,7 @@ int probs_impl(wt_handle *h, const wt_probs_desc *d, cudaStream_t s) {
   const char *call = "wt_probs";
   wt::ServeRanges seen;
   wt::ServeContext ctx;
-  CHECK(wt::serve_context(h, call, &ctx));
+  CHECK(wt::serve_context(h, call, wt::kServeDraw, &ctx));
   if (!d) return serve_error(WT_EINVAL, "%s: NULL descriptor", call);
   if (d->rows < 0 || d->rows > (1 << 27) || d->vocab < 0 || d->vocab > (1 << 30) || d->ldl < d->vocab || d->ldp < d->vocab ||
       d->ldl > kMaxPitch || d->ldp > kMaxPitch)
@@ -476,7 +476,7 @@ int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {
   const char *call = "wt_verify";
   wt::ServeRanges seen;
   wt::ServeContext ctx;
-  CHECK(wt::serve_context(h, call, &ctx));
+  CHECK(wt::serve_context(h, call, wt::kServeDraw, &ctx));
   if (!d) return serve_error(WT_EINVAL, "%s: NULL descriptor", call);
   if (d->n_req < 0 || d->n_req > (1 << 24) || d->n_drafted < 0 || d->n_drafted > kMaxSize || d->max_draft < 0 || d->max_draft > (1 << 20) || d->vocab < 1 ||
       d->vocab > WT_VERIFY_MAX_VOCAB || d->ldp < d->vocab || d->ldp > kMaxPitch ||
@@ -506,14 +506,6 @@ int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {
 }
 
 }  // namespace
-
-cudaError_t wt::serve_prepare() {
-  cudaError_t e = adapt_prepare();
-  if (e == cudaSuccess) e = attend_prepare();
-  if (e == cudaSuccess) e = prefix_prepare();
-  if (e == cudaSuccess) e = draw_prepare();
-  return e;
-}
 
 #pragma GCC visibility push(default)
 extern "C" {

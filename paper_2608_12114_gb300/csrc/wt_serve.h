@@ -16,8 +16,12 @@ struct ServeContext {
   int device;
   int *status;  // device status word
 };
-// Refuses NULL and host-only handles.
-int serve_context(wt_handle *h, const char *call, ServeContext *out);
+// Kernels whose one-time attributes are set by the first call that may launch them (all of them in wt_open
+// took 1.7 of a process's first 20 ms).
+enum ServeKernels { kServeAdapt, kServeAttend, kServeDraw, kServeKernels };
+int serve_prepare(int device, ServeKernels k);
+// Refuses NULL and host-only handles, and prepares the call's kernels.
+int serve_context(wt_handle *h, const char *call, ServeKernels kernels, ServeContext *out);
 bool serve_inside_mapping(const wt_handle *h, const void *p, uint64_t n);
 // Device allocations that a call has met: its small buffers often share one, and each look-up costs
 // the driver's time.
@@ -45,8 +49,6 @@ int serve_tensor_map(void *out, const void *base, int rank, const uint64_t *dims
                      const uint32_t *box);
 int serve_error(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 int serve_cuda_error(cudaError_t e, const char *what);
-
-cudaError_t serve_prepare();  // one-time function attributes of every kernel below
 
 // ---------------------------------------------------------------- wt_adapt.cu
 constexpr int kAdaptProjs = 8;  // projections of one launch

@@ -1,5 +1,8 @@
 """How a program makes the serving calls: from threads and streams, into graphs, many at a time, again and again."""
 import ctypes as C
+import os
+import subprocess
+import sys
 import threading
 import time
 
@@ -220,3 +223,42 @@ def test_a_handle_used_and_closed_while_another_thread_captures(torch, mode):
     torch.cuda.synchronize()
     assert (acc.tolist(), tok.tolist()) == want
     a.check(torch, wa)
+
+
+FIRST = """
+import sys, torch
+from paper_2608_12114_gb300 import serving, wt
+from tests.test_gpu_serve_adapt import make
+from tests.test_gpu_serve_attend import Set
+from tests.test_gpu_serve_draw import drafts
+x, y, slot, A, B, scale, base = make(torch, 300, 64, 32, 2, 8, torch.bfloat16)
+s = Set(torch, [2] * 20, [9] * 20, 900, 4, 2, 64)
+l, p = torch.randn(3, 50021, device="cuda"), torch.empty(3, 50021, device="cuda")
+v = drafts(torch, [2, 1], 500, 1.0, False)
+acc, tok = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(2, 3, dtype=torch.int32, device="cuda")
+ds = dict(adapt=[serving.adapters(x, y, slot, A, B, scale, base=base)], attend=s.desc(), probs=serving.probabilities(l, p),
+          verify=serving.verification(v[0], v[2], v[3], v[4], v[5], acc, tok, q=v[1]))
+outs = (y, s.out, p, acc, tok)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with wt.Handle([]) as h:
+    with torch.cuda.graph(g):
+        for name, d in ds.items():
+            getattr(h, name)(d, torch.cuda.current_stream().cuda_stream)
+    g.replay()
+    torch.cuda.synchronize()
+    first = [t.clone() for t in outs]
+    for name, d in ds.items():
+        getattr(h, name)(d)
+    torch.cuda.synchronize()
+    assert h.device_status() == 0
+    assert all(torch.equal(a, b) for a, b in zip(first, outs)) and not any(torch.isnan(t.float()).any() for t in outs)
+print("same")
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured(torch):
+    """No warm-up: kernels are loaded and made ready inside the capture."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST], cwd=root, capture_output=True, text=True, timeout=240)
+    assert r.returncode == 0 and r.stdout.strip().endswith("same"), r.stderr[-2000:]
