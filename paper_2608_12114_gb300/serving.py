@@ -10,8 +10,8 @@ One step of several requests over one set of weights, beside Handle.pass_:
 
 Each function here checks types, shapes and strides and returns the C descriptor, which holds the
 tensors it points at; the values in them (lengths, slots, tokens) may change from step to step, so
-a program makes its descriptors once and calls with them every step.  PyTorch supplies device memory
-and streams only.
+a program makes its descriptors once and calls with them every step (wt.adapt_array keeps several
+for one call).  PyTorch supplies device memory and streams only.
 """
 from __future__ import annotations
 

@@ -73,6 +73,14 @@ class AdaptDesc(C.Structure):
                 ("R", C.c_int32)]
 
 
+def adapt_array(descs):
+    """An array of AdaptDesc for Handle.adapt, made once for a step that repeats.  It holds the
+    descriptors that it copies, and so the tensors that they point at."""
+    a = (AdaptDesc * len(descs))(*descs)
+    a.descs = list(descs)
+    return a
+
+
 class AttendDesc(C.Structure):
     """wt_attend_desc (serving.attention makes one from tensors)."""
     _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("begin", C.c_void_p), ("prefix_k", C.c_void_p),
@@ -348,8 +356,8 @@ class Handle:
             _check(rc)
 
     def adapt(self, descs, stream: int = 0):
-        """wt_adapt over a list of AdaptDesc, or a ctypes array of them (which a step that repeats
-        keeps: (AdaptDesc * n)(*descs) copies every descriptor)."""
+        """wt_adapt over a list of AdaptDesc, or over adapt_array's array of them, which a step that
+        repeats keeps: it spares copying every descriptor."""
         n = len(descs)
         if n == 1:
             descs = C.byref(descs[0])

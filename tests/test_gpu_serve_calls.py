@@ -1,5 +1,6 @@
 """How a program makes the serving calls: from threads and streams, into graphs, many at a time, again and again."""
 import ctypes as C
+import gc
 import os
 import subprocess
 import sys
@@ -262,3 +263,23 @@ def test_the_first_calls_of_a_process_may_be_captured(torch):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST], cwd=root, capture_output=True, text=True, timeout=240)
     assert r.returncode == 0 and r.stdout.strip().endswith("same"), r.stderr[-2000:]
+
+
+def test_an_array_of_descriptors_keeps_its_tensors(torch, h):
+    x, y, slot, A, B, scale, base = make(torch, 12, 64, 40, 3, 8, torch.bfloat16)
+    want = _serve.adapt(x, slot, A, B, scale, None, base)
+
+    def step():
+        y2 = [y.clone(), y.clone()]
+        a = wt.adapt_array([serving.adapters(x.clone(), t, slot.clone(), A.clone(), B.clone(), scale.clone(), base=base.clone())
+                            for t in y2])
+        return a, y2
+
+    a, ys = step()
+    gc.collect()
+    junk = [torch.full((1 << 16,), _serve.NAN, device="cuda") for _ in range(64)]
+    h.adapt(a)
+    torch.cuda.synchronize()
+    assert len(a) == 2 and len(junk) == 64
+    for t in ys:
+        close(torch, t, want, 64, 8)
