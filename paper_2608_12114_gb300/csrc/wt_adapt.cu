@@ -923,14 +923,19 @@ constexpr size_t shrink_smem() {
 template <int DT, int MT>
 cudaError_t run_few(const AdaptLaunch &L, int *status, cudaStream_t s) {
   uint32_t items = 0;
-  for (int i = 0; i < L.n; ++i) items += L.p[i].items;
+  int64_t tokens = 0, slots = 0;
+  for (int i = 0; i < L.n; ++i) {
+    items += L.p[i].items;
+    tokens += L.p[i].d.T;
+    slots += L.p[i].d.S;
+  }
   if (items == 0) return cudaSuccess;
   // 48 tokens of 24 adapters through three projections: 11.7 us in clusters of 4 (432 CTAs), 18.4 of 8;
   // one token 5.8 us in a cluster of 8, 7.2 of 4.  Above rank 32 an SM holds one CTA, but the number of
-  // items is a bound, which is near only where slots have several tokens each (106 tokens of 4 adapters
-  // of rank 64: 18 us in clusters of 4, 26 of 8; 34 tokens of up to 38 adapters, in fact 4: 20 and 14).
-  const wt_adapt_desc &d = L.p[0].d;
-  const int per_sm = MT <= 2 ? 3 : d.T >= 4 * d.S ? 1 : 2;
+  // items is a bound, which is near only where slots have several tokens each, over all projections (106
+  // tokens of 4 adapters of rank 64: 18 us in clusters of 4, 26 of 8; 34 tokens of up to 38 adapters, in
+  // fact 4: 20 and 14).
+  const int per_sm = MT <= 2 ? 3 : tokens >= 4 * slots ? 1 : 2;
   int c = kMostCluster;
   while (c > 2 && (int64_t)items * c > per_sm * num_sms()) c /= 2;
   return launch(adapt_kernel<DT, MT>, items * (unsigned)c, kThreads, c, few_smem<MT>(most_slots(L)), false, s, L, status);

@@ -283,3 +283,18 @@ def test_an_array_of_descriptors_keeps_its_tensors(torch, h):
     assert len(a) == 2 and len(junk) == 64
     for t in ys:
         close(torch, t, want, 64, 8)
+
+
+def test_the_order_of_projections_changes_nothing(torch, h):
+    """A launch's clusters, and with them the order of the sums, go by all its projections, not by the first."""
+    sets = [make(torch, T, 512, 64, S, 64, torch.bfloat16, seed=T) for T, S in ((1, 1), (250, 20))]
+
+    def call(order):
+        for i in order:
+            sets[i][1].fill_(_serve.NAN)
+        h.adapt([serving.adapters(x, y, s, A, B, c, base=b) for x, y, s, A, B, c, b in (sets[i] for i in order)])
+        torch.cuda.synchronize()
+        return [sets[i][1].clone() for i in (0, 1)]
+
+    for a, b in zip(call((0, 1)), call((1, 0))):
+        assert torch.equal(a, b)
