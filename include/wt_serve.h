@@ -28,7 +28,9 @@
  *     rank) or treats its element as absent (a page, a slot, a drafted token), reads and writes
  *     nothing outside the descriptor's buffers, and records WT_EINVAL in the handle's status word
  *     (wt_device_status) if nothing was recorded there before.
- *   - Results are deterministic: no floating-point atomics, and no result depends on timing.
+ *   - Results are deterministic: no floating-point atomics, and no result depends on timing.  A
+ *     token's last bits may depend on what else a call holds: how its sums are split over CTAs
+ *     follows the numbers of tokens, slots and keys.  (wt_verify's tokens never do.)
  */
 #ifndef WT_SERVE_H_
 #define WT_SERVE_H_

@@ -298,3 +298,77 @@ def test_the_order_of_projections_changes_nothing(torch, h):
 
     for a, b in zip(call((0, 1)), call((1, 0))):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dt", ["bfloat16", "float16"])
+def test_many_tokens_through_many_projections(torch, h, dt):
+    """More projections than a launch takes, of several slot maps, lengths and ranks, some in place."""
+    sets = []
+    for i in range(11):
+        T = (300, 300, 270, 5)[i % 4]
+        x, y, slot, A, B, scale, base = make(torch, T, 72 + 8 * i, 50 + i, 3 + i % 2, 1 + 5 * i, getattr(torch, dt), seed=i)
+        if i % 4 == 1:  # the map of the one before
+            slot = sets[-1][2] if sets[-1][3].shape[0] >= A.shape[0] else slot
+        if i % 3 == 2:
+            y = base.clone()
+        sets.append((x, y, slot, A, B, scale, base, i % 3 == 2))
+    want = [_serve.adapt(x, s, A, B, c, None, b) for x, y, s, A, B, c, b, _ in sets]
+    for _ in range(2):
+        for x, y, s, A, B, c, b, inplace in sets:
+            y.copy_(b) if inplace else y.fill_(_serve.NAN)
+        h.adapt([serving.adapters(x, y, s, A, B, c, base=None if inplace else b) for x, y, s, A, B, c, b, inplace in sets])
+        torch.cuda.synchronize()
+        for (x, y, s, A, B, c, b, _), r in zip(sets, want):
+            close(torch, y, r, x.shape[1], A.shape[1])
+
+
+def test_a_batch_that_takes_small_clusters(torch, h):
+    """48 tokens of 32 slots through three projections: A x is split otherwise than for one token, so bits
+    may differ, but no more than the order of the sums."""
+    sets = [make(torch, 48, 512, M, 32, 32, torch.bfloat16, seed=3) for M in (256, 64, 64)]
+    x, _, slot, _, _, _, _ = sets[0]
+    descs = [serving.adapters(x, y, slot, A, B, c, base=b) for _, y, _, A, B, c, b in sets]
+    h.adapt(descs)
+    torch.cuda.synchronize()
+    for _, y, _, A, B, c, b in sets:
+        want = _serve.adapt(x, slot, A, B, c, None, b)
+        close(torch, y, want, 512, 32)
+        one = torch.full_like(y, _serve.NAN)
+        for t in range(48):
+            h.adapt([serving.adapters(x[t:t + 1], one[t:t + 1], slot[t:t + 1], A, B, c, base=b[t:t + 1])])
+        torch.cuda.synchronize()
+        close(torch, one, want, 512, 32)
+
+
+@pytest.mark.parametrize("new,lens,P", [([300], [300], 0), ([257, 1, 190], [400, 9, 190], 0), ([200, 150], [210, 150], 140)])
+def test_prompts(torch, h, new, lens, P):
+    s = Set(torch, new, lens, P, 4, 2, 64)
+    want = s.want()
+    h.attend(s.desc())
+    torch.cuda.synchronize()
+    s.check(torch, want)
+
+
+@pytest.mark.parametrize("new,lens,P", [([1], [37], 500), ([1] * 24, [900 - 30 * i for i in range(24)], 6000), ([3] * 20, [200] * 20, 3000)])
+def test_calls_repeat_themselves(torch, h, new, lens, P):
+    s = Set(torch, new, lens, P, 8, 2, 128)
+    h.attend(s.desc())
+    first = s.out.clone()
+    for _ in range(30):
+        s.out.fill_(_serve.NAN)
+        h.attend(s.desc())
+        assert torch.equal(s.out, first)
+
+
+def test_a_later_draft_changes_nothing_before_it(torch, h):
+    s = Set(torch, [6], [50], 40, 4, 2, 64)
+    h.attend(s.desc())
+    first, k, v = s.out.clone(), s.k.clone(), s.v.clone()
+    for j in range(45, 50):
+        s.k.copy_(k), s.v.copy_(v)
+        at = s.table[0, j // 16]
+        s.k[at, j % 16], s.v[at, j % 16] = 3.0, -5.0
+        h.attend(s.desc())
+        torch.cuda.synchronize()
+        assert torch.equal(s.out[:j - 44], first[:j - 44])
+        assert not torch.equal(s.out[j - 44:], first[j - 44:])
