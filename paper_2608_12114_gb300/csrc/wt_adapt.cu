@@ -18,8 +18,7 @@
 
 #include <cooperative_groups.h>
 
-#include "wt_device.cuh"
-#include "wt_serve.h"
+#include "wt_serve.cuh"
 
 namespace wt {
 
@@ -30,7 +29,6 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 256;
 constexpr int kWarps = 8;
 constexpr int kMostCluster = 8;
-constexpr int kStatusInvalid = -1;
 
 __device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
@@ -90,9 +88,6 @@ __device__ __forceinline__ uint4 load8_shifted(const uint16_t *row, int k, int n
 __device__ __forceinline__ uint4 keep8(const uint4 &v, int keep) {
   return keep >= 8 ? v : and4(v, byte_mask(0, 2 * keep));
 }
-
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 struct Item {
   int slot;   // S: tokens without an adapter
@@ -558,12 +553,6 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void *src) {
 }
 __device__ __forceinline__ void sts128(uint32_t dst, const uint4 &v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t a) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(a)
-               : "memory");
 }
 
 // MT: 16-row tiles of the rank, as for adapt_kernel.  A warp takes 16 tokens.

@@ -6,8 +6,7 @@
 // shared memory.
 #include <cooperative_groups.h>
 
-#include "wt_device.cuh"
-#include "wt_serve.h"
+#include "wt_serve.cuh"
 
 namespace wt {
 
@@ -15,7 +14,6 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kStatusInvalid = -1;  // WT_EINVAL
 constexpr int kMaxCluster = 8;
 
 __device__ __forceinline__ void note_invalid(int *status) {
@@ -37,9 +35,6 @@ __device__ __forceinline__ unsigned long long warp_sum(unsigned long long v) {
   for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 // The part of a row of n elements that CTA c of C takes: whole groups of 4 elements, evenly.
 __device__ __forceinline__ void row_part(int n, int c, int C, int &lo, int &hi) {
@@ -71,8 +66,7 @@ struct RowPart {
 
 // 2^(2 x): the square keeps subnormal results, without the tests that the function's own way takes.
 __device__ __forceinline__ float exp2_twice(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  const float y = exp2_approx(x);
   return y * y;
 }
 

@@ -30,8 +30,7 @@
 // Every mbarrier wait is bounded; a timeout records WT_ETIMEDOUT and every role stops.
 #include <cuda.h>
 
-#include "wt_device.cuh"
-#include "wt_serve.h"
+#include "wt_serve.cuh"
 
 namespace wt {
 
@@ -126,11 +125,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t a, const uint32_t *r) {
       : "memory");
 }
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -144,26 +138,6 @@ __device__ __forceinline__ void fma_x2(float &x0, float &x1, float s, float c) {
       : "+f"(x0), "+f"(x1)
       : "f"(s), "f"(c));
 }
-template <int DT>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  uint32_t r;
-  if constexpr (DT == WT_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-
-template <int DT>
-__device__ __forceinline__ void unpack2(uint32_t w, float &lo, float &hi) {
-  if constexpr (DT == WT_BF16) {
-    lo = __uint_as_float(w << 16);
-    hi = __uint_as_float(w & 0xffff0000u);
-  } else {
-    asm("{\n\t.reg .f16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.f32.f16 %0, x;\n\tcvt.f32.f16 %1, y;\n\t}"
-        : "=f"(lo), "=f"(hi)
-        : "r"(w));
-  }
-}
-
 // A bounded wait of a whole warp: every lane gets the same answer, so a warp whose wait runs out
 // leaves together.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status) {
@@ -442,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
           fence_after();
-          const float f = grown ? ex2(m - (top - kBelow<DT>)) : 1.0f;
+          const float f = grown ? exp2_approx(m - (top - kBelow<DT>)) : 1.0f;
           if (grown) m = top - kBelow<DT>;
           l0 *= f;
           l1 *= f;
@@ -464,8 +438,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int k = 0; k < 64; k += 2) {
             const int c = hf * 64 + k;
             fma_x2(v[c], v[c + 1], P.scale_log2, -ref);
-            v[c] = ex2(v[c]);
-            v[c + 1] = ex2(v[c + 1]);
+            v[c] = exp2_approx(v[c]);
+            v[c + 1] = exp2_approx(v[c + 1]);
             u[k / 2] = pack2<DT>(v[c], v[c + 1]);
             float r0, r1;
             unpack2<DT>(u[k / 2], r0, r1);
