@@ -459,11 +459,10 @@ __global__ void __launch_bounds__(kThreads, MT <= 2 ? 2 : 1) adapt_kernel(const 
 // slot.  adapt_shrink_kernel computes v = scale A x of an item, a cluster of 4 or 8 CTAs splitting K, with
 // x and A staged in shared memory by 16-byte cp.async.  adapt_expand_kernel adds B v, a CTA taking
 // several tiles of 64 tokens x 64 outputs of an item, with the base and B of the next tile always on
-// their way to shared memory.  Measured for 4001 tokens of two projections of 6912 outputs, ranks up to
-// 64: in one launch, as for few tokens, 350 us; three launches 175, of which the expand kernel took 152
-// (each tile waited for its base) or 166 (base ahead, B into registers as needed: each tile waited for
-// L2 twice); both ahead through shared memory, 8 warps 124, 16 warps 107, three CTAs of 8 warps 82 of
-// 111 in all.  Base to y alone, as torch copies it, takes 85.
+// their way to shared memory.  Measured for 4001 f16 tokens of two projections of 6912 outputs, ranks up to
+// 64: 111 us, of which the expand kernel takes 82 (base to y alone, as torch copies it, 85); in one launch,
+// as for few tokens, 350.  bf16 takes 130, as its third part of v leaves room for two CTAs to an SM at
+// ranks 33 to 64, and 104 at ranks up to 32; f16 at ranks up to 128, one CTA to an SM, 156.
 //
 // v crosses between the two as 16-bit parts that add up to it, so that the second product's operands
 // need no conversion: bf16 in three parts (24 bits); f16 in two (22 bits), after a power of two for
@@ -473,7 +472,7 @@ constexpr int kItem = 64;     // tokens of an item
 constexpr int kMTile = kAdaptMTile;   // outputs of a tile of the expand kernel
 constexpr int kPlanThreads = 1024;
 static_assert(kPlanThreads == 32 * 32, "a lane for each warp");
-constexpr int kEThreads = 256;  // the expand kernel, three to an SM: products run while other CTAs wait for a tile
+constexpr int kEThreads = 256;  // the expand kernel, up to three to an SM: products run while other CTAs wait for a tile
 constexpr int kEAcross = kMTile / 32;  // warps side by side in a tile
 constexpr int kSThreads = 128;
 constexpr int kSK = 64;       // elements of K of a stage
@@ -723,7 +722,7 @@ __global__ void __launch_bounds__(kSThreads) adapt_shrink_kernel(const __grid_co
 }
 
 // Shared memory of the expand kernel: a ring of tiles (base, 4 vectors that only their thread reads;
-// then the 128 rows of B), and the item's v.
+// then the kMTile rows of B), and the item's v.  Three CTAs fit an SM up to rank 32, and to rank 64 in f16.
 template <int DT, int MT>
 struct Expand {
   static constexpr int stages = 2;

@@ -15,7 +15,7 @@
 // them.  The rows of absent keys arrive as zeros and their scores are masked, so what a page holds past
 // its last key never reaches a product.  No warp waits for another before the end.  Bound: HBM (or
 // L2) for up to 32 rows, latency for few keys: 134 MB of own keys of 64 requests (lengths up to 1024)
-// take 37 us, 3.6 TB/s over all and 7 while every SM has long ones; 44 MB of 24 requests 15 us.
+// take 38 us, 3.6 TB/s over all and 7 while every SM has long ones; 44 MB of 24 requests 16 us.
 #include <algorithm>
 
 #include "wt_serve.cuh"

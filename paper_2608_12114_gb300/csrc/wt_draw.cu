@@ -64,7 +64,10 @@ struct RowPart {
   int first;  // first index of m
 };
 
-// 2^(2 x): the square keeps subnormal results, without the tests that the function's own way takes.
+// 2^(2 x): the square keeps subnormal results, without the tests that the function's own way takes, at twice
+// its relative error, 2^-21 at most.  A probability is off by that, by its sum's (the same and the additions'),
+// and by 3 2^-24 ln 2 of its exponent for the roundings of x: over 257 rows of 128256 6.5e-8 in the 2-norm,
+// elementary fp32 operations 8.4e-8.
 __device__ __forceinline__ float exp2_twice(float x) {
   const float y = exp2_approx(x);
   return y * y;

@@ -227,7 +227,8 @@ int adapt_impl(wt_handle *h, const wt_adapt_desc *d, size_t n, cudaStream_t s) {
     wt::AdaptWide W = {};
     int64_t items = 0, v = 0, back = 0;
     const int64_t row = 16 * wt::adapt_rank_tiles(max_R), parts = dtype == WT_BF16 ? 3 : 2;
-    // tiles of outputs that a CTA takes one after another: about three waves of three CTAs per SM in all
+    // tiles of outputs that a CTA takes one after another: about nine CTAs per SM in all, three waves of three
+    // where three fit an SM
     const int64_t run = std::max<int64_t>(1, ceil_div((int64_t)all, 9 * wt::num_sms()));
     for (int k = 0; k < L.n; ++k) {
       const wt_adapt_desc &e = L.p[k].d;
