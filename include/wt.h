@@ -393,8 +393,8 @@ int wt_kernel_launches(const wt_handle *h, uint64_t *n);
 
 /* Objects the library holds right now, over all handles of the process: open handles,
  * cached launch plans, CUDA events it created, and the device and pinned host bytes it
- * allocated itself and has handed out (status words, plan tables, split-K workspaces, the
- * staged ring).  Buffers the caller owns are not counted.  After wt_close of every handle
+ * allocated itself and has handed out (status words, plan tables, split-K and serving
+ * workspaces, the staged ring).  Buffers the caller owns are not counted.  After wt_close of every handle
  * these five return to their earlier values (Sec. 5.1: a producer's lifetime leaves nothing
  * behind; the 200-cycle checks read these), except that the first staged adopt on a device
  * adds its ring for good: 4 events and 268,435,456 pinned bytes.
