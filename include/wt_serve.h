@@ -2,13 +2,15 @@
  * wt_serve — one step of many requests over one set of weights.  C ABI.
  *
  * wt_pass (wt.h) streams a checkpoint's matrices for up to 16 activation columns.  A program that
- * answers several requests with them needs four more things beside that pass, every step:
+ * answers several requests with them needs six more things beside that pass, every step:
  *
- *   wt_adapt   each request's low-rank adapter beside a projection all requests share;
- *   wt_attend  attention over a prefix that all requests share, read once for all of them, and
- *              over each request's own paged cache;
- *   wt_probs   fp32 logits (wt_pass's y over the head) to probabilities at a temperature;
- *   wt_verify  drafted tokens against the target's probabilities, from given random numbers.
+ *   wt_adapt     each request's low-rank adapter beside a projection all requests share;
+ *   wt_place     the projections' rows to normed and rotated queries, and keys and values in their pages;
+ *   wt_attend    attention over a prefix that all requests share, read once for all of them, and
+ *                over each request's own paged cache;
+ *   wt_probs     fp32 logits (wt_pass's y over the head) to probabilities at a temperature;
+ *   wt_logprobs  log probabilities of given tokens, entropy and the likeliest tokens of such logits;
+ *   wt_verify    drafted tokens against the target's probabilities, from given random numbers.
  *
  * Conventions are those of wt.h: int status codes and wt_last_error, void* streams, caller-owned
  * device memory, no C++ exception across the boundary.  Besides:
@@ -79,6 +81,61 @@ typedef struct {
  * its device allocation, y inside a mapping), WT_ENOTSUP (dtype, host-only handle), WT_ECUDA. */
 int wt_adapt(wt_handle *h, const wt_adapt_desc *d, size_t n, void *stream);
 
+/* ---- wt_place -------------------------------------------------------------------------------
+ * What stands between the projections and wt_attend, in one pass over their rows.  For token i of
+ * request b (row t = begin[b] + i), each head of q and k goes
+ *
+ *   y  = x * w / sqrt(mean(x^2) + eps)          where q_norm (k_norm) gives w, over the whole head
+ *   (y0, y1) <- (y0 cos a - y1 sin a, y1 cos a + y0 sin a)   for pair j of the first rot_dim elements
+ *
+ * and is rounded once: q to q_out[t], k and (unchanged) v to the caches' row of the token's place
+ * len[b] - n_b + i, which wt_attend finds again: row place % page of page table[b, place / page].
+ * Any of q, k and v may be NULL (with its output): then it is not looked at.  q alone needs no pages.
+ *
+ * Pair j is elements j and j + rot_dim / 2, or with WT_PLACE_NEIGHBOURS 2j and 2j + 1.  Its angle is
+ * pos * 2 pi * turns[j] / 2^64: turns[j] holds the turns that a position adds, modulo one, as a fraction
+ * in 64 bits, so the angle is exact modulo a turn at any position (2^64 f / 2 pi for f radians a position;
+ * serving.turns).  pos is the token's own position on axis[j] of the axes of `pos` (time, height, width),
+ * or without `pos` first_pos + place.
+ *
+ * The rows are fp32 (as wt_pass and wt_adapt leave them) or of the caches' type; sums and products are
+ * fp32.  Rows of tokens that no request holds are left as they are; without `begin` (q alone, with pos or
+ * without rotation) every row counts.  A token whose place is negative (more new tokens than len) or whose
+ * page is out of range is not cached, and WT_EINVAL recorded; its query is made all the same.  Where two
+ * new tokens share a place (one page in the tables of two requests) either may stand there.
+ *
+ * head_dim is a multiple of 8 up to 256, rot_dim one up to head_dim; heads and kv_heads go up to 65536;
+ * n_tokens, max_len and first_pos up to 2^30.  Pointers to rows and pages lie on 16-byte boundaries and
+ * their strides are multiples of 8 elements.  q_out may be q (of one type, at its pitch); otherwise no
+ * output may overlap an input or another output, as rows of tokens. */
+#define WT_PLACE_MAX_DIM 256
+#define WT_PLACE_MAX_AXES 8
+#define WT_PLACE_NEIGHBOURS 1 /* a flag */
+typedef struct {
+  const void *q;            /* [n_tokens, heads, head_dim], token pitch q_stride elements */
+  const void *k, *v;        /* [n_tokens, kv_heads, head_dim], token pitches k_stride and v_stride */
+  void *q_out;              /* [n_tokens, heads, head_dim], token pitch out_stride */
+  void *k_pages, *v_pages;  /* [n_pages, page, kv_heads, head_dim], dense */
+  const void *q_norm, *k_norm; /* [head_dim] of norm_dtype; NULL: no norm */
+  const int32_t *begin;     /* [n_req + 1]: first token of each request, ascending, begin[n_req] <= n_tokens */
+  const int32_t *table;     /* [n_req, pages of max_len keys] page numbers, row pitch table_stride */
+  const int32_t *len;       /* [n_req] own keys, the new tokens' included; <= max_len */
+  const uint64_t *turns;    /* [rot_dim / 2] */
+  const int32_t *pos;       /* [n_tokens, axes], row pitch pos_stride, or NULL */
+  int64_t q_stride, k_stride, v_stride, out_stride, table_stride, pos_stride;
+  int32_t in_dtype;         /* of q, k, v: WT_F32 or dtype */
+  int32_t dtype;            /* WT_BF16 or WT_F16 */
+  int32_t norm_dtype;       /* WT_F32, WT_BF16 or WT_F16 */
+  int32_t n_req, n_tokens, heads, kv_heads, head_dim, rot_dim, axes;
+  int32_t page, n_pages, max_len, first_pos, flags;
+  float eps;                /* >= 0 */
+  uint8_t axis[WT_PLACE_MAX_DIM / 2]; /* of each pair, < axes */
+} wt_place_desc;
+
+/* Errors: WT_EINVAL (NULL, sizes, alignment, strides, an output inside a mapping or over an input, a buffer
+ * that runs past its device allocation), WT_ENOTSUP (dtype, head_dim, host-only handle), WT_ECUDA. */
+int wt_place(wt_handle *h, const wt_place_desc *d, void *stream);
+
 /* ---- wt_attend ------------------------------------------------------------------------------
  * Token i of request b (row t = begin[b] + i of q, i < n_b = begin[b + 1] - begin[b]) attends to the
  * whole shared prefix and to its request's own keys 0 .. len[b] - n_b + i (its own key included: the
@@ -140,6 +197,36 @@ typedef struct {
 
 /* Errors: WT_EINVAL, WT_ENOTSUP (host-only handle), WT_ECUDA. */
 int wt_probs(wt_handle *h, const wt_probs_desc *d, void *stream);
+
+/* ---- wt_logprobs ----------------------------------------------------------------------------
+ * Of the distribution p that wt_probs gives a row, from one reading of its logits:
+ *
+ *   given_lp[r, i] = log p[r, given[r, i]]     (given negative: no token, 0)
+ *   entropy[r]     = -sum p log p
+ *   top[r, i]      the i-th largest logit's token, of equal logits the first token first; top_lp its log p
+ *
+ * A token of probability 0 has -infinity.  top lists no NaN and no logit of -infinity; where a row has
+ * fewer others than n_top the rest is token -1 with -infinity.  A row with temp <= 0 is certain of its
+ * first largest logit (0 for it, -infinity for all others, entropy 0); top still goes by the logits.  A
+ * row of -infinity alone has -infinity everywhere and entropy 0; a row that wt_probs makes NaN has NaN
+ * (its tokens in top are those of its largest logits).  A given token past the vocabulary counts as none,
+ * and WT_EINVAL is recorded.  given, entropy and top may each be NULL.  Outputs are dense and must not
+ * overlap the inputs or each other. */
+#define WT_LOGPROBS_MAX_TOP 32
+typedef struct {
+  const float *logits;   /* [rows, vocab], row pitch ldl */
+  const float *temp;     /* [rows], or NULL: 1 */
+  const int32_t *given;  /* [rows, n_given], row pitch given_stride */
+  float *given_lp;       /* [rows, n_given] */
+  float *entropy;        /* [rows] */
+  int32_t *top;          /* [rows, n_top] */
+  float *top_lp;         /* [rows, n_top] */
+  int64_t ldl, given_stride;
+  int32_t rows, vocab, n_given, n_top;
+} wt_logprobs_desc;
+
+/* Errors: WT_EINVAL, WT_ENOTSUP (host-only handle), WT_ECUDA. */
+int wt_logprobs(wt_handle *h, const wt_logprobs_desc *d, void *stream);
 
 /* ---- wt_verify ------------------------------------------------------------------------------
  * Request b drafted n_b = begin[b + 1] - begin[b] tokens.  Row begin[b] + b + i of p holds the

@@ -473,6 +473,161 @@ int probs_impl(wt_handle *h, const wt_probs_desc *d, cudaStream_t s) {
   return launch_alone(h, s, [&] { return wt::launch_probs(*d, ctx.status, s); });
 }
 
+int check_place(wt_handle *h, const wt_place_desc &d) {
+  const char *call = "wt_place";
+  wt::ServeRanges seen;
+  if (d.dtype != WT_BF16 && d.dtype != WT_F16)
+    return serve_error(d.dtype >= WT_F32 && d.dtype <= WT_U8 ? WT_ENOTSUP : WT_EINVAL,
+                       "%s: dtype %d: caches and q_out are bf16 or f16", call, d.dtype);
+  if (d.in_dtype != WT_F32 && d.in_dtype != d.dtype)
+    return serve_error(d.in_dtype >= WT_F32 && d.in_dtype <= WT_U8 ? WT_ENOTSUP : WT_EINVAL,
+                       "%s: in_dtype %d: q, k and v are fp32 or of the caches' type", call, d.in_dtype);
+  const bool kv = d.k || d.v, norms = d.q_norm || d.k_norm;
+  if (norms && d.norm_dtype != WT_F32 && d.norm_dtype != WT_BF16 && d.norm_dtype != WT_F16)
+    return serve_error(d.norm_dtype >= WT_F32 && d.norm_dtype <= WT_U8 ? WT_ENOTSUP : WT_EINVAL,
+                       "%s: norm_dtype %d: norms are fp32, bf16 or f16", call, d.norm_dtype);
+  if (d.n_req < 0 || d.n_req >= kMaxSize || d.n_tokens < 0 || d.n_tokens > kMaxSize || d.max_len < 0 || d.max_len > kMaxSize ||
+      d.n_pages < 0)
+    return serve_error(WT_EINVAL, "%s: n_req %d, n_tokens %d, max_len %d or n_pages %d out of range", call, d.n_req, d.n_tokens, d.max_len,
+                       d.n_pages);
+  if ((d.q && (d.heads < 1 || d.heads > 65536)) || (kv && (d.kv_heads < 1 || d.kv_heads > 65536)))
+    return serve_error(WT_EINVAL, "%s: heads %d or kv_heads %d is not from 1 to 65536", call, d.heads, d.kv_heads);
+  if (d.head_dim < 8 || d.head_dim % 8) return serve_error(WT_EINVAL, "%s: head_dim %d is not a multiple of 8", call, d.head_dim);
+  if (d.head_dim > WT_PLACE_MAX_DIM) return serve_error(WT_ENOTSUP, "%s: head_dim %d is above %d", call, d.head_dim, WT_PLACE_MAX_DIM);
+  if (d.rot_dim < 0 || d.rot_dim % 8 || d.rot_dim > d.head_dim)
+    return serve_error(WT_EINVAL, "%s: rot_dim %d is not a multiple of 8 up to head_dim", call, d.rot_dim);
+  if (d.flags & ~WT_PLACE_NEIGHBOURS) return serve_error(WT_EINVAL, "%s: unknown flags 0x%x", call, (unsigned)d.flags);
+  if (norms && !(d.eps >= 0.0f && std::isfinite(d.eps))) return serve_error(WT_EINVAL, "%s: eps is not a finite number from 0 on", call);
+  const bool turned = d.rot_dim && (d.q || d.k), by_place = turned && !d.pos;
+  if (by_place && (d.first_pos < 0 || d.first_pos > kMaxSize))
+    return serve_error(WT_EINVAL, "%s: first_pos %d is not from 0 to 2^30", call, d.first_pos);
+  if (turned && d.pos) {
+    if (d.axes < 1 || d.axes > WT_PLACE_MAX_AXES || d.pos_stride < d.axes || d.pos_stride > kMaxPitch)
+      return serve_error(WT_EINVAL, "%s: axes %d is not from 1 to %d, or the pitch of pos not at least that", call, d.axes, WT_PLACE_MAX_AXES);
+    for (int j = 0; j < d.rot_dim / 2; ++j)
+      if (d.axis[j] >= d.axes) return serve_error(WT_EINVAL, "%s: pair %d has axis %d of %d", call, j, d.axis[j], d.axes);
+  }
+  const uint64_t N = d.n_tokens, D = d.head_dim, H = d.q ? d.heads : 0, Hkv = kv ? d.kv_heads : 0, in = d.in_dtype == WT_F32 ? 4 : 2;
+  auto pitch = [&](const void *p, int64_t stride, uint64_t heads) {
+    return !p || (stride >= (int64_t)(heads * D) && stride % 8 == 0 && stride <= kMaxPitch);
+  };
+  if (!pitch(d.q, d.q_stride, H) || !pitch(d.q, d.out_stride, H) || !pitch(d.k, d.k_stride, Hkv) || !pitch(d.v, d.v_stride, Hkv))
+    return serve_error(WT_EINVAL, "%s: a token pitch is not a multiple of 8 of at least heads * head_dim", call);
+  if (!d.begin && (kv || by_place))
+    return serve_error(WT_EINVAL, "%s: without begin tokens have no place: no k, no v and no rotation without pos", call);
+  if (N == 0 || (!d.q && !kv) || (d.begin && d.n_req == 0)) return WT_OK;
+  const uint64_t B = d.n_req, kv_row = Hkv * D, q_row = H * D, norm = d.norm_dtype == WT_F32 ? 4 : 2;
+  const Rows none("", nullptr, 0);
+  Rows outs[3] = {none, none, none}, reads[10] = {none, none, none, none, none, none, none, none, none, none};
+  int n_reads = 0;
+  // q_out may be q: what a lane writes, it alone reads, before
+  const bool in_place = d.q && d.q_out == d.q && in == 2 && d.q_stride == d.out_stride;
+  auto read = [&](const char *name, const void *p, uint64_t rows, uint64_t pitch_bytes, uint64_t row, uintptr_t align) -> int {
+    CHECK(check_buffer(&seen, call, name, p, extent(rows, pitch_bytes, row, 1), align));
+    reads[n_reads++] = Rows(name, p, rows, pitch_bytes, row);
+    return WT_OK;
+  };
+  if (d.q) {
+    CHECK(read("q", d.q, N, in * d.q_stride, in * q_row, 16));
+    CHECK(check_output(h, &seen, call, "q_out", d.q_out, extent(N, d.out_stride, q_row, 2), 16));
+    outs[0] = Rows("q_out", d.q_out, N, 2 * (uint64_t)d.out_stride, 2 * q_row);
+    if (d.q_norm) CHECK(read("q_norm", d.q_norm, 1, 0, D * norm, norm));
+  }
+  if (kv) {
+    if (d.page < 1 || d.table_stride < 0 || d.table_stride > 0x7fffffff || (int64_t)d.max_len > d.table_stride * d.page)
+      return serve_error(WT_EINVAL, "%s: max_len %d does not fit %lld pages of %d keys", call, d.max_len, (long long)d.table_stride,
+                         d.page);
+    const uint64_t n = (Bytes(d.n_pages) * d.page * d.kv_heads * D * 2).n;
+    if (d.k) {
+      CHECK(read("k", d.k, N, in * d.k_stride, in * kv_row, 16));
+      CHECK(check_output(h, &seen, call, "k_pages", d.k_pages, n, 16));
+      outs[1] = Rows("k_pages", d.k_pages, n);
+      if (d.k_norm) CHECK(read("k_norm", d.k_norm, 1, 0, D * norm, norm));
+    }
+    if (d.v) {
+      CHECK(read("v", d.v, N, in * d.v_stride, in * kv_row, 16));
+      CHECK(check_output(h, &seen, call, "v_pages", d.v_pages, n, 16));
+      outs[2] = Rows("v_pages", d.v_pages, n);
+    }
+    const uint64_t pages = ceil_div(d.max_len, d.page);
+    CHECK(read("table", d.table, B, 4 * (uint64_t)d.table_stride, 4 * pages, 4));
+  }
+  if (d.begin) CHECK(read("begin", d.begin, 1, 0, 4 * (B + 1), 4));
+  if (kv || by_place) CHECK(read("len", d.len, 1, 0, 4 * B, 4));
+  if (turned) {
+    CHECK(read("turns", d.turns, 1, 0, 4 * (uint64_t)d.rot_dim, 8));
+    if (d.pos) CHECK(read("pos", d.pos, N, 4 * (uint64_t)d.pos_stride, 4 * (uint64_t)d.axes, 4));
+  }
+  for (int i = 0; i < 3; ++i) {
+    for (int j = 0; j < n_reads; ++j)
+      if (!(i == 0 && j == 0 && in_place) && overlap(outs[i], reads[j]))
+        return serve_error(WT_EINVAL, "%s: %s overlaps %s", call, outs[i].name, reads[j].name);
+    for (int j = 0; j < i; ++j)
+      if (overlap(outs[i], outs[j])) return serve_error(WT_EINVAL, "%s: %s overlaps %s", call, outs[i].name, outs[j].name);
+  }
+  return WT_OK;
+}
+
+int place_impl(wt_handle *h, const wt_place_desc *dp, cudaStream_t s) {
+  wt::ServeContext ctx;
+  CHECK(wt::serve_context(h, "wt_place", wt::kServePlain, &ctx));
+  if (!dp) return serve_error(WT_EINVAL, "wt_place: NULL descriptor");
+  CHECK(check_place(h, *dp));
+  wt::PlacePlan P = {};
+  P.d = *dp;
+  wt_place_desc &d = P.d;
+  if (d.n_tokens == 0 || (!d.q && !d.k && !d.v) || (d.begin && d.n_req == 0)) return WT_OK;
+  // what is not asked for is not looked at
+  if (!d.q) d.q_norm = nullptr;
+  if (!d.k) d.k_norm = nullptr;
+  if (!d.k && !d.v) d.table = nullptr;
+  if (!d.k && !d.v && (d.pos || !d.rot_dim || !d.q)) d.len = nullptr;
+  P.status = ctx.status;
+  if (!wt::plan_place(&P)) return serve_error(WT_EINVAL, "wt_place: too many tokens and heads for one launch");
+  return launch_alone(h, s, [&] { return wt::launch_place(P, s); });
+}
+
+int logprobs_impl(wt_handle *h, const wt_logprobs_desc *d, cudaStream_t s) {
+  const char *call = "wt_logprobs";
+  wt::ServeRanges seen;
+  wt::ServeContext ctx;
+  CHECK(wt::serve_context(h, call, wt::kServePlain, &ctx));
+  if (!d) return serve_error(WT_EINVAL, "%s: NULL descriptor", call);
+  if (d->rows < 0 || d->rows > (1 << 27) || d->vocab < 0 || d->vocab > (1 << 30) || d->ldl < d->vocab || d->ldl > kMaxPitch)
+    return serve_error(WT_EINVAL, "%s: rows %d, vocab %d or a pitch out of range", call, d->rows, d->vocab);
+  if (d->n_given < 0 || d->n_given > (1 << 20) || d->n_top < 0 || d->n_top > WT_LOGPROBS_MAX_TOP ||
+      (d->given && (d->given_stride < d->n_given || d->given_stride > kMaxPitch)))
+    return serve_error(WT_EINVAL, "%s: n_given %d (up to 2^20), its pitch, or n_top %d (up to %d) out of range", call, d->n_given, d->n_top,
+                       WT_LOGPROBS_MAX_TOP);
+  wt_logprobs_desc e = *d;
+  if (!e.given) e.n_given = 0;
+  if (!e.top) e.n_top = 0;
+  if (e.rows == 0 || (!e.n_given && !e.n_top && !e.entropy)) return WT_OK;
+  const uint64_t rows = e.rows, V = e.vocab, given = 4 * (uint64_t)e.n_given, top = 4 * (uint64_t)e.n_top;
+  CHECK(check_buffer(&seen, call, "logits", e.logits, extent(rows, e.ldl, V, 4), 4));
+  if (e.temp) CHECK(check_buffer(&seen, call, "temp", e.temp, 4 * rows, 4));
+  if (given) {
+    CHECK(check_buffer(&seen, call, "given", e.given, extent(rows, e.given_stride, e.n_given, 4), 4));
+    CHECK(check_output(h, &seen, call, "given_lp", e.given_lp, rows * given, 4));
+  }
+  if (e.entropy) CHECK(check_output(h, &seen, call, "entropy", e.entropy, 4 * rows, 4));
+  if (top) {
+    CHECK(check_output(h, &seen, call, "top", e.top, rows * top, 4));
+    CHECK(check_output(h, &seen, call, "top_lp", e.top_lp, rows * top, 4));
+  }
+  const Rows outs[] = {{"given_lp", e.given_lp, rows * given}, {"entropy", e.entropy, e.entropy ? 4 * rows : 0},
+                       {"top", e.top, rows * top}, {"top_lp", e.top_lp, rows * top}};
+  const Rows reads[] = {{"the logits", e.logits, rows, 4 * (uint64_t)e.ldl, 4 * V}, {"temp", e.temp, e.temp ? 4 * rows : 0},
+                        {"given", e.given, e.n_given ? rows : 0, 4 * (uint64_t)e.given_stride, given}};
+  for (const Rows &o : outs) {
+    for (const Rows &r : reads)
+      if (overlap(o, r)) return serve_error(WT_EINVAL, "%s: %s overlaps %s", call, o.name, r.name);
+    for (const Rows &p : outs)
+      if (&p < &o && overlap(o, p)) return serve_error(WT_EINVAL, "%s: %s overlaps %s", call, o.name, p.name);
+  }
+  return launch_alone(h, s, [&] { return wt::launch_logprobs(e, ctx.status, s); });
+}
+
 int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {
   const char *call = "wt_verify";
   wt::ServeRanges seen;
@@ -515,12 +670,20 @@ int wt_adapt(wt_handle *h, const wt_adapt_desc *d, size_t n, void *stream) {
   return adapt_impl(h, d, n, static_cast<cudaStream_t>(stream));
 }
 
+int wt_place(wt_handle *h, const wt_place_desc *d, void *stream) {
+  return place_impl(h, d, static_cast<cudaStream_t>(stream));
+}
+
 int wt_attend(wt_handle *h, const wt_attend_desc *d, void *stream) {
   return attend_impl(h, d, static_cast<cudaStream_t>(stream));
 }
 
 int wt_probs(wt_handle *h, const wt_probs_desc *d, void *stream) {
   return probs_impl(h, d, static_cast<cudaStream_t>(stream));
+}
+
+int wt_logprobs(wt_handle *h, const wt_logprobs_desc *d, void *stream) {
+  return logprobs_impl(h, d, static_cast<cudaStream_t>(stream));
 }
 
 int wt_verify(wt_handle *h, const wt_verify_desc *d, void *stream) {

@@ -18,7 +18,7 @@ struct ServeContext {
 };
 // Kernels whose one-time attributes are set by the first call that may launch them (all of them in wt_open
 // took 1.7 of a process's first 20 ms).
-enum ServeKernels { kServeAdapt, kServeAttend, kServeDraw, kServeKernels };
+enum ServeKernels { kServeAdapt, kServeAttend, kServeDraw, kServePlain, kServeKernels };  // plain: none to set
 int serve_prepare(int device, ServeKernels k);
 // Refuses NULL and host-only handles, and prepares the call's kernels.
 int serve_context(wt_handle *h, const char *call, ServeKernels kernels, ServeContext *out);
@@ -87,6 +87,22 @@ cudaError_t launch_adapt(const AdaptLaunch &L, const AdaptWide *W, int max_R, in
 cudaError_t draw_prepare();
 cudaError_t launch_probs(const wt_probs_desc &d, int *status, cudaStream_t s);
 cudaError_t launch_verify(const wt_verify_desc &d, int *status, cudaStream_t s);
+
+// ---------------------------------------------------------------- wt_place.cu
+struct PlacePlan {
+  wt_place_desc d;
+  int width_log2;   // lanes of a head: 8 elements each
+  int chunk_heads;  // heads of a warp, of those of q, k and v in a row
+  int chunks;       // warps of a token
+  float inv_dim;
+  int *status;
+};
+// Sets the plan's split; false where it does not fit one launch.
+bool plan_place(PlacePlan *P);
+cudaError_t launch_place(const PlacePlan &P, cudaStream_t s);
+
+// ---------------------------------------------------------------- wt_logprobs.cu
+cudaError_t launch_logprobs(const wt_logprobs_desc &d, int *status, cudaStream_t s);
 
 // ---------------------------------------------------------------- wt_attend.cu, wt_prefix.cu
 // Weights p = 2^(s - m) are rounded to the caches' type.  The reference m lies kBelow under the largest

@@ -4,8 +4,10 @@ One step of several requests over one set of weights, beside Handle.pass_:
 
     h.pass_(...)                                   # projections, for every token of the step
     h.adapt([adapters(...), ...], stream)          # each request's low-rank adapter
+    h.place(placement(...), stream)                # norms, rotation; keys and values to their pages
     h.attend(attention(...), stream)               # over the shared prefix and the paged caches
     h.probs(probabilities(...), stream)            # the head's logits, at each row's temperature
+    h.logprobs(log_probabilities(...), stream)     # of given tokens, with entropy and alternatives
     h.verify(verification(...), stream)            # which drafted tokens stay, and the next one
 
 Each function here checks types, shapes and strides and returns the C descriptor, which holds the
@@ -15,7 +17,9 @@ for one call).  PyTorch supplies device memory and streams only.
 """
 from __future__ import annotations
 
-from typing import Optional
+import math
+from fractions import Fraction
+from typing import Optional, Sequence
 
 import torch
 
@@ -82,6 +86,110 @@ def adapters(x, y, slot, A, B, scale=None, rank=None, base=None) -> wt.AdaptDesc
     return d
 
 
+_PI = Fraction(31415926535897932384626433832795028841971, 10 ** 40)  # off by less than 2^-132
+
+
+def turns(freq: Sequence[float], device="cuda") -> torch.Tensor:
+    """For placement: the turns that a position adds for each pair, modulo one, as 64-bit fractions (int64
+    bits).  freq holds radians a position, as floats in 64 bits; the quotient by 2 pi is rounded once."""
+    v = []
+    for f in freq:
+        _need(math.isfinite(f), "freq is finite")
+        t = round(Fraction(f) * 2 ** 63 / _PI) % 2 ** 64
+        v.append(t - 2 ** 64 if t >= 2 ** 63 else t)
+    return torch.tensor(v, dtype=torch.int64, device=device)
+
+
+def placement(begin=None, k_pages=None, v_pages=None, table=None, lens=None, *, q=None, q_out=None, k=None, v=None, max_len=0,
+              q_norm=None, k_norm=None, eps=1e-6, turns=None, axis=None, pos=None, first_pos=0,
+              neighbours=False) -> wt.PlaceDesc:
+    """Queries to q_out, keys and values to their requests' pages, normed and rotated on the way (see wt_place).
+
+    q [tokens, heads, head_dim] and k, v [tokens, kv_heads, head_dim] (the heads of a token contiguous, any
+    token pitch) are fp32 or of the outputs' type, bf16 or f16; any of them may be None.  q_out has q's shape.
+    begin, the pages, table, lens and max_len are attention's.  q_norm, k_norm [head_dim] (None: no norm).
+    turns (of serving.turns) rotates the first 2 len(turns) elements of each head, by the token's place plus
+    first_pos, or by pos int32 [tokens, axes], pair j by its axis[j] (None: all by the first)."""
+    _need(q is not None or k is not None or v is not None, "one of q, k and v at least")
+    _need((q is None) == (q_out is None), "q and q_out come together")
+    _need(k is None or k_pages is not None, "k goes with k_pages")
+    _need(v is None or v_pages is not None, "v goes with v_pages")
+    out = q_out if q is not None else k_pages if k is not None else v_pages
+    _need(out.dtype in _TYPES, "q_out and the pages are bf16 or f16, not %s" % out.dtype)
+    src = q if q is not None else k if k is not None else v
+    _need(src.dtype in (torch.float32, out.dtype), "q, k and v are fp32 or %s, not %s" % (out.dtype, src.dtype))
+    N, D = src.shape[0], src.shape[-1]
+    d = wt.PlaceDesc(in_dtype=wt.WT_F32 if src.dtype == torch.float32 else _TYPES[out.dtype], dtype=_TYPES[out.dtype],
+                     n_tokens=N, head_dim=D, eps=eps, first_pos=first_pos, flags=wt.WT_PLACE_NEIGHBOURS if neighbours else 0)
+    Hkv = None
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        if t is None:
+            continue
+        _is(t, name, src.dtype, 3)
+        _need(t.shape[0] == N and t.shape[2] == D, "%s is [%d, heads, %d]" % (name, N, D))
+        _need(N == 0 or t[0].is_contiguous(), "the heads of a token of %s are contiguous" % name)
+        setattr(d, name, _ptr(t))
+        setattr(d, name + "_stride", t.stride(0) if N > 1 else t.shape[1] * D)
+        if name != "q":
+            _need(Hkv in (None, t.shape[1]), "k and v have as many heads")
+            Hkv = t.shape[1]
+    if q is not None:
+        _is(q_out, "q_out", out.dtype, 3)
+        _need(q_out.shape == q.shape, "q_out has the shape of q")
+        _need(N == 0 or q_out[0].is_contiguous(), "the heads of a token of q_out are contiguous")
+        d.q_out, d.heads, d.out_stride = _ptr(q_out), q.shape[1], q_out.stride(0) if N > 1 else q.shape[1] * D
+    norm = q_norm if q_norm is not None else k_norm
+    for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if t is not None:
+            _need(t.dtype in (torch.float32, torch.bfloat16, torch.float16), "%s is fp32, bf16 or f16, not %s" % (name, t.dtype))
+            _is(t, name, norm.dtype, 1), _dense(t, name)
+            _need(t.shape[0] == D, "%s is [%d]" % (name, D))
+            setattr(d, name, _ptr(t))
+            d.norm_dtype = wt.WT_F32 if t.dtype == torch.float32 else _TYPES[t.dtype]
+    if begin is not None:
+        _is(begin, "begin", torch.int32, 1), _dense(begin, "begin")
+        _need(begin.shape[0] >= 1, "begin is [requests + 1]")
+        d.begin, d.n_req = _ptr(begin), begin.shape[0] - 1
+    if lens is not None:
+        _is(lens, "lens", torch.int32, 1), _dense(lens, "lens")
+        _need(begin is not None and lens.shape[0] == d.n_req, "lens has a row for each request")
+        _need(max_len >= 1, "max_len bounds what lens will hold")
+        d.len, d.max_len = _ptr(lens), max_len
+    if Hkv is not None:
+        _need(begin is not None and table is not None and lens is not None, "k and v go with begin, table and lens")
+        _is(table, "table", torch.int32, 2)
+        _need(table.shape[0] == d.n_req, "table has a row for each request")
+        shape = None
+        for t, p, name in ((k, k_pages, "k_pages"), (v, v_pages, "v_pages")):
+            if t is None:
+                continue
+            _is(p, name, out.dtype, 4), _dense(p, name)
+            _need(p.shape[2:] == (Hkv, D) and shape in (None, p.shape), "k_pages and v_pages are [pages, page, %d, %d]" % (Hkv, D))
+            shape = p.shape
+            setattr(d, name, _ptr(p))
+        d.kv_heads, d.n_pages, d.page = Hkv, shape[0], shape[1]
+        d.table, d.table_stride = _ptr(table), _rows(table, "table")
+        _need(max_len <= table.shape[1] * d.page, "max_len %d fits table's %d pages of %d" % (max_len, table.shape[1], d.page))
+    if turns is not None:
+        _is(turns, "turns", torch.int64, 1), _dense(turns, "turns")
+        d.turns, d.rot_dim = _ptr(turns), 2 * turns.shape[0]
+        _need(d.rot_dim <= D and d.rot_dim % 8 == 0, "turns are for a multiple of 4 pairs of a head's %d elements" % D)
+        if pos is not None:
+            _is(pos, "pos", torch.int32, 2)
+            _need(pos.shape[0] == N and 1 <= pos.shape[1] <= wt.WT_PLACE_MAX_AXES, "pos is [%d, up to %d axes]" % (N, wt.WT_PLACE_MAX_AXES))
+            d.pos, d.pos_stride, d.axes = _ptr(pos), _rows(pos, "pos"), pos.shape[1]
+            if axis is not None:
+                _need(len(axis) == turns.shape[0] and all(0 <= a < d.axes for a in axis), "axis has one of %d for each pair" % d.axes)
+                d.axis[:len(axis)] = [int(a) for a in axis]
+        else:
+            _need(axis is None, "axis goes with pos")
+            _need(begin is not None and lens is not None, "tokens without pos have a place by begin and lens")
+    else:
+        _need(pos is None and axis is None, "pos and axis go with turns")
+    d.tensors = (q, q_out, k, v, q_norm, k_norm, begin, k_pages, v_pages, table, lens, turns, pos)
+    return d
+
+
 def attention(q, out, begin, k_pages=None, v_pages=None, table=None, lens=None, *, max_new, max_len=0, prefix_k=None,
               prefix_v=None, scale=None) -> wt.AttendDesc:
     """Attention of each request's new tokens over a prefix all requests share and its own cache.
@@ -143,6 +251,36 @@ def probabilities(logits, p, temperature=None) -> wt.ProbsDesc:
     d = wt.ProbsDesc(logits=_ptr(logits), p=_ptr(p), temp=_ptr(temperature), ldl=_rows(logits, "logits"),
                      ldp=_rows(p, "p"), rows=logits.shape[0], vocab=logits.shape[1])
     d.tensors = (logits, p, temperature)
+    return d
+
+
+def log_probabilities(logits, *, given=None, given_lp=None, entropy=None, top=None, top_lp=None,
+                      temperature=None) -> wt.LogprobsDesc:
+    """Log probabilities of given tokens, entropy and the likeliest tokens of each row (see wt_logprobs).
+
+    logits fp32 [rows, vocab]; given int32 [rows, n] (negative: none) with given_lp fp32 [rows, n]; entropy
+    fp32 [rows]; top int32 [rows, up to 32] with top_lp fp32; temperature fp32 [rows] (None: 1).  What is
+    None is not made."""
+    _is(logits, "logits", torch.float32, 2)
+    rows, V = logits.shape
+    _need((given is None) == (given_lp is None), "given and given_lp come together")
+    _need((top is None) == (top_lp is None), "top and top_lp come together")
+    d = wt.LogprobsDesc(logits=_ptr(logits), ldl=_rows(logits, "logits"), rows=rows, vocab=V)
+    if given is not None:
+        _is(given, "given", torch.int32, 2), _is(given_lp, "given_lp", torch.float32, 2), _dense(given_lp, "given_lp")
+        _need(given.shape[0] == rows and given_lp.shape == given.shape, "given and given_lp are [%d, tokens]" % rows)
+        d.given, d.given_lp, d.n_given, d.given_stride = _ptr(given), _ptr(given_lp), given.shape[1], _rows(given, "given")
+    if top is not None:
+        _is(top, "top", torch.int32, 2), _is(top_lp, "top_lp", torch.float32, 2), _dense(top, "top"), _dense(top_lp, "top_lp")
+        _need(top.shape[0] == rows and top_lp.shape == top.shape and top.shape[1] <= wt.WT_LOGPROBS_MAX_TOP,
+              "top and top_lp are [%d, up to %d]" % (rows, wt.WT_LOGPROBS_MAX_TOP))
+        d.top, d.top_lp, d.n_top = _ptr(top), _ptr(top_lp), top.shape[1]
+    for t, name in ((entropy, "entropy"), (temperature, "temperature")):
+        if t is not None:
+            _is(t, name, torch.float32, 1), _dense(t, name)
+            _need(t.shape[0] == rows, "%s is [rows]" % name)
+    d.entropy, d.temp = _ptr(entropy), _ptr(temperature)
+    d.tensors = (logits, given, given_lp, entropy, top, top_lp, temperature)
     return d
 
 

@@ -40,9 +40,10 @@ SYMBOLS = ("wt_last_error", "wt_abi_version", "wt_open", "wt_num_tensors", "wt_n
            # include/wt_dlpack.h
            "wt_dlpack_file", "wt_dlpack_tensor", "wt_dlpack_release", "wt_dlpack_live",
            # include/wt_serve.h
-           "wt_adapt", "wt_attend", "wt_probs", "wt_verify")
+           "wt_adapt", "wt_place", "wt_attend", "wt_probs", "wt_logprobs", "wt_verify")
 WT_DLPACK_DEVICE, WT_DLPACK_HOST = 0, 1
 WT_ADAPT_MAX_RANK, WT_ADAPT_MAX_SLOTS, WT_VERIFY_MAX_VOCAB = 128, 4096, 1 << 18
+WT_PLACE_MAX_DIM, WT_PLACE_MAX_AXES, WT_PLACE_NEIGHBOURS, WT_LOGPROBS_MAX_TOP = 256, 8, 1, 32
 kDLCPU, kDLCUDA = 1, 2
 
 
@@ -81,6 +82,19 @@ def adapt_array(descs):
     return a
 
 
+class PlaceDesc(C.Structure):
+    """wt_place_desc (serving.placement makes one from tensors)."""
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p), ("k_pages", C.c_void_p),
+                ("v_pages", C.c_void_p), ("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("begin", C.c_void_p),
+                ("table", C.c_void_p), ("len", C.c_void_p), ("turns", C.c_void_p), ("pos", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("table_stride", C.c_int64), ("pos_stride", C.c_int64), ("in_dtype", C.c_int32), ("dtype", C.c_int32),
+                ("norm_dtype", C.c_int32), ("n_req", C.c_int32), ("n_tokens", C.c_int32), ("heads", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("axes", C.c_int32),
+                ("page", C.c_int32), ("n_pages", C.c_int32), ("max_len", C.c_int32), ("first_pos", C.c_int32),
+                ("flags", C.c_int32), ("eps", C.c_float), ("axis", C.c_uint8 * (WT_PLACE_MAX_DIM // 2))]
+
+
 class AttendDesc(C.Structure):
     """wt_attend_desc (serving.attention makes one from tensors)."""
     _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("begin", C.c_void_p), ("prefix_k", C.c_void_p),
@@ -96,6 +110,14 @@ class ProbsDesc(C.Structure):
     """wt_probs_desc (serving.probabilities makes one from tensors)."""
     _fields_ = [("logits", C.c_void_p), ("p", C.c_void_p), ("temp", C.c_void_p), ("ldl", C.c_int64), ("ldp", C.c_int64),
                 ("rows", C.c_int32), ("vocab", C.c_int32)]
+
+
+class LogprobsDesc(C.Structure):
+    """wt_logprobs_desc (serving.log_probabilities makes one from tensors)."""
+    _fields_ = [("logits", C.c_void_p), ("temp", C.c_void_p), ("given", C.c_void_p), ("given_lp", C.c_void_p),
+                ("entropy", C.c_void_p), ("top", C.c_void_p), ("top_lp", C.c_void_p), ("ldl", C.c_int64),
+                ("given_stride", C.c_int64), ("rows", C.c_int32), ("vocab", C.c_int32), ("n_given", C.c_int32),
+                ("n_top", C.c_int32)]
 
 
 class VerifyDesc(C.Structure):
@@ -175,8 +197,10 @@ def lib(path: str = LIB_PATH):
     L.wt_live.argtypes = [C.POINTER(LiveCounts)]
     L.wt_close.argtypes = [vp]
     L.wt_adapt.argtypes = [vp, C.POINTER(AdaptDesc), sz, vp]
+    L.wt_place.argtypes = [vp, C.POINTER(PlaceDesc), vp]
     L.wt_attend.argtypes = [vp, C.POINTER(AttendDesc), vp]
     L.wt_probs.argtypes = [vp, C.POINTER(ProbsDesc), vp]
+    L.wt_logprobs.argtypes = [vp, C.POINTER(LogprobsDesc), vp]
     L.wt_verify.argtypes = [vp, C.POINTER(VerifyDesc), vp]
     L.wt_dlpack_file.argtypes = [C.c_char_p, C.c_int32, C.c_uint64, C.c_uint64, C.c_uint, C.POINTER(vp)]
     L.wt_dlpack_tensor.argtypes = [vp, sz, C.c_uint, C.POINTER(vp)]
@@ -367,6 +391,12 @@ class Handle:
         if rc:
             _check(rc)
 
+    def place(self, desc: PlaceDesc, stream: int = 0):
+        """wt_place."""
+        rc = lib().wt_place(self.ptr, C.byref(desc), stream)
+        if rc:
+            _check(rc)
+
     def attend(self, desc: AttendDesc, stream: int = 0):
         """wt_attend."""
         rc = lib().wt_attend(self.ptr, C.byref(desc), stream)
@@ -376,6 +406,12 @@ class Handle:
     def probs(self, desc: ProbsDesc, stream: int = 0):
         """wt_probs."""
         rc = lib().wt_probs(self.ptr, C.byref(desc), stream)
+        if rc:
+            _check(rc)
+
+    def logprobs(self, desc: LogprobsDesc, stream: int = 0):
+        """wt_logprobs."""
+        rc = lib().wt_logprobs(self.ptr, C.byref(desc), stream)
         if rc:
             _check(rc)
 
