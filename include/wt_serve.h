@@ -2,12 +2,13 @@
  * wt_serve — one step of many requests over one set of weights.  C ABI.
  *
  * wt_pass (wt.h) streams a checkpoint's matrices for up to 16 activation columns.  A program that
- * answers several requests with them needs six more things beside that pass, every step:
+ * answers several requests with them needs seven more things beside that pass, every step:
  *
  *   wt_adapt     each request's low-rank adapter beside a projection all requests share;
  *   wt_place     the projections' rows to normed and rotated queries, and keys and values in their pages;
  *   wt_attend    attention over a prefix that all requests share, read once for all of them, and
  *                over each request's own paged cache;
+ *   wt_cross     attention of each request's tokens to a memory of its own, as an encoder's states;
  *   wt_probs     fp32 logits (wt_pass's y over the head) to probabilities at a temperature;
  *   wt_logprobs  log probabilities of given tokens, entropy and the likeliest tokens of such logits;
  *   wt_verify    drafted tokens against the target's probabilities, from given random numbers.
@@ -179,6 +180,41 @@ typedef struct {
 /* Errors: WT_EINVAL (NULL, sizes, alignment, strides, out inside a mapping, a buffer that runs past
  * its device allocation), WT_ENOTSUP (dtype, head_dim, host-only handle), WT_ENOMEM, WT_ECUDA. */
 int wt_attend(wt_handle *h, const wt_attend_desc *d, void *stream);
+
+/* ---- wt_cross -------------------------------------------------------------------------------
+ * Token i of request b (row begin[b] + i of q) attends to its request's memory, the states
+ * mem_begin[b] .. mem_begin[b] + mem_len[b] - 1 of k and v, whole (nothing is causal here):
+ *
+ *   out[t, h] = sum_j p_j v_j,   p = softmax_j(scale * q[t, h] . k_j),   kv head h / (heads / kv_heads)
+ *
+ * over the states with keep[j] != 0 (keep NULL: all).  Memories may overlap or be one; a request's tokens
+ * read theirs once, so beams or drafts over one memory are best one request's tokens.  A token that sees
+ * no state gets zeros, and so does one all of whose scores are -infinity.  NaN and infinities show as
+ * wt_attend's do; what is not in the memory, or not kept, never reaches a result, whatever stands there.
+ * Rows of tokens that no request holds are left as they are.
+ *
+ * Types, head sizes and limits are wt_attend's; n_mem goes up to 2^30.  out may be q itself (at its
+ * pitch); otherwise it must not overlap any input, as rows of tokens. */
+typedef struct {
+  const void *q;            /* [n_tokens, heads, head_dim], token pitch q_stride elements */
+  void *out;                /* [n_tokens, heads, head_dim], token pitch out_stride */
+  const int32_t *begin;     /* [n_req + 1]: first token of each request, ascending, begin[n_req] <= n_tokens */
+  const void *k;            /* [n_mem, kv_heads, head_dim], state pitch mem_stride, head pitch mem_head */
+  const void *v;            /* the same pitches */
+  const int32_t *mem_begin; /* [n_req] first state of each request's memory */
+  const int32_t *mem_len;   /* [n_req] <= max_mem */
+  const uint8_t *keep;      /* [n_mem], or NULL */
+  int64_t q_stride, out_stride, mem_stride, mem_head, n_mem;
+  int32_t dtype;            /* WT_BF16 or WT_F16 */
+  int32_t n_req, n_tokens, max_new, max_mem; /* no request has more new tokens, no memory more states */
+  int32_t heads, kv_heads, head_dim;
+  float scale;
+  int32_t pad;
+} wt_cross_desc;
+
+/* Errors: WT_EINVAL (NULL, sizes, alignment, strides, out inside a mapping, a buffer that runs past
+ * its device allocation), WT_ENOTSUP (dtype, head_dim, host-only handle), WT_ENOMEM, WT_ECUDA. */
+int wt_cross(wt_handle *h, const wt_cross_desc *d, void *stream);
 
 /* ---- wt_probs -------------------------------------------------------------------------------
  * p[r, v] = exp((l[r, v] - m_r) / temp[r]) / sum,  m_r the row's largest logit.

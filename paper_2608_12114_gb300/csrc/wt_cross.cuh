@@ -1,0 +1,104 @@
+// What the kernels of attention to memories share (include/wt_serve.h): requests, and the cells of a CTA.
+// Internal to the library (each translation unit gets its own copies).
+#pragma once
+
+#include "wt_serve.cuh"
+
+namespace wt {
+namespace {
+
+// Tokens and memory of request b, clamped to the descriptor.
+struct Asker {
+  int t0, n;         // first token, tokens
+  int mem, len;      // first state, states
+  int row_tiles, key_tiles;
+  __device__ long long cells(int kv_heads) const { return (long long)row_tiles * key_tiles * kv_heads; }
+};
+
+__device__ __forceinline__ Asker asker_of(const CrossPlan &P, int b, bool tell) {
+  const wt_cross_desc &d = P.d;
+  int t0 = __ldg(d.begin + b), t1 = __ldg(d.begin + b + 1), mem = 0, len = 0;
+  if (d.mem_len) mem = __ldg(d.mem_begin + b), len = __ldg(d.mem_len + b);
+  if (t0 < 0 || t1 < t0 || t1 > d.n_tokens || t1 - t0 > d.max_new || mem < 0 || len < 0 || len > d.max_mem || mem + (int64_t)len > d.n_mem) {
+    if (tell && P.status) atomicCAS(P.status, 0, kStatusInvalid);
+    t0 = min(max(t0, 0), d.n_tokens);
+    t1 = min(max(t1, t0), t0 + min(d.max_new, d.n_tokens - t0));
+    mem = min(max(mem, 0), (int)d.n_mem);
+    len = min(min(max(len, 0), d.max_mem), (int)d.n_mem - mem);
+  }
+  const int n = t1 - t0;
+  // tokens without a state have a tile all the same: it writes their zeros
+  return {t0, n, mem, len, (n * P.G + P.rows - 1) / P.rows, max(1, (len + P.keys - 1) / P.keys)};
+}
+
+// This CTA's cells, and the request that the first of them lies in.
+struct Share {
+  long long lo, hi;  // cells of all requests in a row
+  long long first;   // of request b
+  int b;
+};
+
+// By the whole block, N threads.  Each thread adds up the cells of a run of requests; the runs' sums are scanned.
+template <int N>
+__device__ __forceinline__ Share share_of(const CrossPlan &P) {
+  constexpr int kWarps = N / 32;
+  __shared__ long long sums[kWarps];
+  __shared__ Share found;
+  const wt_cross_desc &d = P.d;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int run = (d.n_req + N - 1) / N, b0 = min(tid * run, d.n_req), b1 = min(b0 + run, d.n_req);
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) mine += asker_of(P, b, blockIdx.x == 0).cells(d.kv_heads);
+  long long upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 31) sums[warp] = upto;
+  if (tid == 0) found = {0, 0, 0, d.n_req};
+  __syncthreads();
+  long long all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w == warp) upto += all;
+    all += sums[w];
+  }
+  const long long per = max(1ll, (all + gridDim.x - 1) / gridDim.x), lo = per * blockIdx.x, hi = min(all, lo + per);
+  long long first = upto - mine;
+  const bool here = lo < hi && first <= lo && lo < upto;
+  if (here || blockIdx.x == 0)
+    for (int b = b0; b < b1; ++b) {
+      const long long n = asker_of(P, b, false).cells(d.kv_heads);
+      if (blockIdx.x == 0) P.first[b] = first;
+      if (here && first <= lo && lo < first + n) found = {lo, hi, first, b};
+      first += n;
+    }
+  if (blockIdx.x == 0 && tid == 0) P.first[d.n_req] = per;
+  __syncthreads();
+  return found;
+}
+
+// One row tile's states that this CTA takes.
+struct Segment {
+  int hk, row_tile;
+  int tile0, tiles;   // tiles of P.keys states
+  bool whole;         // all of the row tile's
+  long long slot;     // where the part goes else
+};
+
+// The segment that starts at cell `at` of request a, whose first cell is `first`.
+__device__ __forceinline__ Segment segment_at(const Asker &a, long long first, long long at, const Share &s) {
+  const long long u = (at - first) / a.key_tiles, begin = first + u * a.key_tiles, end = min(s.hi, begin + a.key_tiles);
+  Segment g;
+  g.hk = (int)(u / a.row_tiles);
+  g.row_tile = (int)(u - (long long)g.hk * a.row_tiles);
+  g.tile0 = (int)(at - begin);
+  g.tiles = (int)(end - at);
+  g.whole = g.tiles == a.key_tiles;
+  g.slot = 2 * blockIdx.x + (begin >= s.lo && at > s.lo);
+  return g;
+}
+
+}  // namespace
+}  // namespace wt

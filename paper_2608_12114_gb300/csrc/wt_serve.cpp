@@ -452,6 +452,115 @@ int attend_impl(wt_handle *h, const wt_attend_desc *dp, cudaStream_t s) {
   return rc;
 }
 
+int check_cross(wt_handle *h, const wt_cross_desc &d) {
+  const char *call = "wt_cross";
+  wt::ServeRanges seen;
+  if (d.dtype != WT_BF16 && d.dtype != WT_F16)
+    return serve_error(d.dtype >= WT_F32 && d.dtype <= WT_U8 ? WT_ENOTSUP : WT_EINVAL,
+                       "%s: dtype %d: queries and memories are bf16 or f16", call, d.dtype);
+  if (d.n_req < 0 || d.n_req > 65535 || d.n_tokens < 0 || d.n_tokens > kMaxSize || d.max_new < 0 || d.max_mem < 0 ||
+      d.max_mem > kMaxSize || d.n_mem < 0 || d.n_mem > kMaxSize)
+    return serve_error(WT_EINVAL, "%s: n_req %d, n_tokens %d, max_new %d, max_mem %d or n_mem %lld out of range", call, d.n_req,
+                       d.n_tokens, d.max_new, d.max_mem, (long long)d.n_mem);
+  if (d.heads < 1 || d.kv_heads < 1 || d.heads > 65536 || d.heads % d.kv_heads || d.heads / d.kv_heads > 128)
+    return serve_error(WT_EINVAL, "%s: heads %d is not up to 128 times kv_heads %d", call, d.heads, d.kv_heads);
+  if (d.head_dim < 8 || d.head_dim % 8)
+    return serve_error(WT_EINVAL, "%s: head_dim %d is not a multiple of 8", call, d.head_dim);
+  if (d.head_dim > 128) return serve_error(WT_ENOTSUP, "%s: head_dim %d is above 128", call, d.head_dim);
+  if (!std::isfinite(d.scale)) return serve_error(WT_EINVAL, "%s: scale is not finite", call);
+  const int64_t row = (int64_t)d.heads * d.head_dim, D = d.head_dim;
+  if (d.q_stride < row || d.out_stride < row || d.q_stride % 8 || d.out_stride % 8 || d.q_stride > kMaxPitch ||
+      d.out_stride > kMaxPitch)
+    return serve_error(WT_EINVAL, "%s: token pitches %lld and %lld are not multiples of 8 of at least heads * head_dim", call,
+                       (long long)d.q_stride, (long long)d.out_stride);
+  if ((int64_t)d.n_tokens * d.heads > 0x7fffffff) return serve_error(WT_EINVAL, "%s: n_tokens * heads above 2^31-1", call);
+  if (d.n_req == 0 || d.n_tokens == 0 || d.max_new == 0) return WT_OK;
+  CHECK(check_buffer(&seen, call, "q", d.q, extent(d.n_tokens, d.q_stride, row, 2), 16));
+  CHECK(check_output(h, &seen, call, "out", d.out, extent(d.n_tokens, d.out_stride, row, 2), 16));
+  CHECK(check_buffer(&seen, call, "begin", d.begin, 4 * ((uint64_t)d.n_req + 1), 4));
+  const Rows out("out", d.out, d.n_tokens, 2 * (uint64_t)d.out_stride, 2 * (uint64_t)row);
+  auto apart = [&](const Rows &r) {
+    return overlap(out, r) ? serve_error(WT_EINVAL, "%s: out overlaps %s", call, r.name) : WT_OK;
+  };
+  // out may be q: a token's head is written once all that reads it has been read
+  if (d.out != d.q || d.out_stride != d.q_stride)
+    CHECK(apart({"q", d.q, (uint64_t)d.n_tokens, 2 * (uint64_t)d.q_stride, 2 * (uint64_t)row}));
+  CHECK(apart({"begin", d.begin, 4 * ((uint64_t)d.n_req + 1)}));
+  if (d.max_mem == 0) return WT_OK;
+  const uint64_t B = d.n_req;
+  CHECK(check_buffer(&seen, call, "mem_begin", d.mem_begin, 4 * B, 4));
+  CHECK(check_buffer(&seen, call, "mem_len", d.mem_len, 4 * B, 4));
+  CHECK(apart({"mem_begin", d.mem_begin, 4 * B}));
+  CHECK(apart({"mem_len", d.mem_len, 4 * B}));
+  if (d.n_mem == 0) return WT_OK;
+  if (d.mem_head < D || d.mem_head % 8 || d.mem_stride < D || d.mem_stride % 8 || d.mem_head > kMaxPitch || d.mem_stride > kMaxPitch)
+    return serve_error(WT_EINVAL, "%s: memory pitches %lld and %lld are not multiples of 8 of at least head_dim", call,
+                       (long long)d.mem_stride, (long long)d.mem_head);
+  // either way round: [state, head, dim] or [head, state, dim]
+  const uint64_t M = d.n_mem, H = d.kv_heads, n = (Bytes(2) * (Bytes(M - 1) * d.mem_stride + Bytes(H - 1) * d.mem_head + D)).n;
+  CHECK(check_buffer(&seen, call, "k", d.k, n, 16));
+  CHECK(check_buffer(&seen, call, "v", d.v, n, 16));
+  if (d.keep) {
+    CHECK(check_buffer(&seen, call, "keep", d.keep, M, 1));
+    CHECK(apart({"keep", d.keep, M}));
+  }
+  // as rows of whole states where those lie apart, else of whole heads, or one
+  const uint64_t state = 2 * ((H - 1) * d.mem_head + D), head = 2 * ((M - 1) * d.mem_stride + D);
+  const bool states = M > 1 && 2 * (uint64_t)d.mem_stride >= state, heads = H > 1 && 2 * (uint64_t)d.mem_head >= head;
+  for (const void *p : {d.k, d.v})
+    CHECK(apart(states  ? Rows("the memory", p, M, 2 * (uint64_t)d.mem_stride, state)
+                : heads ? Rows("the memory", p, H, 2 * (uint64_t)d.mem_head, head)
+                        : Rows("the memory", p, n)));
+  return WT_OK;
+}
+
+int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
+  wt::ServeContext ctx;
+  CHECK(wt::serve_context(h, "wt_cross", wt::kServeCross, &ctx));
+  if (!dp) return serve_error(WT_EINVAL, "wt_cross: NULL descriptor");
+  CHECK(check_cross(h, *dp));
+  wt::CrossPlan P = {};
+  P.d = *dp;
+  wt_cross_desc &d = P.d;
+  if (d.n_req == 0 || d.n_tokens == 0 || d.max_new == 0) return WT_OK;
+  if (d.max_mem == 0) d.mem_len = nullptr;
+  d.max_new = std::min(d.max_new, d.n_tokens);
+  d.max_mem = (int32_t)std::min<int64_t>(d.max_mem, d.n_mem);
+  P.G = d.heads / d.kv_heads;
+  P.status = ctx.status;
+  P.keys = 64;
+  P.rows = (int64_t)d.max_new * P.G <= 16 ? 16 : 32;
+  // No more CTAs than run at once, or than there can be cells.  (Requests' row tiles: whole ones of all tokens,
+  // and one more each.)
+  const double tiles = std::min((double)d.n_req * (double)ceil_div((int64_t)d.max_new * P.G, P.rows),
+                                (double)d.n_tokens * P.G / P.rows + d.n_req);
+  const double cells = tiles * d.kv_heads * (double)std::max<int64_t>(1, ceil_div(d.max_mem, P.keys));
+  P.ctas = (int)std::max(1.0, std::min((double)wt::cross_few_resident(P.rows, d.head_dim) * wt::num_sms(), cells));
+  auto take = [](size_t &at, size_t n) {
+    const size_t o = at;
+    at += (n + 255) / 256 * 256;
+    return o;
+  };
+  size_t bytes = 0;
+  const size_t slots = 2 * (size_t)P.ctas * P.rows;
+  const size_t o = take(bytes, slots * d.head_dim * 4), ml = take(bytes, slots * sizeof(float2)),
+               first = take(bytes, ((size_t)d.n_req + 2) * sizeof(long long));
+  Lock lock(h);
+  wt::ServeWorkspace w;
+  CHECK(wt::serve_workspace(h, s, bytes, &w));
+  uint8_t *ws = static_cast<uint8_t *>(w.p);
+  P.o = reinterpret_cast<float *>(ws + o);
+  P.ml = reinterpret_cast<float2 *>(ws + ml);
+  P.first = reinterpret_cast<long long *>(ws + first);
+  const bool joined = d.max_mem > P.keys;  // memories of one cell: no row tile has two parts
+  cudaError_t e = wt::launch_cross_few(P, s);
+  if (e == cudaSuccess && joined) e = wt::launch_cross_merge(P, s);
+  const int rc = wt::serve_done(h, s, w);
+  CU(e);
+  wt::serve_launched(h, 1 + joined);
+  return rc;
+}
+
 int probs_impl(wt_handle *h, const wt_probs_desc *d, cudaStream_t s) {
   const char *call = "wt_probs";
   wt::ServeRanges seen;
@@ -676,6 +785,10 @@ int wt_place(wt_handle *h, const wt_place_desc *d, void *stream) {
 
 int wt_attend(wt_handle *h, const wt_attend_desc *d, void *stream) {
   return attend_impl(h, d, static_cast<cudaStream_t>(stream));
+}
+
+int wt_cross(wt_handle *h, const wt_cross_desc *d, void *stream) {
+  return cross_impl(h, d, static_cast<cudaStream_t>(stream));
 }
 
 int wt_probs(wt_handle *h, const wt_probs_desc *d, void *stream) {

@@ -18,7 +18,7 @@ struct ServeContext {
 };
 // Kernels whose one-time attributes are set by the first call that may launch them (all of them in wt_open
 // took 1.7 of a process's first 20 ms).
-enum ServeKernels { kServeAdapt, kServeAttend, kServeDraw, kServePlain, kServeKernels };  // plain: none to set
+enum ServeKernels { kServeAdapt, kServeAttend, kServeCross, kServeDraw, kServePlain, kServeKernels };  // plain: none to set
 int serve_prepare(int device, ServeKernels k);
 // Refuses NULL and host-only handles, and prepares the call's kernels.
 int serve_context(wt_handle *h, const char *call, ServeKernels kernels, ServeContext *out);
@@ -156,5 +156,27 @@ struct AttendPlan {
 cudaError_t attend_prepare();
 cudaError_t launch_attend_warp(const AttendPlan &P, cudaStream_t s);
 cudaError_t launch_attend_merge(const AttendPlan &P, cudaStream_t s);
+
+// ---------------------------------------------------------------- wt_cross.cu
+// The work of a call is cut into cells: `keys` states of one request's memory for one kv head and one tile of
+// up to `rows` (token, head-in-group) rows, in the order request, kv head, row tile, states.  CTA c takes the
+// cells from c * per on, per of them.  A row tile whose cells one CTA takes whole is written as it is; else each
+// CTA leaves its part of O (fp32, not divided), m and l in a slot: 2c where the CTA's cells start in the row
+// tile or with it, 2c + 1 where the row tile starts behind them.
+struct CrossPlan {
+  wt_cross_desc d;
+  int G;           // heads / kv_heads
+  int rows, keys;
+  int ctas;
+  float *o;        // [2 ctas][rows][head_dim]
+  float2 *ml;      // [2 ctas][rows]
+  long long *first;  // [n_req + 1]: a request's first cell; then per
+  int *status;
+};
+cudaError_t cross_prepare();
+cudaError_t launch_cross_few(const CrossPlan &P, cudaStream_t s);
+cudaError_t launch_cross_merge(const CrossPlan &P, cudaStream_t s);
+// CTAs of the kernel for few rows that run at once on an SM
+int cross_few_resident(int rows, int head_dim);
 
 }  // namespace wt

@@ -6,6 +6,7 @@ One step of several requests over one set of weights, beside Handle.pass_:
     h.adapt([adapters(...), ...], stream)          # each request's low-rank adapter
     h.place(placement(...), stream)                # norms, rotation; keys and values to their pages
     h.attend(attention(...), stream)               # over the shared prefix and the paged caches
+    h.cross(cross_attention(...), stream)          # to each request's memory, as an encoder's states
     h.probs(probabilities(...), stream)            # the head's logits, at each row's temperature
     h.logprobs(log_probabilities(...), stream)     # of given tokens, with entropy and alternatives
     h.verify(verification(...), stream)            # which drafted tokens stay, and the next one
@@ -237,6 +238,41 @@ def attention(q, out, begin, k_pages=None, v_pages=None, table=None, lens=None, 
         _need(max_len <= table.shape[1] * page, "max_len %d fits table's %d pages of %d" % (max_len, table.shape[1], page))
     d.kv_heads = H if Hkv is None else Hkv
     d.tensors = (q, out, begin, prefix_k, prefix_v, k_pages, v_pages, table, lens)
+    return d
+
+
+def cross_attention(q, out, begin, k, v, mem_begin, mem_len, *, max_new, max_mem, keep=None, scale=None) -> wt.CrossDesc:
+    """Attention of each request's tokens to a memory of its own (see wt_cross).
+
+    q, out and begin are attention's.  k and v [states, kv_heads, head_dim], of q's type, each state and head
+    at any pitch (both tensors' alike); mem_begin and mem_len int32 [requests].  keep uint8 [states] (None:
+    all).  max_new and max_mem bound what begin and mem_len will hold.  scale None: head_dim ** -0.5."""
+    _need(q.dtype in _TYPES, "q is bf16 or f16, not %s" % q.dtype)
+    _is(q, "q", q.dtype, 3), _is(out, "out", q.dtype, 3), _is(k, "k", q.dtype, 3), _is(v, "v", q.dtype, 3)
+    N, H, D = q.shape
+    M, Hkv, Dk = k.shape
+    _need(out.shape == q.shape, "out has the shape of q")
+    _need(Dk == D and v.shape == k.shape, "k and v are [states, kv_heads, %d]" % D)
+    for t, name in ((q, "q"), (out, "out")):
+        _need(N == 0 or t[0].is_contiguous(), "the heads of a token of %s are contiguous" % name)
+    # the stride of a dimension of one says nothing
+    _need(M == 0 or (all(n == 1 or a == b for n, a, b in zip(k.shape, k.stride(), v.stride())) and (D == 1 or k.stride(2) == 1)),
+          "k and v have the same strides and contiguous head rows")
+    for t, name in ((begin, "begin"), (mem_begin, "mem_begin"), (mem_len, "mem_len")):
+        _is(t, name, torch.int32, 1), _dense(t, name)
+    _need(begin.shape[0] >= 1, "begin is [requests + 1]")
+    n_req = begin.shape[0] - 1
+    _need(mem_begin.shape[0] == n_req and mem_len.shape[0] == n_req, "mem_begin and mem_len have one for each request")
+    if keep is not None:
+        _is(keep, "keep", torch.uint8, 1), _dense(keep, "keep")
+        _need(keep.shape[0] == M, "keep is [states]")
+    d = wt.CrossDesc(q=_ptr(q), out=_ptr(out), begin=_ptr(begin), k=_ptr(k), v=_ptr(v), mem_begin=_ptr(mem_begin),
+                     mem_len=_ptr(mem_len), keep=_ptr(keep), q_stride=q.stride(0) if N > 1 else H * D,
+                     out_stride=out.stride(0) if N > 1 else H * D, mem_stride=k.stride(0) if M > 1 else Hkv * D,
+                     mem_head=k.stride(1) if Hkv > 1 else D, n_mem=M, dtype=_TYPES[q.dtype], n_req=n_req, n_tokens=N,
+                     max_new=max_new, max_mem=max_mem, heads=H, kv_heads=Hkv, head_dim=D,
+                     scale=D ** -0.5 if scale is None else scale)
+    d.tensors = (q, out, begin, k, v, mem_begin, mem_len, keep)
     return d
 
 

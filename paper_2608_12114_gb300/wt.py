@@ -40,7 +40,7 @@ SYMBOLS = ("wt_last_error", "wt_abi_version", "wt_open", "wt_num_tensors", "wt_n
            # include/wt_dlpack.h
            "wt_dlpack_file", "wt_dlpack_tensor", "wt_dlpack_release", "wt_dlpack_live",
            # include/wt_serve.h
-           "wt_adapt", "wt_place", "wt_attend", "wt_probs", "wt_logprobs", "wt_verify")
+           "wt_adapt", "wt_place", "wt_attend", "wt_cross", "wt_probs", "wt_logprobs", "wt_verify")
 WT_DLPACK_DEVICE, WT_DLPACK_HOST = 0, 1
 WT_ADAPT_MAX_RANK, WT_ADAPT_MAX_SLOTS, WT_VERIFY_MAX_VOCAB = 128, 4096, 1 << 18
 WT_PLACE_MAX_DIM, WT_PLACE_MAX_AXES, WT_PLACE_NEIGHBOURS, WT_LOGPROBS_MAX_TOP = 256, 8, 1, 32
@@ -104,6 +104,16 @@ class AttendDesc(C.Structure):
                 ("dtype", C.c_int32), ("n_req", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32),
                 ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page", C.c_int32),
                 ("n_pages", C.c_int32), ("max_len", C.c_int32), ("scale", C.c_float), ("pad", C.c_int32)]
+
+
+class CrossDesc(C.Structure):
+    """wt_cross_desc (serving.cross_attention makes one from tensors)."""
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("begin", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("mem_begin", C.c_void_p), ("mem_len", C.c_void_p), ("keep", C.c_void_p), ("q_stride", C.c_int64),
+                ("out_stride", C.c_int64), ("mem_stride", C.c_int64), ("mem_head", C.c_int64), ("n_mem", C.c_int64),
+                ("dtype", C.c_int32), ("n_req", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32),
+                ("max_mem", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("scale", C.c_float), ("pad", C.c_int32)]
 
 
 class ProbsDesc(C.Structure):
@@ -199,6 +209,7 @@ def lib(path: str = LIB_PATH):
     L.wt_adapt.argtypes = [vp, C.POINTER(AdaptDesc), sz, vp]
     L.wt_place.argtypes = [vp, C.POINTER(PlaceDesc), vp]
     L.wt_attend.argtypes = [vp, C.POINTER(AttendDesc), vp]
+    L.wt_cross.argtypes = [vp, C.POINTER(CrossDesc), vp]
     L.wt_probs.argtypes = [vp, C.POINTER(ProbsDesc), vp]
     L.wt_logprobs.argtypes = [vp, C.POINTER(LogprobsDesc), vp]
     L.wt_verify.argtypes = [vp, C.POINTER(VerifyDesc), vp]
@@ -400,6 +411,12 @@ class Handle:
     def attend(self, desc: AttendDesc, stream: int = 0):
         """wt_attend."""
         rc = lib().wt_attend(self.ptr, C.byref(desc), stream)
+        if rc:
+            _check(rc)
+
+    def cross(self, desc: CrossDesc, stream: int = 0):
+        """wt_cross."""
+        rc = lib().wt_cross(self.ptr, C.byref(desc), stream)
         if rc:
             _check(rc)
 

@@ -74,3 +74,32 @@ def top(logits, n):
     l = logits.tolist()
     order = sorted((v for v in range(len(l)) if l[v] == l[v] and l[v] > -INF), key=lambda v: (-l[v], v))[:n]
     return order + [-1] * (n - len(order))
+
+
+def cross(q, begin, k, v, mem_begin, mem_len, keep, scale):
+    """(out, sum p |v|, the states' largest sum |q| |k|), float64 on the CPU; rows no request holds stay NaN."""
+    q, k, v = q.double().cpu(), k.double().cpu(), v.double().cpu()
+    N, H, D = q.shape
+    G = H // k.shape[1]
+    out = torch.full((N, H, D), float("nan"), dtype=torch.float64)
+    mag, qk = torch.zeros_like(out), torch.zeros(N, H, 1, dtype=torch.float64)
+    begin, mem_begin, mem_len = begin.tolist(), mem_begin.tolist(), mem_len.tolist()
+    for b in range(len(mem_len)):
+        t = slice(begin[b], begin[b + 1])
+        rows = torch.arange(mem_begin[b], mem_begin[b] + mem_len[b])
+        if keep is not None:
+            rows = rows[keep.cpu()[rows] != 0]
+        if len(rows) == 0:
+            out[t] = 0
+            continue
+        for h in range(H):
+            kk, vv = k[rows, h // G], v[rows, h // G]
+            s = scale * (q[t, h] @ kk.t())
+            top = s.amax(dim=1, keepdim=True)
+            e = torch.exp(s - torch.where(top == -INF, torch.zeros_like(top), top))
+            p = e / torch.where(top == -INF, torch.ones_like(top), e.sum(dim=1, keepdim=True))
+            # a weight of 0 does not hide a value that is not finite
+            out[t, h] = p @ vv
+            mag[t, h] = p @ vv.abs()
+            qk[t, h, 0] = abs(scale) * (q[t, h].abs() @ kk.abs().t()).amax(dim=1)
+    return out, mag, qk

@@ -1,4 +1,4 @@
-"""Placing and log probabilities without a GPU: structures, constants, turns, and what is refused before any CUDA call."""
+"""Placing, attention to memories and log probabilities without a GPU: structures, constants, turns, and what is refused before any CUDA call."""
 import ctypes as C
 import math
 import os
@@ -13,7 +13,7 @@ from tests import _serve_more
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HEADER = os.path.join(ROOT, "include", "wt_serve.h")
-STRUCTS = {"wt_place_desc": wt.PlaceDesc, "wt_logprobs_desc": wt.LogprobsDesc}
+STRUCTS = {"wt_place_desc": wt.PlaceDesc, "wt_cross_desc": wt.CrossDesc, "wt_logprobs_desc": wt.LogprobsDesc}
 
 
 @pytest.fixture(scope="module")
@@ -45,7 +45,7 @@ def test_constants_match_the_header():
 
 def test_null_and_host_only_handles_are_refused(L):
     with wt.Handle([], wt.WT_OPEN_HOST_ONLY) as h:
-        for call, d in (("wt_place", wt.PlaceDesc()), ("wt_logprobs", wt.LogprobsDesc())):
+        for call, d in (("wt_place", wt.PlaceDesc()), ("wt_cross", wt.CrossDesc()), ("wt_logprobs", wt.LogprobsDesc())):
             assert getattr(L, call)(None, C.byref(d), None) == wt.WT_EINVAL and call in L.wt_last_error().decode()
             assert getattr(L, call)(h.ptr, C.byref(d), None) == wt.WT_ENOTSUP and call in L.wt_last_error().decode()
 
