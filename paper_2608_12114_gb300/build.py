@@ -9,8 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwt.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["wt_kernels.cu", "wt_fnv.cu", "wt_cols.cu", "wt_umma.cu", "wt_q8rows.cu", "wt_colshort.cu", "wt_host.cpp", "wt_dlpack.cpp",
-           "wt_noalloc.cu", "wt_serve.cpp", "wt_adapt.cu", "wt_attend.cu", "wt_prefix.cu", "wt_draw.cu", "wt_place.cu", "wt_cross.cu", "wt_logprobs.cu"]
-HEADERS = ["wt_cross.cuh", "wt_kernels.h", "wt_fnv.h", "wt_q8rows.h", "wt_device.cuh", "wt_serve.h", "wt_serve.cuh", os.path.join("..", "..", "include", "wt.h"),
+           "wt_noalloc.cu", "wt_serve.cpp", "wt_adapt.cu", "wt_attend.cu", "wt_prefix.cu", "wt_draw.cu", "wt_place.cu", "wt_cross.cu", "wt_crosswide.cu", "wt_logprobs.cu"]
+HEADERS = ["wt_cross.cuh", "wt_tmem.cuh", "wt_kernels.h", "wt_fnv.h", "wt_q8rows.h", "wt_device.cuh", "wt_serve.h", "wt_serve.cuh", os.path.join("..", "..", "include", "wt.h"),
            os.path.join("..", "..", "include", "wt_dlpack.h"), os.path.join("..", "..", "include", "wt_serve.h")]
 
 

@@ -49,8 +49,8 @@ __global__ void __launch_bounds__(kThreads, MT > 1 ? 2 : ND == 4 ? 4 : 3) cross_
       first += a.cells(d.kv_heads);
       a = asker_of(P, ++b, false);
     }
-    const Segment sg = segment_at(a, first, cell, share);
-    cell += sg.tiles;
+    const Segment sg = segment_at(P, a, first, cell, share);
+    cell += sg.cells;
     const int rows = a.n * G, row0 = sg.row_tile * kRows;
     const int k0 = sg.tile0 * kCell, k1 = min(a.len, k0 + sg.tiles * kCell);
     const int tiles = max(0, (k1 - k0 + kKeys - 1) / kKeys);
@@ -290,8 +290,8 @@ __global__ void __launch_bounds__(kThreads) cross_merge_kernel(const __grid_cons
   const int D = d.head_dim, h = i % d.heads, t = i / d.heads, hk = h / P.G;
   const int row = t * P.G + h % P.G, row_tile = row / P.rows, r = row - row_tile * P.rows;
   const long long per = P.first[d.n_req];
-  const long long u0 = P.first[b] + ((long long)hk * a.row_tiles + row_tile) * a.key_tiles;
-  const long long c0 = u0 / per, c1 = (u0 + a.key_tiles - 1) / per;
+  const long long u0 = P.first[b] + hk * a.head_cells() + (long long)row_tile * a.key_tiles;
+  const long long c0 = u0 / per, c1 = (u0 + (row_tile == a.row_tiles - 1 ? a.last : a.key_tiles) - 1) / per;
   if (c0 == c1) return;  // one CTA took it whole
   auto slot = [&](long long c) { return (2 * c + (c * per < u0)) * P.rows + r; };
   float m = -INFINITY;

@@ -12,7 +12,9 @@ struct Asker {
   int t0, n;         // first token, tokens
   int mem, len;      // first state, states
   int row_tiles, key_tiles;
-  __device__ long long cells(int kv_heads) const { return (long long)row_tiles * key_tiles * kv_heads; }
+  int last;          // cells of the last row tile
+  __device__ long long head_cells() const { return (row_tiles - 1ll) * key_tiles + last; }
+  __device__ long long cells(int kv_heads) const { return row_tiles ? head_cells() * kv_heads : 0; }
 };
 
 __device__ __forceinline__ Asker asker_of(const CrossPlan &P, int b, bool tell) {
@@ -26,9 +28,11 @@ __device__ __forceinline__ Asker asker_of(const CrossPlan &P, int b, bool tell) 
     mem = min(max(mem, 0), (int)d.n_mem);
     len = min(min(max(len, 0), d.max_mem), (int)d.n_mem - mem);
   }
-  const int n = t1 - t0;
+  const int n = t1 - t0, row_tiles = (n * P.G + P.rows - 1) / P.rows;
   // tokens without a state have a tile all the same: it writes their zeros
-  return {t0, n, mem, len, (n * P.G + P.rows - 1) / P.rows, max(1, (len + P.keys - 1) / P.keys)};
+  const int key_tiles = max(1, (len + P.keys - 1) / P.keys);
+  const bool half = n * P.G - (row_tiles - 1) * P.rows <= P.half;
+  return {t0, n, mem, len, row_tiles, key_tiles, half ? (key_tiles + 1) / 2 : key_tiles};
 }
 
 // This CTA's cells, and the request that the first of them lies in.
@@ -83,19 +87,25 @@ __device__ __forceinline__ Share share_of(const CrossPlan &P) {
 struct Segment {
   int hk, row_tile;
   int tile0, tiles;   // tiles of P.keys states
-  bool whole;         // all of the row tile's
+  int cells;          // as many, or half of them (P.half)
+  bool half, whole;   // whole: all of the row tile's
   long long slot;     // where the part goes else
 };
 
 // The segment that starts at cell `at` of request a, whose first cell is `first`.
-__device__ __forceinline__ Segment segment_at(const Asker &a, long long first, long long at, const Share &s) {
-  const long long u = (at - first) / a.key_tiles, begin = first + u * a.key_tiles, end = min(s.hi, begin + a.key_tiles);
+__device__ __forceinline__ Segment segment_at(const CrossPlan &P, const Asker &a, long long first, long long at, const Share &s) {
   Segment g;
-  g.hk = (int)(u / a.row_tiles);
-  g.row_tile = (int)(u - (long long)g.hk * a.row_tiles);
-  g.tile0 = (int)(at - begin);
-  g.tiles = (int)(end - at);
-  g.whole = g.tiles == a.key_tiles;
+  const long long per_head = a.head_cells();
+  g.hk = (int)((at - first) / per_head);
+  const long long head = first + g.hk * per_head;
+  g.row_tile = (int)min((at - head) / a.key_tiles, a.row_tiles - 1ll);
+  const long long begin = head + (long long)g.row_tile * a.key_tiles;
+  const int all = g.row_tile == a.row_tiles - 1 ? a.last : a.key_tiles;
+  g.half = a.n * P.G - g.row_tile * P.rows <= P.half;
+  g.cells = (int)(min(s.hi, begin + all) - at);
+  g.whole = g.cells == all;
+  g.tile0 = (int)(at - begin) << g.half;
+  g.tiles = min(g.cells << g.half, a.key_tiles - g.tile0);
   g.slot = 2 * blockIdx.x + (begin >= s.lo && at > s.lo);
   return g;
 }

@@ -2375,7 +2375,10 @@ int wt::serve_prepare(int device, ServeKernels k) {
     CU(attend_prepare());
     CU(prefix_prepare());
   }
-  if (k == kServeCross) CU(cross_prepare());
+  if (k == kServeCross) {
+    CU(cross_prepare());
+    CU(cross_wide_prepare());
+  }
   if (k == kServeDraw) CU(draw_prepare());
   if (device < 64) ready[device][k].store(true, std::memory_order_release);
   return WT_OK;

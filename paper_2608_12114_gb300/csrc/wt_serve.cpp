@@ -514,6 +514,13 @@ int check_cross(wt_handle *h, const wt_cross_desc &d) {
   return WT_OK;
 }
 
+// Many rows (token, head-in-group) of a request go to tcgen05.  Its softmax takes the largest product for the
+// largest score, so the scale has to be positive; and a pitch has to fit a tensor map.
+bool cross_on_tcgen05(const wt_cross_desc &d) {
+  return (int64_t)d.max_new * (d.heads / d.kv_heads) > 32 && d.max_mem > 0 && d.scale > 0.0f && d.q_stride < (1ll << 38) &&
+         d.mem_stride < (1ll << 38) && d.mem_head < (1ll << 38);
+}
+
 int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
   wt::ServeContext ctx;
   CHECK(wt::serve_context(h, "wt_cross", wt::kServeCross, &ctx));
@@ -528,14 +535,32 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
   d.max_mem = (int32_t)std::min<int64_t>(d.max_mem, d.n_mem);
   P.G = d.heads / d.kv_heads;
   P.status = ctx.status;
-  P.keys = 64;
-  P.rows = (int64_t)d.max_new * P.G <= 16 ? 16 : 32;
+  wt::CrossMaps maps;
+  const bool wide = cross_on_tcgen05(d);
+  if (wide) {
+    P.tile_tokens = 128 / P.G;
+    P.half = P.tile_tokens * P.G;
+    P.rows = 2 * P.half;
+    P.keys = 128;
+    const uint64_t D = d.head_dim;
+    const uint64_t qd[3] = {D, (uint64_t)d.heads, (uint64_t)d.n_tokens}, qs[2] = {2 * D, 2 * (uint64_t)d.q_stride};
+    const uint32_t qb[3] = {64, (uint32_t)P.G, (uint32_t)P.tile_tokens};
+    const uint64_t kd[3] = {D, (uint64_t)d.kv_heads, (uint64_t)d.n_mem}, ks[2] = {2 * (uint64_t)d.mem_head, 2 * (uint64_t)d.mem_stride};
+    const uint32_t kb[3] = {64, 1, 128};
+    CHECK(wt::serve_tensor_map(maps.q, d.q, 3, qd, qs, qb));
+    CHECK(wt::serve_tensor_map(maps.k, d.k, 3, kd, ks, kb));
+    CHECK(wt::serve_tensor_map(maps.v, d.v, 3, kd, ks, kb));
+  } else {
+    P.keys = 64;
+    P.rows = (int64_t)d.max_new * P.G <= 16 ? 16 : 32;
+  }
   // No more CTAs than run at once, or than there can be cells.  (Requests' row tiles: whole ones of all tokens,
   // and one more each.)
   const double tiles = std::min((double)d.n_req * (double)ceil_div((int64_t)d.max_new * P.G, P.rows),
                                 (double)d.n_tokens * P.G / P.rows + d.n_req);
   const double cells = tiles * d.kv_heads * (double)std::max<int64_t>(1, ceil_div(d.max_mem, P.keys));
-  P.ctas = (int)std::max(1.0, std::min((double)wt::cross_few_resident(P.rows, d.head_dim) * wt::num_sms(), cells));
+  const int resident = wide ? 1 : wt::cross_few_resident(P.rows, d.head_dim);
+  P.ctas = (int)std::max(1.0, std::min((double)resident * wt::num_sms(), cells));
   auto take = [](size_t &at, size_t n) {
     const size_t o = at;
     at += (n + 255) / 256 * 256;
@@ -553,7 +578,7 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
   P.ml = reinterpret_cast<float2 *>(ws + ml);
   P.first = reinterpret_cast<long long *>(ws + first);
   const bool joined = d.max_mem > P.keys;  // memories of one cell: no row tile has two parts
-  cudaError_t e = wt::launch_cross_few(P, s);
+  cudaError_t e = wide ? wt::launch_cross_wide(P, maps, s) : wt::launch_cross_few(P, s);
   if (e == cudaSuccess && joined) e = wt::launch_cross_merge(P, s);
   const int rc = wt::serve_done(h, s, w);
   CU(e);

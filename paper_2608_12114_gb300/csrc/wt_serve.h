@@ -159,14 +159,16 @@ cudaError_t launch_attend_merge(const AttendPlan &P, cudaStream_t s);
 
 // ---------------------------------------------------------------- wt_cross.cu
 // The work of a call is cut into cells: `keys` states of one request's memory for one kv head and one tile of
-// up to `rows` (token, head-in-group) rows, in the order request, kv head, row tile, states.  CTA c takes the
-// cells from c * per on, per of them.  A row tile whose cells one CTA takes whole is written as it is; else each
-// CTA leaves its part of O (fp32, not divided), m and l in a slot: 2c where the CTA's cells start in the row
+// up to `rows` (token, head-in-group) rows, in the order request, kv head, row tile, states.  A row tile of no
+// more than `half` rows takes as long for 2 keys as others for keys, and a cell of it has as many.  CTA c takes
+// the cells from c * per on, per of them.  A row tile whose cells one CTA takes whole is written as it is; else
+// each CTA leaves its part of O (fp32, not divided), m and l in a slot: 2c where the CTA's cells start in the row
 // tile or with it, 2c + 1 where the row tile starts behind them.
 struct CrossPlan {
   wt_cross_desc d;
   int G;           // heads / kv_heads
-  int rows, keys;
+  int rows, half, keys;
+  int tile_tokens;  // many rows: whole tokens of a tile of up to 128 rows
   int ctas;
   float *o;        // [2 ctas][rows][head_dim]
   float2 *ml;      // [2 ctas][rows]
@@ -176,6 +178,14 @@ struct CrossPlan {
 cudaError_t cross_prepare();
 cudaError_t launch_cross_few(const CrossPlan &P, cudaStream_t s);
 cudaError_t launch_cross_merge(const CrossPlan &P, cudaStream_t s);
+// Many rows, on tcgen05 (wt_crosswide.cu)
+struct CrossMaps {
+  alignas(64) uint8_t q[128];  // CUtensorMaps
+  alignas(64) uint8_t k[128];
+  alignas(64) uint8_t v[128];
+};
+cudaError_t cross_wide_prepare();
+cudaError_t launch_cross_wide(const CrossPlan &P, const CrossMaps &m, cudaStream_t s);
 // CTAs of the kernel for few rows that run at once on an SM
 int cross_few_resident(int rows, int head_dim);
 
