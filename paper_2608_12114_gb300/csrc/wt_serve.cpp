@@ -717,7 +717,7 @@ int place_impl(wt_handle *h, const wt_place_desc *dp, cudaStream_t s) {
   if (!d.k && !d.v) d.table = nullptr;
   if (!d.k && !d.v && (d.pos || !d.rot_dim || !d.q)) d.len = nullptr;
   P.status = ctx.status;
-  if (!wt::plan_place(&P)) return serve_error(WT_EINVAL, "wt_place: too many tokens and heads for one launch");
+  wt::plan_place(&P);
   return launch_alone(h, s, [&] { return wt::launch_place(P, s); });
 }
 

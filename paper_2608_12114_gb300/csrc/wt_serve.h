@@ -91,14 +91,13 @@ cudaError_t launch_verify(const wt_verify_desc &d, int *status, cudaStream_t s);
 // ---------------------------------------------------------------- wt_place.cu
 struct PlacePlan {
   wt_place_desc d;
-  int width_log2;   // lanes of a head: 8 elements each
-  int chunk_heads;  // heads of a warp, of those of q, k and v in a row
-  int chunks;       // warps of a token
+  int unit;    // elements of a lane: 8 or 16
+  int rounds;  // times that a warp takes as many heads as its lanes hold
+  int chunks;  // CTAs of a token
   float inv_dim;
   int *status;
 };
-// Sets the plan's split; false where it does not fit one launch.
-bool plan_place(PlacePlan *P);
+void plan_place(PlacePlan *P);
 cudaError_t launch_place(const PlacePlan &P, cudaStream_t s);
 
 // ---------------------------------------------------------------- wt_logprobs.cu
