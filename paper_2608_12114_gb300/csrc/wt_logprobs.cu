@@ -1,22 +1,30 @@
 // Log probabilities, entropy and the likeliest tokens of logits rows (include/wt_serve.h).
 //
-// One reading of each row, spread over a cluster of CTAs where rows are few.  Per row, with
-// x = (l - m) log2(e) / t for the largest logit m:
+// One reading of all rows.  Per row, with x = (l - m) log2(e) / t for the largest logit m:
 //
 //   s = sum over all but one of the largest of 2^x,      log S = log1p(s)
 //   w = sum of x 2^x,                                    H = log1p(s) - ln 2 w / (1 + s)
 //
 // The largest logit's own 1 stays out of s, so that a sharp row keeps its entropy and its likeliest token's
-// log probability to fp32's precision: nothing is subtracted (w <= 0).  A thread keeps (m, s, w) of what it has
-// seen; two of them, m1 >= m2, join as s1 + f (s2 + 1) and w1 + f (w2 + d (s2 + 1)), d = (m2 - m1) log2(e) / t,
-// f = 2^d: threads, warps and CTAs in a fixed order.
+// log probability to fp32's precision: nothing is subtracted.  A thread keeps four largest logits, of every
+// fourth that it sees, out of its sums: of a new logit and the one kept, the smaller goes in.  Its sums are against
+// a reference of its warp, the first largest logit, which moves when one is 2^60 above it.  At the end all of the
+// kept ones but one go in, too.  Two parts, m1 >= m2, join as s1 + f (s2 + 1) and w1 + f (w2 + d (s2 + 1)),
+// d = (m2 - m1) log2(e) / t, f = 2^d: warps and CTAs in a fixed order.  (With the thread's one largest logit as its
+// reference, which half the time moved in one lane of a warp or another, the kernel was bound by its
+// instructions: 2047 rows of 50021 logits took 97 us, and 67 this way, 6.1 TB/s.)
 //
-// Alternatives: a warp keeps the 32 largest (logit, token) it has seen, one a lane, in order.  The warps of a CTA
-// share the best of their n_top-th logits: what lies under it is not among the row's n_top, whatever the timing.
-// A candidate is found by one comparison of 16 logits' maximum; n ln(V / n) of a row's V are taken up.  At the
-// end each of up to 256 candidates counts those above it, first among the warps, then among the CTAs.
-#include <cooperative_groups.h>
-
+// The rows' 16-byte vectors, one row after another, are cut into equal shares, one a CTA, so that no number of
+// rows leaves SMs idle.  A row that one CTA has whole is answered there; the parts of others go to the workspace,
+// and a second kernel joins them.
+//
+// Alternatives: a warp keeps the 32 largest (logit, token) it has seen, one a lane, in order.  What lies under the
+// n_top-th largest of several disjoint groups' maxima, or under any warp's n_top-th, is not among the row's
+// n_top, whatever the timing; so 64 groups of four threads tell the CTA's warps where to look, from the first
+// 4096 logits on and better after 2, 4, 8, ... times as many: some n_top / i random logits of the i-th 4096 are
+// taken up.  At the end each of them counts those above it, which is its place: many comparisons at once, where
+// sorting is a chain of them.  A warp that takes up more than its room sorts 32 and joins them to a list of its
+// own: the larger of each and its opposite, sorted in five exchanges.
 #include <algorithm>
 
 #include "wt_serve.cuh"
@@ -25,14 +33,17 @@ namespace wt {
 
 namespace {
 
-namespace cg = cooperative_groups;
-
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
-constexpr int kVecs = 4;  // 16-byte vectors of a lane in flight
+constexpr int kResident = 4;  // CTAs to an SM
+constexpr int kVecs = 4;      // 16-byte vectors of a lane in flight (the next ones, too, in registers or by bulk
+                              // copies: no faster, as other CTAs load meanwhile)
+constexpr int kTurn = kThreads * kVecs;  // vectors that a CTA takes at a time
 constexpr int kTop = WT_LOGPROBS_MAX_TOP;
+constexpr int kGroups = 64;
+constexpr float kGrow = 60.0f;  // in log2: weights and their sums stay far below 2^127
 static_assert(kTop == 32, "one candidate a lane");
+static_assert(kGroups == kThreads / 4 && kGroups >= kTop, "groups of four threads, enough of them");
 
 typedef unsigned long long Key;  // order of the logit, then ~token: the larger comes first; 0: none
 
@@ -63,217 +74,450 @@ __device__ __forceinline__ Sums shuffle(const Sums &a, int o) {
           __shfl_xor_sync(0xffffffffu, a.w, o)};
 }
 
-// Into the warp's list (descending over the lanes).
-__device__ __forceinline__ void insert(Key &mine, Key c, int lane) {
-  const Key up = __shfl_up_sync(0xffffffffu, mine, 1);
-  if (mine < c) mine = lane && up < c ? up : c;
+__device__ __forceinline__ float min_or_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// (x0, x1) * k, and (w0, w1) + (p0, p1) * (x0, x1), in one instruction each.
+__device__ __forceinline__ void mul_x2(float &x0, float &x1, float k) {
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "+f"(x0), "+f"(x1)
+      : "f"(k));
+}
+__device__ __forceinline__ void fma_x2(float &w0, float &w1, float p0, float p1, float x0, float x1) {
+  asm("{\n\t.reg .b64 w, p, x;\n\tmov.b64 w, {%0, %1};\n\tmov.b64 p, {%2, %3};\n\tmov.b64 x, {%4, %5};\n\t"
+      "fma.rn.f32x2 w, p, x, w;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "+f"(w0), "+f"(w1)
+      : "f"(p0), "f"(p1), "f"(x0), "f"(x1));
+}
+
+// The 32 largest of two ordered lists, in order.
+__device__ __noinline__ Key merged(Key mine, Key other, int lane) {
+  const Key opposite = __shfl_sync(0xffffffffu, other, 31 - lane);
+  mine = mine > opposite ? mine : opposite;
+#pragma unroll 1
+  for (int o = 16; o; o >>= 1) {
+    const Key x = __shfl_xor_sync(0xffffffffu, mine, o);
+    mine = ((lane & o) == 0) == (mine > x) ? mine : x;
+  }
+  return mine;
+}
+
+// 32 keys in order, the largest first.
+__device__ __noinline__ Key sorted(Key mine, int lane) {
+#pragma unroll 1
+  for (int n = 2; n <= 32; n *= 2)
+#pragma unroll 1
+    for (int o = n / 2; o; o >>= 1) {
+      const Key x = __shfl_xor_sync(0xffffffffu, mine, o);
+      const bool larger = ((lane & o) == 0) == ((lane & n) == 0);
+      mine = larger == (mine > x) ? mine : x;
+    }
+  return mine;
+}
+
+// The n-th largest of the 64 groups' maxima.  Other warps may write larger ones meanwhile.
+__device__ __noinline__ unsigned bound_of(const volatile unsigned *maxima, int n, int lane) {
+  const unsigned m0 = maxima[lane], m1 = maxima[lane + 32];
+  int above0 = 0, above1 = 0;
+#pragma unroll 8
+  for (int i = 0; i < 32; ++i) {
+    const unsigned x = __shfl_sync(0xffffffffu, m0, i), y = __shfl_sync(0xffffffffu, m1, i);
+    above0 += (x > m0) + (y > m0);
+    above1 += (x > m1) + (y > m1);
+  }
+  // the smallest that fewer than n are above
+  return __reduce_min_sync(0xffffffffu, min(above0 < n ? m0 : ~0u, above1 < n ? m1 : ~0u));
+}
+
+// put(place, key) for those of n different keys in shared memory that fewer than n_top are above; by the block.
+template <typename F>
+__device__ __forceinline__ void placed(const Key *keys, int n, int n_top, F put) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const Key mine = keys[i];
+    int above = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) above += keys[j] > mine;
+    if (above < n_top) put(above, mine);
+  }
+  for (int i = n + threadIdx.x; i < n_top; i += blockDim.x) put(i, 0);
+}
+
+// What a row's sums answer.
+struct Answer {
+  const wt_logprobs_desc &d;
+  int row;
+  const float *l;
+  Sums a;
+  float t, log_s;
+  bool draw, bad, none;
+  __device__ Answer(const wt_logprobs_desc &desc, int r, const Sums &sums, float temp)
+      : d(desc), row(r), l(desc.logits + (int64_t)r * desc.ldl), a(sums), t(temp), log_s(log1pf(sums.s)), draw(temp > 0.0f),
+        bad(draw && (sums.m == INFINITY || sums.s != sums.s)), none(!(sums.m > -INFINITY)) {}
+  __device__ float logp(float x, int token) const {
+    if (bad) return NAN;
+    if (none || !(x > -INFINITY)) return -INFINITY;
+    if (!draw) return token == a.first ? 0.0f : -INFINITY;
+    return (x - a.m) / t - log_s;
+  }
+  // by a warp
+  __device__ void write(int i, int *status) const {
+    const int token = i < d.n_given ? d.given[(int64_t)row * d.given_stride + i] : -1;
+    write(i, token, token >= 0 && token < d.vocab ? l[token] : 0.0f, status);
+  }
+  // whose first 32 given tokens and their logits are in hand
+  __device__ void write(int i, int token, float logit, int *status) const {
+    if (i == 0 && d.entropy) d.entropy[row] = bad ? NAN : none || !draw ? 0.0f : log_s - 0.69314718055994531f * a.w / (1.0f + a.s);
+    for (int g = i; g < d.n_given; g += 32) {
+      if (g >= 32) {
+        token = d.given[(int64_t)row * d.given_stride + g];
+        if (token >= 0 && token < d.vocab) logit = l[token];
+      }
+      if (token >= d.vocab && status) atomicCAS(status, 0, kStatusInvalid);
+      d.given_lp[(int64_t)row * d.n_given + g] = token >= 0 && token < d.vocab ? logp(logit, token) : 0.0f;
+    }
+  }
+  __device__ void write_top(int at, Key key) const {
+    if (at >= d.n_top) return;
+    const int token = (int)~(uint32_t)key;
+    d.top[(int64_t)row * d.n_top + at] = key ? token : -1;
+    d.top_lp[(int64_t)row * d.n_top + at] = key ? logp(logit_of((uint32_t)(key >> 32)), token) : bad ? NAN : -INFINITY;
+  }
+};
+
+// Beyond the largest number any factor sends every logit but the largest to 0, and one above 0 a logit of
+// -infinity, whatever the temperature.
+__device__ __forceinline__ float factor_of(float t) { return t > 0.0f ? fmaxf(fminf(1.4426950408889634f / t, 3.4028234e38f), 1.1754944e-38f) : 1.0f; }
+
+// a / b for numbers from 0 on; most are small
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
 }
 
 template <bool TOP>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const wt_logprobs_desc d, int *status) {
-  __shared__ Sums warp_sums[kWarps];
-  __shared__ Sums cta_sums;
-  __shared__ Key cand[kWarps * kTop];  // of the warps; then, in the first CTA, of the CTAs
-  __shared__ Key best[kTop];           // of the CTA
-  __shared__ unsigned floor_order;
-  cg::cluster_group cl = cg::this_cluster();
-  const int C = cl.num_blocks(), c = cl.block_rank();
-  const int row = blockIdx.x / C, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const float *l = d.logits + (int64_t)row * d.ldl;
-  const float t = d.temp ? d.temp[row] : 1.0f;
-  const bool draw = t > 0.0f;
-  // Beyond the largest number any factor sends every logit but the largest to 0, and one above 0 a logit of
-  // -infinity, whatever the temperature.
-  const float k = draw ? fmaxf(fminf(1.4426950408889634f / t, 3.4028234e38f), 1.1754944e-38f) : 1.0f;
-  if (TOP) {
-    if (tid == 0) floor_order = 0;
-    for (int i = tid; i < kWarps * kTop; i += kThreads) cand[i] = 0;
-    for (int i = tid; i < kTop; i += kThreads) best[i] = 0;
-    __syncthreads();
-  }
-
-  // The row's vectors start at the 16-byte boundary at or before it: `off` elements of the first are not its.
-  const int off = (int)(reinterpret_cast<uintptr_t>(l) / 4 % 4);
-  const int64_t vecs = ((int64_t)d.vocab + off + 3) / 4, per = (vecs + C - 1) / C;
-  const int64_t lo = c * per, hi = min(vecs, lo + per);
-  Sums a = {-INFINITY, INT32_MAX, 0.0f, 0.0f};
-  Key list = 0;
-  float least = -3.4028234e38f;  // a candidate is at least that: neither NaN nor -infinity
-  for (int64_t j0 = lo; j0 < hi; j0 += kThreads * kVecs) {
-    float v[kVecs][4];
-    const int64_t j1 = j0 + warp * 32 * kVecs + lane;  // a warp's vectors lie together, in ascending order
+__global__ void __launch_bounds__(kThreads, kResident) logprobs_kernel(const __grid_constant__ LogprobsPlan P) {
+  __shared__ Sums warp_sums[kWarps], row_sums;
+  __shared__ __align__(16) unsigned maxima[kGroups];
+  __shared__ unsigned floor_order, first_bound;
+  __shared__ Key taken[TOP ? kWarps : 1][2 * kTop];  // up by each warp
+  __shared__ Key candidates[TOP ? kWarps * 2 * kTop : 1];
+  __shared__ int counts[kWarps];
+  const wt_logprobs_desc &d = P.d;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const long long begin = P.per * blockIdx.x, end = min((long long)d.rows * P.row_vecs, begin + P.per);
+  for (long long at = begin; at < end;) {
+    const int row = (int)quotient(at, P.row_vecs);
+    const long long row0 = (long long)row * P.row_vecs;
+    const int lo = (int)(at - row0), hi = (int)(min(end, row0 + P.row_vecs) - row0);
+    const bool whole = lo == 0 && hi == P.row_vecs;
+    const long long slot = 2 * blockIdx.x + (lo == 0 && at > begin);
+    at = row0 + hi;
+    const float *l = d.logits + (int64_t)row * d.ldl;
+    const float t = d.temp ? d.temp[row] : 1.0f, k = factor_of(t);
+    // The row's vectors start at the 16-byte boundary at or before it: `off` elements of the first are not its.
+    const int off = (int)(reinterpret_cast<uintptr_t>(l) / 4 % 4);
+    if (TOP) {
+      __syncthreads();  // the last row's lists have been read
+      if (tid == 0) floor_order = 0, first_bound = ~0u;
+    }
+    float kept[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, ref = -INFINITY;
+    float s[2] = {0.0f, 0.0f}, w[2] = {0.0f, 0.0f};
+    int first = INT32_MAX;         // a greedy row's: the first of the thread's largest logits
+    Key list = 0;
+    int n_taken = 0;
+    float least = -3.4028234e38f;  // a candidate is at least that: neither NaN nor -infinity
+    const bool greedy = !(t > 0.0f);
+    for (int j0 = lo; j0 < hi; j0 += kTurn) {
+      float v[kVecs][4];
+      const int j1 = j0 + warp * 32 * kVecs + lane;  // a warp's vectors lie together, in ascending order
+      const int e1 = 4 * j1 - off;                   // token of v[0][0]
+      if (j0 > 0 && j0 + kTurn <= hi && 4 * (j0 + kTurn) - off <= d.vocab) {  // all of them are the row's
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int64_t j = j1 + i * 32, e0 = 4 * j - off;
-      if (j < hi && e0 >= 0 && e0 + 4 <= d.vocab) {
-        const float4 x = __ldcs(reinterpret_cast<const float4 *>(l + e0));
-        v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
+        for (int i = 0; i < kVecs; ++i) {
+          const float4 x = __ldcs(reinterpret_cast<const float4 *>(l + e1) + i * 32);
+          v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
+        }
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[i][e] = j < hi && e0 + e >= 0 && e0 + e < d.vocab ? __ldcs(l + e0 + e) : -INFINITY;
+        for (int i = 0; i < kVecs; ++i) {
+          const int j = j1 + i * 32, e0 = 4 * j - off;
+          if (j < hi && e0 >= 0 && e0 + 4 <= d.vocab) {
+            const float4 x = __ldcs(reinterpret_cast<const float4 *>(l + e0));
+            v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i][e] = j < hi && e0 + e >= 0 && e0 + e < d.vocab ? __ldcs(l + e0 + e) : -INFINITY;
+          }
+        }
       }
-    }
-    float top = -INFINITY;
+      float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) top = fmaxf(top, fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3])));
-    const int e1 = (int)(4 * j1 - off);  // token of v[0][0]
-    int skip = -1;  // the new largest one's place
-    if (top > a.m) {
+      for (int i = 0; i < kVecs; ++i) top = fmaxf(top, fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3])));
+      if (__any_sync(0xffffffffu, (top - ref) * k > kGrow)) {
+        float to = top;
 #pragma unroll
-      for (int i = kVecs - 1; i >= 0; --i)
+        for (int o = 16; o; o >>= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, o));
+        const float by = fmaxf((ref - to) * k, -200.0f), f = exp2_approx(by);
 #pragma unroll
-        for (int e = 3; e >= 0; --e)
-          if (v[i][e] == top) skip = i * 4 + e;
-      if (a.m > -INFINITY) {
-        const float dd = fmaxf((a.m - top) * k, -200.0f), f = exp2_approx(dd), n = a.s + 1.0f;
-        a.w = f * (a.w + dd * n);
-        a.s = f * n;
+        for (int i = 0; i < 2; ++i) w[i] = f * (w[i] + by * s[i]), s[i] *= f;
+        ref = to;
       }
-      a.m = top;
-      a.first = e1 + (skip >> 2) * 128 + (skip & 3);
-    }
-    const float mz = a.m > -INFINITY ? a.m : 0.0f;
-    float s[2] = {0.0f, 0.0f}, w[2] = {0.0f, 0.0f};
-    if (skip >= 0) {
+      if (greedy && top > fmaxf(fmaxf(kept[0], kept[1]), fmaxf(kept[2], kept[3]))) {
+#pragma unroll
+        for (int i = kVecs - 1; i >= 0; --i)
+#pragma unroll
+          for (int e = 3; e >= 0; --e)
+            if (v[i][e] == top) first = e1 + i * 128 + e;
+      }
+      const float z = ref > -INFINITY ? ref : 0.0f;
 #pragma unroll
       for (int i = 0; i < kVecs; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = (v[i][e] - mz) * k, p = i * 4 + e == skip ? 0.0f : exp2_approx(x);
-          s[e & 1] += p;
-          w[e & 1] += p * fmaxf(x, -200.0f);
+        for (int e = 0; e < 4; e += 2) {
+          float x0 = min_or_nan(v[i][e], kept[e]), x1 = min_or_nan(v[i][e + 1], kept[e + 1]);
+          kept[e] = fmaxf(kept[e], v[i][e]);
+          kept[e + 1] = fmaxf(kept[e + 1], v[i][e + 1]);
+          sub_x2(x0, x1, x0, x1, z, z);
+          mul_x2(x0, x1, k);
+          const float p0 = exp2_approx(x0), p1 = exp2_approx(x1);
+          add_x2(s[0], s[1], p0, p1);
+          fma_x2(w[0], w[1], p0, p1, fmaxf(x0, -200.0f), fmaxf(x1, -200.0f));  // 0 where p is
         }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = (v[i][e] - mz) * k, p = exp2_approx(x);
-          s[e & 1] += p;
-          w[e & 1] += p * fmaxf(x, -200.0f);  // 0 where p is
-        }
-    }
-    a.s += s[0] + s[1];
-    a.w += w[0] + w[1];
 
-    if (TOP) {
-      if (__any_sync(0xffffffffu, top >= least)) {
-        least = fmaxf(least, logit_of(max(*reinterpret_cast<volatile unsigned *>(&floor_order), order_of(-3.4028234e38f))));
-        Key last = __shfl_sync(0xffffffffu, list, d.n_top - 1);
-        bool more = false;
+      if (TOP) {
+        // the groups' largest so far; one warp after another looks where the n_top largest can be
+        float most = fmaxf(fmaxf(kept[0], kept[1]), fmaxf(kept[2], kept[3]));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        if (lane % 4 == 0) reinterpret_cast<volatile unsigned *>(maxima)[tid / 4] = order_of(most);
+        const int turn = (j0 - lo) / kTurn;
+        if (turn == 0) {
+          __syncthreads();
+          const unsigned mine = maxima[tid / 4];
+          int above = 0;
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i)
+          for (int i = 0; i < kGroups / 4; i += 4) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(maxima + tid % 4 * (kGroups / 4) + i);
+            above += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
+          }
+          above += __shfl_xor_sync(0xffffffffu, above, 1);
+          above += __shfl_xor_sync(0xffffffffu, above, 2);
+          // the smallest that fewer than n_top are above
+          const unsigned low = __reduce_min_sync(0xffffffffu, above < d.n_top ? mine : ~0u);
+          if (lane == 0) atomicMin(&first_bound, low);
+          __syncthreads();
+          least = fmaxf(least, logit_of(first_bound));
+        } else if ((turn & (turn + 1)) == 0 && __popc(turn) % kWarps == warp) {
+          __syncwarp();
+          const unsigned low = bound_of(maxima, d.n_top, lane);
+          if (lane == 0) atomicMax(&floor_order, low);
+          least = fmaxf(least, logit_of(low));
+        }
+        if (__any_sync(0xffffffffu, top >= least)) {
+          least = fmaxf(least, logit_of(max(*reinterpret_cast<volatile unsigned *>(&floor_order), order_of(-3.4028234e38f))));
+          unsigned mine = 0;  // this thread's to take up
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const Key mine = v[i][e] >= least ? key_of(v[i][e], e1 + i * 128 + e) : 0;
-            unsigned who = __ballot_sync(0xffffffffu, mine > last);
-            while (who) {
-              const int from = __ffs(who) - 1;
-              insert(list, __shfl_sync(0xffffffffu, mine, from), lane);
-              last = __shfl_sync(0xffffffffu, list, d.n_top - 1);
-              who = __ballot_sync(0xffffffffu, mine > last) & ~((2u << from) - 1);
-              more = true;
+          for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine |= v[i][e] >= least ? 1u << (i * 4 + e) : 0u;
+          unsigned who;
+          while ((who = __ballot_sync(0xffffffffu, mine != 0))) {
+            const int which = __ffs(mine) - 1;
+            float x = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x = which == i * 4 + e ? v[i][e] : x;
+            if (mine) taken[warp][n_taken + __popc(who & ((1u << lane) - 1))] = key_of(x, e1 + (which >> 2) * 128 + (which & 3));
+            mine &= mine - 1;
+            n_taken += __popc(who);
+            if (n_taken >= kTop) {
+              __syncwarp();
+              list = merged(list, sorted(taken[warp][lane], lane), lane);
+              n_taken -= kTop;
+              const Key rest = taken[warp][kTop + lane];
+              __syncwarp();
+              if (lane < n_taken) taken[warp][lane] = rest;
+              const uint32_t o = (uint32_t)(__shfl_sync(0xffffffffu, list, d.n_top - 1) >> 32);
+              if (o) {
+                least = fmaxf(least, logit_of(o));
+                if (lane == 0) atomicMax(&floor_order, o);
+              }
             }
           }
-        if (more && last) {
-          const uint32_t o = (uint32_t)(last >> 32);
-          least = fmaxf(least, logit_of(o));
-          if (lane == 0) atomicMax(&floor_order, o);
         }
       }
     }
-  }
-
-  // the warps' sums, in order
+    // the warp's sums: all that its threads kept go in but one, a largest
+    Sums a;
+    {
+      const float mine = fmaxf(fmaxf(kept[0], kept[1]), fmaxf(kept[2], kept[3]));
+      float m = mine;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const Sums b = shuffle(a, o);
-    a = lane & o ? join(b, a, k) : join(a, b, k);
-  }
-  if (lane == 0) warp_sums[warp] = a;
-  if (TOP && lane < d.n_top) cand[warp * kTop + lane] = list;
-  __syncthreads();
-  if (tid == 0) {
-    a = warp_sums[0];
-    for (int i = 1; i < kWarps; ++i) a = join(a, warp_sums[i], k);
-    cta_sums = a;
-  }
-  // a candidate's place is the number of those above it
-  auto choose = [&](Key mine, int n, auto put) {
-    if (!mine) return;
-    int above = 0;
-    for (int i = 0; i < n; ++i) above += cand[i] > mine;
-    if (above < d.n_top) put(above, mine);
-  };
-  if (TOP) choose(cand[tid], kWarps * kTop, [&](int at, Key mine) { best[at] = mine; });
-  static_assert(kWarps * kTop == kThreads && kMaxCluster <= kWarps, "a candidate a thread");
-  cl.sync();
-  if (c == 0) {
-    a = cta_sums;
-    for (int q = 1; q < C; ++q) a = join(a, *cl.map_shared_rank(&cta_sums, q), k);
-    const bool bad = draw && (a.m == INFINITY || a.s != a.s), none = !(a.m > -INFINITY);
-    const float log_s = log1pf(a.s);
-    auto logp = [&](float x, int token) -> float {
-      if (bad) return NAN;
-      if (none || !(x > -INFINITY)) return -INFINITY;
-      if (!draw) return token == a.first ? 0.0f : -INFINITY;
-      return (x - a.m) / t - log_s;
-    };
-    if (tid == 0 && d.entropy) d.entropy[row] = bad ? NAN : none || !draw ? 0.0f : log_s - 0.69314718055994531f * a.w / (1.0f + a.s);
-    for (int i = tid; i < d.n_given; i += kThreads) {
-      const int token = d.given[(int64_t)row * d.given_stride + i];
-      float lp = 0.0f;
-      if (token >= d.vocab) {
-        if (status) atomicCAS(status, 0, kStatusInvalid);
-      } else if (token >= 0) {
-        lp = logp(l[token], token);
+      for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      const int out = __ffs(__ballot_sync(0xffffffffu, mine == m)) - 1;  // NaN is never kept
+      const float z = ref > -INFINITY ? ref : 0.0f;
+      bool left = lane != out;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool in = left || kept[e] != m;
+        left |= !in;
+        const float x = (kept[e] - z) * k, p = exp2_approx(x);
+        if (in) s[0] += p, w[0] += p * fmaxf(x, -200.0f);
       }
-      d.given_lp[(int64_t)row * d.n_given + i] = lp;
+      a.s = s[0] + s[1];
+      a.w = w[0] + w[1];
+      a.first = mine == m ? first : INT32_MAX;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+        a.w += __shfl_xor_sync(0xffffffffu, a.w, o);
+      }
+      a.first = __reduce_min_sync(0xffffffffu, a.first);
+      a.m = m;
+      // against m, which is not below the reference
+      const float by = m > -INFINITY ? fmaxf((z - m) * k, -200.0f) : 0.0f, f = exp2_approx(by);
+      a.w = f * (a.w + by * a.s);
+      a.s *= f;
+    }
+    const bool flushed = __shfl_sync(0xffffffffu, list, 0) != 0;
+    if (lane == 0) {
+      warp_sums[warp] = a;
+      counts[warp] = n_taken + (flushed ? d.n_top : 0);
+    }
+    __syncthreads();
+    if (warp == 0) {
+      a = warp_sums[lane & (kWarps - 1)];
+#pragma unroll
+      for (int o = 1; o < kWarps; o <<= 1) {
+        const Sums b = shuffle(a, o);
+        a = lane & o ? join(b, a, k) : join(a, b, k);
+      }
+      if (TOP && lane == 0) row_sums = a;
+      if (whole) Answer(d, row, a, t).write(lane, P.status);
+      else if (lane == 0) P.sums[slot] = make_float4(a.m, __int_as_float(a.first), a.s, a.w);
     }
     if (TOP) {
-      auto put = [&](int at, Key key) {
-        const int token = (int)~(uint32_t)key;
-        d.top[(int64_t)row * d.n_top + at] = key ? token : -1;
-        d.top_lp[(int64_t)row * d.n_top + at] = key ? logp(logit_of((uint32_t)(key >> 32)), token) : bad ? NAN : -INFINITY;
-      };
-      if (C > 1) {
-        const int q = tid / kTop, i = tid % kTop;
-        const Key mine = q < C ? cl.map_shared_rank(best, q)[i] : 0;
-        __syncthreads();  // the warps' candidates have been read
-        cand[tid] = mine;
-        if (tid < kTop) best[tid] = 0;  // no other CTA reads it
-        __syncthreads();
-        choose(mine, C * kTop, [&](int at, Key key) { best[at] = key; });
-        __syncthreads();
+      int n = 0, to = 0;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        if (i == warp) to = n;
+        n += counts[i];
       }
-      if (tid < d.n_top) put(tid, best[tid]);
+      if (lane < n_taken) candidates[to + lane] = taken[warp][lane];
+      if (flushed && lane < d.n_top) candidates[to + n_taken + lane] = list;
+      __syncthreads();
+      if (whole) {
+        const Answer r(d, row, row_sums, t);
+        placed(candidates, n, d.n_top, [&](int i, Key key) { r.write_top(i, key); });
+      } else {
+        placed(candidates, n, d.n_top, [&](int i, Key key) { P.keys[slot * kTop + i] = key; });
+      }
+    } else {
+      __syncthreads();  // warp_sums have been read
     }
   }
-  cl.sync();  // no CTA leaves while the first may still read its numbers
 }
 
+// The parts of rows that have more than one: a warp to a row, or four with alternatives.
+constexpr int kJoinWarps = 4;
+constexpr int kJoinParts = 8;  // whose alternatives are taken together
 template <bool TOP>
-cudaError_t run(const wt_logprobs_desc &d, int cluster, int *status, cudaStream_t s) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(d.rows * cluster));
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = s;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)cluster;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, logprobs_kernel<TOP>, d, status);
+__global__ void __launch_bounds__(32 * kJoinWarps) logprobs_join_kernel(const __grid_constant__ LogprobsPlan P) {
+  __shared__ Sums row_sums;
+  __shared__ Key candidates[TOP ? (kJoinParts + 1) * kTop : 1], best[kTop];
+  const wt_logprobs_desc &d = P.d;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long row = TOP ? blockIdx.x : (long long)blockIdx.x * kJoinWarps + warp;
+  if (row >= d.rows) return;
+  const long long u0 = row * P.row_vecs, c0 = quotient(u0, P.per), c1 = quotient(u0 + P.row_vecs - 1, P.per);
+  if (c0 == c1) return;  // one CTA had it whole
+  const float t = d.temp ? d.temp[row] : 1.0f, k = factor_of(t);
+  // the first given tokens' logits are on their way while the rest is joined
+  const int token = lane < d.n_given ? d.given[row * d.given_stride + lane] : -1;
+  const float logit = token >= 0 && token < d.vocab ? d.logits[row * d.ldl + token] : 0.0f;
+  auto slot = [&](long long c) { return 2 * c + (c * P.per < u0); };
+  griddep_wait();  // launched while the kernel before it ends
+  if (!TOP || warp == 0) {
+    Sums a = {-INFINITY, INT32_MAX, 0.0f, 0.0f};
+    for (long long q0 = c0; q0 <= c1; q0 += 32) {
+      Sums b = {-INFINITY, INT32_MAX, 0.0f, 0.0f};
+      if (q0 + lane <= c1) {
+        const float4 v = P.sums[slot(q0 + lane)];
+        b = {v.x, __float_as_int(v.y), v.z, v.w};
+      }
+      const int n = (int)min(32ll, c1 - q0 + 1);
+      for (int o = 1; o < n; o <<= 1) {
+        const Sums x = shuffle(b, o);
+        b = lane & o ? join(x, b, k) : join(b, x, k);
+      }
+      // lane 0 has them all
+      b = {__shfl_sync(0xffffffffu, b.m, 0), __shfl_sync(0xffffffffu, b.first, 0), __shfl_sync(0xffffffffu, b.s, 0),
+           __shfl_sync(0xffffffffu, b.w, 0)};
+      a = q0 == c0 ? b : join(a, b, k);
+    }
+    if (lane == 0 && TOP) row_sums = a;
+    Answer(d, (int)row, a, t).write(lane, token, logit, P.status);
+  }
+  if (TOP) {
+    int kept = 0;  // of the parts before
+    for (long long q0 = c0; q0 <= c1; q0 += kJoinParts) {
+      const int parts = (int)min((long long)kJoinParts, c1 - q0 + 1), n = kept + parts * d.n_top;
+      for (int i = tid; i < parts * d.n_top; i += blockDim.x) {
+        const int q = i / d.n_top;
+        candidates[kept + i] = P.keys[slot(q0 + q) * kTop + (i - q * d.n_top)];
+      }
+      if (tid < kept) candidates[tid] = best[tid];
+      __syncthreads();
+      const bool last = q0 + kJoinParts > c1;
+      const Answer r(d, (int)row, row_sums, t);
+      // no key (0) may stand many times, at the end
+      placed(candidates, n, d.n_top, [&](int i, Key key) {
+        if (!key) return;
+        if (last) r.write_top(i, key);
+        else best[i] = key;
+      });
+      int some = 0;
+      for (int i = lane; i < n; i += 32) some += candidates[i] != 0;
+      some = min((int)__reduce_add_sync(0xffffffffu, (unsigned)some), d.n_top);
+      if (last)
+        for (int i = some + tid; i < d.n_top; i += blockDim.x) r.write_top(i, 0);
+      kept = some;
+      __syncthreads();
+    }
+  }
 }
 
 }  // namespace
 
-cudaError_t launch_logprobs(const wt_logprobs_desc &d, int *status, cudaStream_t s) {
-  // Parts of at least 4096 logits, one for each vector a lane has in flight, and as many CTAs as eight to an SM hold.
-  int c = 1;
-  while (c < kMaxCluster && (int64_t)d.rows * c < 6ll * num_sms() && d.vocab / (2 * c) >= 4096) c *= 2;
-  return d.n_top ? run<true>(d, c, status, s) : run<false>(d, c, status, s);
+size_t plan_logprobs(LogprobsPlan *P) {
+  const wt_logprobs_desc &d = P->d;
+  // a row's vectors, wherever in a vector it starts
+  P->row_vecs = (d.vocab + 6) / 4;
+  const long long all = (long long)d.rows * P->row_vecs, ctas = (long long)kResident * num_sms();
+  // shares of one turn of a CTA's threads at least
+  P->per = std::max<long long>((all + ctas - 1) / ctas, kTurn);
+  P->ctas = (int)((all + P->per - 1) / P->per);
+  P->split = P->per % P->row_vecs != 0 && d.rows * (long long)P->row_vecs > P->per;
+  return P->split ? (size_t)P->ctas * 2 * (sizeof(float4) + (d.n_top ? kTop * sizeof(Key) : 0)) : 0;
+}
+
+cudaError_t launch_logprobs(const LogprobsPlan &P, cudaStream_t s) {
+  if (P.d.n_top) logprobs_kernel<true><<<P.ctas, kThreads, 0, s>>>(P);
+  else logprobs_kernel<false><<<P.ctas, kThreads, 0, s>>>(P);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || !P.split) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(P.d.n_top ? P.d.rows : (P.d.rows + kJoinWarps - 1) / kJoinWarps));
+  cfg.blockDim = dim3(32 * kJoinWarps);
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, P.d.n_top ? logprobs_join_kernel<true> : logprobs_join_kernel<false>, P);
 }
 
 }  // namespace wt

@@ -759,7 +759,20 @@ int logprobs_impl(wt_handle *h, const wt_logprobs_desc *d, cudaStream_t s) {
     for (const Rows &p : outs)
       if (&p < &o && overlap(o, p)) return serve_error(WT_EINVAL, "%s: %s overlaps %s", call, o.name, p.name);
   }
-  return launch_alone(h, s, [&] { return wt::launch_logprobs(e, ctx.status, s); });
+  wt::LogprobsPlan P = {};
+  P.d = e;
+  P.status = ctx.status;
+  const size_t bytes = wt::plan_logprobs(&P);
+  Lock lock(h);
+  wt::ServeWorkspace w;
+  CHECK(wt::serve_workspace(h, s, bytes, &w));
+  P.sums = static_cast<float4 *>(w.p);
+  P.keys = reinterpret_cast<unsigned long long *>(P.sums + 2 * (size_t)P.ctas);
+  const cudaError_t err = wt::launch_logprobs(P, s);
+  const int rc = wt::serve_done(h, s, w);
+  CU(err);
+  wt::serve_launched(h, 1 + P.split);
+  return rc;
 }
 
 int verify_impl(wt_handle *h, const wt_verify_desc *d, cudaStream_t s) {

@@ -101,7 +101,21 @@ void plan_place(PlacePlan *P);
 cudaError_t launch_place(const PlacePlan &P, cudaStream_t s);
 
 // ---------------------------------------------------------------- wt_logprobs.cu
-cudaError_t launch_logprobs(const wt_logprobs_desc &d, int *status, cudaStream_t s);
+// CTA c takes the vectors from c * per on of all rows' one after another.  The part of a row that does not lie in
+// one share whole is slot 2c where the share starts in the row or with it, 2c + 1 where the row starts behind it.
+struct LogprobsPlan {
+  wt_logprobs_desc d;
+  long long per;
+  int row_vecs;
+  int ctas;
+  bool split;                 // whether any row has parts
+  float4 *sums;               // [2 ctas]
+  unsigned long long *keys;   // [2 ctas][WT_LOGPROBS_MAX_TOP]
+  int *status;
+};
+// Sets the plan's shares; the workspace's bytes (sums, then keys).
+size_t plan_logprobs(LogprobsPlan *P);
+cudaError_t launch_logprobs(const LogprobsPlan &P, cudaStream_t s);
 
 // ---------------------------------------------------------------- wt_attend.cu, wt_prefix.cu
 // Weights p = 2^(s - m) are rounded to the caches' type.  The reference m lies kBelow under the largest
