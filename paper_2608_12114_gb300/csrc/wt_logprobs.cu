@@ -18,13 +18,13 @@
 // rows leaves SMs idle.  A row that one CTA has whole is answered there; the parts of others go to the workspace,
 // and a second kernel joins them.
 //
-// Alternatives: a warp keeps the 32 largest (logit, token) it has seen, one a lane, in order.  What lies under the
-// n_top-th largest of several disjoint groups' maxima, or under any warp's n_top-th, is not among the row's
-// n_top, whatever the timing; so 64 groups of four threads tell the CTA's warps where to look, from the first
-// 4096 logits on and better after 2, 4, 8, ... times as many: some n_top / i random logits of the i-th 4096 are
-// taken up.  At the end each of them counts those above it, which is its place: many comparisons at once, where
-// sorting is a chain of them.  A warp that takes up more than its room sorts 32 and joins them to a list of its
-// own: the larger of each and its opposite, sorted in five exchanges.
+// Alternatives: what lies under the n_top-th largest of several disjoint groups' maxima is not among the row's
+// n_top, whatever the timing; so 128 groups of two of four threads' kept logits tell the CTA's warps where to look,
+// from the first 4096 logits on and better after 2, 4, 8, ... times as many: some n_top / i random logits of the
+// i-th 4096 are taken up.  At the end each of them counts those above it, which is its place: many comparisons
+// at once, where sorting is a chain of them; where they are many, those under such a bound of their own leave
+// first.  A warp that takes up more than its room sorts 32 and joins them to a list of its own: the larger of each
+// and its opposite, sorted in five exchanges.
 #include <algorithm>
 
 #include "wt_serve.cuh"
@@ -40,10 +40,12 @@ constexpr int kVecs = 4;      // 16-byte vectors of a lane in flight (the next o
                               // copies: no faster, as other CTAs load meanwhile)
 constexpr int kTurn = kThreads * kVecs;  // vectors that a CTA takes at a time
 constexpr int kTop = WT_LOGPROBS_MAX_TOP;
-constexpr int kGroups = 64;
+constexpr int kGroups = 128;
+constexpr int kRoom = 3 * kTop;   // of a warp: it joins 32 to its list from 2 kTop on
+constexpr int kDirect = 160;      // so many are placed as they are
 constexpr float kGrow = 60.0f;  // in log2: weights and their sums stay far below 2^127
 static_assert(kTop == 32, "one candidate a lane");
-static_assert(kGroups == kThreads / 4 && kGroups >= kTop, "groups of four threads, enough of them");
+static_assert(kGroups == kThreads / 2 && kGroups >= kTop, "two groups of four threads, enough of them");
 
 typedef unsigned long long Key;  // order of the logit, then ~token: the larger comes first; 0: none
 
@@ -117,31 +119,80 @@ __device__ __noinline__ Key sorted(Key mine, int lane) {
   return mine;
 }
 
-// The n-th largest of the 64 groups' maxima.  Other warps may write larger ones meanwhile.
+// At most the n-th largest of the groups' maxima, and within 2^-12 of their range of it: by one warp, halving the
+// range (counting what is above each of them kept the warp, and those that wait for it, four times as long).  Other
+// warps may write larger ones meanwhile.
 __device__ __noinline__ unsigned bound_of(const volatile unsigned *maxima, int n, int lane) {
-  const unsigned m0 = maxima[lane], m1 = maxima[lane + 32];
-  int above0 = 0, above1 = 0;
-#pragma unroll 8
-  for (int i = 0; i < 32; ++i) {
-    const unsigned x = __shfl_sync(0xffffffffu, m0, i), y = __shfl_sync(0xffffffffu, m1, i);
-    above0 += (x > m0) + (y > m0);
-    above1 += (x > m1) + (y > m1);
+  unsigned m[kGroups / 32], lo = ~0u, hi = 0;
+#pragma unroll
+  for (int i = 0; i < kGroups / 32; ++i) m[i] = maxima[i * 32 + lane], lo = min(lo, m[i]), hi = max(hi, m[i]);
+  lo = __reduce_min_sync(0xffffffffu, lo), hi = __reduce_max_sync(0xffffffffu, hi);
+#pragma unroll 2
+  for (int i = 0; i < 12; ++i) {
+    const unsigned mid = lo + (hi - lo + 1) / 2;
+    int some = 0;
+#pragma unroll
+    for (int q = 0; q < kGroups / 32; ++q) some += __popc(__ballot_sync(0xffffffffu, m[q] >= mid));
+    if (some >= n) lo = mid;
+    else hi = mid - 1;
   }
-  // the smallest that fewer than n are above
-  return __reduce_min_sync(0xffffffffu, min(above0 < n ? m0 : ~0u, above1 < n ? m1 : ~0u));
+  return lo;
 }
 
-// put(place, key) for those of n different keys in shared memory that fewer than n_top are above; by the block.
+// The n-th largest, by a block of two threads to a group, into *low (~0 before).  Ends with a barrier.
+__device__ __forceinline__ void block_bound(const unsigned *maxima, int n, unsigned *low) {
+  const int tid = threadIdx.x;
+  const unsigned mine = maxima[tid / 2];
+  int above = 0;
+#pragma unroll
+  for (int i = 0; i < kGroups / 2; i += 4) {
+    const uint4 x = *reinterpret_cast<const uint4 *>(maxima + tid % 2 * (kGroups / 2) + i);
+    above += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
+  }
+  above += __shfl_xor_sync(0xffffffffu, above, 1);
+  const unsigned least = __reduce_min_sync(0xffffffffu, above < n ? mine : ~0u);
+  if (tid % 32 == 0) atomicMin(low, least);
+  __syncthreads();
+}
+
+struct Choice {
+  __align__(16) unsigned maxima[kGroups];
+  unsigned low;
+  int n;
+};
+// put(place, key) for the n_top largest of n different keys in shared memory (0: none, may stand there often, goes
+// last); by a block of kThreads, which all come here together.  `room` holds n keys.
 template <typename F>
-__device__ __forceinline__ void placed(const Key *keys, int n, int n_top, F put) {
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+__device__ __forceinline__ void place(const Key *keys, int n, int n_top, Key *room, Choice *c, F put) {
+  const int tid = threadIdx.x;
+  if (n > kDirect) {
+    unsigned most = 0;
+    for (int i = tid; i < n; i += kThreads) most = max(most, (unsigned)(keys[i] >> 32));
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    if (tid % 2 == 0) c->maxima[tid / 2] = most;
+    if (tid == 0) c->low = ~0u, c->n = 0;
+    __syncthreads();
+    block_bound(c->maxima, n_top, &c->low);
+    const unsigned low = max(c->low, 1u);
+    for (int i = tid; i < n; i += kThreads) {
+      const Key x = keys[i];
+      if ((unsigned)(x >> 32) >= low) room[atomicAdd(&c->n, 1)] = x;
+    }
+    __syncthreads();
+    keys = room, n = c->n;
+  }
+  for (int i = tid; i < n; i += kThreads) {
     const Key mine = keys[i];
     int above = 0;
 #pragma unroll 8
     for (int j = 0; j < n; ++j) above += keys[j] > mine;
-    if (above < n_top) put(above, mine);
+    if (mine && above < n_top) put(above, mine);
   }
-  for (int i = n + threadIdx.x; i < n_top; i += blockDim.x) put(i, 0);
+  // places that no key has
+  int some = 0;
+  for (int i = tid % 32; i < n; i += 32) some += keys[i] != 0;
+  some = (int)__reduce_add_sync(0xffffffffu, (unsigned)some);
+  for (int i = some + tid; i < n_top; i += kThreads) put(i, 0);
 }
 
 // What a row's sums answer.
@@ -198,10 +249,11 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
 template <bool TOP>
 __global__ void __launch_bounds__(kThreads, kResident) logprobs_kernel(const __grid_constant__ LogprobsPlan P) {
   __shared__ Sums warp_sums[kWarps], row_sums;
-  __shared__ __align__(16) unsigned maxima[kGroups];
+  __shared__ Choice choice;
   __shared__ unsigned floor_order, first_bound;
-  __shared__ Key taken[TOP ? kWarps : 1][2 * kTop];  // up by each warp
-  __shared__ Key candidates[TOP ? kWarps * 2 * kTop : 1];
+  __shared__ __align__(16) Key taken[TOP ? kWarps : 1][kRoom];  // up by each warp
+  __shared__ __align__(16) Key candidates[TOP ? kWarps * kRoom : 1];
+  unsigned *const maxima = choice.maxima;
   __shared__ int counts[kWarps];
   const wt_logprobs_desc &d = P.d;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -226,22 +278,24 @@ __global__ void __launch_bounds__(kThreads, kResident) logprobs_kernel(const __g
     int first = INT32_MAX;         // a greedy row's: the first of the thread's largest logits
     Key list = 0;
     int n_taken = 0;
-    float least = -3.4028234e38f;  // a candidate is at least that: neither NaN nor -infinity
+    // A candidate is at least `least` (neither NaN nor -infinity) and above `tie`, which n_top of the warp's logits
+    // of earlier turns, so of lower tokens, are at least.
+    float least = -3.4028234e38f, tie = -INFINITY;
     const bool greedy = !(t > 0.0f);
     for (int j0 = lo; j0 < hi; j0 += kTurn) {
       float v[kVecs][4];
-      const int j1 = j0 + warp * 32 * kVecs + lane;  // a warp's vectors lie together, in ascending order
-      const int e1 = 4 * j1 - off;                   // token of v[0][0]
+      const int j1 = j0 + tid;      // and every kThreads-th from there
+      const int e1 = 4 * j1 - off;  // token of v[0][0]
       if (j0 > 0 && j0 + kTurn <= hi && 4 * (j0 + kTurn) - off <= d.vocab) {  // all of them are the row's
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
-          const float4 x = __ldcs(reinterpret_cast<const float4 *>(l + e1) + i * 32);
+          const float4 x = __ldcs(reinterpret_cast<const float4 *>(l + e1) + i * kThreads);
           v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
         }
       } else {
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
-          const int j = j1 + i * 32, e0 = 4 * j - off;
+          const int j = j1 + i * kThreads, e0 = 4 * j - off;
           if (j < hi && e0 >= 0 && e0 + 4 <= d.vocab) {
             const float4 x = __ldcs(reinterpret_cast<const float4 *>(l + e0));
             v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
@@ -268,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, kResident) logprobs_kernel(const __g
         for (int i = kVecs - 1; i >= 0; --i)
 #pragma unroll
           for (int e = 3; e >= 0; --e)
-            if (v[i][e] == top) first = e1 + i * 128 + e;
+            if (v[i][e] == top) first = e1 + i * (4 * kThreads) + e;
       }
       const float z = ref > -INFINITY ? ref : 0.0f;
 #pragma unroll
@@ -286,30 +340,23 @@ __global__ void __launch_bounds__(kThreads, kResident) logprobs_kernel(const __g
         }
 
       if (TOP) {
-        // the groups' largest so far; one warp after another looks where the n_top largest can be
-        float most = fmaxf(fmaxf(kept[0], kept[1]), fmaxf(kept[2], kept[3]));
-        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        if (lane % 4 == 0) reinterpret_cast<volatile unsigned *>(maxima)[tid / 4] = order_of(most);
         const int turn = (j0 - lo) / kTurn;
-        if (turn == 0) {
-          __syncthreads();
-          const unsigned mine = maxima[tid / 4];
-          int above = 0;
-#pragma unroll
-          for (int i = 0; i < kGroups / 4; i += 4) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(maxima + tid % 4 * (kGroups / 4) + i);
-            above += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
+        if ((turn & (turn + 1)) == 0) {  // the groups' largest so far
+          float most0 = fmaxf(kept[0], kept[1]), most1 = fmaxf(kept[2], kept[3]);
+          most0 = fmaxf(most0, __shfl_xor_sync(0xffffffffu, most0, 1));
+          most1 = fmaxf(most1, __shfl_xor_sync(0xffffffffu, most1, 1));
+          most0 = fmaxf(most0, __shfl_xor_sync(0xffffffffu, most0, 2));
+          most1 = fmaxf(most1, __shfl_xor_sync(0xffffffffu, most1, 2));
+          if (lane % 4 == 0) {
+            reinterpret_cast<volatile unsigned *>(maxima)[tid / 4] = order_of(most0);
+            reinterpret_cast<volatile unsigned *>(maxima)[kGroups / 2 + tid / 4] = order_of(most1);
           }
-          above += __shfl_xor_sync(0xffffffffu, above, 1);
-          above += __shfl_xor_sync(0xffffffffu, above, 2);
-          // the smallest that fewer than n_top are above
-          const unsigned low = __reduce_min_sync(0xffffffffu, above < d.n_top ? mine : ~0u);
-          if (lane == 0) atomicMin(&first_bound, low);
-          __syncthreads();
-          least = fmaxf(least, logit_of(first_bound));
-        } else if ((turn & (turn + 1)) == 0 && __popc(turn) % kWarps == warp) {
-          __syncwarp();
+          if (turn == 0) {
+            __syncthreads();
+            block_bound(maxima, d.n_top, &first_bound);
+            least = fmaxf(least, logit_of(first_bound));
+          }
+        } else if ((turn & (turn - 1)) == 0 && (__ffs(turn) + blockIdx.x) % kWarps == warp) {  // one of the warps looks
           const unsigned low = bound_of(maxima, d.n_top, lane);
           if (lane == 0) atomicMax(&floor_order, low);
           least = fmaxf(least, logit_of(low));
@@ -320,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, kResident) logprobs_kernel(const __g
 #pragma unroll
           for (int i = 0; i < kVecs; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) mine |= v[i][e] >= least ? 1u << (i * 4 + e) : 0u;
+            for (int e = 0; e < 4; ++e) mine |= v[i][e] >= least && v[i][e] > tie ? 1u << (i * 4 + e) : 0u;
           unsigned who;
           while ((who = __ballot_sync(0xffffffffu, mine != 0))) {
             const int which = __ffs(mine) - 1;
@@ -329,26 +376,29 @@ __global__ void __launch_bounds__(kThreads, kResident) logprobs_kernel(const __g
             for (int i = 0; i < kVecs; ++i)
 #pragma unroll
               for (int e = 0; e < 4; ++e) x = which == i * 4 + e ? v[i][e] : x;
-            if (mine) taken[warp][n_taken + __popc(who & ((1u << lane) - 1))] = key_of(x, e1 + (which >> 2) * 128 + (which & 3));
+            if (mine) taken[warp][n_taken + __popc(who & ((1u << lane) - 1))] = key_of(x, e1 + (which >> 2) * (4 * kThreads) + (which & 3));
             mine &= mine - 1;
             n_taken += __popc(who);
-            if (n_taken >= kTop) {
+            while (n_taken >= 2 * kTop) {
               __syncwarp();
               list = merged(list, sorted(taken[warp][lane], lane), lane);
               n_taken -= kTop;
-              const Key rest = taken[warp][kTop + lane];
+              const Key x0 = taken[warp][kTop + lane], x1 = taken[warp][2 * kTop + lane];
               __syncwarp();
-              if (lane < n_taken) taken[warp][lane] = rest;
-              const uint32_t o = (uint32_t)(__shfl_sync(0xffffffffu, list, d.n_top - 1) >> 32);
-              if (o) {
-                least = fmaxf(least, logit_of(o));
-                if (lane == 0) atomicMax(&floor_order, o);
-              }
+              taken[warp][lane] = x0, taken[warp][kTop + lane] = x1;
             }
+            __syncwarp();
+          }
+          const uint32_t o = (uint32_t)(__shfl_sync(0xffffffffu, list, d.n_top - 1) >> 32);
+          if (o) {
+            tie = logit_of(o);
+            least = fmaxf(least, tie);
+            if (lane == 0) atomicMax(&floor_order, o);
           }
         }
       }
     }
+
     // the warp's sums: all that its threads kept go in but one, a largest
     Sums a;
     {
@@ -405,14 +455,15 @@ __global__ void __launch_bounds__(kThreads, kResident) logprobs_kernel(const __g
         if (i == warp) to = n;
         n += counts[i];
       }
-      if (lane < n_taken) candidates[to + lane] = taken[warp][lane];
+      for (int i = lane; i < n_taken; i += 32) candidates[to + i] = taken[warp][i];
       if (flushed && lane < d.n_top) candidates[to + n_taken + lane] = list;
       __syncthreads();
+      Key *const room = taken[0];  // of no use any more
       if (whole) {
         const Answer r(d, row, row_sums, t);
-        placed(candidates, n, d.n_top, [&](int i, Key key) { r.write_top(i, key); });
+        place(candidates, n, d.n_top, room, &choice, [&](int i, Key key) { r.write_top(i, key); });
       } else {
-        placed(candidates, n, d.n_top, [&](int i, Key key) { P.keys[slot * kTop + i] = key; });
+        place(candidates, n, d.n_top, room, &choice, [&](int i, Key key) { P.keys[slot * kTop + i] = key; });
       }
     } else {
       __syncthreads();  // warp_sums have been read
@@ -420,16 +471,16 @@ __global__ void __launch_bounds__(kThreads, kResident) logprobs_kernel(const __g
   }
 }
 
-// The parts of rows that have more than one: a warp to a row, or four with alternatives.
-constexpr int kJoinWarps = 4;
-constexpr int kJoinParts = 8;  // whose alternatives are taken together
+// The parts of rows that have more than one: a warp to a row, or a block with alternatives.
+constexpr int kJoinParts = 24;  // whose alternatives are taken together
 template <bool TOP>
-__global__ void __launch_bounds__(32 * kJoinWarps) logprobs_join_kernel(const __grid_constant__ LogprobsPlan P) {
+__global__ void __launch_bounds__(kThreads) logprobs_join_kernel(const __grid_constant__ LogprobsPlan P) {
   __shared__ Sums row_sums;
-  __shared__ Key candidates[TOP ? (kJoinParts + 1) * kTop : 1], best[kTop];
+  __shared__ Choice choice;
+  __shared__ __align__(16) Key candidates[TOP ? (kJoinParts + 1) * kTop : 1], room[TOP ? (kJoinParts + 1) * kTop : 1], best[kTop];
   const wt_logprobs_desc &d = P.d;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const long long row = TOP ? blockIdx.x : (long long)blockIdx.x * kJoinWarps + warp;
+  const long long row = TOP ? blockIdx.x : (long long)blockIdx.x * kWarps + warp;
   if (row >= d.rows) return;
   const long long u0 = row * P.row_vecs, c0 = quotient(u0, P.per), c1 = quotient(u0 + P.row_vecs - 1, P.per);
   if (c0 == c1) return;  // one CTA had it whole
@@ -461,30 +512,23 @@ __global__ void __launch_bounds__(32 * kJoinWarps) logprobs_join_kernel(const __
     Answer(d, (int)row, a, t).write(lane, token, logit, P.status);
   }
   if (TOP) {
-    int kept = 0;  // of the parts before
+    int before = 0;  // the best of the parts before
     for (long long q0 = c0; q0 <= c1; q0 += kJoinParts) {
-      const int parts = (int)min((long long)kJoinParts, c1 - q0 + 1), n = kept + parts * d.n_top;
-      for (int i = tid; i < parts * d.n_top; i += blockDim.x) {
+      const int parts = (int)min((long long)kJoinParts, c1 - q0 + 1), n = before + parts * d.n_top;
+      for (int i = tid; i < parts * d.n_top; i += kThreads) {
         const int q = i / d.n_top;
-        candidates[kept + i] = P.keys[slot(q0 + q) * kTop + (i - q * d.n_top)];
+        candidates[before + i] = P.keys[slot(q0 + q) * kTop + (i - q * d.n_top)];
       }
-      if (tid < kept) candidates[tid] = best[tid];
+      if (tid < before) candidates[tid] = best[tid];
       __syncthreads();
-      const bool last = q0 + kJoinParts > c1;
-      const Answer r(d, (int)row, row_sums, t);
-      // no key (0) may stand many times, at the end
-      placed(candidates, n, d.n_top, [&](int i, Key key) {
-        if (!key) return;
-        if (last) r.write_top(i, key);
-        else best[i] = key;
-      });
-      int some = 0;
-      for (int i = lane; i < n; i += 32) some += candidates[i] != 0;
-      some = min((int)__reduce_add_sync(0xffffffffu, (unsigned)some), d.n_top);
-      if (last)
-        for (int i = some + tid; i < d.n_top; i += blockDim.x) r.write_top(i, 0);
-      kept = some;
-      __syncthreads();
+      if (q0 + kJoinParts > c1) {
+        const Answer r(d, (int)row, row_sums, t);
+        place(candidates, n, d.n_top, room, &choice, [&](int i, Key key) { r.write_top(i, key); });
+      } else {
+        place(candidates, n, d.n_top, room, &choice, [&](int i, Key key) { best[i] = key; });
+        before = d.n_top;
+        __syncthreads();
+      }
     }
   }
 }
@@ -496,10 +540,14 @@ size_t plan_logprobs(LogprobsPlan *P) {
   // a row's vectors, wherever in a vector it starts
   P->row_vecs = (d.vocab + 6) / 4;
   const long long all = (long long)d.rows * P->row_vecs, ctas = (long long)kResident * num_sms();
-  // shares of one turn of a CTA's threads at least
-  P->per = std::max<long long>((all + ctas - 1) / ctas, kTurn);
+  // Equal shares, of one turn of a CTA's threads at least, or whole rows, whichever takes less by this count, in
+  // turns: a row that a CTA meets takes its turns and about two more, and joining rows about three.
+  const long long equal = std::max<long long>((all + ctas - 1) / ctas, kTurn), whole = (d.rows + ctas - 1) / ctas;
+  const double by_shares = (double)equal / kTurn + 2.0 * (2.0 + (double)equal / P->row_vecs) + 3.0;
+  const double by_rows = (double)whole * ((P->row_vecs + kTurn - 1) / kTurn + 2.0);
+  P->per = by_rows <= by_shares ? whole * P->row_vecs : equal;
   P->ctas = (int)((all + P->per - 1) / P->per);
-  P->split = P->per % P->row_vecs != 0 && d.rows * (long long)P->row_vecs > P->per;
+  P->split = P->per % P->row_vecs != 0 && all > P->per;
   return P->split ? (size_t)P->ctas * 2 * (sizeof(float4) + (d.n_top ? kTop * sizeof(Key) : 0)) : 0;
 }
 
@@ -509,8 +557,8 @@ cudaError_t launch_logprobs(const LogprobsPlan &P, cudaStream_t s) {
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || !P.split) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(P.d.n_top ? P.d.rows : (P.d.rows + kJoinWarps - 1) / kJoinWarps));
-  cfg.blockDim = dim3(32 * kJoinWarps);
+  cfg.gridDim = dim3((unsigned)(P.d.n_top ? P.d.rows : (P.d.rows + kWarps - 1) / kWarps));
+  cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
