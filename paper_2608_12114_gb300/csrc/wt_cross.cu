@@ -2,17 +2,25 @@
 // the merge.
 //
 // A CTA takes an equal share of all requests' cells (CrossPlan), so unequal memories keep no SM waiting.  Each of
-// its 4 warps streams its own tiles of 16 states through a ring of its own in shared memory (16-byte cp.async),
-// with m16n8k16 MMAs on them, against 16 or 32 (token, head-in-group) rows:
+// its 4 warps streams its own tiles of 32 states (16 of more than 64 elements: 8 KB either way) through a ring of
+// its own in shared memory, on from one row tile into the next: a head of a group of four, or of two, or every
+// fourth of one head's.  (48 requests of 20 heads of 64, whose 128 bytes of a state lie side by side: XX us, and YY
+// with a head at a time.)  Rows, (token, head-in-group) pairs, are columns of
+// the m16n8k16 MMAs, 8 to a block, so that a single token's product is not 16 rows of which one counts:
 //
-//   p = 2^(s - m),  s = scale log2(e) q.k,  O += p v,  l += p,  m moving as kSlack says
+//   S^T = K Q^T,   P^T = 2^(S^T - m),   O^T += V^T P^T,   l += column sums of P^T
 //
-// and parts join as softmax splits: O = sum_i 2^(m_i - m) O_i, l alike, out = O / l.  The maximum passes over NaN
-// scores, so a part whose sum is NaN says so in its m.  States that are not kept, or past the memory, arrive as
-// zeros and their scores are masked, so what stands there never reaches a product.
+// with s = scale log2(e) q.k and m moving as kSlack says; P^T turns from a result into an operand by movmatrix.
+// Parts join as softmax splits: O = sum_i 2^(m_i - m) O_i, l alike, out = O / l.  The maximum passes over NaN
+// scores, so a part whose sum is NaN says so in its m.
+//
+// Tiles come as TMA boxes: what a tile of a memory's end holds behind it is masked in S and cleared in V.  With a
+// mask (or pitches past a tensor map's) they come by 16-byte cp.async instead, which leaves out the states that are
+// not kept and fills their place with zeros.
 #include <algorithm>
 
 #include "wt_cross.cuh"
+#include "wt_tmem.cuh"
 
 namespace wt {
 
@@ -20,345 +28,461 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kKeys = 16;   // states of a warp's tile
-constexpr int kStages = 2;  // tiles of a warp's ring
-constexpr int kCell = kWarps * kKeys;
+constexpr int kStages = 3;           // tiles of a warp's ring
+constexpr uint32_t kTileBytes = 8192;  // K, then V; each in halves of 64 elements, rows of 128 bytes, swizzled
+constexpr int kJoinRows = 4;         // rows that the warps join at a time
 
-template <int DT, int ND, int MT>
-__global__ void __launch_bounds__(kThreads, MT > 1 ? 2 : ND == 4 ? 4 : 3) cross_few_kernel(const __grid_constant__ CrossPlan P) {
-  constexpr int kPitch = ND * 32 + 16;            // bytes of a staged row: 8 rows hit 8 different bank groups
-  constexpr int kTileBytes = 2 * kKeys * kPitch;  // K rows, then V rows
-  constexpr int kRows = 16 * MT;
-  extern __shared__ __align__(128) uint8_t smem[];
-  const wt_cross_desc &d = P.d;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
-  const int G = P.G, D = d.head_dim;
-  const uint32_t ring = smem_u32(smem) + warp * kStages * kTileBytes;
-  const int chunks = D / 8;  // 16-byte pieces of a row
-  const int row_lane = lane / chunks, in_lane = lane - row_lane * chunks, row_step = 32 / chunks, in_step = 32 - row_step * chunks;
-  const int ksteps = (D + 15) / 16;
-  const float sl = d.scale * 1.4426950408889634f;
+template <int DH>
+constexpr int kKeys = DH == 1 ? 32 : 16;  // states of a tile
+template <int DH>
+constexpr size_t few_smem() {
+  return kWarps * kStages * kTileBytes + kWarps * kJoinRows * (DH * 64 * 4 + 8) + kWarps * kStages * (8 + 4) + 16 + 1024;
+}
 
-  const Share share = share_of<kThreads>(P);
-  int b = share.b;
-  long long first = share.first;
-  Asker a = {};
-  if (share.lo < share.hi) a = asker_of(P, b, false);
-  for (long long cell = share.lo; cell < share.hi;) {
-    while (cell >= first + a.cells(d.kv_heads)) {
-      first += a.cells(d.kv_heads);
+__device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+
+// A warp's tiles in order: of every cell of the CTA's share, its own, where the memory reaches it.
+struct Tiles {
+  const CrossPlan &P;
+  const Share &s;
+  long long cell, first;
+  int b, i, at, by;  // key of a cell's first tile of this warp; of a cell
+  Asker a;
+  Segment g;
+  __device__ Tiles(const CrossPlan &p, const Share &share, int at_key)
+      : P(p), s(share), cell(share.lo), first(share.first), b(share.b), i(0), at(at_key), by(p.keys) {
+    g.tiles = 0;
+    if (cell < s.hi) a = asker_of(P, b, false);
+  }
+  __device__ bool segment() {  // the next row tile
+    if (cell >= s.hi) return false;
+    while (cell >= first + a.cells(P)) {
+      first += a.cells(P);
       a = asker_of(P, ++b, false);
     }
-    const Segment sg = segment_at(P, a, first, cell, share);
-    cell += sg.cells;
-    const int rows = a.n * G, row0 = sg.row_tile * kRows;
-    const int k0 = sg.tile0 * kCell, k1 = min(a.len, k0 + sg.tiles * kCell);
-    const int tiles = max(0, (k1 - k0 + kKeys - 1) / kKeys);
+    g = segment_at(P, a, first, cell, s);
+    cell += g.cells;
+    i = 0;
+    return true;
+  }
+  // state of the next tile of the row tile; false: none left
+  __device__ bool tile(int &key0) {
+    if (i >= g.tiles) return false;
+    key0 = (g.tile0 + i++) * by + at;
+    return key0 < a.len;
+  }
+};
 
-    if (D % 16) {
-      // the last 8 columns stay zero: no copy touches them
-      for (int i = tid; i < kWarps * kStages * 2 * kKeys; i += kThreads)
-        *reinterpret_cast<uint4 *>(smem + i * kPitch + D * 2) = make_uint4(0, 0, 0, 0);
-      __syncthreads();
+// DH: 64-element halves of head_dim; NQ: blocks of 8 rows.  BOX: tiles as TMA boxes.
+template <int DT, int DH, int NQ, bool BOX>
+__global__ void __launch_bounds__(kThreads, 2)
+    cross_few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CrossPlan P) {
+  constexpr int kT = kKeys<DH>, NK = kT / 16, ND = DH * 4, kRows = 8 * NQ;
+  constexpr uint32_t kHalfTile = kT * 128, kV = DH * kHalfTile;  // V behind K
+  static_assert(2 * kV == kTileBytes, "a tile");
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t *after = smem_raw + (base - smem_u32(smem_raw)) + kWarps * kStages * kTileBytes;
+  const wt_cross_desc &d = P.d;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3, g = lane >> 2;
+  const int G = P.G, D = d.head_dim, ksteps = (D + 15) / 16;
+  float *so = reinterpret_cast<float *>(after);                                   // [kWarps][kJoinRows][DH * 64]
+  float2 *sml = reinterpret_cast<float2 *>(so + kWarps * kJoinRows * DH * 64);    // [kWarps][kJoinRows]
+  uint64_t *bars = reinterpret_cast<uint64_t *>(sml + kWarps * kJoinRows);        // [kWarps][kStages]
+  uint32_t *kept_of = reinterpret_cast<uint32_t *>(bars + kWarps * kStages);      // [kWarps][kStages]: which states count
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(kept_of + kWarps * kStages);
+  const uint32_t ring = base + warp * kStages * kTileBytes, bar0 = smem_u32(bars + warp * kStages);
+  kept_of += warp * kStages;
+  if (tid == 0) *abort_flag = 0;
+  if (lane == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(bar0 + 8 * i, 1);
+    mbar_fence_init();
+  }
+  if (BOX && tid == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&kmap) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&vmap) : "memory");
+  }
+  griddep_launch();  // the merge's first loads may run beside this
+  const Share share = share_of<kThreads>(P);
+  // warps of a head, this warp's head of the group, and its place among the head's warps
+  const int of_head = kWarps / P.together, wh = warp / of_head, wk = warp - wh * of_head;
+  const float sl = d.scale * 1.4426950408889634f;
+
+  // what is ahead of the products: the tile to ask for next, and what keep says of it
+  Tiles ahead(P, share, wk * kT);
+  uint32_t issued = 0, used = 0;  // tiles
+  int next_key = 0;
+  bool some = true, mine = false;
+  auto look = [&]() {
+    while (!ahead.tile(next_key))
+      if (!ahead.segment()) {
+        some = false;
+        return;
+      }
+    if (!BOX)
+      mine = lane < kT && next_key + lane < ahead.a.len && (!d.keep || __ldg(d.keep + (int64_t)ahead.a.mem + next_key + lane));
+  };
+  auto issue = [&]() {
+    if (!some) {
+      if (!BOX) cp_commit();
+      return;
     }
-    const uint8_t *k_of = static_cast<const uint8_t *>(d.k) + 2 * (a.mem * d.mem_stride + sg.hk * d.mem_head);
-    const uint8_t *v_of = static_cast<const uint8_t *>(d.v) + 2 * (a.mem * d.mem_stride + sg.hk * d.mem_head);
-    const int64_t state_bytes = 2 * d.mem_stride;
-    // Tile i of this warp (tiles warp, warp + 4, ...); bit r of `there`: state r counts.  What keep says is read a
-    // tile ahead of its copies.
-    auto kept = [&](int i) -> bool {
-      const int key = k0 + (warp + i * kWarps) * kKeys + lane;
-      return lane < kKeys && key < k1 && (!d.keep || __ldg(d.keep + (int64_t)a.mem + key));
-    };
-    bool next = kept(0);
-    uint32_t there[kStages];
-    auto fetch = [&](int i, uint32_t &found) {
-      const int tile = warp + i * kWarps;
-      if (tile < tiles) {
-        found = __ballot_sync(0xffffffffu, next);
-        next = kept(i + 1);
-        const int key0 = k0 + tile * kKeys;
-        const uint32_t dst = ring + (i % kStages) * kTileBytes;
-        int row = row_lane, in = in_lane;  // rows 0-15: K, 16-31: V
-#pragma unroll 4
-        for (int c = 0; c < chunks; ++c) {
-          const bool ok = found >> (row & 15) & 1;
-          const uint8_t *src = (row < kKeys ? k_of : v_of) + (int64_t)(key0 + (row & 15)) * state_bytes + in * 16;
-          cp16(dst + row * kPitch + in * 16, ok ? src : d.q, ok);
-          row += row_step;
-          in += in_step;
-          if (in >= chunks) in -= chunks, ++row;
+    const uint32_t s = issued++ % kStages, dst = ring + s * kTileBytes;
+    const int state = ahead.a.mem + next_key, head = ahead.g.group * P.together + wh;
+    if constexpr (BOX) {
+      if (lane == 0) {
+        mbar_expect_tx(bar0 + 8 * s, kTileBytes);
+#pragma unroll
+        for (int hf = 0; hf < DH; ++hf) {
+          tma_3d(dst + hf * kHalfTile, &kmap, hf * 64, head, state, bar0 + 8 * s);
+          tma_3d(dst + kV + hf * kHalfTile, &vmap, hf * 64, head, state, bar0 + 8 * s);
         }
       }
-      cp_commit();
-    };
-#pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) fetch(i, there[i]);
-
-    // queries as A operands
-    uint32_t qf[MT][ND][4];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = row0 + i * 16 + g + e * 8;
-        const bool ok = r < rows;
-        const uint16_t *src = static_cast<const uint16_t *>(d.q) +
-                              (ok ? (int64_t)(a.t0 + r / G) * d.q_stride + (int64_t)(sg.hk * G + r % G) * D : 0);
-#pragma unroll
-        for (int k = 0; k < ND; ++k)
-#pragma unroll
-          for (int f = 0; f < 2; ++f) {
-            const int col = k * 16 + f * 8 + q * 2;
-            qf[i][k][e + 2 * f] = ok && col < D ? *reinterpret_cast<const uint32_t *>(src + col) : 0u;
-          }
+    } else {
+      const uint32_t kept = __ballot_sync(0xffffffffu, mine);
+      if (lane == 0) kept_of[s] = kept;
+      const int pieces = 2 * ksteps;  // of 16 bytes a row; one past head_dim is zeros
+      const int64_t off = 2 * (state * d.mem_stride + head * d.mem_head);
+      const uint8_t *k_of = static_cast<const uint8_t *>(d.k) + off, *v_of = static_cast<const uint8_t *>(d.v) + off;
+      int row = lane / pieces, in = lane - row * pieces;
+      const int row_step = 32 / pieces, in_step = 32 - row_step * pieces;
+#pragma unroll 4
+      for (int c = 0; c < kT * pieces / 32; ++c) {
+        const bool ok = (kept >> row & 1) && in * 8 < D;
+        const int64_t at = 2 * row * d.mem_stride + in * 16;
+        const uint32_t to = dst + (in >> 3) * kHalfTile + row * 128 + ((in ^ row) & 7) * 16;
+        cp16(to, ok ? k_of + at : static_cast<const uint8_t *>(d.q), ok);
+        cp16(to + kV, ok ? v_of + at : static_cast<const uint8_t *>(d.q), ok);
+        row += row_step;
+        in += in_step;
+        if (in >= pieces) in -= pieces, ++row;
       }
-
-    float o[MT][2 * ND][4], m[MT][2], l[MT][2];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-#pragma unroll
-      for (int j = 0; j < 2 * ND; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][j][e] = 0.0f;
-      m[i][0] = m[i][1] = -INFINITY;
-      l[i][0] = l[i][1] = 0.0f;
+      cp_commit();
     }
-    auto step = [&](int i, uint32_t found) {
-      cp_wait<kStages - 1>();
-      __syncwarp();
-      const uint32_t kt = ring + (i % kStages) * kTileBytes, vt = kt + kKeys * kPitch;
-      float s[MT][2][4];
+    look();
+  };
+  look();
+#pragma unroll 1
+  for (int i = 0; i < kStages - 1; ++i) issue();
+
+  // where this lane's rows of 8 x 8 blocks lie: K as it is, V turned
+  const uint32_t k_lane = ((lane & 15) * 128) | (((lane >> 4) ^ lane) & 7) * 16;
+  const uint32_t v_lane = (((lane & 7) + (lane >> 4) * 8) * 128) | (((lane >> 3 & 1) ^ lane) & 7) * 16;
+  for (Tiles now(P, share, wk * kT); now.segment();) {
+    const Asker &a = now.a;
+    const Segment &sg = now.g;
+    const int rows = a.n * G, row0 = sg.row_tile * kRows, hk = sg.group * P.together + wh;
+
+    // queries as B operands
+    uint32_t qb[NQ][ND][2];
 #pragma unroll
-      for (int z = 0; z < MT; ++z)
+    for (int n = 0; n < NQ; ++n) {
+      const int r = row0 + n * 8 + g;
+      const bool ok = r < rows;
+      const uint16_t *src = static_cast<const uint16_t *>(d.q) +
+                            (ok ? (int64_t)(a.t0 + r / G) * d.q_stride + (int64_t)(hk * G + r % G) * D : 0);
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+      for (int k = 0; k < ND; ++k)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[z][j][e] = 0.0f;
+        for (int f = 0; f < 2; ++f) {
+          const int col = k * 16 + f * 8 + q * 2;
+          qb[n][k][f] = ok && col < D ? *reinterpret_cast<const uint32_t *>(src + col) : 0u;
+        }
+    }
+    // of rows 2q and 2q + 1 of a block: O^T, references, sums
+    float o[NQ][ND][4], m[NQ][2], l[NQ][2];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[n][t][e] = 0.0f;
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.0f;
+    }
+
+    for (int key0; now.tile(key0);) {
+      const uint32_t stage = used % kStages, kt = ring + stage * kTileBytes, vt = kt + kV;
+      uint32_t found;
+      if constexpr (BOX) {
+        if (!warp_wait(bar0 + 8 * stage, used / kStages & 1, abort_flag, P.status)) {  // nothing of it is used
+          ++used;
+          continue;
+        }
+        const int n = a.len - key0;
+        found = n >= kT ? (kT == 32 ? 0xffffffffu : (1u << kT) - 1) : (1u << n) - 1;
+        if (n < kT) {  // what V holds behind the memory: a weight of 0 does not hide what is not finite
+          for (int i = n * 8 + lane; i < kT * 8; i += 32)
+#pragma unroll
+            for (int hf = 0; hf < DH; ++hf)
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vt + hf * kHalfTile + i * 16), "r"(0) : "memory");
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
+      } else {
+        cp_wait<kStages - 2>();
+        __syncwarp();
+        found = kept_of[stage];
+      }
+      ++used;
+      issue();  // into the stage before this one: every lane has read it
+
+      float s[NQ][NK][4];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int j = 0; j < NK; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n][j][e] = 0.0f;
 #pragma unroll
       for (int k = 0; k < ND; ++k) {
         if (k >= ksteps) break;
-        uint32_t kf[4];  // states 0-7 and 8-15, each in two halves of 8 elements
-        ldsm4(kf, kt + ((lane & 7) + (lane >> 4) * 8) * kPitch + k * 32 + ((lane >> 3) & 1) * 16);
 #pragma unroll
-        for (int z = 0; z < MT; ++z) {
-          mma16816<DT>(s[z][0], qf[z][k][0], qf[z][k][1], qf[z][k][2], qf[z][k][3], kf[0], kf[1]);
-          mma16816<DT>(s[z][1], qf[z][k][0], qf[z][k][1], qf[z][k][2], qf[z][k][3], kf[2], kf[3]);
+        for (int j = 0; j < NK; ++j) {
+          uint32_t kf[4];  // 16 states x 16 elements
+          ldsm4(kf, (kt + (k >> 2) * kHalfTile + j * 2048 + k_lane) ^ (k & 3) * 32);
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) mma16816<DT>(s[n][j], kf[0], kf[1], kf[2], kf[3], qb[n][k][0], qb[n][k][1]);
         }
       }
-      const bool all = found == 0xffffu;
-      uint32_t pf[MT][4];
+      const bool all = found == (kT == 32 ? 0xffffffffu : (1u << kT) - 1);
+      uint32_t pf[NQ][NK][2];
 #pragma unroll
-      for (int z = 0; z < MT; ++z) {
+      for (int n = 0; n < NQ; ++n) {
         float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < NK; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            s[z][j][e] *= sl;
-            if (!all && !(found >> (j * 8 + q * 2 + (e & 1)) & 1)) s[z][j][e] = -INFINITY;
-            mx[e >> 1] = fmaxf(mx[e >> 1], s[z][j][e]);
+            s[n][j][e] *= sl;
+            if (!all && !(found >> (j * 16 + (e >> 1) * 8 + g) & 1)) s[n][j][e] = -INFINITY;
+            mx[e & 1] = fmaxf(mx[e & 1], s[n][j][e]);
           }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
-          mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
+          mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 4));
+          mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 8));
+          mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 16));
         }
         constexpr float kGrow = kSlack + kBelow<DT>;
-        const bool grown0 = mx[0] > m[z][0] + kGrow, grown1 = mx[1] > m[z][1] + kGrow;
+        const bool grown0 = mx[0] > m[n][0] + kGrow, grown1 = mx[1] > m[n][1] + kGrow;
         if (__any_sync(0xffffffffu, grown0 || grown1)) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float to = (e ? grown1 : grown0) ? mx[e] - kBelow<DT> : m[z][e];
-            const float f = to > -INFINITY ? exp2_approx(m[z][e] - to) : 1.0f;
-            m[z][e] = to;
-            l[z][e] *= f;
+            const float to = (e ? grown1 : grown0) ? mx[e] - kBelow<DT> : m[n][e];
+            const float f = to > -INFINITY ? exp2_approx(m[n][e] - to) : 1.0f;
+            m[n][e] = to;
+            l[n][e] *= f;
 #pragma unroll
-            for (int j = 0; j < 2 * ND; ++j) {
-              o[z][j][2 * e] *= f;
-              o[z][j][2 * e + 1] *= f;
+            for (int t = 0; t < ND; ++t) {
+              o[n][t][e] *= f;
+              o[n][t][2 + e] *= f;
             }
           }
         }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float ref = m[z][e] > -INFINITY ? m[z][e] : 0.0f;
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int y = 0; y < 2; ++y) s[z][j][2 * e + y] = exp2_approx(s[z][j][2 * e + y] - ref);
-        }
+        const float ref0 = m[n][0] > -INFINITY ? m[n][0] : 0.0f, ref1 = m[n][1] > -INFINITY ? m[n][1] : 0.0f;
         // l from the rounded weights: what their roundings have in common cancels
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < NK; ++j)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            pf[z][2 * j + e] = pack2<DT>(s[z][j][2 * e], s[z][j][2 * e + 1]);
-            float lo, hi;
-            unpack2<DT>(pf[z][2 * j + e], lo, hi);
-            l[z][e] += lo + hi;
+            const uint32_t w = pack2<DT>(exp2_approx(s[n][j][2 * e] - ref0), exp2_approx(s[n][j][2 * e + 1] - ref1));
+            float p0, p1;
+            unpack2<DT>(w, p0, p1);
+            l[n][0] += p0;
+            l[n][1] += p1;
+            pf[n][j][e] = movmatrix(w);
           }
       }
 #pragma unroll
-      for (int k = 0; k < ND; ++k) {
-        if (k >= ksteps) break;
-        uint32_t vf[4];  // 16 states x 16 elements
-        ldsm4t(vf, vt + (lane & 15) * kPitch + k * 32 + (lane >> 4) * 16);
+      for (int t = 0; t < ND; ++t) {
+        if (t >= ksteps) break;
 #pragma unroll
-        for (int z = 0; z < MT; ++z) {
-          mma16816<DT>(o[z][2 * k], pf[z][0], pf[z][1], pf[z][2], pf[z][3], vf[0], vf[1]);
-          mma16816<DT>(o[z][2 * k + 1], pf[z][0], pf[z][1], pf[z][2], pf[z][3], vf[2], vf[3]);
+        for (int j = 0; j < NK; ++j) {
+          uint32_t vf[4];  // 16 elements x 16 states
+          ldsm4t(vf, (vt + (t >> 2) * kHalfTile + j * 2048 + v_lane) ^ (t & 3) * 32);
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) mma16816<DT>(o[n][t], vf[0], vf[1], vf[2], vf[3], pf[n][j][0], pf[n][j][1]);
         }
       }
-      __syncwarp();  // every lane has read the tile before a later fetch overwrites it
-    };
-    const int mine = (tiles - warp + kWarps - 1) / kWarps;  // tiles of this warp
-    for (int i = 0; i < mine; i += kStages)
-#pragma unroll
-      for (int u = 0; u < kStages; ++u)  // unrolled: the ring's slots and `there` are constants
-        if (i + u < mine) {
-          fetch(i + u + kStages - 1, there[(u + kStages - 1) % kStages]);
-          step(i + u, there[u]);
-        }
-    cp_wait<0>();
-    __syncthreads();
+      __syncwarp();
+    }
 
-    // join the four warps: one row of tiles at a time
-    constexpr int kCols = ND * 16;
-    float *so = reinterpret_cast<float *>(smem);                         // [kWarps][16][kCols]
-    float2 *sml = reinterpret_cast<float2 *>(so + kWarps * 16 * kCols);  // [kWarps][16]
-    static_assert((kWarps * 16 * kCols + 2 * kWarps * 16) * 4 <= kWarps * kStages * kTileBytes, "fits the rings");
+    // join the head's warps, four rows at a time
 #pragma unroll
-    for (int z = 0; z < MT; ++z) {
+    for (int n = 0; n < NQ; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float s = l[z][e];
-        s += __shfl_xor_sync(0xffffffffu, s, 1);
-        s += __shfl_xor_sync(0xffffffffu, s, 2);
-        if (q == 0) sml[warp * 16 + g + e * 8] = make_float2(m[z][e], s);
-#pragma unroll
-        for (int j = 0; j < 2 * ND; ++j)
-          *reinterpret_cast<float2 *>(so + (warp * 16 + g + e * 8) * kCols + j * 8 + q * 2) =
-              make_float2(o[z][j][2 * e], o[z][j][2 * e + 1]);
+        l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 4);
+        l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 8);
+        l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 16);
       }
-      __syncthreads();
-      for (int r = warp; r < 16; r += kWarps) {
-        const int row = row0 + z * 16 + r;
+    auto together = [&]() {
+      if (of_head == 1) __syncwarp();
+      else __syncthreads();
+    };
+#pragma unroll
+    for (int h = 0; h < 2 * NQ; ++h) {
+      if (row0 + h * kJoinRows >= rows) break;
+      const int n = h >> 1;
+      if (q >> 1 == (h & 1)) {  // rows 4 (h & 1) + 2 (q & 1) + e of block n
+        const int at = warp * kJoinRows + 2 * (q & 1);
+        if (g == 0) sml[at] = make_float2(m[n][0], l[n][0]), sml[at + 1] = make_float2(m[n][1], l[n][1]);
+#pragma unroll
+        for (int t = 0; t < ND; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) so[(at + (e & 1)) * DH * 64 + t * 16 + (e >> 1) * 8 + g] = o[n][t][e];
+      }
+      together();
+      for (int i = wk; i < kJoinRows; i += of_head) {
+        const int r = h * kJoinRows + i, row = row0 + r, part = wh * of_head * kJoinRows + i;
         if (row >= rows) break;
-        float mm = -INFINITY, f[kWarps], ll = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) mm = fmaxf(mm, sml[w * 16 + r].x);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float2 v = sml[w * 16 + r];
-          f[w] = v.x > -INFINITY ? exp2_approx(v.x - mm) : 0.0f;
-          ll += f[w] * v.y;
+        float mm = -INFINITY, ll = 0.0f;
+        for (int w = 0; w < of_head; ++w) mm = fmaxf(mm, sml[part + w * kJoinRows].x);
+        float4 v = make_float4(0, 0, 0, 0);
+        for (int w = 0; w < of_head; ++w) {
+          const float2 y = sml[part + w * kJoinRows];
+          const float f = y.x > -INFINITY ? exp2_approx(y.x - mm) : 0.0f;
+          ll += f * y.y;
+          const float4 x = lane * 4 < D ? *reinterpret_cast<const float4 *>(so + (part + w * kJoinRows) * DH * 64 + lane * 4) : v;
+          v.x += f * x.x, v.y += f * x.y, v.z += f * x.z, v.w += f * x.w;
         }
+        const int64_t slot = (sg.slot * P.together + wh) * kRows + r;
         if (lane * 4 < D) {
-          float4 v = make_float4(0, 0, 0, 0);
-#pragma unroll
-          for (int w = 0; w < kWarps; ++w) {
-            const float4 x = *reinterpret_cast<const float4 *>(so + (w * 16 + r) * kCols + lane * 4);
-            v.x += f[w] * x.x, v.y += f[w] * x.y, v.z += f[w] * x.z, v.w += f[w] * x.w;
-          }
           if (sg.whole) {
             const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
             *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(d.out) + (int64_t)(a.t0 + row / G) * d.out_stride +
-                                       (sg.hk * G + row % G) * D + lane * 4) =
+                                       (hk * G + row % G) * D + lane * 4) =
                 make_uint2(pack2<DT>(v.x * inv, v.y * inv), pack2<DT>(v.z * inv, v.w * inv));
           } else {
-            *reinterpret_cast<float4 *>(P.o + (sg.slot * kRows + z * 16 + r) * D + lane * 4) = v;
+            *reinterpret_cast<float4 *>(P.o + slot * D + lane * 4) = v;
           }
         }
-        if (lane == 0 && !sg.whole) P.ml[sg.slot * kRows + z * 16 + r] = make_float2(ll == ll ? mm : ll, ll);
+        if (lane == 0 && !sg.whole) P.ml[slot] = make_float2(ll == ll ? mm : ll, ll);
       }
-      __syncthreads();
+      together();
+    }
+  }
+  if (!BOX) {
+    cp_wait<0>();
+  } else if (*abort_flag && lane == 0) {  // a copy may still be landing
+    for (uint32_t i = issued > (uint32_t)kStages ? issued - kStages : 0; i < issued; ++i) {
+      const long long t0 = clock64();
+      while (!mbar_try_wait(bar0 + 8 * (i % kStages), i / kStages & 1) && clock64() - t0 < kWaitCycles) {
+      }
     }
   }
 }
 
-// A warp to a (token, head): the parts of its row tile, where that has more than one.
+// How many of v[0 .. n), which ascend, are at most x.  The whole warp looks at 32 entries at once.
+__device__ __forceinline__ int count_upto(const long long *v, int n, long long x, int lane) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32, i = lo + (lane + 1) * step - 1;
+    const unsigned past = ~__ballot_sync(0xffffffffu, i < hi && v[min(i, n - 1)] <= x);
+    const int c = past ? __ffs(past) - 1 : 32;
+    lo += c * step;
+    hi = min(hi, lo + step - 1);
+  }
+  return min(lo, n);
+}
+
+// The parts of row tiles that several CTAs took: blocks (x, y) look at the border between CTA x's cells and the next,
+// and, where it is the first within a row tile, join the tile's rows, L lanes to a row.  The references, sums and O of
+// 8 parts are asked for at once.
 constexpr int kMergeParts = 8;
-template <int DT>
+template <int DT, int L>
 __global__ void __launch_bounds__(kThreads) cross_merge_kernel(const __grid_constant__ CrossPlan P) {
   const wt_cross_desc &d = P.d;
-  const int lane = threadIdx.x & 31, b = blockIdx.y;
-  const Asker a = asker_of(P, b, false);
+  const int lane = threadIdx.x & 31;
   griddep_wait();  // launched while the kernel before it ends
-  const int i = blockIdx.x * kWarps + (threadIdx.x >> 5);
-  if (i >= a.n * d.heads) return;
-  const int D = d.head_dim, h = i % d.heads, t = i / d.heads, hk = h / P.G;
-  const int row = t * P.G + h % P.G, row_tile = row / P.rows, r = row - row_tile * P.rows;
-  const long long per = P.first[d.n_req];
-  const long long u0 = P.first[b] + hk * a.head_cells() + (long long)row_tile * a.key_tiles;
-  const long long c0 = u0 / per, c1 = (u0 + (row_tile == a.row_tiles - 1 ? a.last : a.key_tiles) - 1) / per;
-  if (c0 == c1) return;  // one CTA took it whole
-  auto slot = [&](long long c) { return (2 * c + (c * per < u0)) * P.rows + r; };
-  float m = -INFINITY;
-  for (long long c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, P.ml[slot(c)].x);
-#pragma unroll
-  for (int s = 16; s; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+  const long long per = P.first[d.n_req], all = P.first[d.n_req + 1], border = per * (blockIdx.x + 1);
+  if (border >= all) return;
+  const int b = count_upto(P.first, d.n_req, border - 1, lane) - 1;
+  const Asker a = asker_of(P, b, false);
+  Share s;
+  s.lo = border - 1, s.hi = all;
+  const long long first = P.first[b];
+  const Segment g = segment_at(P, a, first, border - 1, s);  // from the cell before the border to the row tile's end
+  const long long u0 = first + g.group * a.head_cells() + (long long)g.row_tile * a.key_tiles, u1 = border - 1 + g.cells;
+  if (u1 <= border || u0 < per * blockIdx.x) return;
+  const int D = d.head_dim, i = blockIdx.y * (kThreads / L) + threadIdx.x / L, wh = i / P.rows, r = i - wh * P.rows;
+  const int row = g.row_tile * P.rows + r, col = threadIdx.x % L * 4;
+  if (wh >= P.together || row >= a.n * P.G || col >= D) return;
+  const int c0 = blockIdx.x, c1 = (int)quotient(u1 - 1, per);
+  float m = -INFINITY, l = 0.0f;
   float4 o = make_float4(0, 0, 0, 0);
-  float l = 0.0f;
-  for (long long k0 = c0; k0 <= c1; k0 += 32) {
-    const float2 mine = k0 + lane <= c1 ? P.ml[slot(k0 + lane)] : make_float2(-INFINITY, 0.0f);
-    // a part whose factor is 0 still counts: what is not finite in it has to show
-    const float f = mine.x > -INFINITY || mine.x != mine.x ? exp2_approx(mine.x - m) : 0.0f;
-    l += f * mine.y;
-    const int n = (int)min(32ll, c1 - k0 + 1);
-    for (int k = 0; k < n; k += kMergeParts) {
-      float4 x[kMergeParts];
+  for (int c = c0; c <= c1; c += kMergeParts) {
+    float2 ml[kMergeParts];
+    float4 x[kMergeParts];
 #pragma unroll
-      for (int u = 0; u < kMergeParts; ++u)
-        x[u] = k + u < n && lane * 4 < D ? *reinterpret_cast<const float4 *>(P.o + slot(k0 + k + u) * D + lane * 4)
-                                         : make_float4(0, 0, 0, 0);
+    for (int k = 0; k < kMergeParts; ++k) {
+      const long long at = ((2ll * (c + k) + (c + k == c0 && per * c0 < u0)) * P.together + wh) * P.rows + r;
+      ml[k] = c + k <= c1 ? P.ml[at] : make_float2(-INFINITY, 0.0f);
+      x[k] = c + k <= c1 ? *reinterpret_cast<const float4 *>(P.o + at * D + col) : make_float4(0, 0, 0, 0);
+    }
+    float to = m;
 #pragma unroll
-      for (int u = 0; u < kMergeParts; ++u) {
-        const float w = __shfl_sync(0xffffffffu, f, (k + u) & 31);
-        o.x += w * x[u].x, o.y += w * x[u].y, o.z += w * x[u].z, o.w += w * x[u].w;
-      }
+    for (int k = 0; k < kMergeParts; ++k) to = fmaxf(to, ml[k].x);
+    const float by = m > -INFINITY ? exp2_approx(m - to) : 0.0f;
+    m = to;
+    l *= by, o.x *= by, o.y *= by, o.z *= by, o.w *= by;
+#pragma unroll
+    for (int k = 0; k < kMergeParts; ++k) {
+      // a part whose factor is 0 still counts: what is not finite in it has to show
+      const float f = ml[k].x > -INFINITY || ml[k].x != ml[k].x ? exp2_approx(ml[k].x - m) : 0.0f;
+      l += f * ml[k].y;
+      o.x += f * x[k].x, o.y += f * x[k].y, o.z += f * x[k].z, o.w += f * x[k].w;
     }
   }
-#pragma unroll
-  for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
-  if (lane * 4 < D) {
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(d.out) + (int64_t)(a.t0 + t) * d.out_stride + h * D + lane * 4) =
-        make_uint2(pack2<DT>(o.x * inv, o.y * inv), pack2<DT>(o.z * inv, o.w * inv));
-  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const int hk = g.group * P.together + wh;
+  *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(d.out) + (int64_t)(a.t0 + row / P.G) * d.out_stride + (hk * P.G + row % P.G) * D + col) =
+      make_uint2(pack2<DT>(o.x * inv, o.y * inv), pack2<DT>(o.z * inv, o.w * inv));
 }
 
-template <int ND>
-constexpr size_t few_smem() {
-  return (size_t)kWarps * kStages * 2 * kKeys * (ND * 32 + 16);
-}
-
-template <int DT, int ND>
-cudaError_t run_few(const CrossPlan &P, cudaStream_t s) {
-  if (P.rows == 16) cross_few_kernel<DT, ND, 1><<<P.ctas, kThreads, few_smem<ND>(), s>>>(P);
-  else cross_few_kernel<DT, ND, 2><<<P.ctas, kThreads, few_smem<ND>(), s>>>(P);
+template <int DT, int DH, int NQ>
+cudaError_t run_few(const CrossPlan &P, const CrossMaps &m, cudaStream_t s) {
+  const CUtensorMap &k = *reinterpret_cast<const CUtensorMap *>(m.k), &v = *reinterpret_cast<const CUtensorMap *>(m.v);
+  if (P.box) cross_few_kernel<DT, DH, NQ, true><<<P.ctas, kThreads, few_smem<DH>(), s>>>(k, v, P);
+  else cross_few_kernel<DT, DH, NQ, false><<<P.ctas, kThreads, few_smem<DH>(), s>>>(k, v, P);
   return cudaGetLastError();
 }
 
-template <int DT>
-cudaError_t run_dim(const CrossPlan &P, cudaStream_t s) {
-  if (P.d.head_dim <= 64) return run_few<DT, 4>(P, s);
-  if (P.d.head_dim <= 96) return run_few<DT, 6>(P, s);
-  return run_few<DT, 8>(P, s);
+template <int DT, int DH>
+cudaError_t run_rows(const CrossPlan &P, const CrossMaps &m, cudaStream_t s) {
+  if (P.rows == 8) return run_few<DT, DH, 1>(P, m, s);
+  if (P.rows == 16) return run_few<DT, DH, 2>(P, m, s);
+  return run_few<DT, DH, 4>(P, m, s);
 }
 
-template <int DT, int ND>
+template <int DT, int DH, int NQ>
 cudaError_t prepare_few() {
-  cudaError_t e = cudaFuncSetAttribute(cross_few_kernel<DT, ND, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_smem<ND>());
+  cudaError_t e = cudaFuncSetAttribute(cross_few_kernel<DT, DH, NQ, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_smem<DH>());
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(cross_few_kernel<DT, ND, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_smem<ND>());
+    e = cudaFuncSetAttribute(cross_few_kernel<DT, DH, NQ, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_smem<DH>());
+  return e;
+}
+
+template <int DT, int DH>
+cudaError_t prepare_dim() {
+  cudaError_t e = prepare_few<DT, DH, 1>();
+  if (e == cudaSuccess) e = prepare_few<DT, DH, 2>();
+  if (e == cudaSuccess) e = prepare_few<DT, DH, 4>();
   return e;
 }
 
 template <int DT>
 cudaError_t run_merge(const CrossPlan &P, cudaStream_t s) {
+  if (P.ctas < 2) return cudaSuccess;
+  const int lanes = P.d.head_dim <= 64 ? 16 : 32, most = (int)std::min<int64_t>(P.rows, (int64_t)P.d.max_new * P.G);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(((int64_t)P.d.max_new * P.d.heads + kWarps - 1) / kWarps), (unsigned)P.d.n_req);
+  // rows of a head stand `rows` apart, so with several heads all count
+  cfg.gridDim = dim3((unsigned)P.ctas - 1, (unsigned)(((P.together > 1 ? P.together * P.rows : most) * lanes + kThreads - 1) / kThreads));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
   cudaLaunchAttribute at[1];
@@ -366,25 +490,24 @@ cudaError_t run_merge(const CrossPlan &P, cudaStream_t s) {
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, cross_merge_kernel<DT>, P);
+  return cudaLaunchKernelEx(&cfg, lanes == 16 ? cross_merge_kernel<DT, 16> : cross_merge_kernel<DT, 32>, P);
 }
 
 }  // namespace
 
-int cross_few_resident(int rows, int head_dim) { return rows > 16 ? 2 : head_dim <= 64 ? 4 : 3; }
-
 cudaError_t cross_prepare() {
-  cudaError_t e = prepare_few<WT_BF16, 4>();
-  if (e == cudaSuccess) e = prepare_few<WT_BF16, 6>();
-  if (e == cudaSuccess) e = prepare_few<WT_BF16, 8>();
-  if (e == cudaSuccess) e = prepare_few<WT_F16, 4>();
-  if (e == cudaSuccess) e = prepare_few<WT_F16, 6>();
-  if (e == cudaSuccess) e = prepare_few<WT_F16, 8>();
+  cudaError_t e = prepare_dim<WT_BF16, 1>();
+  if (e == cudaSuccess) e = prepare_dim<WT_BF16, 2>();
+  if (e == cudaSuccess) e = prepare_dim<WT_F16, 1>();
+  if (e == cudaSuccess) e = prepare_dim<WT_F16, 2>();
   return e;
 }
 
-cudaError_t launch_cross_few(const CrossPlan &P, cudaStream_t s) {
-  return P.d.dtype == WT_BF16 ? run_dim<WT_BF16>(P, s) : run_dim<WT_F16>(P, s);
+int cross_few_keys(int head_dim) { return head_dim <= 64 ? kKeys<1> : kKeys<2>; }
+
+cudaError_t launch_cross_few(const CrossPlan &P, const CrossMaps &m, cudaStream_t s) {
+  if (P.d.dtype == WT_BF16) return P.d.head_dim <= 64 ? run_rows<WT_BF16, 1>(P, m, s) : run_rows<WT_BF16, 2>(P, m, s);
+  return P.d.head_dim <= 64 ? run_rows<WT_F16, 1>(P, m, s) : run_rows<WT_F16, 2>(P, m, s);
 }
 
 cudaError_t launch_cross_merge(const CrossPlan &P, cudaStream_t s) {

@@ -14,7 +14,7 @@ struct Asker {
   int row_tiles, key_tiles;
   int last;          // cells of the last row tile
   __device__ long long head_cells() const { return (row_tiles - 1ll) * key_tiles + last; }
-  __device__ long long cells(int kv_heads) const { return row_tiles ? head_cells() * kv_heads : 0; }
+  __device__ long long cells(const CrossPlan &P) const { return row_tiles ? head_cells() * P.groups : 0; }
 };
 
 __device__ __forceinline__ Asker asker_of(const CrossPlan &P, int b, bool tell) {
@@ -52,7 +52,7 @@ __device__ __forceinline__ Share share_of(const CrossPlan &P) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int run = (d.n_req + N - 1) / N, b0 = min(tid * run, d.n_req), b1 = min(b0 + run, d.n_req);
   long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += asker_of(P, b, blockIdx.x == 0).cells(d.kv_heads);
+  for (int b = b0; b < b1; ++b) mine += asker_of(P, b, blockIdx.x == 0).cells(P);
   long long upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -68,24 +68,24 @@ __device__ __forceinline__ Share share_of(const CrossPlan &P) {
     if (w == warp) upto += all;
     all += sums[w];
   }
-  const long long per = max(1ll, (all + gridDim.x - 1) / gridDim.x), lo = per * blockIdx.x, hi = min(all, lo + per);
+  const long long per = max((long long)P.least, quotient(all + gridDim.x - 1, gridDim.x)), lo = per * blockIdx.x, hi = min(all, lo + per);
   long long first = upto - mine;
   const bool here = lo < hi && first <= lo && lo < upto;
   if (here || blockIdx.x == 0)
     for (int b = b0; b < b1; ++b) {
-      const long long n = asker_of(P, b, false).cells(d.kv_heads);
+      const long long n = asker_of(P, b, false).cells(P);
       if (blockIdx.x == 0) P.first[b] = first;
       if (here && first <= lo && lo < first + n) found = {lo, hi, first, b};
       first += n;
     }
-  if (blockIdx.x == 0 && tid == 0) P.first[d.n_req] = per;
+  if (blockIdx.x == 0 && tid == 0) P.first[d.n_req] = per, P.first[d.n_req + 1] = all;
   __syncthreads();
   return found;
 }
 
 // One row tile's states that this CTA takes.
 struct Segment {
-  int hk, row_tile;
+  int group, row_tile;  // of kv heads, of rows
   int tile0, tiles;   // tiles of P.keys states
   int cells;          // as many, or half of them (P.half)
   bool half, whole;   // whole: all of the row tile's
@@ -96,9 +96,9 @@ struct Segment {
 __device__ __forceinline__ Segment segment_at(const CrossPlan &P, const Asker &a, long long first, long long at, const Share &s) {
   Segment g;
   const long long per_head = a.head_cells();
-  g.hk = (int)((at - first) / per_head);
-  const long long head = first + g.hk * per_head;
-  g.row_tile = (int)min((at - head) / a.key_tiles, a.row_tiles - 1ll);
+  g.group = (int)quotient(at - first, per_head);
+  const long long head = first + g.group * per_head;
+  g.row_tile = (int)min(quotient(at - head, a.key_tiles), a.row_tiles - 1ll);
   const long long begin = head + (long long)g.row_tile * a.key_tiles;
   const int all = g.row_tile == a.row_tiles - 1 ? a.last : a.key_tiles;
   g.half = a.n * P.G - g.row_tile * P.rows <= P.half;

@@ -10,7 +10,8 @@
 //   producer warp    TMA boxes of Q (two tiles), and of K and V into a ring (128-byte swizzle)
 //   MMA warp         S_i = Q_i K^T for the two streams i, then O_i += P_i V as each P_i arrives
 //   two warpgroups   one per stream; a thread owns a row: it reads the row of S from tensor memory, takes the
-//                    exponentials and writes P (16-bit) back over S, where it is the next product's A operand
+//                    exponentials and writes P (16-bit) as the next product's A operand: over S, or for heads of up
+//                    to 64, whose O leaves room, beside it, so that the next S is made meanwhile
 //   a warp           clears the rows of V that are not in the memory, or not kept: a weight of 0 does not hide
 //                    what is not finite.  Without a mask that is a memory's last tile alone.  Such a tile lands
 //                    on a barrier of its own, and this warp makes the arrival that others wait for.
@@ -32,7 +33,15 @@ constexpr int kThreads = 384;  // warps 0-3, 4-7: softmax of stream 0, 1; 8: pro
 // 3 x 168 to the three warpgroups together.
 constexpr int kRegsSoftmax = 224, kRegsRest = 56;
 static_assert(2 * kRegsSoftmax + kRegsRest <= 3 * 168, "what the launch has");
-constexpr uint32_t kTmemCols = 512;  // S_0, S_1 (128 columns each), O_0, O_1
+constexpr uint32_t kTmemCols = 512;
+// Tensor memory of stream i: S (128 columns), P (64), O.  Two halves of a head: P over S.
+template <int DH>
+struct Cols {
+  static constexpr bool apart = DH == 1;
+  static constexpr uint32_t s = DH == 1 ? 256 : 128;  // from S_0 to S_1
+  static constexpr uint32_t p = DH == 1 ? 128 : 0;    // from S to P
+  static constexpr uint32_t o0 = DH == 1 ? 192 : 256, o = DH == 1 ? 256 : 128;
+};
 
 template <int DH>  // 64-element halves of head_dim
 struct Geo {
@@ -40,7 +49,7 @@ struct Geo {
   static constexpr int stages = DH == 2 ? 5 : 8;
   static constexpr uint32_t ring = 2 * stage;  // after the two Q tiles
   static constexpr uint32_t bars = ring + stages * stage;
-  static constexpr int nbars = 3 * stages + 12;
+  static constexpr int nbars = 3 * stages + 14;
   // (m, l) of the rows of both streams of one row tile: with two halves in the second Q tile's place, which such
   // a row tile does not use, behind the 4 KB that its first warp turns rows in
   static constexpr uint32_t join = DH == 2 ? stage + 4096 : bars + nbars * 8 + 16;
@@ -62,8 +71,8 @@ struct Walk {
   }
   __device__ bool next() {
     if (cell >= s.hi) return false;
-    while (cell >= first + a.cells(P.d.kv_heads)) {
-      first += a.cells(P.d.kv_heads);
+    while (cell >= first + a.cells(P)) {
+      first += a.cells(P);
       a = asker_of(P, ++b, false);
     }
     g = segment_at(P, a, first, cell, s);
@@ -73,22 +82,24 @@ struct Walk {
 };
 
 // Whether V of a key tile has rows to clear.
-__device__ __forceinline__ bool to_clear(const CrossPlan &P, const Asker &a, int tile) {
-  return P.d.keep || a.len - tile * kKeysT < kKeysT;
+template <bool KEEP>
+__device__ __forceinline__ bool to_clear(const Asker &a, int tile) {
+  return KEEP || a.len - tile * kKeysT < kKeysT;
 }
 
-template <int DT, int DH>
+template <int DT, int DH, bool KEEP>
 __global__ void __launch_bounds__(kThreads, 1)
     cross_wide_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                       const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CrossPlan P) {
   using X = Geo<DH>;
+  using C = Cols<DH>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t *gbase = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t full0 = base + X::bars, empty0 = full0 + X::stages * 8, raw0 = empty0 + X::stages * 8;
   const uint32_t q_full = raw0 + X::stages * 8, q_empty = q_full + 8;
   const uint32_t s_full = q_empty + 8, p_full = s_full + 16, o_full = p_full + 16;  // [2] each
-  const uint32_t p_half = o_full + 16, fin = p_half + 16, meet = fin + 8;
+  const uint32_t p_half = o_full + 16, fin = p_half + 16, meet = fin + 8, s_free = meet + 8;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gbase + X::bars + X::nbars * 8);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 2);
   float2 *join = reinterpret_cast<float2 *>(gbase + X::join);
@@ -96,6 +107,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
+    for (const CUtensorMap *m : {&qmap, &kmap, &vmap}) asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
     for (int s = 0; s < X::stages; ++s) {
       mbar_init(full0 + 8 * s, 1);
       mbar_init(empty0 + 8 * s, 1);
@@ -110,6 +122,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(p_full + 8 * i, 128);
       mbar_init(p_half + 8 * i, 128);
       mbar_init(o_full + 8 * i, 1);
+      mbar_init(s_free + 8 * i, 128);
     }
     *abort_flag = 0;
     mbar_fence_init();
@@ -120,6 +133,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   fence_before();
+  griddep_launch();  // the merge's first loads may run beside this
   const Share share = share_of<kThreads>(P);  // has the barriers of all that was set up above
   fence_after();
   const uint32_t tmem = *tmem_slot;
@@ -146,18 +160,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (Walk w(P, share); live && w.next(); ++seg) {
         const Segment &g = w.g;
         if (seg && !bounded_wait(q_empty, (seg - 1) & 1, abort_flag, status)) break;
-        const int qtiles = g.half ? 1 : 2, lead = g.half ? 2 : 1;  // key tiles whose K is loaded ahead of their V
+        const int qtiles = g.half ? 1 : 2, lead = (g.half ? 2 : 1) + C::apart;  // key tiles whose K is loaded ahead of their V
         mbar_expect_tx(q_full, (uint32_t)qtiles * DH * P.half * 128);
         ++q_loads;
         for (int i = 0; i < qtiles; ++i)
 #pragma unroll
           for (int hf = 0; hf < DH; ++hf)
-            tma_3d(base + (i * DH + hf) * kHalf, &qmap, hf * 64, g.hk * P.G, w.a.t0 + (g.row_tile * 2 + i) * P.tile_tokens, q_full);
+            tma_3d(base + (i * DH + hf) * kHalf, &qmap, hf * 64, g.group * P.G, w.a.t0 + (g.row_tile * 2 + i) * P.tile_tokens, q_full);
         const int state0 = w.a.mem + g.tile0 * kKeysT;
-        for (int j = 0; j < min(lead, g.tiles) && live; ++j) live = load(&kmap, g.hk, state0 + j * kKeysT, false);
+        for (int j = 0; j < min(lead, g.tiles) && live; ++j) live = load(&kmap, g.group, state0 + j * kKeysT, false);
         for (int j = 0; j < g.tiles && live; ++j) {
-          live = load(&vmap, g.hk, state0 + j * kKeysT, to_clear(P, w.a, g.tile0 + j));
-          if (live && j + lead < g.tiles) live = load(&kmap, g.hk, state0 + (j + lead) * kKeysT, false);
+          live = load(&vmap, g.group, state0 + j * kKeysT, to_clear<KEEP>(w.a, g.tile0 + j));
+          if (live && j + lead < g.tiles) live = load(&kmap, g.group, state0 + (j + lead) * kKeysT, false);
         }
       }
       if (*abort_flag) {
@@ -183,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr uint32_t kIqk = idesc(kBf, kKeysT, 0);
       const int dim_steps = (P.d.head_dim + 15) / 16;
       const uint32_t ipv = idesc(kBf, dim_steps * 16, 1);
-      uint32_t it = 0, seg = 0, np[2] = {0, 0};
+      uint32_t it = 0, seg = 0, np[2] = {0, 0}, ns[2] = {0, 0};
       bool live = true;
       uint32_t stage = 0;
       auto next = [&]() {  // the ring's next tile has landed, and its rows are clear
@@ -199,16 +213,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
       };
       auto scores = [&](int i, int tile_q, uint32_t s) {
+        // where P lies apart, S may be written once it has been read
+        if (C::apart) {
+          if (ns[i] && !warp_wait(s_free + 8 * i, (ns[i] - 1) & 1, abort_flag, status)) return live = false;
+          ++ns[i];
+          fence_after();
+        }
         const uint32_t q = desc_k(base + tile_q * X::stage), k = desc_k(base + X::ring + s * X::stage);
         if (elect_one()) {
 #pragma unroll
           for (int e = 0; e < DH * 4; ++e) {
             const uint32_t off = ((e >> 2) * kHalf + (e & 3) * 32) >> 4;
-            if (e < dim_steps) umma_ss(tmem + i * 128, q + off, k + off, kIqk, e != 0);
+            if (e < dim_steps) umma_ss(tmem + i * C::s, q + off, k + off, kIqk, e != 0);
           }
           commit(s_full + 8 * i);
         }
         __syncwarp();
+        return true;
       };
       auto values = [&](int i, uint32_t s, bool first) {  // false: no P came
         const uint32_t v = desc_mn(base + X::ring + s * X::stage);
@@ -220,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (elect_one()) {
 #pragma unroll
             for (int e = hf * 4; e < hf * 4 + 4; ++e)
-              umma_ts(tmem + 256 + i * 128, tmem + i * 128 + e * 8, v + e * (2048 >> 4), ipv, !first || e != 0);
+              umma_ts(tmem + C::o0 + i * C::o, tmem + i * C::s + C::p + e * 8, v + e * (2048 >> 4), ipv, !first || e != 0);
             if (hf) commit(o_full + 8 * i);
           }
           __syncwarp();
@@ -232,15 +253,39 @@ __global__ void __launch_bounds__(kThreads, 1)
         const Segment &g = w.g;
         if (!warp_wait(q_full, seg & 1, abort_flag, status)) break;
         fence_after();
-        if (!g.half) {
-          if (!next()) break;
-          scores(0, 0, stage);
-          scores(1, 1, stage);
-          release(empty0 + 8 * stage);
-          for (int j = 0; j < g.tiles; ++j) {
+        // the K tile of both streams, or in half row tiles of stream i
+        auto keys = [&](int i) {
+          if (!next()) return false;
+          const uint32_t ks = stage;
+          if (g.half) {
+            if (!scores(i, 0, ks)) return false;
+          } else if (!scores(0, 0, ks) || !scores(1, 1, ks)) {
+            return false;
+          }
+          release(empty0 + 8 * ks);
+          return true;
+        };
+        const int first = g.half ? 2 : 1;  // tiles that start the streams
+        for (int j = 0; j < min(first, g.tiles) && keys(j); ++j) {
+        }
+        if (!live) break;
+        for (int j = 0; j < g.tiles; ++j) {
+          const bool more = j + first < g.tiles;
+          if (C::apart) {  // the next S before this P V
+            if (more && !keys(j & 1)) break;
             if (!next()) break;
             const uint32_t vs = stage;
-            const bool more = j + 1 < g.tiles;
+            if (g.half ? !values(j & 1, vs, j < 2) : !values(0, vs, j == 0) || !values(1, vs, j == 0)) break;
+            release(empty0 + 8 * vs);
+          } else if (g.half) {
+            if (!next()) break;
+            const uint32_t vs = stage;
+            if (!values(j & 1, vs, j < 2)) break;
+            release(empty0 + 8 * vs);
+            if (more && !keys(j & 1)) break;
+          } else {
+            if (!next()) break;
+            const uint32_t vs = stage;
             if (!values(0, vs, j == 0)) break;
             if (more) {
               if (!next()) break;
@@ -250,23 +295,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             release(empty0 + 8 * vs);
             if (more) {
               scores(1, 1, stage);
-              release(empty0 + 8 * stage);
-            }
-          }
-        } else {
-          for (int j = 0; j < min(2, g.tiles) && next(); ++j) {
-            scores(j, 0, stage);
-            release(empty0 + 8 * stage);
-          }
-          if (!live) break;
-          for (int j = 0; j < g.tiles; ++j) {
-            if (!next()) break;
-            const uint32_t vs = stage;
-            if (!values(j & 1, vs, j < 2)) break;
-            release(empty0 + 8 * vs);
-            if (j + 2 < g.tiles) {
-              if (!next()) break;
-              scores(j & 1, 0, stage);
               release(empty0 + 8 * stage);
             }
           }
@@ -286,17 +314,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool live = true;
       for (Walk w(P, share); live && w.next();) {
         const Segment &g = w.g;
-        const int lead = g.half ? 2 : 1;
+        const int lead = (g.half ? 2 : 1) + C::apart;
         it += min(lead, g.tiles);
         for (int j = 0; j < g.tiles && live; ++j) {
-          if (to_clear(P, w.a, g.tile0 + j)) {
+          if (to_clear<KEEP>(w.a, g.tile0 + j)) {
             const uint32_t s = it % X::stages;
             const int state0 = (g.tile0 + j) * kKeysT;
             uint32_t kept[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
               const int at = state0 + c * 32 + lane;
-              kept[c] = __ballot_sync(0xffffffffu, at < w.a.len && (!P.d.keep || __ldg(P.d.keep + (int64_t)w.a.mem + at)));
+              kept[c] = __ballot_sync(0xffffffffu, at < w.a.len && (!KEEP || __ldg(P.d.keep + (int64_t)w.a.mem + at)));
             }
             live = warp_wait(raw0 + 8 * s, parity >> s & 1, abort_flag, status);
             parity ^= 1u << s;
@@ -326,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---------------- softmax: a thread owns row threadIdx.x % 128 of stream i
     const int i = warp >> 2, r = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // 32 lanes of tensor memory per warp
-    const uint32_t S = tmem + lanes + i * 128, O = tmem + lanes + 256 + i * 128;
+    const uint32_t S = tmem + lanes + i * C::s, O = tmem + lanes + C::o0 + i * C::o;
     const float scale_log2 = P.d.scale * 1.4426950408889634f;
     uint32_t done = 0, done_other = 0;  // tiles of this stream, and of the other, over all segments
     uint32_t seg = 0, met = 0;
@@ -336,11 +364,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       // The segment's queries have landed, so every thread has released those before (q_empty).
       if (!warp_wait(q_full, seg & 1, abort_flag, status)) break;
       const int n = g.half ? (g.tiles + 1 - i) / 2 : g.tiles;
-      const uint8_t *keep = P.d.keep ? P.d.keep + (int64_t)w.a.mem : nullptr;
+      const uint8_t *keep = P.d.keep + (int64_t)w.a.mem;
       // what keep says of a tile is read a tile ahead
       uint32_t ahead[4] = {1, 1, 1, 1};
       auto look = [&](int j) {
-        if (!keep) return;
+        if (!KEEP) return;
         const int at = (g.tile0 + (g.half ? 2 * j + i : j)) * kKeysT + lane;
 #pragma unroll
         for (int c = 0; c < 4; ++c) ahead[c] = at + c * 32 < w.a.len ? __ldg(keep + at + c * 32) : 0;
@@ -350,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int j = 0; j < n; ++j) {
         const int keys = w.a.len - (g.tile0 + (g.half ? 2 * j + i : j)) * kKeysT;
         uint32_t gone[4];
-        if (keep) {
+        if (KEEP) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) gone[c] = __ballot_sync(0xffffffffu, ahead[c] == 0);
           look(j + 1);
@@ -369,7 +397,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int c = 0; c < 128; ++c) v[c] = __uint_as_float(u[c]);
         }
-        if (keep) {
+        if (C::apart) {
+          fence_before();
+          mbar_arrive(s_free + 8 * i);
+        }
+        if (KEEP) {
 #pragma unroll
           for (int c = 0; c < 128; ++c)
             if (gone[c >> 5] >> (c & 31) & 1) v[c] = -INFINITY;
@@ -414,6 +446,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         const float ref = m > -INFINITY ? m : 0.0f;  // no score above -infinity yet
+        // where P lies apart, the product before may still read it
+        if (C::apart && done + j > 0) {
+          if (!warp_wait(o_full + 8 * i, (done + j - 1) & 1, abort_flag, status)) {
+            live = false;
+            break;
+          }
+          fence_after();
+        }
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
           uint32_t u[32];
@@ -428,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             unpack2<DT>(u[k / 2], r0, r1);
             add_x2(l0, l1, r0, r1);
           }
-          tmem_st32(S + hf * 32, u);
+          tmem_st32(S + C::p + hf * 32, u);
           wait_st();
           fence_before();
           mbar_arrive((hf ? p_full : p_half) + 8 * i);
@@ -464,12 +504,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       static_assert(32 * 128 <= X::stage / 4, "32 rows of 32 columns");
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
       const int c0 = g.half ? i * DH * 32 : 0, c1 = g.half ? c0 + DH * 32 : DH * 64;
-      const uint32_t O0 = tmem + lanes + 256;
+      const uint32_t O0 = tmem + lanes + C::o0;
 #pragma unroll 1
       for (int c = c0; c < c1 && c < P.d.head_dim; c += 32) {
         uint32_t o[32];
         if (n > 0) {
-          tmem_ld32((g.half ? O0 + i * 128 : O) + c, o);
+          tmem_ld32(O + c, o);
         } else {
 #pragma unroll
           for (int k = 0; k < 32; ++k) o[k] = 0;
@@ -478,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (g.half) {
           if (n_other > 0) {
             uint32_t x[32];
-            tmem_ld32(O0 + (1 - i) * 128 + c, x);
+            tmem_ld32(O0 + (1 - i) * C::o + c, x);
             wait_ld();
 #pragma unroll
             for (int k = 0; k < 32; ++k)
@@ -506,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (at < rows && col < P.d.head_dim) {
               const int row = row0 + at;
               *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(P.d.out) + (int64_t)(w.a.t0 + row / P.G) * P.d.out_stride +
-                                         (g.hk * P.G + row % P.G) * P.d.head_dim + col) = v;
+                                         (g.group * P.G + row % P.G) * P.d.head_dim + col) = v;
             }
           }
         } else {
@@ -548,15 +588,19 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 template <int DT, int DH>
 cudaError_t run(const CrossPlan &P, const CrossMaps &m, cudaStream_t s) {
-  cross_wide_kernel<DT, DH><<<P.ctas, kThreads, Geo<DH>::smem, s>>>(*reinterpret_cast<const CUtensorMap *>(m.q),
-                                                                    *reinterpret_cast<const CUtensorMap *>(m.k),
-                                                                    *reinterpret_cast<const CUtensorMap *>(m.v), P);
+  const CUtensorMap &q = *reinterpret_cast<const CUtensorMap *>(m.q), &k = *reinterpret_cast<const CUtensorMap *>(m.k),
+                    &v = *reinterpret_cast<const CUtensorMap *>(m.v);
+  if (P.d.keep) cross_wide_kernel<DT, DH, true><<<P.ctas, kThreads, Geo<DH>::smem, s>>>(q, k, v, P);
+  else cross_wide_kernel<DT, DH, false><<<P.ctas, kThreads, Geo<DH>::smem, s>>>(q, k, v, P);
   return cudaGetLastError();
 }
 
 template <int DT, int DH>
 cudaError_t prepare_one() {
-  return cudaFuncSetAttribute(cross_wide_kernel<DT, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Geo<DH>::smem);
+  const cudaError_t e = cudaFuncSetAttribute(cross_wide_kernel<DT, DH, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Geo<DH>::smem);
+  return e != cudaSuccess ? e
+                          : cudaFuncSetAttribute(cross_wide_kernel<DT, DH, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)Geo<DH>::smem);
 }
 
 }  // namespace

@@ -241,11 +241,6 @@ struct Answer {
 // -infinity, whatever the temperature.
 __device__ __forceinline__ float factor_of(float t) { return t > 0.0f ? fmaxf(fminf(1.4426950408889634f / t, 3.4028234e38f), 1.1754944e-38f) : 1.0f; }
 
-// a / b for numbers from 0 on; most are small
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-  return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
-}
-
 template <bool TOP>
 __global__ void __launch_bounds__(kThreads, kResident) logprobs_kernel(const __grid_constant__ LogprobsPlan P) {
   __shared__ Sums warp_sums[kWarps], row_sums;

@@ -514,11 +514,15 @@ int check_cross(wt_handle *h, const wt_cross_desc &d) {
   return WT_OK;
 }
 
+// Whether a memory's pitches fit a tensor map.
+bool cross_maps(const wt_cross_desc &d) {
+  return d.max_mem > 0 && d.q_stride < (1ll << 38) && d.mem_stride < (1ll << 38) && d.mem_head < (1ll << 38);
+}
+
 // Many rows (token, head-in-group) of a request go to tcgen05.  Its softmax takes the largest product for the
-// largest score, so the scale has to be positive; and a pitch has to fit a tensor map.
+// largest score, so the scale has to be positive.
 bool cross_on_tcgen05(const wt_cross_desc &d) {
-  return (int64_t)d.max_new * (d.heads / d.kv_heads) > 32 && d.max_mem > 0 && d.scale > 0.0f && d.q_stride < (1ll << 38) &&
-         d.mem_stride < (1ll << 38) && d.mem_head < (1ll << 38);
+  return (int64_t)d.max_new * (d.heads / d.kv_heads) > 32 && d.scale > 0.0f && cross_maps(d);
 }
 
 int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
@@ -535,31 +539,44 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
   d.max_mem = (int32_t)std::min<int64_t>(d.max_mem, d.n_mem);
   P.G = d.heads / d.kv_heads;
   P.status = ctx.status;
-  wt::CrossMaps maps;
+  wt::CrossMaps maps = {};
   const bool wide = cross_on_tcgen05(d);
+  const uint64_t D = d.head_dim;
   if (wide) {
     P.tile_tokens = 128 / P.G;
     P.half = P.tile_tokens * P.G;
     P.rows = 2 * P.half;
     P.keys = 128;
-    const uint64_t D = d.head_dim;
+    P.together = 1;
     const uint64_t qd[3] = {D, (uint64_t)d.heads, (uint64_t)d.n_tokens}, qs[2] = {2 * D, 2 * (uint64_t)d.q_stride};
     const uint32_t qb[3] = {64, (uint32_t)P.G, (uint32_t)P.tile_tokens};
-    const uint64_t kd[3] = {D, (uint64_t)d.kv_heads, (uint64_t)d.n_mem}, ks[2] = {2 * (uint64_t)d.mem_head, 2 * (uint64_t)d.mem_stride};
-    const uint32_t kb[3] = {64, 1, 128};
     CHECK(wt::serve_tensor_map(maps.q, d.q, 3, qd, qs, qb));
+  } else {
+    // A warp to a head, for as many as the heads fill, so that those who read one line after another do it
+    // together; but all to one head where that would leave a warp few tiles.
+    const int keys = wt::cross_few_keys(d.head_dim);
+    const double tiles = (double)d.n_req * d.kv_heads * (double)ceil_div(d.max_mem, keys);
+    P.together = tiles < 16.0 * wt::kCrossFewResident * wt::num_sms() ? 1 : d.kv_heads % 4 == 0 ? 4 : d.kv_heads % 2 == 0 ? 2 : 1;
+    P.keys = keys * 4 / P.together;
+    const int64_t most = (int64_t)d.max_new * P.G;
+    P.rows = most <= 8 ? 8 : most <= 16 ? 16 : 32;
+    P.box = !d.keep && cross_maps(d);
+  }
+  if (wide || P.box) {
+    const uint64_t kd[3] = {D, (uint64_t)d.kv_heads, (uint64_t)d.n_mem}, ks[2] = {2 * (uint64_t)d.mem_head, 2 * (uint64_t)d.mem_stride};
+    const uint32_t kb[3] = {64, 1, (uint32_t)(wide ? 128 : wt::cross_few_keys(d.head_dim))};
     CHECK(wt::serve_tensor_map(maps.k, d.k, 3, kd, ks, kb));
     CHECK(wt::serve_tensor_map(maps.v, d.v, 3, kd, ks, kb));
-  } else {
-    P.keys = 64;
-    P.rows = (int64_t)d.max_new * P.G <= 16 ? 16 : 32;
   }
+  P.groups = d.kv_heads / P.together;
+  // A memory of n cells joins n / least parts, at about a sixth of a cell's time each.
+  P.least = 1 + (int)std::sqrt((double)ceil_div(d.max_mem, P.keys) / 6.0);
   // No more CTAs than run at once, or than there can be cells.  (Requests' row tiles: whole ones of all tokens,
   // and one more each.)
   const double tiles = std::min((double)d.n_req * (double)ceil_div((int64_t)d.max_new * P.G, P.rows),
                                 (double)d.n_tokens * P.G / P.rows + d.n_req);
-  const double cells = tiles * d.kv_heads * (double)std::max<int64_t>(1, ceil_div(d.max_mem, P.keys));
-  const int resident = wide ? 1 : wt::cross_few_resident(P.rows, d.head_dim);
+  const double cells = tiles * P.groups * (double)std::max<int64_t>(1, ceil_div(d.max_mem, P.keys));
+  const int resident = wide ? 1 : wt::kCrossFewResident;
   P.ctas = (int)std::max(1.0, std::min((double)resident * wt::num_sms(), cells));
   auto take = [](size_t &at, size_t n) {
     const size_t o = at;
@@ -567,7 +584,7 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
     return o;
   };
   size_t bytes = 0;
-  const size_t slots = 2 * (size_t)P.ctas * P.rows;
+  const size_t slots = 2 * (size_t)P.ctas * P.together * P.rows;
   const size_t o = take(bytes, slots * d.head_dim * 4), ml = take(bytes, slots * sizeof(float2)),
                first = take(bytes, ((size_t)d.n_req + 2) * sizeof(long long));
   Lock lock(h);
@@ -578,7 +595,7 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
   P.ml = reinterpret_cast<float2 *>(ws + ml);
   P.first = reinterpret_cast<long long *>(ws + first);
   const bool joined = d.max_mem > P.keys;  // memories of one cell: no row tile has two parts
-  cudaError_t e = wide ? wt::launch_cross_wide(P, maps, s) : wt::launch_cross_few(P, s);
+  cudaError_t e = wide ? wt::launch_cross_wide(P, maps, s) : wt::launch_cross_few(P, maps, s);
   if (e == cudaSuccess && joined) e = wt::launch_cross_merge(P, s);
   const int rc = wt::serve_done(h, s, w);
   CU(e);

@@ -41,6 +41,11 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a) {
   return r;
 }
 
+// a / b for numbers from 0 on; most are small
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
+
 // 2^x, off by at most 2^-22 of it (the bound PTX gives); a result below 2^-126 is 0.
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;

@@ -171,35 +171,39 @@ cudaError_t launch_attend_warp(const AttendPlan &P, cudaStream_t s);
 cudaError_t launch_attend_merge(const AttendPlan &P, cudaStream_t s);
 
 // ---------------------------------------------------------------- wt_cross.cu
-// The work of a call is cut into cells: `keys` states of one request's memory for one kv head and one tile of
-// up to `rows` (token, head-in-group) rows, in the order request, kv head, row tile, states.  A row tile of no
-// more than `half` rows takes as long for 2 keys as others for keys, and a cell of it has as many.  CTA c takes
-// the cells from c * per on, per of them.  A row tile whose cells one CTA takes whole is written as it is; else
-// each CTA leaves its part of O (fp32, not divided), m and l in a slot: 2c where the CTA's cells start in the row
-// tile or with it, 2c + 1 where the row tile starts behind them.
+// The work of a call is cut into cells: `keys` states of one request's memory for one group of `together` kv heads
+// and one tile of up to `rows` (token, head-in-group) rows a head, in the order request, group, row tile, states.
+// A row tile of no more than `half` rows takes as long for 2 keys as others for keys, and a cell of it has as many.
+// CTA c takes the cells from c * per on, per of them,
+// `least` or more.  A row tile whose cells one CTA takes whole is written as it
+// is; else each CTA leaves its part of O (fp32, not divided), m and l in a slot: 2c where the CTA's cells start in
+// the row tile or with it, 2c + 1 where the row tile starts behind them.
 struct CrossPlan {
   wt_cross_desc d;
   int G;           // heads / kv_heads
   int rows, half, keys;
+  int together, groups;
+  int least;
+  bool box;         // few rows: tiles of states come as TMA boxes
   int tile_tokens;  // many rows: whole tokens of a tile of up to 128 rows
   int ctas;
-  float *o;        // [2 ctas][rows][head_dim]
-  float2 *ml;      // [2 ctas][rows]
-  long long *first;  // [n_req + 1]: a request's first cell; then per
+  float *o;        // [2 ctas][together][rows][head_dim]
+  float2 *ml;      // [2 ctas][together][rows]
+  long long *first;  // [n_req]: a request's first cell; then per, and all cells
   int *status;
 };
-cudaError_t cross_prepare();
-cudaError_t launch_cross_few(const CrossPlan &P, cudaStream_t s);
-cudaError_t launch_cross_merge(const CrossPlan &P, cudaStream_t s);
-// Many rows, on tcgen05 (wt_crosswide.cu)
 struct CrossMaps {
-  alignas(64) uint8_t q[128];  // CUtensorMaps
+  alignas(64) uint8_t q[128];  // CUtensorMaps; boxes of a tile's states
   alignas(64) uint8_t k[128];
   alignas(64) uint8_t v[128];
 };
+cudaError_t cross_prepare();
+int cross_few_keys(int head_dim);  // states of a warp's tile; a cell has a tile for each of its 4 warps
+constexpr int kCrossFewResident = 2;  // CTAs of the kernel for few rows to an SM
+cudaError_t launch_cross_few(const CrossPlan &P, const CrossMaps &m, cudaStream_t s);
+cudaError_t launch_cross_merge(const CrossPlan &P, cudaStream_t s);
+// Many rows, on tcgen05 (wt_crosswide.cu)
 cudaError_t cross_wide_prepare();
 cudaError_t launch_cross_wide(const CrossPlan &P, const CrossMaps &m, cudaStream_t s);
-// CTAs of the kernel for few rows that run at once on an SM
-int cross_few_resident(int rows, int head_dim);
 
 }  // namespace wt
