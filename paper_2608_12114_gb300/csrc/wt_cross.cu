@@ -4,8 +4,8 @@
 // A CTA takes an equal share of all requests' cells (CrossPlan), so unequal memories keep no SM waiting.  Each of
 // its 4 warps streams its own tiles of 32 states (16 of more than 64 elements: 8 KB either way) through a ring of
 // its own in shared memory, on from one row tile into the next: a head of a group of four, or of two, or every
-// fourth of one head's.  (48 requests of 20 heads of 64, whose 128 bytes of a state lie side by side: XX us, and YY
-// with a head at a time.)  Rows, (token, head-in-group) pairs, are columns of
+// fourth of one head's.  (48 requests' tokens, 20 heads of 64, whose 128 bytes of a state lie side by side: 50.5 us, and
+// 65.1 with all warps at one head.)  Rows, (token, head-in-group) pairs, are columns of
 // the m16n8k16 MMAs, 8 to a block, so that a single token's product is not 16 rows of which one counts:
 //
 //   S^T = K Q^T,   P^T = 2^(S^T - m),   O^T += V^T P^T,   l += column sums of P^T
@@ -14,9 +14,9 @@
 // Parts join as softmax splits: O = sum_i 2^(m_i - m) O_i, l alike, out = O / l.  The maximum passes over NaN
 // scores, so a part whose sum is NaN says so in its m.
 //
-// Tiles come as TMA boxes: what a tile of a memory's end holds behind it is masked in S and cleared in V.  With a
-// mask (or pitches past a tensor map's) they come by 16-byte cp.async instead, which leaves out the states that are
-// not kept and fills their place with zeros.
+// Tiles come as TMA boxes.  States that are not kept, and what a memory's last tile holds behind it, are masked in S
+// and cleared in V.  (13 requests' beams of 32 heads of 80, three in ten states left out: leaving those out of the
+// copies, row by row with cp.async, 31.3 us, as boxes 29.3.)
 #include <algorithm>
 
 #include "wt_cross.cuh"
@@ -46,39 +46,23 @@ __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
 }
 
 // A warp's tiles in order: of every cell of the CTA's share, its own, where the memory reaches it.
-struct Tiles {
-  const CrossPlan &P;
-  const Share &s;
-  long long cell, first;
-  int b, i, at, by;  // key of a cell's first tile of this warp; of a cell
-  Asker a;
-  Segment g;
-  __device__ Tiles(const CrossPlan &p, const Share &share, int at_key)
-      : P(p), s(share), cell(share.lo), first(share.first), b(share.b), i(0), at(at_key), by(p.keys) {
-    g.tiles = 0;
-    if (cell < s.hi) a = asker_of(P, b, false);
-  }
+struct Tiles : Walk {
+  int i, first_key, by;  // key of a cell's first tile of this warp; from cell to cell
+  __device__ Tiles(const CrossPlan &p, const Share &share, int key) : Walk(p, share), i(0), first_key(key), by(p.keys) {}
   __device__ bool segment() {  // the next row tile
-    if (cell >= s.hi) return false;
-    while (cell >= first + a.cells(P)) {
-      first += a.cells(P);
-      a = asker_of(P, ++b, false);
-    }
-    g = segment_at(P, a, first, cell, s);
-    cell += g.cells;
     i = 0;
-    return true;
+    return next();
   }
   // state of the next tile of the row tile; false: none left
   __device__ bool tile(int &key0) {
     if (i >= g.tiles) return false;
-    key0 = (g.tile0 + i++) * by + at;
+    key0 = (g.tile0 + i++) * by + first_key;
     return key0 < a.len;
   }
 };
 
-// DH: 64-element halves of head_dim; NQ: blocks of 8 rows.  BOX: tiles as TMA boxes.
-template <int DT, int DH, int NQ, bool BOX>
+// DH: 64-element halves of head_dim; NQ: blocks of 8 rows.
+template <int DT, int DH, int NQ, bool KEEP>
 __global__ void __launch_bounds__(kThreads, 2)
     cross_few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CrossPlan P) {
   constexpr int kT = kKeys<DH>, NK = kT / 16, ND = DH * 4, kRows = 8 * NQ;
@@ -102,7 +86,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     for (int i = 0; i < kStages; ++i) mbar_init(bar0 + 8 * i, 1);
     mbar_fence_init();
   }
-  if (BOX && tid == 0) {
+  if (tid == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&kmap) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&vmap) : "memory");
   }
@@ -123,47 +107,26 @@ __global__ void __launch_bounds__(kThreads, 2)
         some = false;
         return;
       }
-    if (!BOX)
-      mine = lane < kT && next_key + lane < ahead.a.len && (!d.keep || __ldg(d.keep + (int64_t)ahead.a.mem + next_key + lane));
+    if (KEEP) mine = lane < kT && next_key + lane < ahead.a.len && __ldg(d.keep + (int64_t)ahead.a.mem + next_key + lane);
   };
   auto issue = [&]() {
-    if (!some) {
-      if (!BOX) cp_commit();
-      return;
-    }
+    if (!some) return;
     const uint32_t s = issued++ % kStages, dst = ring + s * kTileBytes;
     const int state = ahead.a.mem + next_key, head = ahead.g.group * P.together + wh;
-    if constexpr (BOX) {
-      if (lane == 0) {
-        mbar_expect_tx(bar0 + 8 * s, kTileBytes);
+    if (lane == 0) {
+      mbar_expect_tx(bar0 + 8 * s, kTileBytes);
 #pragma unroll
-        for (int hf = 0; hf < DH; ++hf) {
-          tma_3d(dst + hf * kHalfTile, &kmap, hf * 64, head, state, bar0 + 8 * s);
-          tma_3d(dst + kV + hf * kHalfTile, &vmap, hf * 64, head, state, bar0 + 8 * s);
-        }
+      for (int hf = 0; hf < DH; ++hf) {
+        tma_3d(dst + hf * kHalfTile, &kmap, hf * 64, head, state, bar0 + 8 * s);
+        tma_3d(dst + kV + hf * kHalfTile, &vmap, hf * 64, head, state, bar0 + 8 * s);
       }
-    } else {
-      const uint32_t kept = __ballot_sync(0xffffffffu, mine);
-      if (lane == 0) kept_of[s] = kept;
-      const int pieces = 2 * ksteps;  // of 16 bytes a row; one past head_dim is zeros
-      const int64_t off = 2 * (state * d.mem_stride + head * d.mem_head);
-      const uint8_t *k_of = static_cast<const uint8_t *>(d.k) + off, *v_of = static_cast<const uint8_t *>(d.v) + off;
-      int row = lane / pieces, in = lane - row * pieces;
-      const int row_step = 32 / pieces, in_step = 32 - row_step * pieces;
-#pragma unroll 4
-      for (int c = 0; c < kT * pieces / 32; ++c) {
-        const bool ok = (kept >> row & 1) && in * 8 < D;
-        const int64_t at = 2 * row * d.mem_stride + in * 16;
-        const uint32_t to = dst + (in >> 3) * kHalfTile + row * 128 + ((in ^ row) & 7) * 16;
-        cp16(to, ok ? k_of + at : static_cast<const uint8_t *>(d.q), ok);
-        cp16(to + kV, ok ? v_of + at : static_cast<const uint8_t *>(d.q), ok);
-        row += row_step;
-        in += in_step;
-        if (in >= pieces) in -= pieces, ++row;
-      }
-      cp_commit();
     }
-    look();
+    const bool kept = mine;
+    look();  // what keep says of the next tile is on its way before that of this one is needed
+    if (KEEP) {
+      const uint32_t bits = __ballot_sync(0xffffffffu, kept);
+      if (lane == 0) kept_of[s] = bits;
+    }
   };
   look();
 #pragma unroll 1
@@ -172,7 +135,8 @@ __global__ void __launch_bounds__(kThreads, 2)
   // where this lane's rows of 8 x 8 blocks lie: K as it is, V turned
   const uint32_t k_lane = ((lane & 15) * 128) | (((lane >> 4) ^ lane) & 7) * 16;
   const uint32_t v_lane = (((lane & 7) + (lane >> 4) * 8) * 128) | (((lane >> 3 & 1) ^ lane) & 7) * 16;
-  for (Tiles now(P, share, wk * kT); now.segment();) {
+  Tiles now(P, share, wk * kT);
+  while (now.segment()) {
     const Asker &a = now.a;
     const Segment &sg = now.g;
     const int rows = a.n * G, row0 = sg.row_tile * kRows, hk = sg.group * P.together + wh;
@@ -207,26 +171,21 @@ __global__ void __launch_bounds__(kThreads, 2)
 
     for (int key0; now.tile(key0);) {
       const uint32_t stage = used % kStages, kt = ring + stage * kTileBytes, vt = kt + kV;
-      uint32_t found;
-      if constexpr (BOX) {
-        if (!warp_wait(bar0 + 8 * stage, used / kStages & 1, abort_flag, P.status)) {  // nothing of it is used
-          ++used;
-          continue;
-        }
-        const int n = a.len - key0;
-        found = n >= kT ? (kT == 32 ? 0xffffffffu : (1u << kT) - 1) : (1u << n) - 1;
-        if (n < kT) {  // what V holds behind the memory: a weight of 0 does not hide what is not finite
-          for (int i = n * 8 + lane; i < kT * 8; i += 32)
+      constexpr uint32_t kAll = kT == 32 ? 0xffffffffu : (1u << kT) - 1;
+      if (!warp_wait(bar0 + 8 * stage, used / kStages & 1, abort_flag, P.status)) {  // nothing of it is used
+        ++used;
+        continue;
+      }
+      const int n = a.len - key0;
+      const uint32_t found = KEEP ? kept_of[stage] : n >= kT ? kAll : (1u << n) - 1;
+      if (found != kAll) {  // a weight of 0 does not hide what is not finite in V
+        for (int i = lane; i < kT * 8; i += 32)
+          if (!(found >> (i >> 3) & 1))
 #pragma unroll
             for (int hf = 0; hf < DH; ++hf)
               asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vt + hf * kHalfTile + i * 16), "r"(0) : "memory");
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-        }
-      } else {
-        cp_wait<kStages - 2>();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        found = kept_of[stage];
       }
       ++used;
       issue();  // into the stage before this one: every lane has read it
@@ -249,7 +208,7 @@ __global__ void __launch_bounds__(kThreads, 2)
           for (int n = 0; n < NQ; ++n) mma16816<DT>(s[n][j], kf[0], kf[1], kf[2], kf[3], qb[n][k][0], qb[n][k][1]);
         }
       }
-      const bool all = found == (kT == 32 ? 0xffffffffu : (1u << kT) - 1);
+      const bool all = found == kAll;
       uint32_t pf[NQ][NK][2];
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
@@ -367,9 +326,8 @@ __global__ void __launch_bounds__(kThreads, 2)
       together();
     }
   }
-  if (!BOX) {
-    cp_wait<0>();
-  } else if (*abort_flag && lane == 0) {  // a copy may still be landing
+  if (tid == 0) note_cut(P, share, now);
+  if (*abort_flag && lane == 0) {  // a copy may still be landing
     for (uint32_t i = issued > (uint32_t)kStages ? issued - kStages : 0; i < issued; ++i) {
       const long long t0 = clock64();
       while (!mbar_try_wait(bar0 + 8 * (i % kStages), i / kStages & 1) && clock64() - t0 < kWaitCycles) {
@@ -378,42 +336,20 @@ __global__ void __launch_bounds__(kThreads, 2)
   }
 }
 
-// How many of v[0 .. n), which ascend, are at most x.  The whole warp looks at 32 entries at once.
-__device__ __forceinline__ int count_upto(const long long *v, int n, long long x, int lane) {
-  int lo = 0, hi = n;
-  while (lo < hi) {
-    const int step = (hi - lo + 31) / 32, i = lo + (lane + 1) * step - 1;
-    const unsigned past = ~__ballot_sync(0xffffffffu, i < hi && v[min(i, n - 1)] <= x);
-    const int c = past ? __ffs(past) - 1 : 32;
-    lo += c * step;
-    hi = min(hi, lo + step - 1);
-  }
-  return min(lo, n);
-}
-
-// The parts of row tiles that several CTAs took: blocks (x, y) look at the border between CTA x's cells and the next,
-// and, where it is the first within a row tile, join the tile's rows, L lanes to a row.  The references, sums and O of
-// 8 parts are asked for at once.
+// The parts of row tiles that several CTAs took: blocks (x, y) join what starts in CTA x's cells, L lanes to a row.
+// The references, sums and O of 8 parts are asked for at once.
 constexpr int kMergeParts = 8;
 template <int DT, int L>
 __global__ void __launch_bounds__(kThreads) cross_merge_kernel(const __grid_constant__ CrossPlan P) {
   const wt_cross_desc &d = P.d;
-  const int lane = threadIdx.x & 31;
-  griddep_wait();  // launched while the kernel before it ends
-  const long long per = P.first[d.n_req], all = P.first[d.n_req + 1], border = per * (blockIdx.x + 1);
-  if (border >= all) return;
-  const int b = count_upto(P.first, d.n_req, border - 1, lane) - 1;
-  const Asker a = asker_of(P, b, false);
-  Share s;
-  s.lo = border - 1, s.hi = all;
-  const long long first = P.first[b];
-  const Segment g = segment_at(P, a, first, border - 1, s);  // from the cell before the border to the row tile's end
-  const long long u0 = first + g.group * a.head_cells() + (long long)g.row_tile * a.key_tiles, u1 = border - 1 + g.cells;
-  if (u1 <= border || u0 < per * blockIdx.x) return;
   const int D = d.head_dim, i = blockIdx.y * (kThreads / L) + threadIdx.x / L, wh = i / P.rows, r = i - wh * P.rows;
-  const int row = g.row_tile * P.rows + r, col = threadIdx.x % L * 4;
-  if (wh >= P.together || row >= a.n * P.G || col >= D) return;
-  const int c0 = blockIdx.x, c1 = (int)quotient(u1 - 1, per);
+  const int col = threadIdx.x % L * 4;
+  if (wh >= P.together || col >= D) return;
+  griddep_wait();  // launched while the kernel before it runs
+  const CrossCut cut = P.cuts[blockIdx.x];
+  const int row = cut.row_tile * P.rows + r;
+  if (cut.parts == 0 || row >= cut.rows) return;
+  const int c0 = blockIdx.x, c1 = c0 + cut.parts - 1;
   float m = -INFINITY, l = 0.0f;
   float4 o = make_float4(0, 0, 0, 0);
   for (int c = c0; c <= c1; c += kMergeParts) {
@@ -421,7 +357,7 @@ __global__ void __launch_bounds__(kThreads) cross_merge_kernel(const __grid_cons
     float4 x[kMergeParts];
 #pragma unroll
     for (int k = 0; k < kMergeParts; ++k) {
-      const long long at = ((2ll * (c + k) + (c + k == c0 && per * c0 < u0)) * P.together + wh) * P.rows + r;
+      const long long at = ((2ll * (c + k) + (c + k == c0 && cut.second)) * P.together + wh) * P.rows + r;
       ml[k] = c + k <= c1 ? P.ml[at] : make_float2(-INFINITY, 0.0f);
       x[k] = c + k <= c1 ? *reinterpret_cast<const float4 *>(P.o + at * D + col) : make_float4(0, 0, 0, 0);
     }
@@ -440,15 +376,15 @@ __global__ void __launch_bounds__(kThreads) cross_merge_kernel(const __grid_cons
     }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const int hk = g.group * P.together + wh;
-  *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(d.out) + (int64_t)(a.t0 + row / P.G) * d.out_stride + (hk * P.G + row % P.G) * D + col) =
+  const int hk = cut.group * P.together + wh;
+  *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(d.out) + (int64_t)(cut.t0 + row / P.G) * d.out_stride + (hk * P.G + row % P.G) * D + col) =
       make_uint2(pack2<DT>(o.x * inv, o.y * inv), pack2<DT>(o.z * inv, o.w * inv));
 }
 
 template <int DT, int DH, int NQ>
 cudaError_t run_few(const CrossPlan &P, const CrossMaps &m, cudaStream_t s) {
   const CUtensorMap &k = *reinterpret_cast<const CUtensorMap *>(m.k), &v = *reinterpret_cast<const CUtensorMap *>(m.v);
-  if (P.box) cross_few_kernel<DT, DH, NQ, true><<<P.ctas, kThreads, few_smem<DH>(), s>>>(k, v, P);
+  if (P.d.keep) cross_few_kernel<DT, DH, NQ, true><<<P.ctas, kThreads, few_smem<DH>(), s>>>(k, v, P);
   else cross_few_kernel<DT, DH, NQ, false><<<P.ctas, kThreads, few_smem<DH>(), s>>>(k, v, P);
   return cudaGetLastError();
 }

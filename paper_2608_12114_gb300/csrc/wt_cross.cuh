@@ -35,14 +35,14 @@ __device__ __forceinline__ Asker asker_of(const CrossPlan &P, int b, bool tell) 
   return {t0, n, mem, len, row_tiles, key_tiles, half ? (key_tiles + 1) / 2 : key_tiles};
 }
 
-// This CTA's cells, and the request that the first of them lies in.
+// This CTA's cells, and the place of the first of them: request, group of kv heads, row tile, cell of that.
 struct Share {
   long long lo, hi;  // cells of all requests in a row
-  long long first;   // of request b
-  int b;
+  int b, group, row_tile, at;
 };
 
-// By the whole block, N threads.  Each thread adds up the cells of a run of requests; the runs' sums are scanned.
+// By the whole block, N threads.  Each thread adds up the cells of a run of requests; the runs' sums are scanned, and
+// the thread whose run has the CTA's first cell finds its place.
 template <int N>
 __device__ __forceinline__ Share share_of(const CrossPlan &P) {
   constexpr int kWarps = N / 32;
@@ -51,8 +51,12 @@ __device__ __forceinline__ Share share_of(const CrossPlan &P) {
   const wt_cross_desc &d = P.d;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int run = (d.n_req + N - 1) / N, b0 = min(tid * run, d.n_req), b1 = min(b0 + run, d.n_req);
+  Asker a = {};
   long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += asker_of(P, b, blockIdx.x == 0).cells(P);
+  for (int b = b0; b < b1; ++b) {
+    a = asker_of(P, b, blockIdx.x == 0);
+    mine += a.cells(P);
+  }
   long long upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -60,7 +64,7 @@ __device__ __forceinline__ Share share_of(const CrossPlan &P) {
     if (lane >= o) upto += v;
   }
   if (lane == 31) sums[warp] = upto;
-  if (tid == 0) found = {0, 0, 0, d.n_req};
+  if (tid == 0) found = {};
   __syncthreads();
   long long all = 0;
 #pragma unroll
@@ -70,44 +74,87 @@ __device__ __forceinline__ Share share_of(const CrossPlan &P) {
   }
   const long long per = max((long long)P.least, quotient(all + gridDim.x - 1, gridDim.x)), lo = per * blockIdx.x, hi = min(all, lo + per);
   long long first = upto - mine;
-  const bool here = lo < hi && first <= lo && lo < upto;
-  if (here || blockIdx.x == 0)
-    for (int b = b0; b < b1; ++b) {
-      const long long n = asker_of(P, b, false).cells(P);
-      if (blockIdx.x == 0) P.first[b] = first;
-      if (here && first <= lo && lo < first + n) found = {lo, hi, first, b};
-      first += n;
-    }
-  if (blockIdx.x == 0 && tid == 0) P.first[d.n_req] = per, P.first[d.n_req + 1] = all;
+  if (lo < hi && first <= lo && lo < upto) {
+    int b = b0;
+    if (run > 1)
+      for (;; ++b) {
+        a = asker_of(P, b, false);
+        const long long n = a.cells(P);
+        if (lo < first + n) break;
+        first += n;
+      }
+    const int group = (int)quotient(lo - first, a.head_cells());
+    const long long at = lo - first - group * a.head_cells();
+    const int row_tile = (int)min(quotient(at, a.key_tiles), a.row_tiles - 1ll);
+    found = {lo, hi, b, group, row_tile, (int)(at - (long long)row_tile * a.key_tiles)};
+  }
   __syncthreads();
   return found;
 }
 
-// One row tile's states that this CTA takes.
+// One row tile's states that a CTA takes.
 struct Segment {
   int group, row_tile;  // of kv heads, of rows
-  int tile0, tiles;   // tiles of P.keys states
-  int cells;          // as many, or half of them (P.half)
-  bool half, whole;   // whole: all of the row tile's
-  long long slot;     // where the part goes else
+  int tile0, tiles;     // tiles of P.keys states
+  bool half, whole;     // half: P.half; whole: all of the row tile's
+  bool cut;             // it starts in this CTA's cells and goes on behind them
+  int cells;            // of the row tile
+  long long slot;       // where the part goes if it is not whole
 };
 
-// The segment that starts at cell `at` of request a, whose first cell is `first`.
-__device__ __forceinline__ Segment segment_at(const CrossPlan &P, const Asker &a, long long first, long long at, const Share &s) {
+// The segments of a CTA, one after another; whoever needs them walks them by itself.
+struct Walk {
+  const CrossPlan &P;
+  const Share &s;
+  long long cell;  // behind the segment
+  int b, at;       // at: the segment's first cell of its row tile
+  int taken;       // its cells
+  bool started;
+  Asker a;
   Segment g;
-  const long long per_head = a.head_cells();
-  g.group = (int)quotient(at - first, per_head);
-  const long long head = first + g.group * per_head;
-  g.row_tile = (int)min(quotient(at - head, a.key_tiles), a.row_tiles - 1ll);
-  const long long begin = head + (long long)g.row_tile * a.key_tiles;
-  const int all = g.row_tile == a.row_tiles - 1 ? a.last : a.key_tiles;
-  g.half = a.n * P.G - g.row_tile * P.rows <= P.half;
-  g.cells = (int)(min(s.hi, begin + all) - at);
-  g.whole = g.cells == all;
-  g.tile0 = (int)(at - begin) << g.half;
-  g.tiles = min(g.cells << g.half, a.key_tiles - g.tile0);
-  g.slot = 2 * blockIdx.x + (begin >= s.lo && at > s.lo);
-  return g;
+  __device__ Walk(const CrossPlan &p, const Share &share) : P(p), s(share), cell(share.lo), b(share.b), at(share.at), started(false) {
+    g.group = share.group, g.row_tile = share.row_tile, g.tiles = 0, g.cut = false;
+    if (cell < s.hi) a = asker_of(P, b, false);
+  }
+  __device__ __forceinline__ bool next() {
+    if (cell >= s.hi) return false;
+    if (started) {
+      at = 0;
+      if (++g.row_tile == a.row_tiles) {
+        g.row_tile = 0;
+        if (++g.group == P.groups) {
+          g.group = 0;
+          do a = asker_of(P, ++b, false);
+          while (a.n == 0);
+        }
+      }
+    }
+    started = true;
+    g.cells = g.row_tile == a.row_tiles - 1 ? a.last : a.key_tiles;
+    g.half = a.n * P.G - g.row_tile * P.rows <= P.half;
+    const int n = taken = (int)min(s.hi - cell, (long long)(g.cells - at));
+    g.whole = n == g.cells;
+    g.cut = at == 0 && n < g.cells;
+    g.tile0 = at << g.half;
+    g.tiles = min(n << g.half, a.key_tiles - g.tile0);
+    g.slot = 2 * blockIdx.x + (at == 0 && cell > s.lo);
+    cell += n;
+    return true;
+  }
+};
+
+// By one thread of every CTA at its end: the row tile that starts among its cells and goes on behind them, if any,
+// for the merge.
+__device__ __forceinline__ void note_cut(const CrossPlan &P, const Share &s, const Walk &w) {
+  CrossCut c = {};
+  if (w.g.cut) {
+    const long long u0 = s.hi - w.taken;  // it is the last segment
+    c.parts = (int)(quotient(u0 + w.g.cells - 1, s.hi - s.lo) - blockIdx.x + 1);
+    c.second = u0 > s.lo;
+    c.t0 = w.a.t0, c.rows = w.a.n * P.G;
+    c.group = w.g.group, c.row_tile = w.g.row_tile;
+  }
+  P.cuts[blockIdx.x] = c;
 }
 
 }  // namespace

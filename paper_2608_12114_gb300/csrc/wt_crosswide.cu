@@ -58,29 +58,6 @@ struct Geo {
 static_assert(Geo<2>::stage / 4 >= 4096 + 2 * 128 * 8, "rows turned, and join");
 static_assert(Geo<2>::smem + 256 <= 232448, "shared memory of one CTA, and share_of's");
 
-// The segments of a CTA, one after another; every role walks them by itself.
-struct Walk {
-  const CrossPlan &P;
-  const Share &s;
-  long long cell, first;
-  int b;
-  Asker a;
-  Segment g;
-  __device__ Walk(const CrossPlan &p, const Share &share) : P(p), s(share), cell(share.lo), first(share.first), b(share.b) {
-    if (cell < s.hi) a = asker_of(P, b, false);
-  }
-  __device__ bool next() {
-    if (cell >= s.hi) return false;
-    while (cell >= first + a.cells(P)) {
-      first += a.cells(P);
-      a = asker_of(P, ++b, false);
-    }
-    g = segment_at(P, a, first, cell, s);
-    cell += g.cells;
-    return true;
-  }
-};
-
 // Whether V of a key tile has rows to clear.
 template <bool KEEP>
 __device__ __forceinline__ bool to_clear(const Asker &a, int tile) {
@@ -359,7 +336,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t done = 0, done_other = 0;  // tiles of this stream, and of the other, over all segments
     uint32_t seg = 0, met = 0;
     bool live = true;
-    for (Walk w(P, share); live && w.next(); ++seg) {
+    Walk w(P, share);
+    for (; live && w.next(); ++seg) {
       const Segment &g = w.g;
       // The segment's queries have landed, so every thread has released those before (q_empty).
       if (!warp_wait(q_full, seg & 1, abort_flag, status)) break;
@@ -577,6 +555,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       mbar_arrive(q_empty);
     }
+    if (threadIdx.x == 0) note_cut(P, share, w);
   }
   fence_before();
   __syncthreads();

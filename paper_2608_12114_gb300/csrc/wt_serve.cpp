@@ -514,15 +514,10 @@ int check_cross(wt_handle *h, const wt_cross_desc &d) {
   return WT_OK;
 }
 
-// Whether a memory's pitches fit a tensor map.
-bool cross_maps(const wt_cross_desc &d) {
-  return d.max_mem > 0 && d.q_stride < (1ll << 38) && d.mem_stride < (1ll << 38) && d.mem_head < (1ll << 38);
-}
-
 // Many rows (token, head-in-group) of a request go to tcgen05.  Its softmax takes the largest product for the
 // largest score, so the scale has to be positive.
 bool cross_on_tcgen05(const wt_cross_desc &d) {
-  return (int64_t)d.max_new * (d.heads / d.kv_heads) > 32 && d.scale > 0.0f && cross_maps(d);
+  return (int64_t)d.max_new * (d.heads / d.kv_heads) > 32 && d.scale > 0.0f && d.max_mem > 0;
 }
 
 int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
@@ -542,6 +537,10 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
   wt::CrossMaps maps = {};
   const bool wide = cross_on_tcgen05(d);
   const uint64_t D = d.head_dim;
+  // the pitch of a dimension of one says nothing, and one that fits no tensor map can only be such a one
+  if (d.n_tokens == 1) d.q_stride = (int64_t)d.heads * d.head_dim;
+  if (d.n_mem == 1) d.mem_stride = (int64_t)d.kv_heads * d.head_dim;
+  if (d.kv_heads == 1) d.mem_head = d.head_dim;
   if (wide) {
     P.tile_tokens = 128 / P.G;
     P.half = P.tile_tokens * P.G;
@@ -560,9 +559,8 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
     P.keys = keys * 4 / P.together;
     const int64_t most = (int64_t)d.max_new * P.G;
     P.rows = most <= 8 ? 8 : most <= 16 ? 16 : 32;
-    P.box = !d.keep && cross_maps(d);
   }
-  if (wide || P.box) {
+  if (d.max_mem > 0) {
     const uint64_t kd[3] = {D, (uint64_t)d.kv_heads, (uint64_t)d.n_mem}, ks[2] = {2 * (uint64_t)d.mem_head, 2 * (uint64_t)d.mem_stride};
     const uint32_t kb[3] = {64, 1, (uint32_t)(wide ? 128 : wt::cross_few_keys(d.head_dim))};
     CHECK(wt::serve_tensor_map(maps.k, d.k, 3, kd, ks, kb));
@@ -586,14 +584,14 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
   size_t bytes = 0;
   const size_t slots = 2 * (size_t)P.ctas * P.together * P.rows;
   const size_t o = take(bytes, slots * d.head_dim * 4), ml = take(bytes, slots * sizeof(float2)),
-               first = take(bytes, ((size_t)d.n_req + 2) * sizeof(long long));
+               cuts = take(bytes, (size_t)P.ctas * sizeof(wt::CrossCut));
   Lock lock(h);
   wt::ServeWorkspace w;
   CHECK(wt::serve_workspace(h, s, bytes, &w));
   uint8_t *ws = static_cast<uint8_t *>(w.p);
   P.o = reinterpret_cast<float *>(ws + o);
   P.ml = reinterpret_cast<float2 *>(ws + ml);
-  P.first = reinterpret_cast<long long *>(ws + first);
+  P.cuts = reinterpret_cast<wt::CrossCut *>(ws + cuts);
   const bool joined = d.max_mem > P.keys;  // memories of one cell: no row tile has two parts
   cudaError_t e = wide ? wt::launch_cross_wide(P, maps, s) : wt::launch_cross_few(P, maps, s);
   if (e == cudaSuccess && joined) e = wt::launch_cross_merge(P, s);

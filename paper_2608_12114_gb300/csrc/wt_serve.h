@@ -178,18 +178,24 @@ cudaError_t launch_attend_merge(const AttendPlan &P, cudaStream_t s);
 // `least` or more.  A row tile whose cells one CTA takes whole is written as it
 // is; else each CTA leaves its part of O (fp32, not divided), m and l in a slot: 2c where the CTA's cells start in
 // the row tile or with it, 2c + 1 where the row tile starts behind them.
+struct CrossCut {  // a row tile that starts in a CTA's cells and goes on behind them
+  int parts;         // CTAs that have some of it; 0: there is none
+  int second;        // whether its first part is the CTA's second slot
+  int t0, rows;      // first token of the request, its rows a kv head
+  int group, row_tile;
+  int pad[2];
+};
 struct CrossPlan {
   wt_cross_desc d;
   int G;           // heads / kv_heads
   int rows, half, keys;
   int together, groups;
   int least;
-  bool box;         // few rows: tiles of states come as TMA boxes
   int tile_tokens;  // many rows: whole tokens of a tile of up to 128 rows
   int ctas;
   float *o;        // [2 ctas][together][rows][head_dim]
   float2 *ml;      // [2 ctas][together][rows]
-  long long *first;  // [n_req]: a request's first cell; then per, and all cells
+  CrossCut *cuts;  // [ctas]
   int *status;
 };
 struct CrossMaps {
