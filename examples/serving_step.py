@@ -5,9 +5,11 @@ values are in hand, have a paged cache of their own, an adapter each (or none), 
 tokens.  The step then
 
   projects     every token with wt_pass (up to 16 activation columns), wt_adapt beside it;
+  places       the queries, and the new keys and values in their requests' pages (wt_place);
   attends      to the shared prompt and each request's own keys (wt_attend);
-  answers      with the head's logits, their probabilities at each request's temperature (wt_probs)
-               and the tokens that stay (wt_verify).
+  answers      with the head's logits, their probabilities at each request's temperature (wt_probs),
+               the tokens that stay (wt_verify), and the log probability of every token that was given
+               or drafted, with the likeliest others (wt_logprobs).
 
     python examples/serving_step.py
 """
@@ -69,12 +71,11 @@ def step(m: Decoder, tokens, begin, slot, adapters, prefix, cache, table, lens, 
     yq, yk, yv = m.project(["layers.0.q", "layers.0.k", "layers.0.v"], xn)
     m.h.adapt([serving.adapters(xn, y, slot, *adapters[n]) for n, y in (("q", yq), ("v", yv))], m.stream)
     # the new tokens' keys and values go to their pages
-    own = torch.cat([torch.arange(n - c, n) for n, c in zip(lens.tolist(), counts)]).cuda()
     of = torch.repeat_interleave(torch.arange(B), torch.tensor(counts)).cuda()
-    page = table[of, own // PAGE].long()
-    for y, c in ((yk, cache[0]), (yv, cache[1])):
-        c[page, own % PAGE] = y.to(torch.bfloat16).view(T, HEADS, DIM)
-    qs = yq.to(torch.bfloat16).view(T, HEADS, DIM)
+    qs = torch.empty(T, HEADS, DIM, dtype=torch.bfloat16, device="cuda")
+    heads = [y.view(T, HEADS, DIM) for y in (yq, yk, yv)]
+    m.h.place(serving.placement(begin, cache[0], cache[1], table, lens, q=heads[0], q_out=qs, k=heads[1], v=heads[2],
+                                max_len=int(lens.max())), m.stream)
     att = torch.empty_like(qs)
     m.h.attend(serving.attention(qs, att, begin, cache[0], cache[1], table, lens, max_new=max(counts),
                                  max_len=int(lens.max()), prefix_k=prefix[0], prefix_v=prefix[1]), m.stream)
@@ -93,8 +94,13 @@ def step(m: Decoder, tokens, begin, slot, adapters, prefix, cache, table, lens, 
     accepted = torch.empty(B, dtype=torch.int32, device="cuda")
     out = torch.empty(B, max(counts), dtype=torch.int32, device="cuda")
     m.h.verify(serving.verification(p, drafted, dbegin, u, u_draw, accepted, out, q=q), m.stream)
+    # what the target gives each token's successor: a draft's, or none
+    given = torch.cat([torch.cat([tokens[int(b) + 1:int(b) + c], tokens.new_full((1,), -1)]) for b, c in zip(begin[:-1], counts)])
+    lp, top, top_lp = torch.empty(T, 1, device="cuda"), torch.empty(T, 5, dtype=torch.int32, device="cuda"), torch.empty(T, 5, device="cuda")
+    m.h.logprobs(serving.log_probabilities(logits, given=given.view(T, 1), given_lp=lp, top=top, top_lp=top_lp,
+                                           temperature=temperature[of]), m.stream)
     return dict(xn=xn, yq=yq, yv=yv, q=qs, att=att, yo=yo, logits=logits, p=p, drafted=drafted, dbegin=dbegin,
-                accepted=accepted, tokens=out)
+                accepted=accepted, tokens=out, given=given, lp=lp, top=top, top_lp=top_lp)
 
 
 def inputs(vocab: int, d: int, seed: int = 0, counts=(4, 1, 6), prompt: int = 700, own=(20, 55, 9), slots: int = 3, rank: int = 16):

@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     for (int i = 0; i < kStages; ++i) mbar_init(bar0 + 8 * i, 1);
     mbar_fence_init();
   }
-  if (tid == 0) {
+  if (tid == 0 && d.max_mem > 0) {  // else there are no maps
     asm volatile("prefetch.tensormap [%0];" ::"l"(&kmap) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&vmap) : "memory");
   }
