@@ -109,8 +109,8 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
     if (KEEP) mine = lane < kT && next_key + lane < ahead.a.len && __ldg(d.keep + (int64_t)ahead.a.mem + next_key + lane);
   };
-  auto issue = [&]() {
-    if (!some) return;
+  auto issue = [&]() -> bool {
+    if (!some) return false;
     const uint32_t s = issued++ % kStages, dst = ring + s * kTileBytes;
     const int state = ahead.a.mem + next_key, head = ahead.g.group * P.together + wh;
     if (lane == 0) {
@@ -122,15 +122,23 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
     }
     const bool kept = mine;
-    look();  // what keep says of the next tile is on its way before that of this one is needed
+    look();
+    return kept;
+  };
+  // What keep says of a tile is asked for before the tile before it is, and noted after that tile's products.
+  auto note = [&](uint32_t tile, bool kept) {
     if (KEEP) {
       const uint32_t bits = __ballot_sync(0xffffffffu, kept);
-      if (lane == 0) kept_of[s] = bits;
+      if (lane == 0) kept_of[tile % kStages] = bits;
     }
   };
   look();
-#pragma unroll 1
-  for (int i = 0; i < kStages - 1; ++i) issue();
+  bool kept[kStages - 1];
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) kept[i] = issue();
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) note(i, kept[i]);
+  __syncwarp();
 
   // where this lane's rows of 8 x 8 blocks lie: K as it is, V turned
   const uint32_t k_lane = ((lane & 15) * 128) | (((lane >> 4) ^ lane) & 7) * 16;
@@ -187,8 +195,9 @@ __global__ void __launch_bounds__(kThreads, 2)
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
       }
+      const uint32_t asked = issued;
       ++used;
-      issue();  // into the stage before this one: every lane has read it
+      const bool asked_kept = issue();  // into the stage before this one: every lane has read it
 
       float s[NQ][NK][4];
 #pragma unroll
@@ -268,6 +277,7 @@ __global__ void __launch_bounds__(kThreads, 2)
           for (int n = 0; n < NQ; ++n) mma16816<DT>(o[n][t], vf[0], vf[1], vf[2], vf[3], pf[n][j][0], pf[n][j][1]);
         }
       }
+      if (issued != asked) note(asked, asked_kept);
       __syncwarp();
     }
 
