@@ -18,6 +18,7 @@
 // and cleared in V.  (13 requests' beams of 32 heads of 80, three in ten states left out: leaving those out of the
 // copies, row by row with cp.async, 31.3 us, as boxes 29.3.)
 #include <algorithm>
+#include <type_traits>
 
 #include "wt_cross.cuh"
 #include "wt_tmem.cuh"
@@ -347,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, 2)
 }
 
 // The parts of row tiles that several CTAs took: blocks (x, y) join what starts in CTA x's cells, L lanes to a row.
-// The references, sums and O of 8 parts are asked for at once.
+// The references, sums and O of 8 parts are asked for at once; of two, which many rows have, by themselves.
 constexpr int kMergeParts = 8;
 template <int DT, int L>
 __global__ void __launch_bounds__(kThreads) cross_merge_kernel(const __grid_constant__ CrossPlan P) {
@@ -362,28 +363,34 @@ __global__ void __launch_bounds__(kThreads) cross_merge_kernel(const __grid_cons
   const int c0 = blockIdx.x, c1 = c0 + cut.parts - 1;
   float m = -INFINITY, l = 0.0f;
   float4 o = make_float4(0, 0, 0, 0);
-  for (int c = c0; c <= c1; c += kMergeParts) {
-    float2 ml[kMergeParts];
-    float4 x[kMergeParts];
+  auto join = [&](auto most, int c) {  // parts c .. c + most - 1, those up to c1
+    constexpr int n = decltype(most)::value;
+    float2 ml[n];
+    float4 x[n];
 #pragma unroll
-    for (int k = 0; k < kMergeParts; ++k) {
+    for (int k = 0; k < n; ++k) {
       const long long at = ((2ll * (c + k) + (c + k == c0 && cut.second)) * P.together + wh) * P.rows + r;
       ml[k] = c + k <= c1 ? P.ml[at] : make_float2(-INFINITY, 0.0f);
       x[k] = c + k <= c1 ? *reinterpret_cast<const float4 *>(P.o + at * D + col) : make_float4(0, 0, 0, 0);
     }
     float to = m;
 #pragma unroll
-    for (int k = 0; k < kMergeParts; ++k) to = fmaxf(to, ml[k].x);
+    for (int k = 0; k < n; ++k) to = fmaxf(to, ml[k].x);
     const float by = m > -INFINITY ? exp2_approx(m - to) : 0.0f;
     m = to;
     l *= by, o.x *= by, o.y *= by, o.z *= by, o.w *= by;
 #pragma unroll
-    for (int k = 0; k < kMergeParts; ++k) {
+    for (int k = 0; k < n; ++k) {
       // a part whose factor is 0 still counts: what is not finite in it has to show
       const float f = ml[k].x > -INFINITY || ml[k].x != ml[k].x ? exp2_approx(ml[k].x - m) : 0.0f;
       l += f * ml[k].y;
       o.x += f * x[k].x, o.y += f * x[k].y, o.z += f * x[k].z, o.w += f * x[k].w;
     }
+  };
+  if (cut.parts == 2) {
+    join(std::integral_constant<int, 2>(), c0);
+  } else {
+    for (int c = c0; c <= c1; c += kMergeParts) join(std::integral_constant<int, kMergeParts>(), c);
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const int hk = cut.group * P.together + wh;
