@@ -39,6 +39,7 @@ __device__ __forceinline__ Asker asker_of(const CrossPlan &P, int b, bool tell) 
 struct Share {
   long long lo, hi;  // cells of all requests in a row
   int b, group, row_tile, at;
+  Asker a;  // request b
 };
 
 // By the whole block, N threads.  Each thread adds up the cells of a run of requests; the runs' sums are scanned, and
@@ -50,6 +51,43 @@ __device__ __forceinline__ Share share_of(const CrossPlan &P) {
   __shared__ Share found;
   const wt_cross_desc &d = P.d;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (d.n_req <= 32) {  // each warp by itself, a request a lane
+    Asker a = {};
+    int mine = 0;  // cells; with tokens, heads and states whose products pass 31 bits the block counts them
+    bool large = false;
+    if (lane < d.n_req) {
+      a = asker_of(P, lane, blockIdx.x == 0 && warp == 0);
+      const long long n = a.cells(P);
+      large = n >= 1 << 25;
+      mine = (int)n;
+    }
+    if (!__any_sync(0xffffffffu, large)) {
+      int upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+      }
+      const unsigned all = __shfl_sync(0xffffffffu, upto, 31), ctas = gridDim.x;
+      const unsigned per = max((unsigned)P.least, (all + ctas - 1) / ctas), lo = min(all, per * blockIdx.x), hi = min(all, lo + per);
+      Share s = {};
+      if (lo < hi) {
+        const int b = __popc(__ballot_sync(0xffffffffu, (unsigned)upto <= lo));  // requests that end before it
+        s.a.t0 = __shfl_sync(0xffffffffu, a.t0, b), s.a.n = __shfl_sync(0xffffffffu, a.n, b);
+        s.a.mem = __shfl_sync(0xffffffffu, a.mem, b), s.a.len = __shfl_sync(0xffffffffu, a.len, b);
+        s.a.row_tiles = __shfl_sync(0xffffffffu, a.row_tiles, b), s.a.key_tiles = __shfl_sync(0xffffffffu, a.key_tiles, b);
+        s.a.last = __shfl_sync(0xffffffffu, a.last, b);
+        const unsigned at = lo - __shfl_sync(0xffffffffu, upto - mine, b), per_head = (unsigned)s.a.head_cells();
+        s.lo = lo, s.hi = hi, s.b = b;
+        s.group = at / per_head;
+        const unsigned in_head = at - s.group * per_head;
+        s.row_tile = min(in_head / s.a.key_tiles, s.a.row_tiles - 1u);
+        s.at = in_head - s.row_tile * s.a.key_tiles;
+      }
+      __syncthreads();  // as below: what the block has set up is there
+      return s;
+    }
+  }
   const int run = (d.n_req + N - 1) / N, b0 = min(tid * run, d.n_req), b1 = min(b0 + run, d.n_req);
   Asker a = {};
   long long mine = 0;
@@ -86,7 +124,7 @@ __device__ __forceinline__ Share share_of(const CrossPlan &P) {
     const int group = (int)quotient(lo - first, a.head_cells());
     const long long at = lo - first - group * a.head_cells();
     const int row_tile = (int)min(quotient(at, a.key_tiles), a.row_tiles - 1ll);
-    found = {lo, hi, b, group, row_tile, (int)(at - (long long)row_tile * a.key_tiles)};
+    found = {lo, hi, b, group, row_tile, (int)(at - (long long)row_tile * a.key_tiles), a};
   }
   __syncthreads();
   return found;
@@ -112,9 +150,8 @@ struct Walk {
   bool started;
   Asker a;
   Segment g;
-  __device__ Walk(const CrossPlan &p, const Share &share) : P(p), s(share), cell(share.lo), b(share.b), at(share.at), started(false) {
+  __device__ Walk(const CrossPlan &p, const Share &share) : P(p), s(share), cell(share.lo), b(share.b), at(share.at), started(false), a(share.a) {
     g.group = share.group, g.row_tile = share.row_tile, g.tiles = 0, g.cut = false;
-    if (cell < s.hi) a = asker_of(P, b, false);
   }
   __device__ __forceinline__ bool next() {
     if (cell >= s.hi) return false;
