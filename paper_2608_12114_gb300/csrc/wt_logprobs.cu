@@ -253,6 +253,7 @@ __global__ void __launch_bounds__(kThreads, kResident) logprobs_kernel(const __g
   const wt_logprobs_desc &d = P.d;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const long long begin = P.per * blockIdx.x, end = min((long long)d.rows * P.row_vecs, begin + P.per);
+  griddep_launch();  // what joins rows may start its first loads
   for (long long at = begin; at < end;) {
     const int row = (int)quotient(at, P.row_vecs);
     const long long row0 = (long long)row * P.row_vecs;
@@ -536,9 +537,11 @@ size_t plan_logprobs(LogprobsPlan *P) {
   P->row_vecs = (d.vocab + 6) / 4;
   const long long all = (long long)d.rows * P->row_vecs, ctas = (long long)kResident * num_sms();
   // Equal shares, of one turn of a CTA's threads at least, or whole rows, whichever takes less by this count, in
-  // turns: a row that a CTA meets takes its turns and about two more, and joining rows about three.
+  // turns: a row that a CTA meets takes its turns and about two more, and parts of rows cost 8 more, 16 with
+  // alternatives.  (Shares against whole rows, us: 100 rows of 30000 with twenty alternatives 20.5, 13.6, without 10.1, 6.9;
+  // 257 of 128256 with twenty 46.4, 43.9; 10 of 100000 with 32 16.7, 26.9; 900 of 128256 without 74.7, 76.2.)
   const long long equal = std::max<long long>((all + ctas - 1) / ctas, kTurn), whole = (d.rows + ctas - 1) / ctas;
-  const double by_shares = (double)equal / kTurn + 2.0 * (2.0 + (double)equal / P->row_vecs) + 3.0;
+  const double by_shares = (double)equal / kTurn + 2.0 * (2.0 + (double)equal / P->row_vecs) + (d.n_top ? 16.0 : 8.0);
   const double by_rows = (double)whole * ((P->row_vecs + kTurn - 1) / kTurn + 2.0);
   P->per = by_rows <= by_shares ? whole * P->row_vecs : equal;
   P->ctas = (int)((all + P->per - 1) / P->per);
