@@ -21,8 +21,8 @@
 // fewer for a pair: 37.4 us against 40.7 for the targets below), so a result is off by up to half a step of each weight.
 //
 // Bound: the softmax warps, two to a scheduler, whose chains (read S, maximum, exponentials, write P) hide one
-// another's latencies only in part.  2 requests of up to 1024 tokens, 32 heads over 8 of 128, against up to 16384 states: 260 us,
-// 1.37 PFLOP/s; 6 requests of up to 448 tokens, 20 heads of 64, against up to 1500: 37 us, of which HBM needs 6 and
+// another's latencies only in part.  2 requests of up to 1024 tokens, 32 heads over 8 of 128, against up to 16384 states: 250 us,
+// 1.43 PFLOP/s; 6 requests of up to 448 tokens, 20 heads of 64, against up to 1500: 34 us, of which HBM needs 6 and
 // the products 5.
 //
 // Every mbarrier wait is bounded; a timeout records WT_ETIMEDOUT and every role stops.
