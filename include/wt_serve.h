@@ -261,7 +261,7 @@ typedef struct {
   int32_t rows, vocab, n_given, n_top;
 } wt_logprobs_desc;
 
-/* Errors: WT_EINVAL, WT_ENOTSUP (host-only handle), WT_ECUDA. */
+/* Errors: WT_EINVAL, WT_ENOTSUP (host-only handle), WT_ENOMEM, WT_ECUDA. */
 int wt_logprobs(wt_handle *h, const wt_logprobs_desc *d, void *stream);
 
 /* ---- wt_verify ------------------------------------------------------------------------------
