@@ -309,6 +309,34 @@ def test_states_past_2_gib(torch, h):
         assert ((out.double().cpu() - want).abs() <= tol).all()
 
 
+def test_more_work_than_a_warp_counts(torch, h):
+    """One request of 65536 tokens and 2^20 states: 2^25 cells, of which a few tokens are checked."""
+    N, M, H, D = 65536, 1 << 20, 16, 8
+    g = torch.Generator("cuda").manual_seed(3)
+    q, k, v = (torch.randn(n, H, D, device="cuda", generator=g).bfloat16() for n in (N, M, M))
+    out = torch.empty_like(q)
+    ints = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    h.cross(serving.cross_attention(q, out, ints(0, N), k, v, ints(0), ints(M), max_new=N, max_mem=M))
+    some = torch.tensor([0, 1, 255, 256, 30001, N - 1], device="cuda")
+    s = torch.einsum("nhd,khd->hnk", q[some].double(), k.double()) * D ** -0.5
+    want = torch.einsum("hnk,khd->nhd", torch.softmax(s, dim=2), v.double())
+    # the mean of 2^20 values near 0: sum p |v| is below 1, weights are rounded by 2^-8 each, sums in fp32 keep 2^-15
+    assert ((out[some].double() - want).abs() <= 2.0 ** -8 + 2.0 ** -15 + 2.0 ** -8 * want.abs()).all()
+    assert ((out[some].double() - want).abs().mean() <= 2.0 ** -12)  # the roundings of 2^20 weights cancel
+
+
+def test_pitches_that_say_nothing(torch, h):
+    """Of one state, one kv head, one token: any pitch does."""
+    for new in (1, 40):
+        s = Set(torch, [new], [1], 4, 1, 64, gap=0)
+        d = s.desc()
+        d.mem_stride, d.mem_head = 1 << 40, 1 << 40
+        if new == 1:
+            d.q_stride = 1 << 40
+        h.cross(d)
+        s.check(torch)
+
+
 def test_what_is_refused(torch, h):
     def refuse(change, code=wt.WT_EINVAL, holes=None):
         s = Set(torch, [2, 1], [300, 20], 8, 2, 64, holes=holes)
