@@ -4,9 +4,9 @@
 // A CTA takes an equal share of all requests' cells (CrossPlan), so unequal memories keep no SM waiting.  Each of
 // its 4 warps streams its own tiles of 32 states (16 of more than 64 elements: 8 KB either way) through a ring of
 // its own in shared memory, on from one row tile into the next: a head of a group of four, or of two, or every
-// fourth of one head's.  (48 requests' tokens, 20 heads of 64, whose 128 bytes of a state lie side by side: 50.5 us, and
-// 65.1 with all warps at one head.)  Rows, (token, head-in-group) pairs, are columns of
-// the m16n8k16 MMAs, 8 to a block, so that a single token's product is not 16 rows of which one counts:
+// fourth of one head's.  (48 requests' tokens, 20 heads of 64, whose 128 bytes of a state lie side by side: 50.5 us,
+// and 65.1 with all warps at one head.)  Rows, (token, head-in-group) pairs, are columns of the m16n8k16 MMAs, 8 to a
+// block, so that a single token's product is not 16 rows of which one counts:
 //
 //   S^T = K Q^T,   P^T = 2^(S^T - m),   O^T += V^T P^T,   l += column sums of P^T
 //

@@ -8,7 +8,8 @@
 // The largest logit's own 1 stays out of s, so that a sharp row keeps its entropy and its likeliest token's
 // log probability to fp32's precision: nothing is subtracted.  A thread keeps four largest logits, of every
 // fourth that it sees, out of its sums: of a new logit and the one kept, the smaller goes in.  Its sums are against
-// a reference of its warp, the first largest logit, which moves when one is 2^60 above it.  At the end all of the
+// a reference of its warp, the first largest logit, which moves when one is 2^8 above it (the
+// move of w to another reference loses that many roundings of s).  At the end all of the
 // kept ones but one go in, too.  Two parts, m1 >= m2, join as s1 + f (s2 + 1) and w1 + f (w2 + d (s2 + 1)),
 // d = (m2 - m1) log2(e) / t, f = 2^d: warps and CTAs in a fixed order.  (With the thread's one largest logit as its
 // reference, which half the time moved in one lane of a warp or another, the kernel was bound by its
@@ -37,8 +38,8 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kResident = 4;  // CTAs to an SM
 // Up to so many CTAs to an SM, of four turns or more each, load a turn ahead, in registers: 257 rows of 128256 with
-// twenty alternatives, a row a CTA, 35.6 us against 44.0.  (More of them load beside one another's work as it is, and bulk copies
-// into rings were slower: 57.)
+// twenty alternatives, a row a CTA, 35.6 us against 44.0.  (More of them load beside one another's work as it is, and
+// bulk copies into rings were slower: 57.)
 constexpr int kFew = 3;
 constexpr int kVecs = 4;      // 16-byte vectors of a lane at a time
 constexpr int kTurn = kThreads * kVecs;  // vectors that a CTA takes at a time
@@ -46,7 +47,7 @@ constexpr int kTop = WT_LOGPROBS_MAX_TOP;
 constexpr int kGroups = 128;
 constexpr int kRoom = 3 * kTop;   // of a warp: it joins 32 to its list from 2 kTop on
 constexpr int kDirect = 160;      // so many are placed as they are
-constexpr float kGrow = 60.0f;  // in log2: weights and their sums stay far below 2^127
+constexpr float kGrow = 8.0f;     // in log2
 static_assert(kTop == 32, "one candidate a lane");
 static_assert(kGroups == kThreads / 2 && kGroups >= kTop, "two groups of four threads, enough of them");
 

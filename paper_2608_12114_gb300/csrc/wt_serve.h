@@ -174,10 +174,9 @@ cudaError_t launch_attend_merge(const AttendPlan &P, cudaStream_t s);
 // The work of a call is cut into cells: `keys` states of one request's memory for one group of `together` kv heads
 // and one tile of up to `rows` (token, head-in-group) rows a head, in the order request, group, row tile, states.
 // A row tile of no more than `half` rows takes as long for 2 keys as others for keys, and a cell of it has as many.
-// CTA c takes the cells from c * per on, per of them,
-// `least` or more.  A row tile whose cells one CTA takes whole is written as it
-// is; else each CTA leaves its part of O (fp32, not divided), m and l in a slot: 2c where the CTA's cells start in
-// the row tile or with it, 2c + 1 where the row tile starts behind them.
+// CTA c takes the cells from c * per on, per of them, `least` or more.  A row tile whose cells one CTA takes whole
+// is written as it is; else each CTA leaves its part of O (fp32, not divided), m and l in a slot: 2c where the CTA's
+// cells start in the row tile or with it, 2c + 1 where the row tile starts behind them.
 struct CrossCut {  // a row tile that starts in a CTA's cells and goes on behind them
   int parts;         // CTAs that have some of it; 0: there is none
   int second;        // whether its first part is the CTA's second slot

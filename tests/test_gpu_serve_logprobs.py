@@ -107,6 +107,19 @@ def test_ascending_and_descending_rows(torch, h):
     s.check(torch)
 
 
+@pytest.mark.parametrize("step", [5.0, 30.0, 80.0, 300.0])
+def test_rows_that_rise_late(torch, h, step):
+    """The first thousands of logits far below the others, which their sums were against."""
+    s = Set(torch, 4, 30000, 2, 20, temp=False)
+    s.logits[0, 9000:] += step
+    s.logits[1, 29990:] += step
+    s.logits[2, 5000:] += step
+    s.logits[2, 15000:] += step
+    s.logits[3] += torch.arange(30000, device="cuda") // 4096 * step
+    h.logprobs(s.desc())
+    s.check(torch)
+
+
 def test_masked_rows(torch, h):
     """Fewer tokens left than are asked for, one, and none; a given token that is masked."""
     s = Set(torch, 4, 9000, 2, 6)
