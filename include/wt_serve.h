@@ -91,7 +91,8 @@ int wt_adapt(wt_handle *h, const wt_adapt_desc *d, size_t n, void *stream);
  *
  * and is rounded once: q to q_out[t], k and (unchanged) v to the caches' row of the token's place
  * len[b] - n_b + i, which wt_attend finds again: row place % page of page table[b, place / page].
- * Any of q, k and v may be NULL (with its output): then it is not looked at.  q alone needs no pages.
+ * Any of q, k and v may be NULL (with its output): then it is not looked at.  q alone needs no pages, and
+ * v alone no turns and no pos.
  *
  * Pair j is elements j and j + rot_dim / 2, or with WT_PLACE_NEIGHBOURS 2j and 2j + 1.  Its angle is
  * pos * 2 pi * turns[j] / 2^64: turns[j] holds the turns that a position adds, modulo one, as a fraction

@@ -730,6 +730,8 @@ int place_impl(wt_handle *h, const wt_place_desc *dp, cudaStream_t s) {
   if (!d.q) d.q_norm = nullptr;
   if (!d.k) d.k_norm = nullptr;
   if (!d.k && !d.v) d.table = nullptr;
+  if (!d.q && !d.k) d.rot_dim = 0;  // values are not turned
+  if (!d.rot_dim) d.turns = nullptr, d.pos = nullptr;
   if (!d.k && !d.v && (d.pos || !d.rot_dim || !d.q)) d.len = nullptr;
   P.status = ctx.status;
   wt::plan_place(&P);
