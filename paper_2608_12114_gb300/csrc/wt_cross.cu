@@ -148,13 +148,14 @@ __global__ void __launch_bounds__(kThreads, 2)
   while (now.segment()) {
     const Asker &a = now.a;
     const Segment &sg = now.g;
-    const int rows = a.n * G, row0 = sg.row_tile * kRows, hk = sg.group * P.together + wh;
+    const int hk = sg.group * P.together + wh;
+    const uint32_t rows = a.n * G, row0 = sg.row_tile * kRows;
 
     // queries as B operands
     uint32_t qb[NQ][ND][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      const int r = row0 + n * 8 + g;
+      const uint32_t r = row0 + n * 8 + g;
       const bool ok = r < rows;
       const uint16_t *src = static_cast<const uint16_t *>(d.q) +
                             (ok ? (int64_t)(a.t0 + r / G) * d.q_stride + (int64_t)(hk * G + r % G) * D : 0);
@@ -309,7 +310,8 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
       together();
       for (int i = wk; i < kJoinRows; i += of_head) {
-        const int r = h * kJoinRows + i, row = row0 + r, part = wh * of_head * kJoinRows + i;
+        const int r = h * kJoinRows + i, part = wh * of_head * kJoinRows + i;
+        const uint32_t row = row0 + r;
         if (row >= rows) break;
         float mm = -INFINITY, ll = 0.0f;
         for (int w = 0; w < of_head; ++w) mm = fmaxf(mm, sml[part + w * kJoinRows].x);
@@ -358,8 +360,8 @@ __global__ void __launch_bounds__(kThreads) cross_merge_kernel(const __grid_cons
   if (wh >= P.together || col >= D) return;
   griddep_wait();  // launched while the kernel before it runs
   const CrossCut cut = P.cuts[blockIdx.x];
-  const int row = cut.row_tile * P.rows + r;
-  if (cut.parts == 0 || row >= cut.rows) return;
+  const uint32_t row = cut.row_tile * P.rows + r;
+  if (cut.parts == 0 || row >= (uint32_t)cut.rows) return;
   const int c0 = blockIdx.x, c1 = c0 + cut.parts - 1;
   float m = -INFINITY, l = 0.0f;
   float4 o = make_float4(0, 0, 0, 0);

@@ -28,7 +28,7 @@ __device__ __forceinline__ Asker asker_of(const CrossPlan &P, int b, bool tell) 
     mem = min(max(mem, 0), (int)d.n_mem);
     len = min(min(max(len, 0), d.max_mem), (int)d.n_mem - mem);
   }
-  const int n = t1 - t0, row_tiles = (n * P.G + P.rows - 1) / P.rows;
+  const int n = t1 - t0, row_tiles = cross_row_tiles(n, P.G, P.rows);
   // tokens without a state have a tile all the same: it writes their zeros
   const int key_tiles = max(1, (len + P.keys - 1) / P.keys);
   const bool half = n * P.G - (row_tiles - 1) * P.rows <= P.half;

@@ -495,8 +495,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       fence_after();
       // Rows out, 32 columns at a time, turned in shared memory so that neighbouring lanes write one row.  The
       // queries have been read by then, and their place is this stream's until q_empty.
-      const int row0 = g.row_tile * P.rows + (g.half ? 0 : i * P.half);
-      const int rows = min(P.half, w.a.n * P.G - row0);  // of the tile; may be none
+      const int part0 = g.half ? 0 : i * P.half;  // in the row tile
+      const uint32_t row0 = g.row_tile * P.rows + part0;
+      const int rows = min(P.half, (int)(w.a.n * P.G - row0));  // of the tile; may be none
       const uint32_t turn = base + i * X::stage + (warp & 3) * (X::stage / 4);
       static_assert(32 * 128 <= X::stage / 4, "32 rows of 32 columns");
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -541,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int t = k * 8 + (lane >> 2), at = (warp & 3) * 32 + t;
             const uint4 v = lds128(turn + t * 64 + ((lane ^ (t >> 1)) & 3) * 16);
             if (at < rows && col < P.d.head_dim) {
-              const int row = row0 + at;
+              const uint32_t row = row0 + at;
               *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(P.d.out) + (int64_t)(w.a.t0 + row / P.G) * P.d.out_stride +
                                          (g.group * P.G + row % P.G) * P.d.head_dim + col) = v;
             }
@@ -559,13 +560,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int t = k * 4 + (lane >> 3), at = (warp & 3) * 32 + t;
             const uint4 v = lds128(turn + t * 128 + ((lane ^ t) & 7) * 16);
             if (at < rows && col < P.d.head_dim)
-              *reinterpret_cast<uint4 *>(P.o + (g.slot * P.rows + (row0 - g.row_tile * P.rows) + at) * P.d.head_dim + col) = v;
+              *reinterpret_cast<uint4 *>(P.o + (g.slot * P.rows + part0 + at) * P.d.head_dim + col) = v;
           }
         }
         __syncwarp();
       }
       if (!g.whole && r < rows && (!g.half || i == 0))
-        P.ml[g.slot * P.rows + (row0 - g.row_tile * P.rows) + r] = make_float2(l == l ? m : l, l);
+        P.ml[g.slot * P.rows + part0 + r] = make_float2(l == l ? m : l, l);
       fence_before();
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the next queries land there
       if (g.half) {  // the other stream's sums have been read

@@ -177,6 +177,9 @@ cudaError_t launch_attend_merge(const AttendPlan &P, cudaStream_t s);
 // CTA c takes the cells from c * per on, per of them, `least` or more.  A row tile whose cells one CTA takes whole
 // is written as it is; else each CTA leaves its part of O (fp32, not divided), m and l in a slot: 2c where the CTA's
 // cells start in the row tile or with it, 2c + 1 where the row tile starts behind them.
+// Row tiles of n tokens.  n * G goes up to 2^31 - 1, so it and the rows of a last tile, which may end past it, count
+// without a sign.
+__host__ __device__ constexpr int cross_row_tiles(int n, int G, int rows) { return (int)(((uint32_t)n * G + rows - 1) / rows); }
 struct CrossCut {  // a row tile that starts in a CTA's cells and goes on behind them
   int parts;         // CTAs that have some of it; 0: there is none
   int second;        // whether its first part is the CTA's second slot

@@ -23,6 +23,7 @@ cudaError_t launched(int n = 1) {
 HOST const char *host_error() { return error; }
 HOST const wt_place_desc *host_place() { return &place.d; }
 HOST int host_cross_ctas() { return cross.ctas; }
+HOST int host_row_tiles(int n, int G, int rows) { return wt::cross_row_tiles(n, G, rows); }
 HOST void host_reset() { launches = counted = 0, place = {}, cross = {}; }
 HOST int host_launches() { return launches; }
 HOST int host_counted() { return counted; }

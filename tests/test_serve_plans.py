@@ -62,3 +62,13 @@ def test_values_alone_are_not_turned(L):
         L.host_reset()
         assert L.wt_place(None, C.byref(d), None) == wt.WT_OK and L.host_place().contents.rot_dim == 64
         assert L.host_place().contents.turns == d.turns
+
+
+def test_row_tiles_up_to_2_31_rows(L):
+    """wt_cross takes n_tokens * heads up to 2^31 - 1; a tile of 8, 16, 32 or up to 256 rows may end past that."""
+    for G in (1, 2, 3, 7, 65, 127, 128):
+        for rows in (8, 16, 32, 2 * (128 // G * G)):
+            most = (2 ** 31 - 1) // G
+            for n in (0, 1, rows // G, rows // G + 1, most - 1, most):
+                if n <= 2 ** 30:
+                    assert L.host_row_tiles(n, G, rows) == -(-n * G // rows), (n, G, rows)
