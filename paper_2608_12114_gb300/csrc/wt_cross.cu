@@ -10,7 +10,9 @@
 //
 //   S^T = K Q^T,   P^T = 2^(S^T - m),   O^T += V^T P^T,   l += column sums of P^T
 //
-// with s = scale log2(e) q.k and m moving as kSlack says; P^T turns from a result into an operand by movmatrix.
+// with s = scale log2(e) q.k and m moving as kSlack says; P^T turns from a result into an operand by movmatrix.  P is
+// rounded to the memory's type, as the MMA takes both operands in one type, and l sums the rounded weights: what their
+// roundings have in common cancels.
 // Parts join as softmax splits: O = sum_i 2^(m_i - m) O_i, l alike, out = O / l.  The maximum passes over NaN
 // scores, so a part whose sum is NaN says so in its m.
 //

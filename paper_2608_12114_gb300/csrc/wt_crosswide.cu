@@ -17,12 +17,14 @@
 //                    on a barrier of its own, and this warp makes the arrival that others wait for.
 //
 // The reference m of a row moves as kSlack says, and O is then rescaled in tensor memory.  P is rounded to the
-// memory's type (the MMA takes both operands in one type); l sums the weights before that (two instructions of nine
-// fewer for a pair: 37.4 us against 40.7 for the targets below), so a result is off by up to half a step of each weight.
+// memory's type (the MMA takes both operands in one type); l sums the rounded weights, so that what their roundings have
+// in common cancels, as in the kernel for few rows.  (Sums of the weights before their rounding took 32.9 us for the
+// targets below and 250 for the long memories; but where many weights are one number, results were off by its rounding,
+// every element the same way, and a request's as soon as another request had more tokens.)
 //
 // Bound: the softmax warps, two to a scheduler, whose chains (read S, maximum, exponentials, write P) hide one
-// another's latencies only in part.  2 requests of up to 1024 tokens, 32 heads over 8 of 128, against up to 16384 states: 250 us,
-// 1.43 PFLOP/s; 6 requests of up to 448 tokens, 20 heads of 64, against up to 1500: 34 us, of which HBM needs 6 and
+// another's latencies only in part.  2 requests of up to 1024 tokens, 32 heads over 8 of 128, against up to 16384 states: 257 us,
+// 1.38 PFLOP/s; 6 requests of up to 448 tokens, 20 heads of 64, against up to 1500: 36 us, of which HBM needs 6 and
 // the products 5.
 //
 // Every mbarrier wait is bounded; a timeout records WT_ETIMEDOUT and every role stops.
@@ -457,7 +459,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             v[c] = exp2_approx(v[c]);
             v[c + 1] = exp2_approx(v[c + 1]);
             u[k / 2] = pack2<DT>(v[c], v[c + 1]);
-            add_x2(l0, l1, v[c], v[c + 1]);
+            float p0, p1;
+            unpack2<DT>(u[k / 2], p0, p1);
+            add_x2(l0, l1, p0, p1);
           }
           // where P lies apart, the product before may still read it
           if (C::apart && hf == 0 && done + j > 0) {

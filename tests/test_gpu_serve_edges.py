@@ -2,6 +2,7 @@
 import pytest
 
 from paper_2608_12114_gb300 import build, serving, wt
+from tests.test_gpu_serve_cross import Set as Cross
 from tests.test_gpu_serve_place import Set as Place
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +51,24 @@ def test_rows_up_to_2_31(torch, h, heads, scale):
         assert (rows[i:i + (1 << 28)] == v.view(1, D)).all(), i
     del q, rows
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dt", ["bfloat16", "float16"])
+@pytest.mark.parametrize("rise", [0.0, 1.3, 5.2])
+@pytest.mark.parametrize("new,D", [([1, 2], 64), ([1, 2], 128), ([16, 9], 128), ([20, 30], 64), ([20, 30], 128), ([200, 3], 64), ([200, 3], 128)])
+def test_roundings_that_weights_share_cancel_on_every_route(torch, h, dt, rise, new, D):
+    """Scores of two kinds, so that most weights are one number and share its rounding: it must not show in
+    the result, which then errs to both sides alike (128 different columns and more, whose roundings have a
+    variance of u^2 / 3 at most: a mean error of 0.2 u would be four standard deviations of these alone)."""
+    s = Cross(torch, new, [4000] * len(new), 4, 2, D, dt=dt, sharp=0.0)
+    s.q[:, :, 0] = 1.0
+    s.scale = 1.0
+    M = s.k.shape[0]
+    steps = rise * (torch.arange(M, device="cuda") // 128 % 2).view(-1, 1).to(s.k.dtype)
+    s.k[:, :, 0] = torch.where(s.inside.view(-1, 1), steps, s.k[:, :, 0])
+    s.v += torch.linspace(1, 8, 2 * D, device="cuda").view(2, D).to(s.v.dtype)
+    h.cross(s.desc())
+    torch.cuda.synchronize()
+    o, _, _ = s.want()
+    off = (s.out.double().cpu() - o) / o
+    assert off.abs().max() <= 1.1 * s.u and off.mean().abs() <= 0.2 * s.u
