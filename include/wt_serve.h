@@ -190,7 +190,8 @@ int wt_attend(wt_handle *h, const wt_attend_desc *d, void *stream);
  *
  * over the states with keep[j] != 0 (keep NULL: all).  Memories may overlap or be one; a request's tokens
  * read theirs once, so beams or drafts over one memory are best one request's tokens.  Scores and sums are
- * fp32; weights are rounded to the memory's type, and divided by the sum of the rounded ones.  A token that sees
+ * fp32, whatever a memory's length; weights are rounded to the memory's type, and divided by the sum of the
+ * rounded ones.  A token that sees
  * no state gets zeros, and so does one all of whose scores are -infinity.  NaN and infinities show as
  * wt_attend's do; what is not in the memory, or not kept, never reaches a result, whatever stands there.
  * Rows of tokens that no request holds are left as they are.

@@ -16,6 +16,9 @@
 // Parts join as softmax splits: O = sum_i 2^(m_i - m) O_i, l alike, out = O / l.  The maximum passes over NaN
 // scores, so a part whose sum is NaN says so in its m.
 //
+// Where a row has so many states that the MMAs' sums would fall short, a warp sets its O^T and l aside in the workspace
+// (cross_fold) and begins anew; at the row tile's end it adds them.
+//
 // Tiles come as TMA boxes.  States that are not kept, and what a memory's last tile holds behind it, are masked in S
 // and cleared in V.  (13 requests' beams of 32 heads of 80, three in ten states left out: leaving those out of the
 // copies, row by row with cp.async, 31.3 us, as boxes 29.3.)
@@ -147,6 +150,9 @@ __global__ void __launch_bounds__(kThreads, 2)
   const uint32_t k_lane = ((lane & 15) * 128) | (((lane >> 4) ^ lane) & 7) * 16;
   const uint32_t v_lane = (((lane & 7) + (lane >> 4) * 8) * 128) | (((lane >> 3 & 1) ^ lane) & 7) * 16;
   Tiles now(P, share, wk * kT);
+  constexpr int kFold = cross_fold(DT) / kT, kAside = NQ * (ND + 1);  // tiles; float4s of a lane: of each block O^T, then l
+  static_assert(kAside * kWarps * 32 * sizeof(float4) == cross_few_fold(kRows, DH * 64), "what a CTA sets aside");
+  float4 *const aside = P.fold + (int64_t)(blockIdx.x * kWarps + warp) * kAside * 32 + lane;
   while (now.segment()) {
     const Asker &a = now.a;
     const Segment &sg = now.g;
@@ -181,7 +187,26 @@ __global__ void __launch_bounds__(kThreads, 2)
       l[n][0] = l[n][1] = 0.0f;
     }
 
+    auto folded = [&]() { return now.i > kFold; };  // whether something lies aside, at tile i - 1 or after the last
     for (int key0; now.tile(key0);) {
+      if (folded() && now.i % kFold == 1) {
+        const bool again = now.i > 2 * kFold;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          float4 *const at = aside + n * (ND + 1) * 32;
+          float4 x = make_float4(0, 0, 0, 0);
+#pragma unroll
+          for (int t = 0; t < ND; ++t) {
+            if (t >= ksteps) break;
+            if (again) x = at[t * 32];
+            at[t * 32] = make_float4(x.x + o[n][t][0], x.y + o[n][t][1], x.z + o[n][t][2], x.w + o[n][t][3]);
+            o[n][t][0] = o[n][t][1] = o[n][t][2] = o[n][t][3] = 0.0f;
+          }
+          if (again) x = at[ND * 32];
+          at[ND * 32] = make_float4(x.x + l[n][0], x.y + l[n][1], 0, 0);
+          l[n][0] = l[n][1] = 0.0f;
+        }
+      }
       const uint32_t stage = used % kStages, kt = ring + stage * kTileBytes, vt = kt + kV;
       constexpr uint32_t kAll = kT == 32 ? 0xffffffffu : (1u << kT) - 1;
       if (!warp_wait(bar0 + 8 * stage, used / kStages & 1, abort_flag, P.status)) {  // nothing of it is used
@@ -243,18 +268,26 @@ __global__ void __launch_bounds__(kThreads, 2)
         constexpr float kGrow = kSlack + kBelow<DT>;
         const bool grown0 = mx[0] > m[n][0] + kGrow, grown1 = mx[1] > m[n][1] + kGrow;
         if (__any_sync(0xffffffffu, grown0 || grown1)) {
+          float f[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const float to = (e ? grown1 : grown0) ? mx[e] - kBelow<DT> : m[n][e];
-            const float f = to > -INFINITY ? exp2_approx(m[n][e] - to) : 1.0f;
+            f[e] = to > -INFINITY ? exp2_approx(m[n][e] - to) : 1.0f;
             m[n][e] = to;
-            l[n][e] *= f;
+            l[n][e] *= f[e];
 #pragma unroll
             for (int t = 0; t < ND; ++t) {
-              o[n][t][e] *= f;
-              o[n][t][2 + e] *= f;
+              o[n][t][e] *= f[e];
+              o[n][t][2 + e] *= f[e];
             }
           }
+          if (folded())
+#pragma unroll 1
+            for (int t = 0; t <= ND; ++t)
+              if (t < ksteps || t == ND) {
+                float4 &x = aside[(n * (ND + 1) + t) * 32];
+                x = make_float4(x.x * f[0], x.y * f[1], x.z * f[0], x.w * f[1]);
+              }
         }
         const float ref0 = m[n][0] > -INFINITY ? m[n][0] : 0.0f, ref1 = m[n][1] > -INFINITY ? m[n][1] : 0.0f;
         // l from the rounded weights: what their roundings have in common cancels
@@ -284,6 +317,20 @@ __global__ void __launch_bounds__(kThreads, 2)
       if (issued != asked) note(asked, asked_kept);
       __syncwarp();
     }
+
+    if (folded())
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const float4 *const at = aside + n * (ND + 1) * 32;
+#pragma unroll
+        for (int t = 0; t < ND; ++t) {
+          if (t >= ksteps) break;
+          const float4 x = at[t * 32];
+          o[n][t][0] += x.x, o[n][t][1] += x.y, o[n][t][2] += x.z, o[n][t][3] += x.w;
+        }
+        const float4 x = at[ND * 32];
+        l[n][0] += x.x, l[n][1] += x.y;
+      }
 
     // join the head's warps, four rows at a time
 #pragma unroll

@@ -19,12 +19,17 @@
 // The reference m of a row moves as kSlack says, and O is then rescaled in tensor memory.  P is rounded to the
 // memory's type (the MMA takes both operands in one type); l sums the rounded weights, so that what their roundings have
 // in common cancels, as in the kernel for few rows.  (Sums of the weights before their rounding took 32.9 us for the
-// targets below and 250 for the long memories; but where many weights are one number, results were off by its rounding,
+// targets below and 250 for the long memories, where this took 36.1 and 257; but where many weights are one number, results were off by its rounding,
 // every element the same way, and a request's as soon as another request had more tokens.)
 //
+// After every kFold tiles of a stream a row's O goes from tensor memory to what was set aside in the workspace
+// (cross_fold), and the next product begins it anew; a reference that moves takes along what lies there.  (One GB300:
+// the targets below, which have nothing to fold, 36.7 us with this code and 36.1 without; the long memories 260 and 257,
+// and 266 where they fold each 8192 states, 279 each 4096.)
+//
 // Bound: the softmax warps, two to a scheduler, whose chains (read S, maximum, exponentials, write P) hide one
-// another's latencies only in part.  2 requests of up to 1024 tokens, 32 heads over 8 of 128, against up to 16384 states: 257 us,
-// 1.38 PFLOP/s; 6 requests of up to 448 tokens, 20 heads of 64, against up to 1500: 36 us, of which HBM needs 6 and
+// another's latencies only in part.  2 requests of up to 1024 tokens, 32 heads over 8 of 128, against up to 16384 states: 260 us,
+// 1.37 PFLOP/s; 6 requests of up to 448 tokens, 20 heads of 64, against up to 1500: 37 us, of which HBM needs 6 and
 // the products 5.
 //
 // Every mbarrier wait is bounded; a timeout records WT_ETIMEDOUT and every role stops.
@@ -78,6 +83,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                       const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CrossPlan P) {
   using X = Geo<DH>;
   using C = Cols<DH>;
+  constexpr int kFold = cross_fold(DT) / kKeysT;  // key tiles of a stream
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t *gbase = smem_raw + (base - smem_u32(smem_raw));
@@ -251,6 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           return true;
         };
         const int first = g.half ? 2 : 1;  // tiles that start the streams
+        auto anew = [&](int j) { return (g.half ? j >> 1 : j) % kFold == 0; };  // O starts with this product
         for (int j = 0; j < min(first, g.tiles) && keys(j); ++j) {
         }
         if (!live) break;
@@ -260,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (more && !keys(j & 1)) break;
             if (!next()) break;
             const uint32_t vs = stage;
-            if (!values(j & 1, vs, j < 2)) break;
+            if (!values(j & 1, vs, anew(j))) break;
             release(empty0 + 8 * vs);
           } else if (C::apart) {
             // stream by stream: neither waits for what the other does next
@@ -272,28 +279,28 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!next()) break;
             const uint32_t vs = stage;
-            if (!values(0, vs, j == 0)) break;
+            if (!values(0, vs, anew(j))) break;
             if (more) {
               if (!scores(1, 1, ks)) break;
               release(empty0 + 8 * ks);
             }
-            if (!values(1, vs, j == 0)) break;
+            if (!values(1, vs, anew(j))) break;
             release(empty0 + 8 * vs);
           } else if (g.half) {
             if (!next()) break;
             const uint32_t vs = stage;
-            if (!values(j & 1, vs, j < 2)) break;
+            if (!values(j & 1, vs, anew(j))) break;
             release(empty0 + 8 * vs);
             if (more && !keys(j & 1)) break;
           } else {
             if (!next()) break;
             const uint32_t vs = stage;
-            if (!values(0, vs, j == 0)) break;
+            if (!values(0, vs, anew(j))) break;
             if (more) {
               if (!next()) break;
               scores(0, 0, stage);
             }
-            if (!values(1, vs, j == 0)) break;
+            if (!values(1, vs, anew(j))) break;
             release(empty0 + 8 * vs);
             if (more) {
               scores(1, 1, stage);
@@ -358,6 +365,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // 32 lanes of tensor memory per warp
     const uint32_t S = tmem + lanes + i * C::s, O = tmem + lanes + C::o0 + i * C::o;
     const float scale_log2 = P.d.scale * 1.4426950408889634f;
+    // set aside: [head_dim / 4][row], so that a warp's accesses are of neighbours, then l
+    float4 *const aside = P.fold + (int64_t)(blockIdx.x * 2 + i) * ((DH * 16 + 1) * 128) + r;
+    static_assert(2 * (DH * 16 + 1) * 128 * sizeof(float4) == cross_wide_fold(DH * 64), "what a CTA sets aside");
     uint32_t done = 0, done_other = 0;  // tiles of this stream, and of the other, over all segments
     uint32_t seg = 0, met = 0;
     bool live = true;
@@ -378,7 +388,49 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       look(0);
       float m = 0.0f, l0 = 0.0f, l1 = 0.0f;
+      // O and l of the tiles before j, a multiple of kFold, to what was set aside; or of the last ones from there to O
+      auto fold = [&](int j, bool last) {
+        const bool again = last || j > kFold;
+        constexpr int kCols = 64;  // whose accesses are on their way together
+#pragma unroll 1
+        for (int c = 0; c < P.d.head_dim; c += kCols) {
+          float4 *const at = aside + c / 4 * 128;
+          float4 x[kCols / 4];
+#pragma unroll
+          for (int k = 0; k < kCols / 4; ++k) x[k] = again && c + 4 * k < P.d.head_dim ? at[k * 128] : make_float4(0, 0, 0, 0);
+          if (c == 0) {
+            live = warp_wait(o_full + 8 * i, (done + j - 1) & 1, abort_flag, status);
+            fence_after();
+          }
+#pragma unroll
+          for (int e = 0; e < kCols; e += 32) {
+            uint32_t o[32];
+            tmem_ld32(O + c + e, o);
+            wait_ld();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              float4 &y = x[e / 4 + k];
+              y.x += __uint_as_float(o[4 * k]), y.y += __uint_as_float(o[4 * k + 1]);
+              y.z += __uint_as_float(o[4 * k + 2]), y.w += __uint_as_float(o[4 * k + 3]);
+              if (!last && c + e + 4 * k < P.d.head_dim) at[(e / 4 + k) * 128] = y;
+              o[4 * k] = __float_as_uint(y.x), o[4 * k + 1] = __float_as_uint(y.y);
+              o[4 * k + 2] = __float_as_uint(y.z), o[4 * k + 3] = __float_as_uint(y.w);
+            }
+            if (last) tmem_st32(O + c + e, o);
+          }
+        }
+        if (last) wait_st();
+        fence_before();
+        float &l = aside[DH * 16 * 128].x;
+        l0 += again ? l1 + l : l1;
+        l1 = 0.0f;
+        if (!last) l = l0, l0 = 0.0f;
+      };
       for (int j = 0; j < n; ++j) {
+        if (j && j % kFold == 0) {
+          fold(j, false);
+          if (!live) break;
+        }
         const int keys = w.a.len - (g.tile0 + (g.half ? 2 * j + i : j)) * kKeysT;
         uint32_t gone[4];
         if (KEEP) {
@@ -438,6 +490,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (grown) m = top - kBelow<DT>;
           l0 *= f;
           l1 *= f;
+          if (j >= kFold) {
+#pragma unroll 4
+            for (int c = 0; c < P.d.head_dim; c += 4) {
+              float4 &x = aside[c / 4 * 128];
+              x = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+            }
+            aside[DH * 16 * 128].x *= f;
+          }
 #pragma unroll 1
           for (int c = 0; c < DH * 64; c += 32) {
             uint32_t o[32];
@@ -482,6 +542,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       float l = l0 + l1;
       if (n == 0) m = -INFINITY;
       if (n > 0 && !warp_wait(o_full + 8 * i, (done - 1) & 1, abort_flag, status)) break;
+      if (n > kFold) {
+        done -= n;
+        fold(n, true);
+        done += n;
+        l = l0;
+      }
       // Two streams of one row tile: both numbers of a row, and each takes half of the columns of both.
       float f = 1.0f, f_other = 0.0f;
       if (g.half) {

@@ -584,7 +584,9 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
   size_t bytes = 0;
   const size_t slots = 2 * (size_t)P.ctas * P.together * P.rows;
   const size_t o = take(bytes, slots * d.head_dim * 4), ml = take(bytes, slots * sizeof(float2)),
-               cuts = take(bytes, (size_t)P.ctas * sizeof(wt::CrossCut));
+               cuts = take(bytes, (size_t)P.ctas * sizeof(wt::CrossCut)),
+               fold = take(bytes, d.max_mem <= wt::cross_fold(d.dtype) ? 0
+                                  : P.ctas * (wide ? wt::cross_wide_fold(d.head_dim) : wt::cross_few_fold(P.rows, d.head_dim)));
   Lock lock(h);
   wt::ServeWorkspace w;
   CHECK(wt::serve_workspace(h, s, bytes, &w));
@@ -592,6 +594,7 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
   P.o = reinterpret_cast<float *>(ws + o);
   P.ml = reinterpret_cast<float2 *>(ws + ml);
   P.cuts = reinterpret_cast<wt::CrossCut *>(ws + cuts);
+  P.fold = reinterpret_cast<float4 *>(ws + fold);
   const bool joined = d.max_mem > P.keys;  // memories of one cell: no row tile has two parts
   cudaError_t e = wide ? wt::launch_cross_wide(P, maps, s) : wt::launch_cross_few(P, maps, s);
   if (e == cudaSuccess && joined) e = wt::launch_cross_merge(P, s);

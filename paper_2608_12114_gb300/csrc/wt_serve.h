@@ -187,6 +187,10 @@ struct CrossCut {  // a row tile that starts in a CTA's cells and goes on behind
   int group, row_tile;
   int pad[2];
 };
+// A matrix unit cuts its sums off where it adds to them, so what it adds up falls short by some 6e-9 of itself a state
+// (2^20 states: 0.6 %).  Where that nears a tenth of half a step of the type, a row's O is therefore set aside, with the
+// sum of the weights: added to what lay there, rounded to nearest, and begun anew.
+__host__ __device__ constexpr int cross_fold(int dtype) { return dtype == WT_F16 ? 8192 : 65536; }  // states
 struct CrossPlan {
   wt_cross_desc d;
   int G;           // heads / kv_heads
@@ -198,6 +202,7 @@ struct CrossPlan {
   float *o;        // [2 ctas][together][rows][head_dim]
   float2 *ml;      // [2 ctas][together][rows]
   CrossCut *cuts;  // [ctas]
+  float4 *fold;    // what the CTAs have set aside; none where no memory has more states than cross_fold
   int *status;
 };
 struct CrossMaps {
@@ -206,6 +211,9 @@ struct CrossMaps {
   alignas(64) uint8_t v[128];
 };
 cudaError_t cross_prepare();
+// Bytes that a CTA sets aside
+__host__ __device__ constexpr size_t cross_few_fold(int rows, int head_dim) { return (size_t)4 * 32 * (rows / 8) * ((head_dim <= 64 ? 4 : 8) + 1) * sizeof(float4); }
+__host__ __device__ constexpr size_t cross_wide_fold(int head_dim) { return (size_t)2 * 128 * (head_dim <= 64 ? 17 : 33) * sizeof(float4); }
 int cross_few_keys(int head_dim);  // states of a warp's tile; a cell has a tile for each of its 4 warps
 constexpr int kCrossFewResident = 2;  // CTAs of the kernel for few rows to an SM
 cudaError_t launch_cross_few(const CrossPlan &P, const CrossMaps &m, cudaStream_t s);

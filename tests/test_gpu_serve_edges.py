@@ -1,4 +1,7 @@
-"""Placing and attention to memories at the edges of what a call may hold: parts without the rest, the most rows."""
+"""Placing and attention to memories at the edges of what a call may hold: parts without the rest, the most rows, and
+long sums."""
+import math
+
 import pytest
 
 from paper_2608_12114_gb300 import build, serving, wt
@@ -72,3 +75,88 @@ def test_roundings_that_weights_share_cancel_on_every_route(torch, h, dt, rise, 
     o, _, _ = s.want()
     off = (s.out.double().cpu() - o) / o
     assert off.abs().max() <= 1.1 * s.u and off.mean().abs() <= 0.2 * s.u
+
+
+@pytest.mark.parametrize("dt", ["bfloat16", "float16"])
+def test_sums_of_2_20_states(torch, h, dt):
+    """One request of 65536 tokens and 2^20 states, 2^25 cells: tokens at the borders of row tiles that two CTAs share,
+    each by itself, of values near 1 as well as near 0."""
+    N, M, H, D = 65536, 1 << 20, 16, 8
+    dt = getattr(torch, dt)
+    u = torch.finfo(dt).eps / 2
+    g = torch.Generator("cuda").manual_seed(5)
+    q, k, v = (torch.randn(n, H, D, device="cuda", generator=g).to(dt) for n in (N, M, M))
+    v[:, :, 0] = 1.0
+    v[:, :, 1] = 1.0 + 0.25 * v[:, :, 1]
+    out = torch.full_like(q, float("nan"))
+    ints = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    h.cross(serving.cross_attention(q, out, ints(0, N), k, v, ints(0), ints(M), max_new=N, max_mem=M))
+    torch.cuda.synchronize()
+    assert not out.isnan().any()
+    # row tiles of 256 tokens and 8192 key tiles, 256 to a head; a CTA to an SM
+    tiles, sms = (N // 256) * (M // 128), torch.cuda.get_device_properties(0).multi_processor_count
+    per = -(-H * tiles // sms)
+    cut = {per * c % tiles // (M // 128) for c in (1, sms // 4, sms // 2, sms - 1)}
+    some = sorted({t for r in cut | {0, N // 256 - 1} for t in (256 * r, 256 * r + 127, 256 * r + 128, 256 * r + 255)})
+    some = torch.tensor(some, device="cuda")
+    p = torch.softmax(torch.einsum("nhd,khd->hnk", q[some].double(), k.double()) * D ** -0.5, dim=2)
+    want = torch.einsum("hnk,khd->nhd", p, v.double())
+    # A weight's rounding is up to u of it, and 2^20 of them cancel: their part of a sum p v has a standard deviation of
+    # u sqrt(sum p^2 v^2 / 3), below u 2^-8 for the sharpest rows here (|q|^2 = 28); eight of them.  The sums: as kept
+    # in wt_serve.h, a tenth of u, and 2^-17 for what is added up to nearest.
+    off = out[some].double() - want
+    sizes = torch.einsum("hnk,khd->nhd", p, v.double().abs())
+    assert (off.abs() <= u * want.abs() + 8 * u * 2.0 ** -8 + (0.1 * u + 2.0 ** -17) * sizes).all()
+    assert off[:, :, :2].mean().abs() <= 0.2 * u  # near 1: the outputs' roundings go both ways, or are none
+    assert (off[:, :, 2:].abs().mean(dim=(1, 2)) <= 2.0 ** -12).all()  # of each token, by values of both signs: zeros are off by 2^-10
+
+
+LONG = {  # new, requests, heads, kv heads, D: one memory for all, so that CTAs have long runs of it
+    "8 rows, heads together": (1, 310, 4, 4, 64), "8 rows": (2, 330, 3, 1, 128), "16 rows": (4, 320, 12, 4, 72), "32 rows": (8, 310, 16, 4, 128),
+    "32 rows of 40": (8, 310, 8, 2, 40), "one row tile": (32, 160, 4, 1, 64), "one row tile of 128": (32, 160, 4, 1, 128),
+    "two row tiles": (64, 160, 4, 1, 56), "two row tiles of 128": (70, 160, 4, 1, 120)}
+
+
+@pytest.mark.parametrize("name", LONG)
+@pytest.mark.parametrize("dt,M", [("float16", 40001), ("bfloat16", 300007)])
+@pytest.mark.parametrize("holes", [False, True])
+def test_long_memories_on_every_route(torch, h, name, dt, M, holes):
+    """Values near 1 over more states than one sum takes, and late a state that outweighs all before it by half, so that what was
+    summed up has to follow a new reference."""
+    new, B, H, Hkv, D = LONG[name]
+    dt = getattr(torch, dt)
+    u = torch.finfo(dt).eps / 2
+    g = torch.Generator("cuda").manual_seed(7)
+    k, v = (torch.randn(M, Hkv, D, device="cuda", generator=g).to(dt) for _ in range(2))
+    q = torch.randn(new * B, H, D, device="cuda", generator=g).to(dt)
+    q[:, :, 0], k[:, :, 0] = 1.0, 0.0
+    v = (torch.linspace(1, 1.9, D, device="cuda") + 0.25 * v.float()).to(dt)
+    k[M * 3 // 4, :, 0] = D ** 0.5 * math.log(M)
+    v[M * 3 // 4] += 1.0
+    keep = None
+    if holes:
+        keep = (torch.rand(M, device="cuda", generator=g) < 0.9).to(torch.uint8)
+        keep[M * 3 // 4] = 1
+        k[keep == 0], v[keep == 0] = float("nan"), float("inf")
+    out = torch.full_like(q, float("nan"))
+    ints = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    h.cross(serving.cross_attention(q, out, ints([new * b for b in range(B + 1)]), k, v, ints([0] * B), ints([M] * B), max_new=new,
+                                    max_mem=M, keep=keep))
+    torch.cuda.synchronize()
+    assert not out.isnan().any()
+    some = torch.arange(0, new * B, new * B // 40 | 1, device="cuda")
+    rows = slice(None) if keep is None else keep != 0
+    off, near = [], []
+    for x in range(H):
+        ks, vs = k[rows, x * Hkv // H].double(), v[rows, x * Hkv // H].double()
+        p = torch.softmax(q[some, x].double() @ ks.t() * D ** -0.5, dim=1)
+        want, sizes = p @ vs, p @ vs.abs()
+        off.append((out[some, x].double() - want) / want)
+        # the late state's weight and the output are rounded by u each, the others' roundings cancel (eight deviations of
+        # u sqrt(sum p^2 v^2 / 3)), scores are off by 2 (D / 16 + 4) 2^-23 of sums |q k|, here up to 12 + log M, and sums as above
+        late = p.amax(dim=1, keepdim=True)
+        rest = (p ** 2 @ vs ** 2 - (late * vs[p.argmax(dim=1)]) ** 2).clamp(min=0).sqrt()
+        near.append((2 * u * want + u * late * 3 + 8 * u * rest + (2 * (D / 16 + 4) * 2.0 ** -23 * 40 + 0.1 * u + 2.0 ** -17) * sizes) / want)
+    off, near = torch.stack(off), torch.stack(near)
+    assert (off.abs() <= near).all(), float((off.abs() / near).max())
+    assert off.mean().abs() <= 0.25 * u, float(off.mean() / u)
