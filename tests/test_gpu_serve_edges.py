@@ -1,10 +1,12 @@
-"""Placing and attention to memories at the edges of what a call may hold: parts without the rest, the most rows, and
-long sums."""
+"""Placing and attention to memories at the edges of what a call may hold: parts without the rest, the most rows, long sums,
+offsets that lie, and what stands around the outputs."""
 import math
 
 import pytest
 
 from paper_2608_12114_gb300 import build, serving, wt
+from tests import _serve_more as plain
+from tests.test_gpu_serve_cross import ROUTES
 from tests.test_gpu_serve_cross import Set as Cross
 from tests.test_gpu_serve_place import Set as Place
 
@@ -160,3 +162,80 @@ def test_long_memories_on_every_route(torch, h, name, dt, M, holes):
     off, near = torch.stack(off), torch.stack(near)
     assert (off.abs() <= near).all(), float((off.abs() / near).max())
     assert off.mean().abs() <= 0.25 * u, float(off.mean() / u)
+
+
+def guarded(torch, t, rows):
+    """A copy of t between `rows` rows of other numbers, and the whole buffer."""
+    g = torch.Generator("cuda").manual_seed(11)
+    whole = torch.randn((len(t) + 2 * rows,) + t.shape[1:], device="cuda", generator=g).to(t.dtype)
+    whole[rows:rows + len(t)] = t
+    return whole[rows:rows + len(t)], whole
+
+
+def bits(torch, t):
+    return t.contiguous().view(torch.int16).clone()
+
+
+@pytest.mark.parametrize("spoil", ["begin", "len", "negative"])
+def test_placing_by_offsets_that_lie_writes_its_own_rows(torch, spoil):
+    """The rows of the request that lies are those of its clamped numbers; all others, and what stands beside the
+    buffers, are as they should be."""
+    with wt.Handle([]) as h:
+        s = Place(torch, [3, 2], [4, 0], pad=4)
+        wholes = []
+        for name in ("q_out", "k_pages", "v_pages"):
+            t, whole = guarded(torch, getattr(s, name), 3)
+            setattr(s, name, t)
+            wholes.append(whole)
+        s.before = [t.clone() for t in (s.q_out, s.k_pages, s.v_pages)]
+        around = [torch.cat([bits(torch, w[:3]), bits(torch, w[-3:])]) for w in wholes]
+        if spoil == "begin":  # up to the last row, of which the last two have places
+            s.begin[2] = len(s.q)
+            want = s.want()
+            s.begin[2] = 10 ** 9
+        elif spoil == "len":  # up to max_len
+            s.lens[1] = s.max_len
+            want = s.want()
+            s.lens[1] = 2 ** 30
+        else:
+            want = s.want()
+            s.begin[0] = -5
+        h.place(s.desc())
+        torch.cuda.synchronize()
+        assert h.device_status() == wt.WT_EINVAL
+        s.check(torch, want)
+        for w, was in zip(wholes, around):
+            assert torch.equal(torch.cat([bits(torch, w[:3]), bits(torch, w[-3:])]), was)
+
+
+@pytest.mark.parametrize("route", ROUTES)
+@pytest.mark.parametrize("name,at,v", [("begin", 3, 10 ** 9), ("begin", 0, -4), ("mem_len", 1, 2 ** 30), ("mem_len", 0, -1), ("mem_begin", 1, -7),
+                                       ("mem_begin", 0, 2 ** 30)])
+def test_attending_by_lengths_that_lie_writes_its_own_rows(torch, route, name, at, v):
+    """As above: the other requests' results are right, and rows that the clamped numbers do not hold are as they were."""
+    with wt.Handle([]) as h:
+        s = Cross(torch, *ROUTES[route], pad=5)
+        N, M = len(s.q), len(s.k)
+        s.out, whole = guarded(torch, s.out, 300)
+        t = getattr(s, name)
+        t[at] = v
+        # the clamped numbers
+        begin, mem, lens = s.begin.tolist(), s.mem_begin.tolist(), s.mem_len.tolist()
+        begin[0], begin[3] = max(begin[0], 0), min(begin[3], N, begin[2] + s.max_new)
+        for b in range(3):
+            mem[b] = min(max(mem[b], 0), M)
+            lens[b] = min(max(lens[b], 0), s.max_mem, M - mem[b])
+        ints = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+        want = plain.cross(s.q, ints(begin), s.k, s.v, ints(mem), ints(lens), None, s.scale)
+        before = bits(torch, whole)
+        h.cross(s.desc())
+        torch.cuda.synchronize()
+        assert h.device_status() == wt.WT_EINVAL
+        s.check(torch, want)  # of a request that the gaps' NaN reach nothing is asked
+        for b in range(3):
+            if not (name.startswith("mem") and b == at):
+                assert not want[0][begin[b]:begin[b + 1]].isnan().any()
+        after = bits(torch, whole)
+        held = torch.zeros(len(whole), dtype=torch.bool, device="cuda")
+        held[300 + begin[0]:300 + begin[3]] = True
+        assert torch.equal(after[~held], before[~held])
