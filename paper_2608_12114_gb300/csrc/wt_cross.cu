@@ -482,7 +482,6 @@ cudaError_t prepare_dim() {
 
 template <int DT>
 cudaError_t run_merge(const CrossPlan &P, cudaStream_t s) {
-  if (P.ctas < 2) return cudaSuccess;
   const int lanes = P.d.head_dim <= 64 ? 16 : 32, most = (int)std::min<int64_t>(P.rows, (int64_t)P.d.max_new * P.G);
   cudaLaunchConfig_t cfg = {};
   // rows of a head stand `rows` apart, so with several heads all count

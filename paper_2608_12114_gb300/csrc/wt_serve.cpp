@@ -595,7 +595,7 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
   P.ml = reinterpret_cast<float2 *>(ws + ml);
   P.cuts = reinterpret_cast<wt::CrossCut *>(ws + cuts);
   P.fold = reinterpret_cast<float4 *>(ws + fold);
-  const bool joined = d.max_mem > P.keys;  // memories of one cell: no row tile has two parts
+  const bool joined = d.max_mem > P.keys;  // memories of one cell: no row tile has two parts.  Else there are two CTAs at least.
   cudaError_t e = wide ? wt::launch_cross_wide(P, maps, s) : wt::launch_cross_few(P, maps, s);
   if (e == cudaSuccess && joined) e = wt::launch_cross_merge(P, s);
   const int rc = wt::serve_done(h, s, w);

@@ -1,6 +1,7 @@
 """What the serving calls' host code hands to the kernels, without a GPU (wt_serve.cpp over recording stand-ins)."""
 import ctypes as C
 import os
+import random
 import subprocess
 
 import pytest
@@ -72,3 +73,24 @@ def test_row_tiles_up_to_2_31_rows(L):
             for n in (0, 1, rows // G, rows // G + 1, most - 1, most):
                 if n <= 2 ** 30:
                     assert L.host_row_tiles(n, G, rows) == -(-n * G // rows), (n, G, rows)
+
+
+def test_a_merge_has_parts_of_two_ctas(L):
+    """wt_cross launches its merge where a memory may have more than one cell; its grid is a CTA less than the parts' own."""
+    r = random.Random(1)
+    merged = 0
+    for _ in range(2000):
+        kv, G, D = r.choice((1, 2, 3, 4, 8)), r.choice((1, 2, 7, 128)), r.choice((8, 64, 72, 128))
+        q, k, v, begin, mem_begin, mem_len = buffers(6)
+        tokens, states = r.choice((1, 2, 9, 33, 700)), r.choice((1, 15, 16, 17, 32, 64, 65, 128, 129, 70000))
+        d = wt.CrossDesc(q=q, out=q, begin=begin, k=k, v=v, mem_begin=mem_begin, mem_len=mem_len, q_stride=kv * G * D, out_stride=kv * G * D,
+                         mem_stride=kv * D, mem_head=D, n_mem=states, dtype=r.choice((wt.WT_BF16, wt.WT_F16)), n_req=r.choice((1, 2, 50)),
+                         n_tokens=tokens, max_new=r.choice((1, tokens)), max_mem=r.choice((0, 1, states, 2 * states)), heads=kv * G,
+                         kv_heads=kv, head_dim=D, scale=r.choice((0.1, 0.0, -1.0)))
+        L.host_reset()
+        assert L.wt_cross(None, C.byref(d), None) == wt.WT_OK, L.host_error()
+        assert L.host_launches() == L.host_counted() in (1, 2)
+        if L.host_launches() == 2:
+            merged += 1
+            assert L.host_cross_ctas() >= 2
+    assert merged > 500
