@@ -93,4 +93,4 @@ def test_a_merge_has_parts_of_two_ctas(L):
         if L.host_launches() == 2:
             merged += 1
             assert L.host_cross_ctas() >= 2
-    assert merged > 500
+    assert merged > 50  # one in ten memories is long, and half of the calls bound theirs by it
