@@ -555,12 +555,18 @@ size_t plan_logprobs(LogprobsPlan *P) {
   P->row_vecs = (d.vocab + 6) / 4;
   const long long all = (long long)d.rows * P->row_vecs, ctas = (long long)kResident * num_sms();
   // Equal shares, of one turn of a CTA's threads at least, or whole rows, whichever takes less by this count, in
-  // turns: a row that a CTA meets takes its turns and about two more, and parts of rows cost 8 more, 16 with
-  // alternatives.  (Shares against whole rows, us: 100 rows of 30000 with twenty alternatives 20.5, 13.6, without 10.1, 6.9;
-  // 257 of 128256 with twenty 46.4, 43.9; 10 of 100000 with 32 16.7, 26.9; 900 of 128256 without 74.7, 76.2.)
+  // turns of SMs full of CTAs: a row that a CTA meets takes its turns and about two more, and parts of rows cost 12 more.
+  // With alternatives parts cost 8, a share's turns half as much again, and turns of whole rows, which load ahead, less
+  // where an SM has fewer CTAs.  (Shares against whole rows, us, with twenty alternatives: 40 rows of 128256 21.9, 24.4;
+  // 60 24.3, 24.6; 80 27.1, 24.5; 128 33.0, 25.0; 200 42.4, 34.9; 254 46.5, 35.9; 257 46.0, 36.0; 300 53.6, 36.7; 620 81.7,
+  // 89.1; 900 112.7, 92.9; 257 of 151936 50.7, 40.4; 20 of 50021 14.5, 15.1; 40 16.9, 15.5; 100 of 30000 20.4, 12.4; 10 of
+  // 100000 with 32 16.6, 22.0.  Without: 128 of 128256 14.6, 12.7; 200 20.0, 24.9; 400 33.9, 32.3; 900 74.1, 72.3; 100 of
+  // 30000 9.7, 5.5; 10 of 100000 6.4, 10.0.  On the wrong side: up to 10 rows of 50021 with twenty, 9 to 13 by shares and 15
+  // as taken, one of 32000 8.6 and 11.4, and without alternatives what lies within 15 %.)
   const long long equal = std::max<long long>((all + ctas - 1) / ctas, kTurn), whole = (d.rows + ctas - 1) / ctas;
-  const double by_shares = (double)equal / kTurn + 2.0 * (2.0 + (double)equal / P->row_vecs) + (d.n_top ? 16.0 : 8.0);
-  const double by_rows = (double)whole * ((P->row_vecs + kTurn - 1) / kTurn + 2.0);
+  const double met = 2.0 * equal / P->row_vecs, to_sm = std::min<double>(kResident, (d.rows + num_sms() - 1) / num_sms());
+  const double by_shares = d.n_top ? 1.44 * equal / kTurn + met + 8.0 : (double)equal / kTurn + met + 12.0;
+  const double by_rows = (double)whole * ((P->row_vecs + kTurn - 1) / kTurn + 2.0) * (d.n_top ? (1.0 + to_sm) / (1.0 + kResident) : 1.0);
   P->per = by_rows <= by_shares ? whole * P->row_vecs : equal;
   P->ctas = (int)((all + P->per - 1) / P->per);
   P->split = P->per % P->row_vecs != 0 && all > P->per;
