@@ -460,8 +460,9 @@ cudaError_t run_few(const CrossPlan &P, const CrossMaps &m, cudaStream_t s) {
 template <int DT, int DH>
 cudaError_t run_rows(const CrossPlan &P, const CrossMaps &m, cudaStream_t s) {
   if (P.rows == 8) return run_few<DT, DH, 1>(P, m, s);
-  if (P.rows == 16) return run_few<DT, DH, 2>(P, m, s);
-  return run_few<DT, DH, 4>(P, m, s);
+  if constexpr (DH == 1)
+    if (P.rows == 32) return run_few<DT, DH, 4>(P, m, s);
+  return run_few<DT, DH, 2>(P, m, s);
 }
 
 template <int DT, int DH, int NQ>
@@ -476,7 +477,8 @@ template <int DT, int DH>
 cudaError_t prepare_dim() {
   cudaError_t e = prepare_few<DT, DH, 1>();
   if (e == cudaSuccess) e = prepare_few<DT, DH, 2>();
-  if (e == cudaSuccess) e = prepare_few<DT, DH, 4>();
+  if constexpr (DH == 1)
+    if (e == cudaSuccess) e = prepare_few<DT, DH, 4>();
   return e;
 }
 

@@ -514,10 +514,15 @@ int check_cross(wt_handle *h, const wt_cross_desc &d) {
   return WT_OK;
 }
 
-// Many rows (token, head-in-group) of a request go to tcgen05.  Its softmax takes the largest product for the
-// largest score, so the scale has to be positive.
+// Rows (token, head-in-group) of a kv head that the kernel for few rows takes at once.
+int cross_few_rows(const wt_cross_desc &d) { return d.head_dim <= 64 ? 32 : 16; }
+
+// More rows of a request go to tcgen05.  (Few against many, us, memories of 1500 states.  8 kv heads of 128: one request of 16
+// rows 11.7, 12.5, of 20 18.0, 12.8; 16 requests of 16 37.4, 20.4, of 20 69.7, 20.9; 48 of 16 68.0, 63.5, of 20 121, 64.3.
+// 20 heads of 64: one request of 32 rows 15.7, 12.6; 16 of 16 38.2, 42.7, of 32 62.9, 42.6; 48 of 32 104, 117.)  Its softmax takes
+// the largest product for the largest score, so the scale has to be positive.
 bool cross_on_tcgen05(const wt_cross_desc &d) {
-  return (int64_t)d.max_new * (d.heads / d.kv_heads) > 32 && d.scale > 0.0f && d.max_mem > 0;
+  return (int64_t)d.max_new * (d.heads / d.kv_heads) > cross_few_rows(d) && d.scale > 0.0f && d.max_mem > 0;
 }
 
 int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
@@ -552,13 +557,15 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
     CHECK(wt::serve_tensor_map(maps.q, d.q, 3, qd, qs, qb));
   } else {
     // A warp to a head, for as many as the heads fill, so that those who read one line after another do it
-    // together; but all to one head where that would leave a warp few tiles.
+    // together; but all to one head where that would leave a warp few tiles.  (Together against one, us, memories of 1500
+    // states.  20 heads of 64, the border at 5 requests: 4 11.6, 9.3; 12 16.4, 15.3; 48 61.2, 86.1.  8 heads of 128, whose
+    // lines are twice as long: 16 requests 22.7, 20.0; 48 55.2, 52.4.)
     const int keys = wt::cross_few_keys(d.head_dim);
     const double tiles = (double)d.n_req * d.kv_heads * (double)ceil_div(d.max_mem, keys);
     P.together = tiles < 16.0 * wt::kCrossFewResident * wt::num_sms() ? 1 : d.kv_heads % 4 == 0 ? 4 : d.kv_heads % 2 == 0 ? 2 : 1;
     P.keys = keys * 4 / P.together;
     const int64_t most = (int64_t)d.max_new * P.G;
-    P.rows = most <= 8 ? 8 : most <= 16 ? 16 : 32;
+    P.rows = most <= 8 ? 8 : most <= 16 ? 16 : cross_few_rows(d);
   }
   if (d.max_mem > 0) {
     const uint64_t kd[3] = {D, (uint64_t)d.kv_heads, (uint64_t)d.n_mem}, ks[2] = {2 * (uint64_t)d.mem_head, 2 * (uint64_t)d.mem_stride};
@@ -567,8 +574,10 @@ int cross_impl(wt_handle *h, const wt_cross_desc *dp, cudaStream_t s) {
     CHECK(wt::serve_tensor_map(maps.v, d.v, 3, kd, ks, kb));
   }
   P.groups = d.kv_heads / P.together;
-  // A memory of n cells joins n / least parts, at about a sixth of a cell's time each.
-  P.least = 1 + (int)std::sqrt((double)ceil_div(d.max_mem, P.keys) / 6.0);
+  // A memory of n cells takes least of them and joins n / least parts, at about a 24th of a cell's time each.  (Without
+  // a least, by a 24th, a sixth, two thirds: one token of 8 kv heads of 128, 1500 states, 8.3, 8.2, 8.6, 11.7 us; of one, 16384
+  // states, 26.4, 14.6, 15.4, 20.9; 131072 35.6, 32.0, 32.9, 45.8; 64 tokens of 4 heads over one, 4096 14.6, 14.2, 15.6, 17.5.)
+  P.least = 1 + (int)std::sqrt((double)ceil_div(d.max_mem, P.keys) / 24.0);
   // No more CTAs than run at once, or than there can be cells.  (Requests' row tiles: whole ones of all tokens,
   // and one more each.)
   const double tiles = std::min((double)d.n_req * (double)ceil_div((int64_t)d.max_new * P.G, P.rows),

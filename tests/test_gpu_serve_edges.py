@@ -114,7 +114,7 @@ def test_sums_of_2_20_states(torch, h, dt):
 
 
 LONG = {  # new, requests, heads, kv heads, D: one memory for all, so that CTAs have long runs of it
-    "8 rows, heads together": (1, 310, 4, 4, 64), "8 rows": (2, 330, 3, 1, 128), "16 rows": (4, 320, 12, 4, 72), "32 rows": (8, 310, 16, 4, 128),
+    "8 rows, heads together": (1, 310, 4, 4, 64), "8 rows": (2, 330, 3, 1, 128), "16 rows": (4, 320, 12, 4, 72), "32 rows": (8, 310, 16, 4, 64),
     "32 rows of 40": (8, 310, 8, 2, 40), "one row tile": (32, 160, 4, 1, 64), "one row tile of 128": (32, 160, 4, 1, 128),
     "two row tiles": (64, 160, 4, 1, 56), "two row tiles of 128": (70, 160, 4, 1, 120)}
 
