@@ -151,7 +151,9 @@ int wt_place(wt_handle *h, const wt_place_desc *d, void *stream);
  * j of request b is row j % page of page table[b, j / page].  Rows of a page past len[b] are never
  * used, and a later token's key and value never reach an earlier one (NaN and infinity there are
  * harmless).  q, caches and out are bf16 or f16; scores, softmax statistics and sums are fp32, and the
- * weights p enter the second product rounded to the caches' type.
+ * weights p enter the second product rounded to the caches' type.  That product's sums are cut off where they
+ * grow: with many rows, results of values of one sign fall short by some 4e-9 of themselves for each key of the
+ * prefix, by two roundings of f16 for 2^18 keys.
  *
  * head_dim is a multiple of 8 up to 128; heads a multiple of kv_heads, heads / kv_heads <= 128; n_req
  * is below 65536, n_tokens, prefix_len and max_len go up to 2^30, n_tokens * heads to 2^31 - 1.
@@ -191,10 +193,9 @@ int wt_attend(wt_handle *h, const wt_attend_desc *d, void *stream);
  * over the states with keep[j] != 0 (keep NULL: all).  Memories may overlap or be one; a request's tokens
  * read theirs once, so beams or drafts over one memory are best one request's tokens.  Scores and sums are
  * fp32, whatever a memory's length; weights are rounded to the memory's type, and divided by the sum of the
- * rounded ones.  A token that sees
- * no state gets zeros, and so does one all of whose scores are -infinity.  NaN and infinities show as
- * wt_attend's do; what is not in the memory, or not kept, never reaches a result, whatever stands there.
- * Rows of tokens that no request holds are left as they are.
+ * rounded ones.  A token that sees no state gets zeros, and so does one all of whose scores are -infinity.
+ * NaN and infinities show as wt_attend's do; what is not in the memory, or not kept, never reaches a result,
+ * whatever stands there.  Rows of tokens that no request holds are left as they are.
  *
  * Types, head sizes and limits are wt_attend's; n_mem goes up to 2^30.  out may be q itself (at its
  * pitch); otherwise it must not overlap any input, as rows of tokens. */
