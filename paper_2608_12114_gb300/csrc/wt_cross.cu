@@ -53,7 +53,7 @@ __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
 
 // A warp's tiles in order: of every cell of the CTA's share, its own, where the memory reaches it.
 struct Tiles : Walk {
-  int i, first_key, by;  // key of a cell's first tile of this warp; from cell to cell
+  int i, first_key, by;  // its tiles so far; key of a cell's first tile of this warp; from cell to cell
   __device__ Tiles(const CrossPlan &p, const Share &share, int key) : Walk(p, share), i(0), first_key(key), by(p.keys) {}
   __device__ bool segment() {  // the next row tile
     i = 0;
@@ -62,8 +62,10 @@ struct Tiles : Walk {
   // state of the next tile of the row tile; false: none left
   __device__ bool tile(int &key0) {
     if (i >= g.tiles) return false;
-    key0 = (g.tile0 + i++) * by + first_key;
-    return key0 < a.len;
+    key0 = (g.tile0 + i) * by + first_key;
+    if (key0 >= a.len) return false;
+    ++i;
+    return true;
   }
 };
 

@@ -164,6 +164,29 @@ def test_long_memories_on_every_route(torch, h, name, dt, M, holes):
     assert off.mean().abs() <= 0.25 * u, float(off.mean() / u)
 
 
+@pytest.mark.parametrize("D,kv", [(64, 1), (64, 2), (128, 1)])
+@pytest.mark.parametrize("more", [1, 15, 33, 70])
+def test_memories_a_little_longer_than_one_sum_takes(torch, h, D, kv, more):
+    """Of the last cell only some warps have states; the others have set nothing aside, whatever an earlier call left there."""
+    B, dt = 400, torch.float16
+    cell = 4 // kv * (32 if D <= 64 else 16)  # states that the warps of a head take at once
+    M = 8192 * cell // (32 if D <= 64 else 16)
+    g = torch.Generator("cuda").manual_seed(9)
+    k, v = (torch.randn(M + 9000, kv, D, device="cuda", generator=g).to(dt) for _ in range(2))
+    v += 100.0
+    q = torch.randn(B, kv, D, device="cuda", generator=g).to(dt)
+    ints = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    for n in (M + 9000, M + more):
+        out = torch.full_like(q, float("nan"))
+        h.cross(serving.cross_attention(q, out, ints(*range(B + 1)), k, v, ints(*[0] * B), ints(*[n] * B), max_new=1, max_mem=n))
+        torch.cuda.synchronize()
+        for x in range(kv):
+            p = torch.softmax(q[:, x].double() @ k[:n, x].double().t() * D ** -0.5, dim=1)
+            want = p @ v[:n, x].double()
+            # the output's rounding, an eighth of it for the weights', and a fifth for the sums
+            assert ((out[:, x].double() - want).abs() <= (1 + 0.125 + 0.2) * 2.0 ** -11 * want.abs()).all(), (n, x)
+
+
 def guarded(torch, t, rows):
     """A copy of t between `rows` rows of other numbers, and the whole buffer."""
     g = torch.Generator("cuda").manual_seed(11)
